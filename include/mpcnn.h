@@ -252,6 +252,50 @@ mpcnn_status mpcnn_seg_backward_banded(mpcnn_net* net, const float* image_dev, c
 mpcnn_status mpcnn_sgd_step(mpcnn_net* net, float lr, float grad_scale, void* hip_stream);
 
 /*
+ * The same step with the gradient's 2-norm bounded: norm = |grad_scale| * sqrt(sum of g^2 over every
+ * parameter), c = min(1, max_norm / norm), theta -= lr * grad_scale * c * g.  max_norm > 0, infinity for
+ * no bound.  norm_dev: one fp64 on the device that receives norm (before the bound), or NULL.  A norm
+ * that is not finite leaves the parameters as they are.  Squares and sums are fp64, in a fixed order.
+ * Errors: EINVAL (also: lr or grad_scale not finite, max_norm not above zero), EHIP.
+ */
+mpcnn_status mpcnn_sgd_step_clipped(mpcnn_net* net, double lr, double grad_scale, double max_norm, double* norm_dev,
+                                    void* hip_stream);
+
+/*
+ * The update step on tensors of the caller's own (the weights behind mpcnn_class_backward, several
+ * models together): a list of gradients, with the parameters they belong to or without any, made once
+ * and used for every step.
+ *   mpcnn_grad_list_create: allocates the list's table on the current device, which is the device of
+ *     every tensor and has to be the current one in every call; synchronous.  The tensors stay the
+ *     caller's and have to live as long as the list is used.  A tensor is n consecutive numbers,
+ *     MPCNN_F32 or MPCNN_BF16 (gradient and parameter types are independent), at any address that is a
+ *     multiple of its element's size; n = 0 is allowed, and so is an empty list.  param_dev: NULL in
+ *     all tensors, or in none.  Errors: EINVAL (null pointer, unknown type, memory of two tensors that
+ *     overlaps), ENOMEM, EHIP.
+ *   mpcnn_grad_norm: *norm_dev = |grad_scale| * 2-norm over all gradients together.
+ *   mpcnn_grad_clip: gradients *= min(1, max_norm / norm), rounded to their type; *norm_dev (may be
+ *     NULL) = norm, before.
+ *   mpcnn_sgd_step_list: parameters -= lr * grad_scale * c * gradient, c as in mpcnn_sgd_step_clipped,
+ *     computed in fp32 and rounded once; gradients are not written.
+ * Norms, bounds and what is not finite: as in mpcnn_sgd_step_clipped.  One list must not be used from
+ * two streams at once.  Errors: EINVAL (also: another device is current, a step without parameters), EHIP.
+ */
+typedef struct {
+    void* grad_dev;
+    void* param_dev;
+    int64_t n;
+    int grad_dtype;  /* mpcnn_dtype */
+    int param_dtype;
+} mpcnn_tensor;
+typedef struct mpcnn_grad_list mpcnn_grad_list;
+mpcnn_status mpcnn_grad_list_create(const mpcnn_tensor* tensors_host, int count, mpcnn_grad_list** out);
+void mpcnn_grad_list_destroy(mpcnn_grad_list* list); /* waits for the device; NULL is allowed */
+mpcnn_status mpcnn_grad_norm(const mpcnn_grad_list* list, double grad_scale, double* norm_dev, void* hip_stream);
+mpcnn_status mpcnn_grad_clip(const mpcnn_grad_list* list, double max_norm, double* norm_dev, void* hip_stream);
+mpcnn_status mpcnn_sgd_step_list(const mpcnn_grad_list* list, double lr, double grad_scale, double max_norm,
+                                 double* norm_dev, void* hip_stream);
+
+/*
  * The loss alone, L as in mpcnn_seg_backward for the current parameters: a forward pass that
  * keeps nothing and computes no gradient (the evaluations of a line search).
  *   loss_dev: one fp64 on the device.  ws_dev: at least mpcnn_workspace_bytes(net,B,H,W,0).

@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -22,6 +23,8 @@
 #include "../../include/mpcnn.h"
 #include "kernels_direct.hpp"
 #include "launchers.hpp"
+#include "status.hpp"
+#include "update.hpp"
 #include "kernels_conv_parts.hpp"   // its LDS geometry (no instance is built here)
 #include "kernels_wgrad_tr.hpp"     // its LDS geometry
 #include "kernels_wgrad_bf16.hpp"   // its LDS geometry, which the planner shares (no instance is built here)
@@ -40,11 +43,9 @@
 // hipGetSymbolAddress; the kernels are given the address that call returns.
 static __device__ __align__(256) unsigned char scratch[MPCNN_STATIC_WORKSPACE_BYTES];
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
-
-mpcnn_status fail(mpcnn_status st, const char* fmt, ...)
+mpcnn_status mpcnn::fail(mpcnn_status st, const char* fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -53,13 +54,9 @@ mpcnn_status fail(mpcnn_status st, const char* fmt, ...)
     return st;
 }
 
-#define HIP_TRY(expr)                                                                      \
-    do {                                                                                   \
-        hipError_t e_ = (expr);                                                            \
-        if (e_ != hipSuccess)                                                              \
-            return fail(MPCNN_EHIP, "%s failed: %s (%s:%d)", #expr, hipGetErrorString(e_), \
-                        __FILE__, __LINE__);                                               \
-    } while (0)
+namespace {
+
+using mpcnn::fail;
 
 constexpr int kLossBlocks = 2048;         // most per-workgroup loss shares (= most workgroups of the class-layer kernel)
 static_assert(kLossBlocks <= mpcnn::kDeltaWords, "each has a word");
@@ -1867,7 +1864,7 @@ mpcnn_status alloc_params(mpcnn_net* net)
     const size_t bytes = sizeof(float) * net->n_params;
     HIP_TRY(hipGetDevice(&net->device));
     HIP_TRY(hipMalloc((void**)&net->d_params, bytes));
-    HIP_TRY(hipMalloc((void**)&net->d_grads, bytes));
+    HIP_TRY(hipMalloc((void**)&net->d_grads, align_up(bytes) + sizeof(double) * mpcnn::kNormParts));   // (and partial sums of their squares)
     if (net->n_params > kSmallVector) HIP_TRY(hipHostMalloc((void**)&net->h_stage, bytes, hipHostMallocDefault));
     HIP_TRY(hipMemset(net->d_grads, 0, bytes));
     if (net->pack_len) HIP_TRY(hipMalloc((void**)&net->d_packs, sizeof(float) * net->pack_len));
@@ -2591,6 +2588,27 @@ mpcnn_status mpcnn_sgd_step(mpcnn_net* net, float lr, float grad_scale, void* hi
     LAUNCH("sgd", -1, 8, 2.0 * n, 12.0 * n,
            mpcnn::sgd_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(net->d_params, net->d_grads,
                                                                           lr * grad_scale, n));
+    HIP_TRY(hipGetLastError());
+    net->packs_stale = true; net->wread_stale = true;
+    return MPCNN_OK;
+}
+
+mpcnn_status mpcnn_sgd_step_clipped(mpcnn_net* net, double lr, double grad_scale, double max_norm, double* norm_dev, void* hip_stream)
+{
+    if (!net) return fail(MPCNN_EINVAL, "null net");
+    if (!net->d_params) return fail(MPCNN_EINVAL, "parameters were never set");
+    if (!std::isfinite(lr) || !std::isfinite(grad_scale)) return fail(MPCNN_EINVAL, "scale %g, rate %g", grad_scale, lr);
+    if (!(max_norm > 0.0)) return fail(MPCNN_EINVAL, "max_norm = %g", max_norm);
+    const long n = (long)net->n_params;
+    hipStream_t st = (hipStream_t)hip_stream;
+    mpcnn::UpdateArgs a{};
+    a.flat.grad = net->d_grads; a.flat.param = net->d_params;
+    a.flat_n = n; a.flat_len = mpcnn::stretch_length(n);
+    a.stretches = (int)((n + a.flat_len - 1) / a.flat_len);
+    a.partial = (double*)((char*)net->d_grads + align_up(sizeof(float) * net->n_params));
+    a.norm = norm_dev;
+    a.scale = std::fabs(grad_scale); a.bound = max_norm; a.rate = (float)(lr * grad_scale);
+    LAUNCH("sgd_clipped", -1, 8, 4.0 * n, 16.0 * n, mpcnn::launch_update(a, mpcnn::kStep, n, st));
     HIP_TRY(hipGetLastError());
     net->packs_stale = true; net->wread_stale = true;
     return MPCNN_OK;

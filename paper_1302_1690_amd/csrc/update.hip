@@ -1,0 +1,192 @@
+// Lists of gradient (and parameter) tensors: their norm, clipping, and the gradient step (see include/mpcnn.h, kernels_update.hpp).
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <new>
+#include <vector>
+
+#include "kernels_update.hpp"
+#include "status.hpp"
+
+using mpcnn::fail;
+
+struct mpcnn_grad_list {
+    int device = -1;
+    long total = 0;
+    int stretches = 0;
+    bool params = false;
+    mpcnn::Stretch* d_table = nullptr;   // and, behind it, the partial sums
+    double* d_partial = nullptr;
+};
+
+namespace mpcnn {
+
+unsigned stretch_length(long total)
+{
+    const long each = (total / 4096 + kStretchLeast - 1) / kStretchLeast * kStretchLeast;
+    return (unsigned)std::min<long>(kStretch, std::max<long>(kStretchLeast, each));
+}
+
+template <bool LONE>
+static void launch_mode(const UpdateArgs& a, int mode, unsigned groups, hipStream_t st)
+{
+    constexpr int threads = LONE ? 1024 : 256;
+    if (mode == kOnlyNorm) update_kernel<kOnlyNorm, LONE><<<1, threads, 0, st>>>(a);
+    else if (mode == kClip) update_kernel<kClip, LONE><<<groups, threads, 0, st>>>(a);
+    else update_kernel<kStep, LONE><<<groups, threads, 0, st>>>(a);
+}
+
+void launch_update(UpdateArgs a, int mode, long total, hipStream_t st)
+{
+    if (total <= kLoneNumbers && a.stretches <= kLoneStretches) {
+        launch_mode<true>(a, mode, 1, st);
+        return;
+    }
+    const int groups = (int)std::min<long>(kNormParts, ((long)a.stretches + 3) / 4);
+    a.parts = groups;
+    norm_parts_kernel<<<(unsigned)groups, 256, 0, st>>>(a);
+    launch_mode<false>(a, mode, (unsigned)groups, st);
+}
+
+}  // namespace mpcnn
+
+namespace {
+
+struct Range { uintptr_t at; uint64_t bytes; };
+
+bool overlap(std::vector<Range>& r)
+{
+    std::sort(r.begin(), r.end(), [](const Range& x, const Range& y) { return x.at < y.at; });
+    for (size_t i = 1; i < r.size(); ++i)
+        if (r[i].at - r[i - 1].at < r[i - 1].bytes) return true;
+    return false;
+}
+
+bool known(int dtype) { return dtype == MPCNN_F32 || dtype == MPCNN_BF16; }
+uint64_t size_of(int dtype) { return dtype == MPCNN_BF16 ? 2 : 4; }
+
+mpcnn_status make_list(const mpcnn_tensor* t, int count, mpcnn_grad_list** out)
+{
+    std::vector<Range> ranges;
+    int64_t total = 0;
+    int with = 0, filled = 0;
+    for (int i = 0; i < count; ++i) {
+        if (t[i].n < 0 || t[i].n > ((int64_t)1 << 40)) return fail(MPCNN_EINVAL, "tensor %d: %lld numbers", i, (long long)t[i].n);
+        if (!known(t[i].grad_dtype) || (t[i].param_dev && !known(t[i].param_dtype))) return fail(MPCNN_EINVAL, "tensor %d: unknown type", i);
+        if (!t[i].n) continue;
+        if (!t[i].grad_dev) return fail(MPCNN_EINVAL, "tensor %d: null gradient", i);
+        const uint64_t gs = size_of(t[i].grad_dtype), ps = size_of(t[i].param_dtype);
+        if ((uintptr_t)t[i].grad_dev % gs || (t[i].param_dev && (uintptr_t)t[i].param_dev % ps))
+            return fail(MPCNN_EINVAL, "tensor %d: address is no multiple of its element's size", i);
+        ++filled;
+        total += t[i].n;
+        ranges.push_back({(uintptr_t)t[i].grad_dev, (uint64_t)t[i].n * gs});
+        if (t[i].param_dev) {
+            ++with;
+            ranges.push_back({(uintptr_t)t[i].param_dev, (uint64_t)t[i].n * ps});
+        }
+    }
+    if (with && with != filled) return fail(MPCNN_EINVAL, "%d of %d tensors have parameters: all or none", with, filled);
+    if (overlap(ranges)) return fail(MPCNN_EINVAL, "two of the tensors overlap in memory");
+    const unsigned len = mpcnn::stretch_length((long)total);
+    std::vector<mpcnn::Stretch> table;
+    for (int i = 0; i < count; ++i)
+        for (int64_t at = 0; at < t[i].n; at += len) {
+            mpcnn::Stretch s{};
+            s.grad = (char*)t[i].grad_dev + at * (int64_t)size_of(t[i].grad_dtype);
+            s.grad_bf16 = t[i].grad_dtype == MPCNN_BF16;
+            if (t[i].param_dev) {
+                s.param = (char*)t[i].param_dev + at * (int64_t)size_of(t[i].param_dtype);
+                s.param_bf16 = t[i].param_dtype == MPCNN_BF16;
+            }
+            s.n = (unsigned)std::min<int64_t>(len, t[i].n - at);
+            table.push_back(s);
+        }
+    if (table.size() > (size_t)1 << 30) return fail(MPCNN_EINVAL, "too many numbers: %lld", (long long)total);
+    mpcnn_grad_list* l = new mpcnn_grad_list;
+    l->total = (long)total;
+    l->stretches = (int)table.size();
+    l->params = with > 0;
+    const size_t bytes = sizeof(mpcnn::Stretch) * table.size(), partial = sizeof(double) * mpcnn::kNormParts;
+    static_assert(sizeof(mpcnn::Stretch) % sizeof(double) == 0, "the partial sums behind the table are aligned");
+    char* dev = nullptr;
+    hipError_t e = hipGetDevice(&l->device);
+    if (e == hipSuccess) e = hipMalloc((void**)&dev, bytes + partial);
+    if (e == hipSuccess && bytes) e = hipMemcpy(dev, table.data(), bytes, hipMemcpyHostToDevice);
+    if (e != hipSuccess) {
+        (void)hipFree(dev);
+        delete l;
+        return fail(e == hipErrorOutOfMemory ? MPCNN_ENOMEM : MPCNN_EHIP, "list of %d tensors: %s", count, hipGetErrorString(e));
+    }
+    l->d_table = (mpcnn::Stretch*)dev;
+    l->d_partial = (double*)(dev + bytes);
+    *out = l;
+    return MPCNN_OK;
+}
+
+mpcnn_status update(const mpcnn_grad_list* l, int mode, double rate, double scale, double bound, double* norm, void* stream)
+{
+    if (!l) return fail(MPCNN_EINVAL, "null list");
+    if (mode == mpcnn::kOnlyNorm && !norm) return fail(MPCNN_EINVAL, "null argument");
+    if (!std::isfinite(scale) || !std::isfinite(rate)) return fail(MPCNN_EINVAL, "scale %g, rate %g", scale, rate);
+    if (!(bound > 0.0)) return fail(MPCNN_EINVAL, "max_norm = %g", bound);
+    if (mode == mpcnn::kStep && l->stretches && !l->params) return fail(MPCNN_EINVAL, "the list has no parameters");
+    int dev = -1;
+    HIP_TRY(hipGetDevice(&dev));
+    if (dev != l->device) return fail(MPCNN_EINVAL, "the list is on device %d, the current device is %d", l->device, dev);
+    mpcnn::UpdateArgs a{};
+    a.table = l->d_table;
+    a.stretches = l->stretches;
+    a.partial = l->d_partial;
+    a.norm = norm;
+    a.scale = std::fabs(scale);
+    a.bound = bound;
+    a.rate = (float)(rate * scale);
+    mpcnn::launch_update(a, mode, l->total, (hipStream_t)stream);
+    HIP_TRY(hipGetLastError());
+    return MPCNN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+mpcnn_status mpcnn_grad_list_create(const mpcnn_tensor* tensors_host, int count, mpcnn_grad_list** out)
+{
+    if (!out || (count > 0 && !tensors_host)) return fail(MPCNN_EINVAL, "null argument");
+    if (count < 0) return fail(MPCNN_EINVAL, "count = %d", count);
+    *out = nullptr;
+    try {
+        return make_list(tensors_host, count, out);
+    } catch (const std::bad_alloc&) {
+        return fail(MPCNN_ENOMEM, "out of host memory");
+    }
+}
+
+void mpcnn_grad_list_destroy(mpcnn_grad_list* list)
+{
+    if (!list) return;
+    int dev = -1;
+    const bool moved = hipGetDevice(&dev) == hipSuccess && dev != list->device && hipSetDevice(list->device) == hipSuccess;
+    (void)hipFree(list->d_table);
+    if (moved) (void)hipSetDevice(dev);
+    delete list;
+}
+
+mpcnn_status mpcnn_grad_norm(const mpcnn_grad_list* list, double grad_scale, double* norm_dev, void* hip_stream)
+{
+    return update(list, mpcnn::kOnlyNorm, 1.0, grad_scale, INFINITY, norm_dev, hip_stream);
+}
+
+mpcnn_status mpcnn_grad_clip(const mpcnn_grad_list* list, double max_norm, double* norm_dev, void* hip_stream)
+{
+    return update(list, mpcnn::kClip, 1.0, 1.0, max_norm, norm_dev, hip_stream);
+}
+
+mpcnn_status mpcnn_sgd_step_list(const mpcnn_grad_list* list, double lr, double grad_scale, double max_norm, double* norm_dev,
+                                 void* hip_stream)
+{
+    return update(list, mpcnn::kStep, lr, grad_scale, max_norm, norm_dev, hip_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,39 @@
+// Launches of the update kernels (update.hip, kernels_update.hpp), for lists of tensors and for a net's own parameters.
+#pragma once
+#include <hip/hip_runtime.h>
+
+namespace mpcnn {
+
+constexpr int kNormParts = 1024;           // most partial sums
+constexpr unsigned kStretch = 8192;        // most numbers of a stretch
+constexpr unsigned kStretchLeast = 512;    // one fetch of every lane
+constexpr long kLoneNumbers = 16384;
+constexpr int kLoneStretches = 64;
+
+struct Stretch {
+    void* grad;
+    void* param;            // null where there are no parameters
+    unsigned n;
+    unsigned short grad_bf16, param_bf16;
+};
+struct UpdateArgs {
+    const Stretch* table;   // null: `flat`, cut into stretches of flat_len
+    Stretch flat;
+    long flat_n;
+    unsigned flat_len;
+    int stretches, parts;
+    double* partial;        // [parts]
+    double* norm;           // result, or null
+    double scale, bound;    // |s|, largest norm
+    float rate;             // signed: rate * s
+    int back;               // stretches from the list's end on: what the norm's pass read last comes first
+};
+enum { kOnlyNorm = 0, kClip = 1, kStep = 2 };
+
+
+// Stretch length for so many numbers in all: enough stretches for every wave that can run, none shorter than one fetch
+unsigned stretch_length(long total);
+// mode: kOnlyNorm, kClip, kStep; fills in a.parts.  `total`: numbers in all.
+void launch_update(UpdateArgs a, int mode, long total, hipStream_t st);
+
+}  // namespace mpcnn

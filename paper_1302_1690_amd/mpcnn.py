@@ -33,7 +33,8 @@ SYMBOLS = [
     "mpcnn_set_loss", "mpcnn_class_balance_weights", "mpcnn_seg_loss", "mpcnn_armijo_step",
     "mpcnn_lbfgs_step", "mpcnn_lbfgs_reset", "mpcnn_set_activation", "mpcnn_set_conv_tiling",
     "mpcnn_workspace_bytes_banded", "mpcnn_seg_backward_banded", "mpcnn_seg_forward_static",
-    "mpcnn_plan_describe",
+    "mpcnn_plan_describe", "mpcnn_sgd_step_clipped", "mpcnn_grad_list_create", "mpcnn_grad_list_destroy",
+    "mpcnn_grad_norm", "mpcnn_grad_clip", "mpcnn_sgd_step_list",
 ]
 
 
@@ -52,6 +53,12 @@ class KernelStat(C.Structure):
     _fields_ = [("name", C.c_char * 48), ("layer", C.c_int), ("step", C.c_int),
                 ("launches", C.c_int), ("ms_total", C.c_double), ("flops", C.c_double),
                 ("bytes", C.c_double)]
+
+
+class _Tensor(C.Structure):
+    """mpcnn_tensor: a gradient and the parameters it belongs to."""
+    _fields_ = [("grad", C.c_void_p), ("param", C.c_void_p), ("n", C.c_int64), ("grad_dtype", C.c_int),
+                ("param_dtype", C.c_int)]
 
 
 _lib = None
@@ -106,6 +113,13 @@ def lib():
         L.mpcnn_class_balance_weights.argtypes = [vp, vp, i, i, i, vp, vp, vp]
         L.mpcnn_seg_backward.argtypes = [vp, vp, vp, vp, i, i, i, vp, vp, vp, sz, vp]
         L.mpcnn_sgd_step.argtypes = [vp, C.c_float, C.c_float, vp]
+        L.mpcnn_sgd_step_clipped.argtypes = [vp, C.c_double, C.c_double, C.c_double, vp, vp]
+        L.mpcnn_grad_list_create.argtypes = [C.POINTER(_Tensor), i, C.POINTER(vp)]
+        L.mpcnn_grad_list_destroy.argtypes = [vp]
+        L.mpcnn_grad_list_destroy.restype = None
+        L.mpcnn_grad_norm.argtypes = [vp, C.c_double, vp, vp]
+        L.mpcnn_grad_clip.argtypes = [vp, C.c_double, vp, vp]
+        L.mpcnn_sgd_step_list.argtypes = [vp, C.c_double, C.c_double, C.c_double, vp, vp]
         L.mpcnn_get_activation.argtypes = [vp, i, vp, sz]
         L.mpcnn_get_argmax.argtypes = [vp, i, vp, sz]
         L.mpcnn_last_error.restype = C.c_char_p
@@ -346,6 +360,14 @@ class Net:
     def sgd_step(self, lr: float, grad_scale: float = 1.0, stream=None):
         _check(lib().mpcnn_sgd_step(self._h, lr, grad_scale, _stream_handle(stream)))
 
+    def sgd_step_clipped(self, lr: float, max_norm: float, grad_scale: float = 1.0, norm=None, stream=None):
+        """sgd_step with the scaled gradient's norm bounded by max_norm; that norm is put into `norm` (one
+        fp64 on the GPU) if it is given."""
+        if norm is not None:
+            _check_norm(norm, None)
+        _check(lib().mpcnn_sgd_step_clipped(self._h, lr, grad_scale, max_norm, _ptr(norm), _stream_handle(stream)))
+        return norm
+
     # ---- per-kernel timing
     def profile_enable(self, on: bool):
         _check(lib().mpcnn_profile_enable(self._h, 1 if on else 0))
@@ -372,3 +394,123 @@ class Net:
         out = np.empty((B, r, c, ch), dtype=np.uint8)
         _check(lib().mpcnn_get_argmax(self._h, layer, out.ctypes.data, out.size))
         return out
+
+
+# ---- tensors of the caller's own: no net needed
+
+def _refuse(text: str):
+    raise MpcnnError(1, text)
+
+
+def _check_norm(norm, device):
+    import torch
+    if norm.dtype != torch.float64 or norm.numel() != 1 or not norm.is_cuda or (device is not None and norm.device != device):
+        _refuse("norm: one fp64 on the tensors' GPU")
+
+
+class _On:
+    """The tensors' GPU and the stream a call goes to (None: that GPU's current one), made current: memory that
+    is allocated inside belongs to that stream, as the work on it does."""
+
+    def __init__(self, device, stream):
+        import torch
+        if stream is None:
+            self.handle = torch.cuda.current_stream(device).cuda_stream
+            self.ctx = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+        else:
+            self.handle = int(getattr(stream, "cuda_stream", stream))
+            if not hasattr(stream, "cuda_stream"):
+                stream = torch.cuda.ExternalStream(self.handle, device=device)
+            self.ctx = torch.cuda.stream(stream)
+            if stream.device != device:
+                _refuse("the stream belongs to %s, the tensors to %s" % (stream.device, device))
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        return self.handle
+
+    def __exit__(self, *error):
+        if self.ctx is not None:
+            self.ctx.__exit__(*error)
+
+
+def _dtype_of(t) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return F32
+    if t.dtype == torch.bfloat16:
+        return BF16
+    _refuse("%s: fp32 and bf16 are supported" % t.dtype)
+
+
+class GradList:
+    """mpcnn_grad_list handle: gradients (dense tensors on one GPU, fp32 or bf16, of any shape) and, for
+    sgd_step, the parameters they belong to.  The list keeps the tensors alive and works on their memory."""
+
+    def __init__(self, grads, params=None):
+        import torch
+        self._h = None
+        self.grads = list(grads)
+        self.params = None if params is None else list(params)
+        if self.params is not None and len(self.params) != len(self.grads):
+            _refuse("%d gradients, %d parameters" % (len(self.grads), len(self.params)))
+        every = self.grads + (self.params or [])
+        self.device = every[0].device if every else torch.device("cuda", torch.cuda.current_device())
+        for t in every:
+            if not t.is_cuda or t.device != self.device:
+                _refuse("every tensor has to be on one GPU: %s, %s" % (t.device, self.device))
+            if not t.is_contiguous():
+                _refuse("tensors have to be contiguous: strides %s of %s" % (tuple(t.stride()), tuple(t.shape)))
+        arr = (_Tensor * max(1, len(self.grads)))()
+        for k, g in enumerate(self.grads):
+            arr[k].grad, arr[k].n, arr[k].grad_dtype = g.data_ptr(), g.numel(), _dtype_of(g)
+            if self.params is not None:
+                p = self.params[k]
+                if p.numel() != g.numel():
+                    _refuse("tensor %d: %d gradients, %d parameters" % (k, g.numel(), p.numel()))
+                arr[k].param, arr[k].param_dtype = p.data_ptr(), _dtype_of(p)
+        h = C.c_void_p()
+        with torch.cuda.device(self.device):
+            _check(lib().mpcnn_grad_list_create(arr, len(self.grads), C.byref(h)))
+        self._h = h
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().mpcnn_grad_list_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except TypeError:     # interpreter shutdown: the module's globals are already gone
+            pass
+
+    def _norm(self, norm):
+        import torch
+        if norm is None:
+            return torch.empty(1, dtype=torch.float64, device=self.device)
+        _check_norm(norm, self.device)
+        return norm
+
+    def norm(self, grad_scale: float = 1.0, norm=None, stream=None):
+        """|grad_scale| times the 2-norm over all gradients: one fp64 on the GPU."""
+        with _On(self.device, stream) as st:
+            norm = self._norm(norm)
+            _check(lib().mpcnn_grad_norm(self._h, grad_scale, norm.data_ptr(), st))
+        return norm
+
+    def clip(self, max_norm: float, norm=None, stream=None):
+        """Scale the gradients down to a norm of at most max_norm -> their norm before."""
+        with _On(self.device, stream) as st:
+            norm = self._norm(norm)
+            _check(lib().mpcnn_grad_clip(self._h, max_norm, norm.data_ptr(), st))
+        return norm
+
+    def sgd_step(self, lr: float, grad_scale: float = 1.0, max_norm: float = float("inf"), norm=None, stream=None):
+        """parameters -= lr * grad_scale * gradients, the scaled gradients' norm bounded by max_norm -> that
+        norm before the bound."""
+        with _On(self.device, stream) as st:
+            norm = self._norm(norm)
+            _check(lib().mpcnn_sgd_step_list(self._h, lr, grad_scale, max_norm, norm.data_ptr(), st))
+        return norm
