@@ -296,6 +296,46 @@ mpcnn_status mpcnn_sgd_step_list(const mpcnn_grad_list* list, double lr, double 
                                  double* norm_dev, void* hip_stream);
 
 /*
+ * The class layer and its softmax cross-entropy on rows of features, for label sets of any size (a
+ * net's own class layer has at most 16 classes):
+ *   scores s[n][v] = x[n] . w[v] + bias[v],   p = softmax over v,   L = sum over n of w[n] * -log p[n][t[n]]
+ * with t = labels, w = roww (1 if roww_dev is NULL); rows with t < 0, t >= classes or w = 0 add nothing,
+ * whatever their features hold.  The scores are taken in pieces of the classes and are not kept; where
+ * all of them fit the room of a piece (2^27) they are computed once.
+ *   x_dev      [rows][x_pitch], w_dev [classes][w_pitch], both `dtype`; pitches in elements, at least
+ *              `features`.  Any address that is a multiple of its element's size; whole blocks of 64
+ *              features at 16-byte aligned rows are read in place with MPCNN_BF16, others copied.
+ *   bias_dev   [classes] fp32 or NULL (minus infinity switches a class off: its p is 0),
+ *   labels_dev [rows] int32, roww_dev [rows] fp32 or NULL.
+ * mpcnn_class_loss: the loss alone.
+ *   rowloss_dev [rows] fp32: w * -log p (0 for rows that add nothing; infinity where the label's class
+ *              is off), lse_dev [rows] fp32: log sum exp s (0 for rows that add nothing),
+ *   loss_dev   one fp64, L.  Each may be NULL.
+ * mpcnn_class_backward: the loss and its gradients, each of which may be NULL:
+ *   dx_dev     [rows][dx_pitch] `dtype` (0 for rows that add nothing), dw_dev [classes][features]
+ *              `dtype`, db_dev [classes] fp32.
+ * Sums, scores and statistics are fp32 or wider; MPCNN_F32 products are made of fp16 parts (two per
+ * number, three products: 22 bits); with MPCNN_BF16 the scores' derivative is rounded to bf16 before
+ * it is multiplied, results once more.  Values that are not finite in rows that add something or in w
+ * give results that are not finite.  The result does not depend on launch timing.
+ *   ws_dev: 256-byte aligned scratch of at least mpcnn_workspace_bytes_class(...) (0 on bad input).
+ * Everything is on the current device.  rows = 0 is allowed (L = 0, dw = db = 0).  Outputs and the
+ * workspace may not overlap an input or each other.
+ * Errors: EINVAL, EUNSUPPORTED (more than 2^20 rows or features, or 2^31 - 1025 classes), EWORKSPACE, EHIP.
+ */
+size_t mpcnn_workspace_bytes_class(int64_t rows, int64_t features, int64_t classes, mpcnn_dtype dtype, int training);
+mpcnn_status mpcnn_class_loss(const void* x_dev, int64_t x_pitch, const void* w_dev, int64_t w_pitch,
+                              const float* bias_dev, const int32_t* labels_dev, const float* roww_dev,
+                              int64_t rows, int64_t features, int64_t classes, mpcnn_dtype dtype,
+                              float* rowloss_dev, float* lse_dev, double* loss_dev, void* ws_dev,
+                              size_t ws_bytes, void* hip_stream);
+mpcnn_status mpcnn_class_backward(const void* x_dev, int64_t x_pitch, const void* w_dev, int64_t w_pitch,
+                                  const float* bias_dev, const int32_t* labels_dev, const float* roww_dev,
+                                  int64_t rows, int64_t features, int64_t classes, mpcnn_dtype dtype,
+                                  float* rowloss_dev, double* loss_dev, void* dx_dev, int64_t dx_pitch,
+                                  void* dw_dev, float* db_dev, void* ws_dev, size_t ws_bytes, void* hip_stream);
+
+/*
  * The loss alone, L as in mpcnn_seg_backward for the current parameters: a forward pass that
  * keeps nothing and computes no gradient (the evaluations of a line search).
  *   loss_dev: one fp64 on the device.  ws_dev: at least mpcnn_workspace_bytes(net,B,H,W,0).

@@ -1,0 +1,376 @@
+// The class layer on rows of features with its softmax cross-entropy and its gradients, for label sets of any size (see include/mpcnn.h,
+// mpcnn_class_loss and mpcnn_class_backward): the plan, the workspace and the launches.
+//
+//   scores s[v][n] = w[v] . x[n] + bias[v],  lse[n] = log sum_v exp s[v][n],  loss[n] = weight[n] (lse[n] - s[label[n]][n])
+//   delta[n][v] = exp(s[v][n] - lse[n]) - [v = label[n]]
+//   dx[n] = weight[n] sum_v delta[n][v] w[v],   dw[v] = sum_n weight[n] delta[n][v] x[n],   db[v] = sum_n weight[n] delta[n][v]
+//
+// The classes are taken in pieces.  A first round over them leaves, per row, each tile's largest score and sum of exponentials, and no scores.
+// The second computes a piece's scores again, turns them into the derivative and multiplies that with the weights and the features
+// (kernels_rows_product.hpp).  Where the scores of all classes fit the room that a piece's take (kRoom), they are kept from the first round.
+#include <algorithm>
+#include <atomic>
+#include <cstdint>
+
+#include "kernels_rows_parts.hpp"
+#include "kernels_rows_product.hpp"
+#include "status.hpp"
+
+using mpcnn::fail;
+
+namespace {
+
+constexpr int64_t kMaxRows = 1 << 20, kMaxFeatures = 1 << 20, kMaxClasses = 0x7fffffff - 1024;   // (32-bit offsets inside a tile)
+constexpr int64_t kRoom = (int64_t)1 << 27;            // scores of a piece: 0.5 GB in fp32, and as much of derivatives in both orders
+constexpr int64_t kWeightRoom = (int64_t)512 << 20;    // bytes of a piece's class weights, brought into blocks
+constexpr int64_t kPartRoom = (int64_t)256 << 20;      // bytes of a product's partial sums
+constexpr int kMaxPiece = 1 << 20;
+constexpr int kCUs = 256;
+
+inline int64_t up_to(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
+
+struct Tiling { bool big; int tiles_m, tiles_n, splits, per_split; };
+
+// Tiles of 256 x 256 where they give most compute units one, of 128 x 128 (two of their workgroups share a compute unit) otherwise.  Where few
+// of either, the sum over k is split, no further than kLeast blocks.
+Tiling tiling_of(int64_t M, int64_t N, int64_t blocks, int64_t most_splits)
+{
+    constexpr int kLeast = 8;
+    Tiling t{};
+    M = std::max<int64_t>(M, 1); N = std::max<int64_t>(N, 1);   // (no rows: nothing is launched)
+    const int64_t big = (M + 255) / 256 * ((N + 255) / 256), small = (M + 127) / 128 * ((N + 127) / 128);
+    int64_t splits = 1;
+    const int64_t can = std::max<int64_t>(1, std::min(most_splits, blocks / kLeast));
+    t.big = big * can >= kCUs * 3 / 4;
+    if (t.big) splits = std::min(can, std::max<int64_t>(1, kCUs / big));
+    else splits = std::min(can, std::max<int64_t>(1, 2 * kCUs / small));
+    const int64_t side = t.big ? 256 : 128;
+    t.tiles_m = (int)((M + side - 1) / side);
+    t.tiles_n = (int)((N + side - 1) / side);
+    t.per_split = (int)((blocks + splits - 1) / splits);
+    t.splits = (int)((blocks + t.per_split - 1) / t.per_split);
+    return t;
+}
+
+struct Plan {
+    bool halves, train, keep;
+    int N, D;
+    int64_t V, Np;                       // Np: rows, padded to whole blocks
+    int64_t d_bytes, n_bytes;            // a row of blocks along the features, along the rows
+    int64_t piece;                       // classes
+    int64_t stat_tiles;
+    Tiling dx, dw;                       // of a whole piece
+    size_t peaks, stats, label_score, lse, weight, loss_part, x_rows, x_cols, w_rows, w_cols, score, delta_rows, delta_cols, db_part,
+        dx_part, dw_part, total;
+    int64_t bytes_along(int64_t n) const { return halves ? up_to(n, 32) * 4 : up_to(n, 64) * 2; }
+    bool dx_parts() const { return dx.splits > 1 || piece < V; }
+};
+
+bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool train, Plan* p)
+{
+    if (rows < 0 || rows > kMaxRows || features < 1 || features > kMaxFeatures || classes < 1 || classes > kMaxClasses) return false;
+    *p = Plan{};
+    p->halves = dtype == MPCNN_F32;
+    p->train = train;
+    p->N = (int)rows; p->D = (int)features; p->V = classes;
+    p->Np = up_to(std::max<int64_t>(rows, 1), 64);
+    p->d_bytes = p->bytes_along(features);
+    p->n_bytes = p->bytes_along(p->Np);
+    int64_t piece = std::min<int64_t>(classes, kMaxPiece);
+    auto bound = [&](int64_t most) { if (piece > most) piece = std::max<int64_t>(256, most / 256 * 256); };
+    bound(kWeightRoom / p->d_bytes);
+    p->keep = train && classes <= kRoom / p->Np;
+    if (train) bound(kRoom / p->Np);
+    p->piece = piece;
+    const int64_t pieces = (classes + piece - 1) / piece;
+    const int64_t v_bytes = p->bytes_along(piece);
+    p->stat_tiles = (classes + 127) / 128 + pieces;
+    size_t at = 0;
+    auto take = [&](int64_t bytes) { const size_t o = at; at += (size_t)up_to(bytes, 256); return o; };
+    const int64_t N = p->N, D = p->D;
+    p->peaks = take(4 * 3 * mpcnn::kPeakGroups);
+    p->stats = take(8 * p->stat_tiles * N);
+    p->label_score = take(4 * N);
+    p->lse = take(4 * N);
+    p->weight = take(4 * N);
+    p->loss_part = take(8 * ((N + mpcnn::kJoinRows - 1) / mpcnn::kJoinRows));
+    p->x_rows = take(N * p->d_bytes);
+    p->w_rows = take(piece * p->d_bytes);
+    if (train) {
+        p->dx = tiling_of(N, D, v_bytes / mpcnn::kBlockBytes, std::max<int64_t>(1, kPartRoom / (4 * N * D + 1)));
+        p->dw = tiling_of(piece, D, p->n_bytes / mpcnn::kBlockBytes, std::max<int64_t>(1, kPartRoom / (4 * piece * D)));
+        p->x_cols = take(D * p->n_bytes);
+        p->w_cols = take(D * v_bytes);
+        p->score = take((p->keep ? classes : piece) * p->Np * 4);
+        p->delta_rows = take(N * v_bytes);
+        p->delta_cols = take(piece * p->n_bytes);
+        p->db_part = take(p->Np / 64 * piece * 4);
+        if (p->dx_parts()) p->dx_part = take(4 * (int64_t)p->dx.splits * N * D);
+        if (p->dw.splits > 1) p->dw_part = take(4 * (int64_t)p->dw.splits * piece * D);
+    }
+    p->total = at;
+    return true;
+}
+
+// ---- launches of the product
+template <int WM, int WN, int MT, int NT, bool HALVES, int RESULT>
+mpcnn_status launch_instance(const mpcnn::ProductArgs& a, hipStream_t st)
+{
+    constexpr int lds = 2 * 32 * (WM * MT + WN * NT) * mpcnn::kBlockBytes;
+    auto* kernel = &mpcnn::rows_product_kernel<WM, WN, MT, NT, HALVES, RESULT>;
+    if constexpr (lds > 64 * 1024) {       // must be said once per device
+        static std::atomic<uint64_t> said{0};
+        int dev = 0;
+        HIP_TRY(hipGetDevice(&dev));
+        if (!(said.load(std::memory_order_relaxed) >> (dev & 63) & 1)) {
+            HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+            said.fetch_or(1ull << (dev & 63), std::memory_order_relaxed);
+        }
+    }
+    const int64_t all = (int64_t)a.tiles_m * a.tiles_n * a.splits;
+    kernel<<<(unsigned)up_to(all, 8), 64 * WM * WN, lds, st>>>(a);
+    return MPCNN_OK;
+}
+template <bool HALVES, int RESULT>
+mpcnn_status launch_product(mpcnn::ProductArgs a, const Tiling& t, hipStream_t st)
+{
+    a.tiles_m = t.tiles_m; a.tiles_n = t.tiles_n; a.splits = t.splits; a.per_split = t.per_split;
+    return t.big ? launch_instance<2, 2, 4, 4, HALVES, RESULT>(a, st) : launch_instance<2, 2, 2, 2, HALVES, RESULT>(a, st);
+}
+
+struct Call {
+    const void *x, *w;
+    int64_t x_pitch, w_pitch;
+    const float* bias;
+    const int32_t* labels;
+    const float* roww;
+    float *rowloss, *lse;
+    double* loss;
+    void* dx;
+    int64_t dx_pitch;
+    void* dw;
+    float* db;
+};
+
+template <typename T>
+mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
+{
+    constexpr bool H = sizeof(T) == 4;
+    constexpr int kStore = H ? mpcnn::kStoreF32 : mpcnn::kStoreBf16;
+    if (!p.N) {
+        mpcnn::rows_none_kernel<<<(unsigned)std::min<int64_t>(4096, (p.V * p.D + 255) / 256), 256, 0, st>>>((char*)c.dw, p.V * p.D * (long)sizeof(T), c.db, p.V,
+                                                                                                      c.loss);
+        HIP_TRY(hipGetLastError());
+        return MPCNN_OK;
+    }
+    const mpcnn::RowMask every{}, mask{c.labels, c.roww, (int)p.V};
+    unsigned* const x_peak = (unsigned*)(ws + p.peaks);
+    unsigned *const w_peak = x_peak + mpcnn::kPeakGroups, *const roww_peak = w_peak + mpcnn::kPeakGroups;
+    if constexpr (H) {
+        auto peak = [&](const void* src, int64_t pitch, int64_t rows, int64_t cols, const mpcnn::RowMask& m, unsigned* words) {
+            mpcnn::PeakArgs a{(const float*)src, pitch, rows, (int)cols, m, words};
+            mpcnn::rows_peak_kernel<<<mpcnn::kPeakGroups, 256, 0, st>>>(a);
+        };
+        peak(c.x, c.x_pitch, p.N, p.D, mask, x_peak);
+        peak(c.w, c.w_pitch, p.V, p.D, every, w_peak);
+        if (p.train && c.roww) peak(c.roww, 1, p.N, 1, mask, roww_peak);
+    }
+    auto pack = [&](const void* src, int64_t pitch, int64_t R, char* rows, char* cols, int64_t col_bytes, const mpcnn::RowMask& m, const unsigned* words) {
+        mpcnn::PackRowsArgs a{};
+        a.src = src; a.pitch = pitch; a.R = (int)R; a.C = p.D;
+        a.rows = rows; a.cols = cols; a.row_bytes = p.d_bytes; a.col_bytes = col_bytes;
+        a.mask = m; a.peak = words;
+        mpcnn::rows_pack_kernel<T><<<dim3((unsigned)((R + 63) / 64), (unsigned)((p.D + 63) / 64)), 256, 0, st>>>(a);
+    };
+    // operands as they are: whole blocks at aligned addresses
+    auto direct = [&](const void* m, int64_t pitch) { return !H && p.D % 64 == 0 && (uintptr_t)m % 16 == 0 && pitch % 8 == 0 && pitch * 512 < (1ll << 31); };
+    const bool x_direct = direct(c.x, c.x_pitch), w_direct = direct(c.w, c.w_pitch);
+    if (!x_direct || p.train)
+        pack(c.x, c.x_pitch, p.N, x_direct ? nullptr : ws + p.x_rows, p.train ? ws + p.x_cols : nullptr, p.n_bytes, mask, x_peak);
+
+    // a piece's scores
+    const int64_t piece = !p.train && w_direct ? std::min<int64_t>(p.V, kMaxPiece) : p.piece;
+    const int d_blocks = (int)(p.d_bytes / mpcnn::kBlockBytes);
+    auto scores = [&](int64_t v0, int64_t n_classes, const char* w_rows, int64_t w_row, float2* stats, float* out, int* tiles) {
+        mpcnn::ProductArgs a{};
+        a.A = w_rows; a.a_row = w_row;
+        a.B = x_direct ? (const char*)c.x : ws + p.x_rows; a.b_row = x_direct ? c.x_pitch * 2 : p.d_bytes;
+        a.M = (int)n_classes; a.N = p.N; a.blocks = d_blocks;
+        a.a_peak = H ? w_peak : nullptr; a.b_peak = H ? x_peak : nullptr; a.a_words = a.b_words = mpcnn::kPeakGroups;
+        a.bias = c.bias ? c.bias + v0 : nullptr;
+        a.labels = c.labels; a.stats = stats; a.label_score = (float*)(ws + p.label_score);
+        a.scores = out; a.score_row = p.Np; a.class0 = (int)v0;
+        const Tiling t = tiling_of(n_classes, p.N, d_blocks, 1);
+        if (tiles) *tiles = t.tiles_m;
+        return launch_product<H, mpcnn::kScores>(a, t, st);
+    };
+    auto weights_of = [&](int64_t v0, int64_t n_classes, bool rows, bool cols, int64_t v_bytes) {   // (and whether blocks along the features are in memory already)
+        if ((!rows || w_direct) && !cols) return;
+        pack((const char*)c.w + v0 * c.w_pitch * (int64_t)sizeof(T), c.w_pitch, n_classes, rows && !w_direct ? ws + p.w_rows : nullptr,
+             cols ? ws + p.w_cols : nullptr, v_bytes, every, w_peak);
+    };
+    auto rows_at = [&](int64_t v0) { return w_direct ? (const char*)c.w + v0 * c.w_pitch * 2 : (const char*)(ws + p.w_rows); };
+    const int64_t w_row = w_direct ? c.w_pitch * 2 : p.d_bytes;
+
+    float* const score = p.train ? (float*)(ws + p.score) : nullptr;
+    const bool one_piece = p.train && p.V <= piece;      // its weights are brought into both orders at once
+    int done = 0;
+    for (int64_t v0 = 0; v0 < p.V; v0 += piece) {
+        const int64_t n = std::min(piece, p.V - v0);
+        weights_of(v0, n, true, one_piece && c.dx, p.bytes_along(n));
+        int tiles = 0;
+        const mpcnn_status rc = scores(v0, n, rows_at(v0), w_row, (float2*)(ws + p.stats) + (int64_t)done * p.N, p.keep ? score + v0 * p.Np : nullptr, &tiles);
+        if (rc != MPCNN_OK) return rc;
+        done += tiles;
+    }
+    const int join_groups = (p.N + mpcnn::kJoinRows - 1) / mpcnn::kJoinRows;
+    mpcnn::JoinArgs j{};
+    j.stats = (const float2*)(ws + p.stats); j.tiles = done; j.N = p.N;
+    j.label_score = (const float*)(ws + p.label_score); j.mask = mask;
+    if (p.train) { j.lse = (float*)(ws + p.lse); j.weight = (float*)(ws + p.weight); }
+    j.lse_out = c.lse; j.rowloss = c.rowloss;
+    j.loss_part = c.loss ? (double*)(ws + p.loss_part) : nullptr;
+    mpcnn::rows_join_kernel<<<(unsigned)join_groups, 256, 0, st>>>(j);
+
+    mpcnn::FinishArgs fin{};
+    fin.loss_part = j.loss_part; fin.loss_parts = join_groups; fin.loss = c.loss;
+    if (!p.train) {
+        if (c.loss) mpcnn::rows_finish_kernel<<<1, 256, 0, st>>>(fin);
+        HIP_TRY(hipGetLastError());
+        return MPCNN_OK;
+    }
+    for (int64_t v0 = 0; v0 < p.V; v0 += piece) {
+        const int64_t n = std::min(piece, p.V - v0), v_bytes = p.bytes_along(n);
+        const bool last = v0 + n == p.V;
+        if (!one_piece) weights_of(v0, n, !p.keep, c.dx != nullptr, v_bytes);
+        float* const s = p.keep ? score + v0 * p.Np : score;
+        if (!p.keep) {
+            const mpcnn_status rc = scores(v0, n, rows_at(v0), w_row, nullptr, s, nullptr);
+            if (rc != MPCNN_OK) return rc;
+        }
+        mpcnn::DeltaArgs d{};
+        d.scores = s; d.score_row = p.Np; d.classes = (int)n; d.class0 = (int)v0; d.N = p.N;
+        d.labels = c.labels; d.lse = j.lse; d.weight = j.weight;
+        if (c.dx) { d.rows = ws + p.delta_rows; d.row_bytes = v_bytes; }
+        if (c.dw) { d.cols = ws + p.delta_cols; d.col_bytes = p.n_bytes; }
+        d.weight_peak = H && c.roww ? roww_peak : nullptr;
+        d.db_part = c.db ? (float*)(ws + p.db_part) : nullptr;
+        mpcnn::rows_delta_kernel<H><<<dim3((unsigned)(p.Np / 64), (unsigned)((n + 63) / 64)), 256, 0, st>>>(d);
+        fin.db_part = d.db_part; fin.tiles = (int)(p.Np / 64); fin.classes = n; fin.db = c.db ? c.db + v0 : nullptr;
+        if (fin.db || fin.loss) mpcnn::rows_finish_kernel<<<fin.db ? (unsigned)((n + 255) / 256) : 1, 256, 0, st>>>(fin);
+        fin.loss = nullptr;
+        if (c.dx) {
+            mpcnn::ProductArgs a{};
+            a.A = ws + p.delta_rows; a.a_row = v_bytes; a.B = ws + p.w_cols; a.b_row = v_bytes;
+            a.M = p.N; a.N = p.D; a.blocks = (int)(v_bytes / mpcnn::kBlockBytes);
+            a.a_up = 14; a.b_peak = H ? w_peak : nullptr; a.b_words = mpcnn::kPeakGroups;
+            a.out = c.dx; a.out_row = c.dx_pitch; a.row_scale = j.weight;
+            Tiling t = p.dx;
+            t.per_split = (int)((a.blocks + t.splits - 1) / t.splits);
+            mpcnn_status rc;
+            if (p.dx_parts()) {
+                a.part = (float*)(ws + p.dx_part); a.add = v0 > 0;
+                rc = launch_product<H, mpcnn::kPart>(a, t, st);
+                if (last) {
+                    mpcnn::SumArgs sum{};
+                    sum.part = a.part; sum.splits = t.splits; sum.M = p.N; sum.N = p.D; sum.out_row = c.dx_pitch;
+                    sum.a_up = 14; sum.b_peak = a.b_peak; sum.halves = H; sum.row_scale = j.weight; sum.out = c.dx; sum.out_bf16 = !H;
+                    mpcnn::rows_sum_kernel<<<(unsigned)std::min<int64_t>(4096, ((int64_t)p.N * p.D + 255) / 256), 256, 0, st>>>(sum);
+                }
+            } else {
+                rc = launch_product<H, kStore>(a, t, st);
+            }
+            if (rc != MPCNN_OK) return rc;
+        }
+        if (c.dw) {
+            mpcnn::ProductArgs a{};
+            a.A = ws + p.delta_cols; a.a_row = p.n_bytes; a.B = ws + p.x_cols; a.b_row = p.n_bytes;
+            a.M = (int)n; a.N = p.D; a.blocks = (int)(p.n_bytes / mpcnn::kBlockBytes);
+            a.a_peak = d.weight_peak; a.a_words = mpcnn::kPeakGroups; a.a_up = 14;
+            a.b_peak = H ? x_peak : nullptr; a.b_words = mpcnn::kPeakGroups;
+            a.out = (char*)c.dw + v0 * p.D * (int64_t)sizeof(T); a.out_row = p.D;
+            Tiling t = p.dw;
+            t.tiles_m = (int)((n + (t.big ? 255 : 127)) / (t.big ? 256 : 128));
+            mpcnn_status rc;
+            if (t.splits > 1) {
+                a.part = (float*)(ws + p.dw_part);
+                rc = launch_product<H, mpcnn::kPart>(a, t, st);
+                mpcnn::SumArgs sum{};
+                sum.part = a.part; sum.splits = t.splits; sum.M = n; sum.N = p.D; sum.out_row = p.D;
+                sum.a_peak = a.a_peak; sum.a_up = 14; sum.b_peak = a.b_peak; sum.halves = H; sum.out = a.out; sum.out_bf16 = !H;
+                mpcnn::rows_sum_kernel<<<(unsigned)std::min<int64_t>(4096, (n * p.D + 255) / 256), 256, 0, st>>>(sum);
+            } else {
+                rc = launch_product<H, kStore>(a, t, st);
+            }
+            if (rc != MPCNN_OK) return rc;
+        }
+    }
+    HIP_TRY(hipGetLastError());
+    return MPCNN_OK;
+}
+
+struct Span { uintptr_t at; uint64_t bytes; };
+bool meet(const Span& a, const Span& b) { return a.at && b.at && a.bytes && b.bytes && a.at < b.at + b.bytes && b.at < a.at + a.bytes; }
+
+mpcnn_status checked(int64_t rows, int64_t features, int64_t classes, mpcnn_dtype dtype, const Call& c, bool train, void* ws, size_t ws_bytes, void* stream)
+{
+    if (rows < 0 || features < 1 || classes < 1) return fail(MPCNN_EINVAL, "%lld rows, %lld features, %lld classes", (long long)rows, (long long)features, (long long)classes);
+    if (dtype != MPCNN_F32 && dtype != MPCNN_BF16) return fail(MPCNN_EINVAL, "unknown type %d", (int)dtype);
+    if (!c.w || !ws || (rows > 0 && (!c.x || !c.labels))) return fail(MPCNN_EINVAL, "null argument");
+    if (c.x_pitch < features || c.w_pitch < features || (c.dx && c.dx_pitch < features))
+        return fail(MPCNN_EINVAL, "a pitch is below the %lld features", (long long)features);
+    const int64_t size = dtype == MPCNN_F32 ? 4 : 2, most_pitch = (int64_t)1 << 40;
+    if (c.x_pitch > most_pitch || c.w_pitch > most_pitch || (c.dx && c.dx_pitch > most_pitch)) return fail(MPCNN_EINVAL, "a pitch is above 2^40");
+    const uintptr_t typed = (uintptr_t)c.x | (uintptr_t)c.w | (uintptr_t)c.dx | (uintptr_t)c.dw;
+    const uintptr_t words = (uintptr_t)c.bias | (uintptr_t)c.labels | (uintptr_t)c.roww | (uintptr_t)c.rowloss | (uintptr_t)c.lse | (uintptr_t)c.db;
+    if (typed % size || words % 4 || (uintptr_t)c.loss % 8) return fail(MPCNN_EINVAL, "an address is no multiple of its element's size");
+    Plan p;
+    if (!make_plan(rows, features, classes, dtype, train, &p))
+        return fail(MPCNN_EUNSUPPORTED, "%lld rows, %lld features, %lld classes: at most %lld, %lld, %lld", (long long)rows, (long long)features,
+                    (long long)classes, (long long)kMaxRows, (long long)kMaxFeatures, (long long)kMaxClasses);
+    if (ws_bytes < p.total) return fail(MPCNN_EWORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, p.total);
+    if ((uintptr_t)ws & 255u) return fail(MPCNN_EINVAL, "workspace must be 256-byte aligned");
+    auto spread = [&](const void* m, int64_t n, int64_t pitch) { return Span{(uintptr_t)m, n ? (uint64_t)(((n - 1) * pitch + features) * size) : 0}; };
+    const uint64_t n4 = 4 * (uint64_t)rows, v4 = 4 * (uint64_t)classes;
+    const Span in[] = {spread(c.x, rows, c.x_pitch), spread(c.w, classes, c.w_pitch), {(uintptr_t)c.bias, v4}, {(uintptr_t)c.labels, n4}, {(uintptr_t)c.roww, n4}};
+    const Span out[] = {{(uintptr_t)ws, p.total}, {(uintptr_t)c.rowloss, n4}, {(uintptr_t)c.lse, n4}, {(uintptr_t)c.loss, 8},
+                        spread(c.dx, rows, c.dx_pitch), spread(c.dw, classes, features), {(uintptr_t)c.db, v4}};
+    for (size_t i = 0; i < sizeof out / sizeof *out; ++i) {
+        for (const Span& s : in)
+            if (meet(out[i], s)) return fail(MPCNN_EINVAL, "an output or the workspace overlaps an input");
+        for (size_t j = 0; j < i; ++j)
+            if (meet(out[i], out[j])) return fail(MPCNN_EINVAL, "two outputs, or one and the workspace, overlap");
+    }
+    return dtype == MPCNN_F32 ? run<float>(p, c, (char*)ws, (hipStream_t)stream) : run<mpcnn::bf16>(p, c, (char*)ws, (hipStream_t)stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t mpcnn_workspace_bytes_class(int64_t rows, int64_t features, int64_t classes, mpcnn_dtype dtype, int training)
+{
+    Plan p;
+    if ((dtype != MPCNN_F32 && dtype != MPCNN_BF16) || !make_plan(rows, features, classes, dtype, training != 0, &p)) return 0;
+    return p.total;
+}
+
+mpcnn_status mpcnn_class_loss(const void* x_dev, int64_t x_pitch, const void* w_dev, int64_t w_pitch, const float* bias_dev,
+                              const int32_t* labels_dev, const float* roww_dev, int64_t rows, int64_t features, int64_t classes,
+                              mpcnn_dtype dtype, float* rowloss_dev, float* lse_dev, double* loss_dev, void* ws_dev, size_t ws_bytes,
+                              void* hip_stream)
+{
+    const Call c{x_dev, w_dev, x_pitch, w_pitch, bias_dev, labels_dev, roww_dev, rowloss_dev, lse_dev, loss_dev, nullptr, 0, nullptr, nullptr};
+    return checked(rows, features, classes, dtype, c, false, ws_dev, ws_bytes, hip_stream);
+}
+
+mpcnn_status mpcnn_class_backward(const void* x_dev, int64_t x_pitch, const void* w_dev, int64_t w_pitch, const float* bias_dev,
+                                  const int32_t* labels_dev, const float* roww_dev, int64_t rows, int64_t features, int64_t classes,
+                                  mpcnn_dtype dtype, float* rowloss_dev, double* loss_dev, void* dx_dev, int64_t dx_pitch, void* dw_dev,
+                                  float* db_dev, void* ws_dev, size_t ws_bytes, void* hip_stream)
+{
+    const Call c{x_dev, w_dev, x_pitch, w_pitch, bias_dev, labels_dev, roww_dev, rowloss_dev, nullptr, loss_dev, dx_dev, dx_pitch, dw_dev, db_dev};
+    return checked(rows, features, classes, dtype, c, true, ws_dev, ws_bytes, hip_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,368 @@
+// Around the matrix products of the class layer on rows of features (class_rows.hip): operands brought into blocks of 16-bit numbers, as they
+// are and transposed; the softmax's statistics joined; scores turned into the loss's derivative; partial sums added up.
+// All of it is bound by memory: 64 x 64 tiles through LDS, each number read once and written in both orders where both are needed.
+#pragma once
+#include "ranges.hpp"
+#include "storage.hpp"
+
+namespace mpcnn {
+
+constexpr int kPeakGroups = 256;           // words of a peak
+constexpr int kJoinRows = 32;              // rows of a workgroup of rows_join_kernel
+
+// Rows that add something: a label among the classes and a weight that is not zero
+struct RowMask {
+    const int* labels;
+    const float* weights;                  // null: 1
+    int classes;
+};
+__device__ __forceinline__ float row_weight(const RowMask& m, int n)
+{
+    const int t = m.labels[n];
+    if (t < 0 || t >= m.classes) return 0.f;
+    return m.weights ? m.weights[n] : 1.f;
+}
+
+// ---- the largest magnitude of a matrix, as bits (one word per workgroup); what is not finite is passed over
+struct PeakArgs {
+    const float* src;
+    long pitch;
+    long rows;
+    int cols;
+    RowMask mask;                          // labels null: every row
+    unsigned* words;                       // [kPeakGroups]
+};
+__global__ __launch_bounds__(256) void rows_peak_kernel(PeakArgs a)
+{
+    __shared__ unsigned red[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    unsigned peak = 0;
+    auto add = [&](float x) {
+        const unsigned b = bits_of(x) & 0x7fffffffu;
+        peak = b < kNoPeak && b > peak ? b : peak;
+    };
+    if (a.pitch == a.cols && !a.mask.labels) {           // one stretch
+        const long n = a.rows * a.cols, step = (long)gridDim.x * 256;
+        long e = (long)blockIdx.x * 256 + threadIdx.x;
+        for (; e + 7 * step < n; e += 8 * step) {        // eight loads in flight
+            float v[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] = a.src[e + q * step];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) add(v[q]);
+        }
+        for (; e < n; e += step) add(a.src[e]);
+    } else {
+        for (long r = (long)blockIdx.x * 4 + wave; r < a.rows; r += (long)gridDim.x * 4) {
+            if (a.mask.labels && row_weight(a.mask, (int)r) == 0.f) continue;
+            for (int c = lane; c < a.cols; c += 64) add(a.src[r * a.pitch + c]);
+        }
+    }
+    peak = wave_largest(peak);
+    if (lane == 0) red[wave] = peak;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        unsigned m = red[0];
+        for (int w = 1; w < 4; ++w) m = red[w] > m ? red[w] : m;
+        a.words[blockIdx.x] = m;
+    }
+}
+
+// ---- blocks: 64 bf16 numbers, or the two parts of 32 fp32 ones (kernels_rows_product.hpp)
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+
+// Piece p (16 bytes) of the 128 (bf16) or 256 (parts) bytes that 64 numbers take; get(i) is the i-th of them, raised
+template <bool HALVES, typename F>
+__device__ __forceinline__ v4f piece_of(int p, F get)
+{
+    if constexpr (HALVES) {
+        f16x8_t v;
+        const int at = 32 * (p >> 3) + 8 * (p & 3);
+        const bool low = (p & 4) != 0;
+#pragma unroll
+        for (int z = 0; z < 8; ++z) {
+            const float x = get(at + z);
+            const _Float16 h = (_Float16)x;
+            v[z] = low ? (_Float16)(x - (float)h) : h;
+        }
+        return __builtin_bit_cast(v4f, v);
+    } else {
+        bf16x8_t v;
+#pragma unroll
+        for (int z = 0; z < 8; ++z) v[z] = (__bf16)get(8 * p + z);
+        return __builtin_bit_cast(v4f, v);
+    }
+}
+
+// ---- a matrix [R][C] into blocks along its rows (`rows`: [R][row_bytes]) and along its columns (`cols`: [C][col_bytes]), either may be null.
+// Padding is zero, rows that add nothing are too.
+struct PackRowsArgs {
+    const void* src;
+    long pitch;                            // elements
+    int R, C;
+    char *rows, *cols;
+    long row_bytes, col_bytes;
+    RowMask mask;                          // labels null: every row
+    const unsigned* peak;                  // fp32: [kPeakGroups], what the numbers are raised by
+};
+template <typename T>
+__global__ __launch_bounds__(256) void rows_pack_kernel(PackRowsArgs a)
+{
+    constexpr bool HALVES = sizeof(T) == 4;
+    constexpr int kPieces = HALVES ? 16 : 8;
+    __shared__ float tile[64][65];
+    const int c0 = 64 * blockIdx.y, r0 = 64 * blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float up = 1.f;
+    if constexpr (HALVES) up = power_of_two(raise_of(peak_of(a.peak, kPeakGroups), 0));
+    const T* src = (const T*)a.src;
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int r = r0 + wave + 4 * i, c = c0 + lane;
+        const bool there = r < a.R && c < a.C && (!a.mask.labels || row_weight(a.mask, r) != 0.f);
+        v[i] = there ? load1(src + (long)r * a.pitch + c) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) tile[wave + 4 * i][lane] = v[i] * up;
+    __syncthreads();
+    if (a.rows)
+        for (int q = threadIdx.x; q < 64 * kPieces; q += 256) {
+            const int r = q / kPieces, p = q % kPieces;
+            const long at = (long)blockIdx.y * (kPieces * 16) + 16 * p;
+            if (r0 + r >= a.R || at >= a.row_bytes) continue;
+            *reinterpret_cast<v4f*>(a.rows + (long)(r0 + r) * a.row_bytes + at) = piece_of<HALVES>(p, [&](int i) { return tile[r][i]; });
+        }
+    if (a.cols)
+        for (int q = threadIdx.x; q < 64 * kPieces; q += 256) {
+            const int c = q / kPieces, p = q % kPieces;
+            const long at = (long)blockIdx.x * (kPieces * 16) + 16 * p;
+            if (c0 + c >= a.C || at >= a.col_bytes) continue;
+            *reinterpret_cast<v4f*>(a.cols + (long)(c0 + c) * a.col_bytes + at) = piece_of<HALVES>(p, [&](int i) { return tile[i][c]; });
+        }
+}
+
+// ---- per row: the statistics of all tiles of classes joined; the loss; per workgroup its share of the summed loss
+struct JoinArgs {
+    const float2* stats;                   // [tiles][N]
+    int tiles, N;
+    const float* label_score;              // [N]
+    RowMask mask;
+    float *lse, *rowloss, *weight;         // [N]: lse for the derivative, results (null: not asked for), the row's weight or 0
+    float* lse_out;
+    double* loss_part;                     // per workgroup, or null
+};
+__global__ __launch_bounds__(256) void rows_join_kernel(JoinArgs a)
+{
+    __shared__ float2 red[8][kJoinRows];
+    __shared__ double sums[kJoinRows];
+    const int own = threadIdx.x % kJoinRows, deal = threadIdx.x / kJoinRows;
+    const int n = blockIdx.x * kJoinRows + own;
+    constexpr float kNone = -__builtin_inff();
+    auto join = [](float2 s, float2 o) {
+        const float top = fmaxf(s.x, o.x), base = top == kNone ? 0.f : top;
+        return float2{top, s.y * __expf(s.x - base) + o.y * __expf(o.x - base)};
+    };
+    float2 s{kNone, 0.f};
+    if (n < a.N) {
+        int t = deal;
+        for (; t + 24 < a.tiles; t += 32) {
+            float2 v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = a.stats[(long)(t + 8 * q) * a.N + n];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) s = join(s, v[q]);
+        }
+        for (; t < a.tiles; t += 8) s = join(s, a.stats[(long)t * a.N + n]);
+    }
+    red[deal][own] = s;
+    __syncthreads();
+    if (deal == 0) {
+        double share = 0.0;
+        if (n < a.N) {
+            for (int d = 1; d < 8; ++d) s = join(s, red[d][own]);
+            const float lse = s.x == kNone ? kNone : s.x + logf(s.y);
+            const float w = row_weight(a.mask, n);
+            float loss = 0.f;
+            if (w != 0.f) {
+                const float score = a.label_score[n];
+                loss = w * (score == kNone ? __builtin_inff() : lse - score);   // (a class that is switched off)
+            }
+            if (a.lse) a.lse[n] = lse;
+            if (a.weight) a.weight[n] = w;
+            if (a.lse_out) a.lse_out[n] = w != 0.f ? lse : 0.f;
+            if (a.rowloss) a.rowloss[n] = loss;
+            share = (double)loss;
+        }
+        sums[own] = share;
+    }
+    if (!a.loss_part) return;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double all = 0.0;
+        for (int i = 0; i < kJoinRows; ++i) all += sums[i];
+        a.loss_part[blockIdx.x] = all;
+    }
+}
+
+// ---- scores [classes][score_row] of a piece of the classes into the derivative p - [class = label], in blocks: along the classes as it is
+// (`rows`: [N][row_bytes], the data gradient's operand; the row's weight follows behind the product) and along the rows times the row's
+// weight (`cols`: [classes][col_bytes], the weight gradient's).  db_part: per tile of 64 rows the sums over them.
+struct DeltaArgs {
+    const float* scores;
+    long score_row;
+    int classes, class0, N;
+    const int* labels;
+    const float *lse, *weight;             // [N]
+    char *rows, *cols;
+    long row_bytes, col_bytes;
+    const unsigned* weight_peak;           // fp32: the weights' (null: all are 1)
+    float* db_part;                        // [tiles of rows][classes], or null
+};
+template <bool HALVES>
+__global__ __launch_bounds__(256) void rows_delta_kernel(DeltaArgs a)
+{
+    constexpr int kPieces = HALVES ? 16 : 8;
+    __shared__ float tile[64][65];
+    __shared__ float weight[64];
+    __shared__ float sums[4][64];
+    const int n0 = 64 * blockIdx.x, v0 = 64 * blockIdx.y;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = n0 + lane;
+    const bool real = n < a.N;
+    const float w = real ? a.weight[n] : 0.f, lse = real ? a.lse[n] : 0.f;
+    const int label = real ? a.labels[n] - a.class0 : -1;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int v = v0 + wave + 4 * i;
+        x[i] = v < a.classes && w != 0.f ? a.scores[(long)v * a.score_row + n] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int v = v0 + wave + 4 * i;
+        float g = 0.f;
+        if (v < a.classes && w != 0.f) {
+            g = x[i] == -__builtin_inff() ? 0.f : expf(x[i] - lse);
+            if (v == label) g -= 1.f;
+        }
+        tile[wave + 4 * i][lane] = g;
+    }
+    if (wave == 0) weight[lane] = w;
+    __syncthreads();
+    float up_r = 1.f, up_c = 1.f;
+    if constexpr (HALVES) {
+        up_r = power_of_two(14);
+        up_c = power_of_two(a.weight_peak ? raise_of(peak_of(a.weight_peak, kPeakGroups), 0) : 14);
+    }
+    if (a.db_part) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += tile[lane][16 * wave + i] * weight[16 * wave + i];
+        sums[wave][lane] = s;
+    }
+    if (a.rows)
+        for (int q = threadIdx.x; q < 64 * kPieces; q += 256) {
+            const int r = q / kPieces, p = q % kPieces;
+            const long at = (long)blockIdx.y * (kPieces * 16) + 16 * p;
+            if (n0 + r >= a.N || at >= a.row_bytes) continue;
+            *reinterpret_cast<v4f*>(a.rows + (long)(n0 + r) * a.row_bytes + at) = piece_of<HALVES>(p, [&](int i) { return tile[i][r] * up_r; });
+        }
+    if (a.cols)
+        for (int q = threadIdx.x; q < 64 * kPieces; q += 256) {
+            const int c = q / kPieces, p = q % kPieces;
+            const long at = (long)blockIdx.x * (kPieces * 16) + 16 * p;
+            if (v0 + c >= a.classes || at >= a.col_bytes) continue;
+            *reinterpret_cast<v4f*>(a.cols + (long)(v0 + c) * a.col_bytes + at) = piece_of<HALVES>(p, [&](int i) { return tile[c][i] * weight[i] * up_c; });
+        }
+    if (a.db_part) {
+        __syncthreads();
+        if (wave == 0 && v0 + lane < a.classes)
+            a.db_part[(long)blockIdx.x * a.classes + v0 + lane] = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    }
+}
+
+// ---- partial sums [splits][M][N] of a product added up, lowered, scaled and rounded
+struct SumArgs {
+    const float* part;
+    int splits;
+    long M, N, out_row;
+    const unsigned *a_peak, *b_peak;       // as in ProductArgs
+    int a_up, b_up, halves;
+    const float* row_scale;
+    void* out;
+    int out_bf16;
+};
+__global__ __launch_bounds__(256) void rows_sum_kernel(SumArgs a)
+{
+    Lower f{1.f, 1.f};
+    if (a.halves) {
+        const int ua = a.a_peak ? raise_of(peak_of(a.a_peak, kPeakGroups), 0) : a.a_up;
+        const int ub = a.b_peak ? raise_of(peak_of(a.b_peak, kPeakGroups), 0) : a.b_up;
+        f = lower_by(ua + ub);
+    }
+    const long all = a.M * a.N;
+    for (long e = (long)blockIdx.x * 256 + threadIdx.x; e < all; e += (long)gridDim.x * 256) {
+        double s = 0.0;
+        for (int i = 0; i < a.splits; ++i) s += (double)a.part[i * all + e];
+        const long m = e / a.N, n = e - m * a.N;
+        const float scale = a.row_scale ? a.row_scale[m] : 1.f;
+        const float v = scale == 0.f ? 0.f : (float)s * f.first * f.second * scale;
+        if (a.out_bf16) ((bf16*)a.out)[m * a.out_row + n] = (bf16)v;
+        else ((float*)a.out)[m * a.out_row + n] = v;
+    }
+}
+
+// ---- no rows: gradients and loss are zero
+__global__ __launch_bounds__(256) void rows_none_kernel(char* dw, long bytes, float* db, long classes, double* loss)
+{
+    const long at = (long)blockIdx.x * 256 + threadIdx.x, step = (long)gridDim.x * 256;
+    if (dw)
+        for (long e = at; e < bytes / 2; e += step) reinterpret_cast<unsigned short*>(dw)[e] = 0;
+    if (db)
+        for (long e = at; e < classes; e += step) db[e] = 0.f;
+    if (loss && at == 0) *loss = 0.0;
+}
+
+// ---- bias gradients from the sums per tile of rows; the summed loss (workgroup 0); both in a fixed order
+struct FinishArgs {
+    const float* db_part;                  // [tiles][classes]
+    int tiles;
+    long classes;
+    float* db;                             // or null
+    const double* loss_part;
+    int loss_parts;
+    double* loss;                          // or null
+};
+__global__ __launch_bounds__(256) void rows_finish_kernel(FinishArgs a)
+{
+    __shared__ double red[256];
+    if (blockIdx.x == 0 && a.loss) {
+        double s = 0.0;
+        for (int i = threadIdx.x; i < a.loss_parts; i += 256) s += a.loss_part[i];
+        red[threadIdx.x] = s;
+        __syncthreads();
+        for (int w = 128; w > 0; w >>= 1) {
+            if ((int)threadIdx.x < w) red[threadIdx.x] += red[threadIdx.x + w];
+            __syncthreads();
+        }
+        if (threadIdx.x == 0) *a.loss = red[0];
+    }
+    if (!a.db) return;
+    const long v = (long)blockIdx.x * 256 + threadIdx.x;
+    if (v >= a.classes) return;
+    double s0 = 0.0, s1 = 0.0;
+    int t = 0;
+    for (; t + 3 < a.tiles; t += 4) {
+        float u[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) u[q] = a.db_part[(t + q) * a.classes + v];
+        s0 += (double)u[0] + (double)u[1];
+        s1 += (double)u[2] + (double)u[3];
+    }
+    for (; t < a.tiles; ++t) s0 += (double)a.db_part[t * a.classes + v];
+    a.db[v] = (float)(s0 + s1);
+}
+
+}  // namespace mpcnn

@@ -35,6 +35,7 @@ SYMBOLS = [
     "mpcnn_workspace_bytes_banded", "mpcnn_seg_backward_banded", "mpcnn_seg_forward_static",
     "mpcnn_plan_describe", "mpcnn_sgd_step_clipped", "mpcnn_grad_list_create", "mpcnn_grad_list_destroy",
     "mpcnn_grad_norm", "mpcnn_grad_clip", "mpcnn_sgd_step_list",
+    "mpcnn_workspace_bytes_class", "mpcnn_class_loss", "mpcnn_class_backward",
 ]
 
 
@@ -120,6 +121,11 @@ def lib():
         L.mpcnn_grad_norm.argtypes = [vp, C.c_double, vp, vp]
         L.mpcnn_grad_clip.argtypes = [vp, C.c_double, vp, vp]
         L.mpcnn_sgd_step_list.argtypes = [vp, C.c_double, C.c_double, C.c_double, vp, vp]
+        l = C.c_int64
+        L.mpcnn_workspace_bytes_class.argtypes = [l, l, l, i, i]
+        L.mpcnn_workspace_bytes_class.restype = sz
+        L.mpcnn_class_loss.argtypes = [vp, l, vp, l, vp, vp, vp, l, l, l, i, vp, vp, vp, vp, sz, vp]
+        L.mpcnn_class_backward.argtypes = [vp, l, vp, l, vp, vp, vp, l, l, l, i, vp, vp, vp, l, vp, vp, vp, sz, vp]
         L.mpcnn_get_activation.argtypes = [vp, i, vp, sz]
         L.mpcnn_get_argmax.argtypes = [vp, i, vp, sz]
         L.mpcnn_last_error.restype = C.c_char_p
@@ -514,3 +520,99 @@ class GradList:
             norm = self._norm(norm)
             _check(lib().mpcnn_sgd_step_list(self._h, lr, grad_scale, max_norm, norm.data_ptr(), st))
         return norm
+
+
+def class_workspace_bytes(rows: int, features: int, classes: int, dtype: int, training: bool) -> int:
+    return lib().mpcnn_workspace_bytes_class(rows, features, classes, dtype, 1 if training else 0)
+
+
+def _rows_of(name, t, device, dtype):
+    """A matrix whose rows are dense -> its pitch in elements."""
+    if t.dim() != 2 or t.device != device or t.dtype != dtype:
+        _refuse("%s: a %s matrix on %s is wanted" % (name, dtype, device))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        _refuse("%s: the numbers of a row have to be consecutive" % name)
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+def _vector(name, t, n, dtype, device):
+    if t.dtype != dtype or t.device != device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        _refuse("%s: %d numbers %s on %s are wanted, consecutive" % (name, n, dtype, device))
+    return t.data_ptr()
+
+
+class _ClassCall:
+    """Arguments of class_loss and class_backward, checked."""
+
+    def __init__(self, x, w, labels, bias, roww):
+        import torch
+        if not x.is_cuda:
+            _refuse("x: a tensor on a GPU is wanted")
+        self.device, self.dtype = x.device, _dtype_of(x)
+        self.x_pitch = _rows_of("x", x, x.device, x.dtype)
+        self.w_pitch = _rows_of("w", w, x.device, x.dtype)
+        self.rows, self.features, self.classes = x.shape[0], x.shape[1], w.shape[0]
+        if w.shape[1] != self.features:
+            _refuse("x has %d features, w %d" % (self.features, w.shape[1]))
+        self.args = (x.data_ptr(), self.x_pitch, w.data_ptr(), self.w_pitch,
+                     None if bias is None else _vector("bias", bias, self.classes, torch.float32, x.device),
+                     _vector("labels", labels, self.rows, torch.int32, x.device),
+                     None if roww is None else _vector("roww", roww, self.rows, torch.float32, x.device),
+                     self.rows, self.features, self.classes, self.dtype)
+
+    def output(self, name, given, shape, dtype):
+        """Given (checked), allocated (None) or not asked for (False) -> the tensor or None."""
+        import torch
+        if given is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        if given is False:
+            return None
+        if given.dtype != dtype or given.device != self.device or tuple(given.shape) != shape:
+            _refuse("%s: %s of shape %s on %s is wanted" % (name, dtype, shape, self.device))
+        if not given.is_contiguous() and name != "dx":
+            _refuse("%s has to be contiguous" % name)
+        return given
+
+    def workspace(self, ws, training):
+        import torch
+        need = class_workspace_bytes(self.rows, self.features, self.classes, self.dtype, training)
+        if ws is None:
+            return torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+        if ws.device != self.device or not ws.is_contiguous():
+            _refuse("ws: contiguous memory on %s is wanted" % self.device)
+        return ws
+
+
+def class_loss(x, w, labels, bias=None, roww=None, rowloss=None, lse=None, loss=None, ws=None, stream=None):
+    """Softmax cross-entropy of a class layer on rows of features, for any number of classes (the scores are not kept).
+
+    x [rows, features] and w [classes, features], fp32 or bf16, rows dense; labels [rows] int32; bias [classes]
+    and roww [rows] fp32 or None.  -> (loss, rowloss, lse): the summed loss (one fp64), w * -log p[label] and
+    log sum exp of the scores per row (fp32), put into the tensors given, allocated for None, left out for False."""
+    import torch
+    c = _ClassCall(x, w, labels, bias, roww)
+    with _On(c.device, stream) as st:
+        loss = c.output("loss", loss, (1,), torch.float64)
+        rowloss = c.output("rowloss", rowloss, (c.rows,), torch.float32)
+        lse = c.output("lse", lse, (c.rows,), torch.float32)
+        ws = c.workspace(ws, False)
+        _check(lib().mpcnn_class_loss(*c.args, _ptr(rowloss), _ptr(lse), _ptr(loss), ws.data_ptr(), ws.numel() * ws.element_size(), st))
+    return loss, rowloss, lse
+
+
+def class_backward(x, w, labels, bias=None, roww=None, rowloss=None, loss=None, dx=None, dw=None, db=None, ws=None, stream=None):
+    """class_loss and its gradients -> (loss, rowloss, dx, dw, db); dx and dw have x's type, db (None without
+    a bias) is fp32.  Each is put into the tensor given (dx: its rows dense), allocated for None, left out for False."""
+    import torch
+    c = _ClassCall(x, w, labels, bias, roww)
+    with _On(c.device, stream) as st:
+        loss = c.output("loss", loss, (1,), torch.float64)
+        rowloss = c.output("rowloss", rowloss, (c.rows,), torch.float32)
+        dx = c.output("dx", dx, (c.rows, c.features), x.dtype)
+        dw = c.output("dw", dw, (c.classes, c.features), x.dtype)
+        db = c.output("db", False if bias is None and db is None else db, (c.classes,), torch.float32)
+        ws = c.workspace(ws, True)
+        pitch = c.features if dx is None else _rows_of("dx", dx, c.device, x.dtype)
+        _check(lib().mpcnn_class_backward(*c.args, _ptr(rowloss), _ptr(loss), _ptr(dx), pitch, _ptr(dw), _ptr(db),
+                                          ws.data_ptr(), ws.numel() * ws.element_size(), st))
+    return loss, rowloss, dx, dw, db
