@@ -1,0 +1,59 @@
+// Eight consecutive numbers at any address that is a multiple of an element's size, as one or two 128-bit words
+// (global memory takes them unaligned).
+#pragma once
+#include "storage.hpp"
+
+namespace mpcnn {
+
+typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 b8_any __attribute__((ext_vector_type(8), aligned(2)));
+typedef float v8f __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ v8f load8(const float* p)
+{
+    const f4_any a = *reinterpret_cast<const f4_any*>(p), b = *reinterpret_cast<const f4_any*>(p + 4);
+    return v8f{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+__device__ __forceinline__ v8f load8(const bf16* p)
+{
+    return __builtin_convertvector(*reinterpret_cast<const b8_any*>(p), v8f);
+}
+__device__ __forceinline__ void store8(float* p, v8f v)
+{
+    *reinterpret_cast<f4_any*>(p) = f4_any{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f4_any*>(p + 4) = f4_any{v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ void store8(bf16* p, v8f v)
+{
+    *reinterpret_cast<b8_any*>(p) = __builtin_convertvector(v, b8_any);
+}
+
+// The same eight as they lie in memory (half the registers for bf16): raw8 fetches, widen converts
+template <typename T> struct Raw8;
+template <> struct Raw8<float> { f4_any a, b; };
+template <> struct Raw8<bf16> { b8_any a; };
+__device__ __forceinline__ Raw8<float> raw8(const float* p) { return {*reinterpret_cast<const f4_any*>(p), *reinterpret_cast<const f4_any*>(p + 4)}; }
+__device__ __forceinline__ Raw8<bf16> raw8(const bf16* p) { return {*reinterpret_cast<const b8_any*>(p)}; }
+__device__ __forceinline__ v8f widen(const Raw8<float>& r) { return v8f{r.a[0], r.a[1], r.a[2], r.a[3], r.b[0], r.b[1], r.b[2], r.b[3]}; }
+__device__ __forceinline__ v8f widen(const Raw8<bf16>& r) { return __builtin_convertvector(r.a, v8f); }
+__device__ __forceinline__ void set_raw(Raw8<float>& r, int z, float v) { if (z < 4) r.a[z] = v; else r.b[z - 4] = v; }
+__device__ __forceinline__ void set_raw(Raw8<bf16>& r, int z, bf16 v) { r.a[z] = v; }
+
+// Numbers row[at .. at + 7] of a row of n, zeros beyond its end (at may be beyond it too).  The loads of a row's end are not conditional,
+// only their addresses and results are chosen: eight branches with a load in each would wait for memory eight times.
+template <typename T>
+__device__ __forceinline__ Raw8<T> raw8_of(const T* row, int at, int n)
+{
+    if (at + 8 <= n) return raw8(row + at);
+    T u[8];
+    Raw8<T> r;
+#pragma unroll
+    for (int z = 0; z < 8; ++z) u[z] = row[at + z < n ? at + z : n - 1];
+#pragma unroll
+    for (int z = 0; z < 8; ++z) set_raw(r, z, at + z < n ? u[z] : (T)0.f);
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ v8f load8_of(const T* row, int at, int n) { return widen(raw8_of(row, at, n)); }
+
+}  // namespace mpcnn

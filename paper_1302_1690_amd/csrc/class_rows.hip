@@ -12,6 +12,8 @@
 #include <atomic>
 #include <cstdint>
 
+#include "kernels_rows_direct.hpp"
+#include "kernels_rows_few.hpp"
 #include "kernels_rows_parts.hpp"
 #include "kernels_rows_product.hpp"
 #include "status.hpp"
@@ -52,8 +54,15 @@ Tiling tiling_of(int64_t M, int64_t N, int64_t blocks, int64_t most_splits)
     return t;
 }
 
+// Three launches (kernels_rows_direct.hpp) instead of a dozen
+constexpr int64_t kDirectWork = 3000000000, kDirectRows = 64;   // rows x features x classes; whatever the work
+
 struct Plan {
-    bool halves, train, keep;
+    bool halves, train, keep, few, direct;
+    int score_groups, grad_groups;       // few: workgroups along the classes, of the scores and of the gradients
+    int64_t score_each, grad_each;       // and their classes
+    int x_tiles, w_tiles, d_tiles, x_splits, x_each, w_splits, w_each;   // direct: tiles, parts of the sums
+    size_t tickets, label;
     int N, D;
     int64_t V, Np;                       // Np: rows, padded to whole blocks
     int64_t d_bytes, n_bytes;            // a row of blocks along the features, along the rows
@@ -76,24 +85,81 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     p->Np = up_to(std::max<int64_t>(rows, 1), 64);
     p->d_bytes = p->bytes_along(features);
     p->n_bytes = p->bytes_along(p->Np);
+    size_t at = 0;
+    auto take = [&](int64_t bytes) { const size_t o = at; at += (size_t)up_to(bytes, 256); return o; };
+    p->keep = train && classes <= kRoom / p->Np;
+    p->few = rows <= mpcnn::kFewRows && rows > 0;
+    if (p->few) {
+        const int64_t rounds = (classes + mpcnn::kFewRound - 1) / mpcnn::kFewRound;
+        auto share = [&](int64_t least, int64_t most, int* groups, int64_t* each) {
+            const int64_t n = std::max<int64_t>(1, std::min(most, classes / least));
+            *each = (classes + n - 1) / n;
+            *groups = (int)((classes + *each - 1) / *each);
+        };
+        p->score_each = (rounds + 8 * kCUs - 1) / (8 * kCUs) * mpcnn::kFewRound;   // whole rounds
+        p->score_groups = (int)((classes + p->score_each - 1) / p->score_each);
+        share(8, 2 * kCUs, &p->grad_groups, &p->grad_each);
+        p->Np = up_to(classes, 64);      // the scores' rows
+        p->stats = take(8 * (int64_t)p->score_groups * rows);
+        p->label_score = take(4 * rows);
+        p->lse = take(4 * rows);
+        p->weight = take(4 * rows);
+        p->loss_part = take(8 * (rows + 1));
+        if (train) {
+            p->score = take(4 * rows * p->Np);
+            p->dx_part = take(4 * (int64_t)p->grad_groups * rows * features);
+        }
+        p->total = at;
+        return true;
+    }
+    p->direct = (rows <= kDirectRows || rows * classes <= kDirectWork / features) && (p->keep || !train) && rows * features < (int64_t)1 << 40;
+    if (p->direct) {
+        const int64_t side = mpcnn::kDirectSide;
+        p->x_tiles = (int)((rows + side - 1) / side); p->w_tiles = (int)((classes + side - 1) / side); p->d_tiles = (int)((features + side - 1) / side);
+        auto split = [&](int64_t tiles, int64_t K, int* splits, int* each) {   // two workgroups per compute unit, four steps each
+            const int64_t most = std::max<int64_t>(1, std::min<int64_t>(32, K / (4 * mpcnn::kDirectK)));
+            const int64_t n = std::min(most, std::max<int64_t>(1, 2 * kCUs / std::max<int64_t>(1, tiles)));
+            *each = (int)up_to(std::max<int64_t>(1, (K + n - 1) / n), mpcnn::kDirectK);
+            *splits = (int)std::max<int64_t>(1, (K + *each - 1) / *each);
+        };
+        const int64_t xt = (int64_t)p->x_tiles * p->d_tiles, wt = (int64_t)p->w_tiles * p->d_tiles;
+        split(xt, classes, &p->x_splits, &p->x_each);
+        split(wt, rows, &p->w_splits, &p->w_each);
+        if (xt * p->x_splits + wt * p->w_splits < 0x7fffffff) {
+            p->stat_tiles = p->w_tiles;
+            p->stats = take(8 * p->stat_tiles * rows);
+            p->label_score = take(4 * rows);
+            p->lse = take(4 * p->Np);
+            p->weight = take(4 * p->Np);
+            p->label = take(4 * p->Np);
+            p->loss_part = take(8 * (p->Np + 1));
+            if (train) {
+                p->score = take(4 * classes * p->Np);
+                p->tickets = take(4 * (xt + wt));
+                p->dx_part = take(p->x_splits > 1 ? 4 * xt * p->x_splits * side * side : 0);
+                p->dw_part = take(p->w_splits > 1 ? 4 * wt * p->w_splits * side * side : 0);
+                p->db_part = take(p->w_splits > 1 ? 4 * p->w_tiles * p->w_splits * side : 0);
+            }
+            p->total = at;
+            return true;
+        }
+        p->direct = false;
+    }
     int64_t piece = std::min<int64_t>(classes, kMaxPiece);
     auto bound = [&](int64_t most) { if (piece > most) piece = std::max<int64_t>(256, most / 256 * 256); };
     bound(kWeightRoom / p->d_bytes);
-    p->keep = train && classes <= kRoom / p->Np;
     if (train) bound(kRoom / p->Np);
     p->piece = piece;
     const int64_t pieces = (classes + piece - 1) / piece;
     const int64_t v_bytes = p->bytes_along(piece);
     p->stat_tiles = (classes + 127) / 128 + pieces;
-    size_t at = 0;
-    auto take = [&](int64_t bytes) { const size_t o = at; at += (size_t)up_to(bytes, 256); return o; };
     const int64_t N = p->N, D = p->D;
     p->peaks = take(4 * 3 * mpcnn::kPeakGroups);
     p->stats = take(8 * p->stat_tiles * N);
     p->label_score = take(4 * N);
     p->lse = take(4 * N);
     p->weight = take(4 * N);
-    p->loss_part = take(8 * ((N + mpcnn::kJoinRows - 1) / mpcnn::kJoinRows));
+    p->loss_part = take(8 * (N + 1));
     p->x_rows = take(N * p->d_bytes);
     p->w_rows = take(piece * p->d_bytes);
     if (train) {
@@ -152,6 +218,100 @@ struct Call {
     float* db;
 };
 
+void launch_join(const mpcnn::JoinArgs& j, hipStream_t st)
+{
+    const int rows = std::max(j.N, j.padded), each = mpcnn::join_rows(rows), groups = (rows + each - 1) / each;
+    if (each == mpcnn::kJoinFew) mpcnn::rows_join_kernel<mpcnn::kJoinFew><<<(unsigned)groups, 256, 0, st>>>(j);
+    else mpcnn::rows_join_kernel<mpcnn::kJoinMany><<<(unsigned)groups, 256, 0, st>>>(j);
+}
+int join_groups_of(int N) { return (N + mpcnn::join_rows(N) - 1) / mpcnn::join_rows(N); }
+
+template <typename T, int NR>
+void launch_few(const mpcnn::FewArgs& a, bool grads, dim3 grid, hipStream_t st)
+{
+    if (grads) mpcnn::rows_few_grads_kernel<T, NR><<<grid, mpcnn::kFewThreads, 0, st>>>(a);
+    else mpcnn::rows_few_scores_kernel<T, NR><<<grid, mpcnn::kFewThreads, 0, st>>>(a);
+}
+template <typename T>
+void launch_few(const mpcnn::FewArgs& a, bool grads, dim3 grid, hipStream_t st)
+{
+    switch (a.N) {
+#define CASE(n) case n: launch_few<T, n>(a, grads, grid, st); break;
+        CASE(1) CASE(2) CASE(3) CASE(4) CASE(5) CASE(6) CASE(7) CASE(8)
+#undef CASE
+    }
+}
+template <typename T>
+mpcnn_status run_few(const Plan& p, const Call& c, char* ws, hipStream_t st)
+{
+    mpcnn::FewArgs a{};
+    a.x = c.x; a.w = c.w; a.x_pitch = c.x_pitch; a.w_pitch = c.w_pitch;
+    a.N = p.N; a.D = p.D; a.V = p.V; a.score_row = p.Np; a.bias = c.bias;
+    a.mask = mpcnn::RowMask{c.labels, c.roww, (int)p.V};
+    a.stats = (float2*)(ws + p.stats); a.label_score = (float*)(ws + p.label_score);
+    a.each = p.score_each;
+    if (p.train) a.scores = (float*)(ws + p.score);
+    launch_few<T>(a, false, dim3((unsigned)p.score_groups), st);
+    mpcnn::JoinArgs j{};
+    j.stats = a.stats; j.tiles = p.score_groups; j.N = p.N; j.label_score = a.label_score; j.mask = a.mask;
+    j.lse = (float*)(ws + p.lse); j.weight = (float*)(ws + p.weight); j.lse_out = c.lse; j.rowloss = c.rowloss;
+    const int groups = join_groups_of(p.N);
+    j.loss_part = groups == 1 && c.loss ? c.loss : (double*)(ws + p.loss_part);
+    launch_join(j, st);
+    a.loss = groups > 1 ? c.loss : nullptr; a.loss_part = j.loss_part; a.loss_parts = groups;
+    if (p.train) {
+        a.lse = j.lse; a.weight = j.weight;
+        a.dw = c.dw; a.db = c.db; a.each = p.grad_each;
+        a.part = c.dx ? (float*)(ws + p.dx_part) : nullptr;
+        a.columns = 16;
+        while (a.columns < mpcnn::kFewThreads && 8 * a.columns < p.D) a.columns *= 2;
+        if (c.dx || c.dw || c.db)
+            launch_few<T>(a, true, dim3((unsigned)p.grad_groups, (unsigned)((p.D + 8 * a.columns - 1) / (8 * a.columns))), st);
+        a.parts = p.grad_groups; a.dx = c.dx; a.dx_pitch = c.dx_pitch;
+    }
+    if (a.part || a.loss)
+        mpcnn::rows_few_sum_kernel<T><<<a.part ? (unsigned)(((int64_t)p.N * p.D + 63) / 64) : 1, 1024, 0, st>>>(a);
+    HIP_TRY(hipGetLastError());
+    return MPCNN_OK;
+}
+
+template <typename T>
+mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
+{
+    mpcnn::DirectArgs a{};
+    a.x = c.x; a.w = c.w; a.x_pitch = c.x_pitch; a.w_pitch = c.w_pitch;
+    a.N = p.N; a.D = p.D; a.V = (int)p.V; a.bias = c.bias;
+    a.mask = mpcnn::RowMask{c.labels, c.roww, (int)p.V};
+    a.stats = (float2*)(ws + p.stats); a.label_score = (float*)(ws + p.label_score);
+    a.score_row = p.Np; a.store = p.train;
+    if (p.train) a.scores = (float*)(ws + p.score);
+    mpcnn::rows_direct_scores_kernel<T><<<dim3((unsigned)p.w_tiles, (unsigned)p.x_tiles), 256, 0, st>>>(a);
+    mpcnn::JoinArgs j{};
+    j.stats = a.stats; j.tiles = p.w_tiles; j.N = p.N; j.label_score = a.label_score; j.mask = a.mask;
+    j.lse = (float*)(ws + p.lse); j.weight = (float*)(ws + p.weight); j.lse_out = c.lse; j.rowloss = c.rowloss;
+    j.label = (int*)(ws + p.label); j.padded = (int)p.Np;
+    const int groups = join_groups_of((int)p.Np);
+    j.loss_part = (double*)(ws + p.loss_part);
+    const int64_t xt = (int64_t)p.x_tiles * p.d_tiles, wt = (int64_t)p.w_tiles * p.d_tiles;
+    if (p.train) { j.tickets = (unsigned*)(ws + p.tickets); j.n_tickets = (int)(xt + wt); }
+    launch_join(j, st);
+    a.loss = c.loss; a.loss_part = j.loss_part; a.loss_parts = groups;
+    if (p.train) {
+        a.lse = j.lse; a.weight = j.weight; a.label = j.label;
+        a.dx = c.dx; a.dx_pitch = c.dx_pitch; a.dw = c.dw; a.db = c.db;
+        a.x_tiles = p.x_tiles; a.w_tiles = p.w_tiles; a.d_tiles = p.d_tiles;
+        a.x_splits = p.x_splits; a.x_each = p.x_each; a.w_splits = p.w_splits; a.w_each = p.w_each;
+        a.x_groups = c.dx ? (int)(xt * p.x_splits) : 0;
+        a.w_groups = c.dw || c.db ? (int)(wt * p.w_splits) : 0;
+        a.x_part = (float*)(ws + p.dx_part); a.w_part = (float*)(ws + p.dw_part); a.db_part = (float*)(ws + p.db_part);
+        a.tickets = j.tickets;
+    }
+    const int64_t all = (int64_t)a.x_groups + a.w_groups;
+    if (all || a.loss) mpcnn::rows_direct_grads_kernel<T><<<(unsigned)std::max<int64_t>(1, all), 256, 0, st>>>(a);
+    HIP_TRY(hipGetLastError());
+    return MPCNN_OK;
+}
+
 template <typename T>
 mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
 {
@@ -163,6 +323,8 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         HIP_TRY(hipGetLastError());
         return MPCNN_OK;
     }
+    if (p.few) return run_few<T>(p, c, ws, st);
+    if (p.direct) return run_direct<T>(p, c, ws, st);
     const mpcnn::RowMask every{}, mask{c.labels, c.roww, (int)p.V};
     unsigned* const x_peak = (unsigned*)(ws + p.peaks);
     unsigned *const w_peak = x_peak + mpcnn::kPeakGroups, *const roww_peak = w_peak + mpcnn::kPeakGroups;
@@ -223,14 +385,14 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         if (rc != MPCNN_OK) return rc;
         done += tiles;
     }
-    const int join_groups = (p.N + mpcnn::kJoinRows - 1) / mpcnn::kJoinRows;
+    const int join_groups = join_groups_of(p.N);
     mpcnn::JoinArgs j{};
     j.stats = (const float2*)(ws + p.stats); j.tiles = done; j.N = p.N;
     j.label_score = (const float*)(ws + p.label_score); j.mask = mask;
     if (p.train) { j.lse = (float*)(ws + p.lse); j.weight = (float*)(ws + p.weight); }
     j.lse_out = c.lse; j.rowloss = c.rowloss;
     j.loss_part = c.loss ? (double*)(ws + p.loss_part) : nullptr;
-    mpcnn::rows_join_kernel<<<(unsigned)join_groups, 256, 0, st>>>(j);
+    launch_join(j, st);
 
     mpcnn::FinishArgs fin{};
     fin.loss_part = j.loss_part; fin.loss_parts = join_groups; fin.loss = c.loss;

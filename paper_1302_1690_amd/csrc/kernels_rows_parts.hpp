@@ -8,7 +8,6 @@
 namespace mpcnn {
 
 constexpr int kPeakGroups = 256;           // words of a peak
-constexpr int kJoinRows = 32;              // rows of a workgroup of rows_join_kernel
 
 // Rows that add something: a label among the classes and a weight that is not zero
 struct RowMask {
@@ -22,6 +21,8 @@ __device__ __forceinline__ float row_weight(const RowMask& m, int n)
     if (t < 0 || t >= m.classes) return 0.f;
     return m.weights ? m.weights[n] : 1.f;
 }
+
+constexpr int kNoLabel = -1;               // in the library's own copy of the labels: a row that adds nothing
 
 // ---- the largest magnitude of a matrix, as bits (one word per workgroup); what is not finite is passed over
 struct PeakArgs {
@@ -150,15 +151,25 @@ struct JoinArgs {
     const float* label_score;              // [N]
     RowMask mask;
     float *lse, *rowloss, *weight;         // [N]: lse for the derivative, results (null: not asked for), the row's weight or 0
+    int* label;                            // the label, or kNoLabel
+    int padded;                            // places of lse, weight and label: those behind the last row are filled as for rows that add nothing
     float* lse_out;
     double* loss_part;                     // per workgroup, or null
+    unsigned* tickets;                     // to be zero afterwards
+    int n_tickets;
 };
+// ROWS rows per workgroup, the tiles dealt to 256 / ROWS threads each: 4 while that leaves compute units without work, 32 beyond (whole lines)
+constexpr int kJoinFew = 4, kJoinMany = 32, kJoinFewMost = 1024;
+inline int join_rows(int N) { return N <= kJoinFewMost ? kJoinFew : kJoinMany; }
+template <int ROWS>
 __global__ __launch_bounds__(256) void rows_join_kernel(JoinArgs a)
 {
-    __shared__ float2 red[8][kJoinRows];
-    __shared__ double sums[kJoinRows];
-    const int own = threadIdx.x % kJoinRows, deal = threadIdx.x / kJoinRows;
-    const int n = blockIdx.x * kJoinRows + own;
+    constexpr int DEALS = 256 / ROWS;
+    __shared__ float2 red[DEALS][ROWS];
+    __shared__ double sums[ROWS];
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < a.n_tickets; i += gridDim.x * 256) a.tickets[i] = 0;
+    const int own = threadIdx.x % ROWS, deal = threadIdx.x / ROWS;
+    const int n = blockIdx.x * ROWS + own;
     constexpr float kNone = -__builtin_inff();
     auto join = [](float2 s, float2 o) {
         const float top = fmaxf(s.x, o.x), base = top == kNone ? 0.f : top;
@@ -167,19 +178,29 @@ __global__ __launch_bounds__(256) void rows_join_kernel(JoinArgs a)
     float2 s{kNone, 0.f};
     if (n < a.N) {
         int t = deal;
-        for (; t + 24 < a.tiles; t += 32) {
-            float2 v[4];
+        for (; t + 7 * DEALS < a.tiles; t += 8 * DEALS) {
+            float2 v[8];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = a.stats[(long)(t + 8 * q) * a.N + n];
+            for (int q = 0; q < 8; ++q) v[q] = a.stats[(long)(t + DEALS * q) * a.N + n];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) s = join(s, v[q]);
+            for (int q = 0; q < 8; ++q) s = join(s, v[q]);
         }
-        for (; t < a.tiles; t += 8) s = join(s, a.stats[(long)t * a.N + n]);
+        for (; t < a.tiles; t += DEALS) s = join(s, a.stats[(long)t * a.N + n]);
     }
     red[deal][own] = s;
     __syncthreads();
+    for (int w = DEALS / 2; w >= 8; w >>= 1) {   // (a tree down to eight, in a fixed order)
+        if (deal < w) red[deal][own] = join(red[deal][own], red[deal + w][own]);
+        __syncthreads();
+    }
+    s = red[0][own];
     if (deal == 0) {
         double share = 0.0;
+        if (n >= a.N && n < a.padded) {
+            if (a.lse) a.lse[n] = 0.f;
+            if (a.weight) a.weight[n] = 0.f;
+            if (a.label) a.label[n] = kNoLabel;
+        }
         if (n < a.N) {
             for (int d = 1; d < 8; ++d) s = join(s, red[d][own]);
             const float lse = s.x == kNone ? kNone : s.x + logf(s.y);
@@ -191,6 +212,7 @@ __global__ __launch_bounds__(256) void rows_join_kernel(JoinArgs a)
             }
             if (a.lse) a.lse[n] = lse;
             if (a.weight) a.weight[n] = w;
+            if (a.label) a.label[n] = w != 0.f ? a.mask.labels[n] : kNoLabel;
             if (a.lse_out) a.lse_out[n] = w != 0.f ? lse : 0.f;
             if (a.rowloss) a.rowloss[n] = loss;
             share = (double)loss;
@@ -201,7 +223,7 @@ __global__ __launch_bounds__(256) void rows_join_kernel(JoinArgs a)
     __syncthreads();
     if (threadIdx.x == 0) {
         double all = 0.0;
-        for (int i = 0; i < kJoinRows; ++i) all += sums[i];
+        for (int i = 0; i < ROWS; ++i) all += sums[i];
         a.loss_part[blockIdx.x] = all;
     }
 }

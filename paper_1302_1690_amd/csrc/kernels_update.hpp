@@ -13,33 +13,10 @@
 // Bound by the passes over memory: one for the norm, two more for clipping (none where the norm is within the bound: the gradients
 // are what they were), three more for a step.
 #pragma once
-#include "storage.hpp"
+#include "any_address.hpp"
 #include "update.hpp"
 
 namespace mpcnn {
-
-typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef __bf16 b8_any __attribute__((ext_vector_type(8), aligned(2)));
-typedef float v8f __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ v8f load8(const float* p)
-{
-    const f4_any a = *reinterpret_cast<const f4_any*>(p), b = *reinterpret_cast<const f4_any*>(p + 4);
-    return v8f{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-}
-__device__ __forceinline__ v8f load8(const bf16* p)
-{
-    return __builtin_convertvector(*reinterpret_cast<const b8_any*>(p), v8f);
-}
-__device__ __forceinline__ void store8(float* p, v8f v)
-{
-    *reinterpret_cast<f4_any*>(p) = f4_any{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f4_any*>(p + 4) = f4_any{v[4], v[5], v[6], v[7]};
-}
-__device__ __forceinline__ void store8(bf16* p, v8f v)
-{
-    *reinterpret_cast<b8_any*>(p) = __builtin_convertvector(v, b8_any);
-}
 
 __device__ __forceinline__ Stretch stretch_at(const UpdateArgs& a, int s)
 {
