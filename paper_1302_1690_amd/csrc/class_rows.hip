@@ -61,8 +61,9 @@ struct Plan {
     bool halves, train, keep, few, direct;
     int score_groups, grad_groups;       // few: workgroups along the classes, of the scores and of the gradients
     int64_t score_each, grad_each;       // and their classes
-    int x_tiles, w_tiles, d_tiles, x_splits, x_each, w_splits, w_each;   // direct: tiles, parts of the sums
-    size_t tickets, label;
+    int score_deal, score_v, score_n;    // direct: waves that share a tile's sum, tiles along classes and rows
+    struct { int deal, m, along, splits, each; } gx, gw;   // of the gradients: tiles along rows or classes and along features, parts of the sum, their length
+    size_t label;
     int N, D;
     int64_t V, Np;                       // Np: rows, padded to whole blocks
     int64_t d_bytes, n_bytes;            // a row of blocks along the features, along the rows
@@ -114,19 +115,24 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     }
     p->direct = (rows <= kDirectRows || rows * classes <= kDirectWork / features) && (p->keep || !train) && rows * features < (int64_t)1 << 40;
     if (p->direct) {
-        const int64_t side = mpcnn::kDirectSide;
-        p->x_tiles = (int)((rows + side - 1) / side); p->w_tiles = (int)((classes + side - 1) / side); p->d_tiles = (int)((features + side - 1) / side);
-        auto split = [&](int64_t tiles, int64_t K, int* splits, int* each) {   // two workgroups per compute unit, four steps each
-            const int64_t most = std::max<int64_t>(1, std::min<int64_t>(32, K / (4 * mpcnn::kDirectK)));
-            const int64_t n = std::min(most, std::max<int64_t>(1, 2 * kCUs / std::max<int64_t>(1, tiles)));
-            *each = (int)up_to(std::max<int64_t>(1, (K + n - 1) / n), mpcnn::kDirectK);
-            *splits = (int)std::max<int64_t>(1, (K + *each - 1) / *each);
+        // a tile of 32 x 32 for four waves, one of 64 x 64 where that gives every compute unit two workgroups or the sum has one step
+        auto deal_of = [](int64_t m, int64_t n, int64_t k) { return (m + 63) / 64 * ((n + 63) / 64) >= 2 * kCUs || k <= mpcnn::kDirectK ? 1 : 4; };
+        auto tiles = [](int64_t n, int deal) { return (int)((n + (deal == 4 ? 31 : 63)) / (deal == 4 ? 32 : 64)); };
+        p->score_deal = deal_of(classes, rows, features);
+        p->score_v = tiles(classes, p->score_deal); p->score_n = tiles(rows, p->score_deal);
+        auto grads = [&](auto& g, int64_t m, int64_t K) {
+            g.deal = deal_of(m, features, K);
+            g.m = tiles(m, g.deal); g.along = tiles(features, g.deal);
+            const int64_t step = mpcnn::kDirectK * g.deal, all = (int64_t)g.m * g.along;   // (a step of each wave)
+            const int64_t most = std::max<int64_t>(1, std::min<int64_t>(32, K / (4 * step)));
+            const int64_t n = std::min(most, std::max<int64_t>(1, 4 * kCUs / std::max<int64_t>(1, all)));
+            g.each = (int)up_to(std::max<int64_t>(1, (K + n - 1) / n), step);
+            g.splits = (int)std::max<int64_t>(1, (K + g.each - 1) / g.each);
+            return all * g.splits;
         };
-        const int64_t xt = (int64_t)p->x_tiles * p->d_tiles, wt = (int64_t)p->w_tiles * p->d_tiles;
-        split(xt, classes, &p->x_splits, &p->x_each);
-        split(wt, rows, &p->w_splits, &p->w_each);
-        if (xt * p->x_splits + wt * p->w_splits < 0x7fffffff) {
-            p->stat_tiles = p->w_tiles;
+        const int64_t groups = grads(p->gx, rows, classes) + grads(p->gw, classes, rows);
+        if (groups < 0x7fffffff) {
+            p->stat_tiles = p->score_v;
             p->stats = take(8 * p->stat_tiles * rows);
             p->label_score = take(4 * rows);
             p->lse = take(4 * p->Np);
@@ -135,10 +141,9 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
             p->loss_part = take(8 * (p->Np + 1));
             if (train) {
                 p->score = take(4 * classes * p->Np);
-                p->tickets = take(4 * (xt + wt));
-                p->dx_part = take(p->x_splits > 1 ? 4 * xt * p->x_splits * side * side : 0);
-                p->dw_part = take(p->w_splits > 1 ? 4 * wt * p->w_splits * side * side : 0);
-                p->db_part = take(p->w_splits > 1 ? 4 * p->w_tiles * p->w_splits * side : 0);
+                p->dx_part = take(p->gx.splits > 1 ? 4 * p->gx.splits * rows * features : 0);
+                p->dw_part = take(p->gw.splits > 1 ? 4 * p->gw.splits * classes * features : 0);
+                p->db_part = take(p->gw.splits > 1 ? 4 * p->gw.splits * classes : 0);
             }
             p->total = at;
             return true;
@@ -283,31 +288,33 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
     a.N = p.N; a.D = p.D; a.V = (int)p.V; a.bias = c.bias;
     a.mask = mpcnn::RowMask{c.labels, c.roww, (int)p.V};
     a.stats = (float2*)(ws + p.stats); a.label_score = (float*)(ws + p.label_score);
-    a.score_row = p.Np; a.store = p.train;
+    a.score_row = p.Np; a.score_deal = p.score_deal;
     if (p.train) a.scores = (float*)(ws + p.score);
-    mpcnn::rows_direct_scores_kernel<T><<<dim3((unsigned)p.w_tiles, (unsigned)p.x_tiles), 256, 0, st>>>(a);
+    mpcnn::rows_direct_scores_kernel<T><<<dim3((unsigned)p.score_v, (unsigned)p.score_n), 256, 0, st>>>(a);
     mpcnn::JoinArgs j{};
-    j.stats = a.stats; j.tiles = p.w_tiles; j.N = p.N; j.label_score = a.label_score; j.mask = a.mask;
+    j.stats = a.stats; j.tiles = p.score_v; j.N = p.N; j.label_score = a.label_score; j.mask = a.mask;
     j.lse = (float*)(ws + p.lse); j.weight = (float*)(ws + p.weight); j.lse_out = c.lse; j.rowloss = c.rowloss;
     j.label = (int*)(ws + p.label); j.padded = (int)p.Np;
     const int groups = join_groups_of((int)p.Np);
-    j.loss_part = (double*)(ws + p.loss_part);
-    const int64_t xt = (int64_t)p.x_tiles * p.d_tiles, wt = (int64_t)p.w_tiles * p.d_tiles;
-    if (p.train) { j.tickets = (unsigned*)(ws + p.tickets); j.n_tickets = (int)(xt + wt); }
+    j.loss_part = groups == 1 && c.loss ? c.loss : (double*)(ws + p.loss_part);
     launch_join(j, st);
-    a.loss = c.loss; a.loss_part = j.loss_part; a.loss_parts = groups;
+    a.loss = groups > 1 ? c.loss : nullptr; a.loss_part = j.loss_part; a.loss_parts = groups;
     if (p.train) {
         a.lse = j.lse; a.weight = j.weight; a.label = j.label;
         a.dx = c.dx; a.dx_pitch = c.dx_pitch; a.dw = c.dw; a.db = c.db;
-        a.x_tiles = p.x_tiles; a.w_tiles = p.w_tiles; a.d_tiles = p.d_tiles;
-        a.x_splits = p.x_splits; a.x_each = p.x_each; a.w_splits = p.w_splits; a.w_each = p.w_each;
-        a.x_groups = c.dx ? (int)(xt * p.x_splits) : 0;
-        a.w_groups = c.dw || c.db ? (int)(wt * p.w_splits) : 0;
-        a.x_part = (float*)(ws + p.dx_part); a.w_part = (float*)(ws + p.dw_part); a.db_part = (float*)(ws + p.db_part);
-        a.tickets = j.tickets;
+        a.x_deal = p.gx.deal; a.w_deal = p.gw.deal; a.x_along = p.gx.along; a.w_along = p.gw.along;
+        a.x_splits = p.gx.splits; a.x_each = p.gx.each; a.w_splits = p.gw.splits; a.w_each = p.gw.each;
+        a.x_groups = c.dx ? p.gx.m * p.gx.along * p.gx.splits : 0;
+        a.w_groups = c.dw || c.db ? p.gw.m * p.gw.along * p.gw.splits : 0;
+        if (c.dx && p.gx.splits > 1) a.x_part = (float*)(ws + p.dx_part);
+        if (a.w_groups && p.gw.splits > 1) { a.w_part = (float*)(ws + p.dw_part); a.db_part = (float*)(ws + p.db_part); }
     }
     const int64_t all = (int64_t)a.x_groups + a.w_groups;
     if (all || a.loss) mpcnn::rows_direct_grads_kernel<T><<<(unsigned)std::max<int64_t>(1, all), 256, 0, st>>>(a);
+    if (a.x_part || a.w_part) {
+        const int64_t n = (a.x_part ? (int64_t)p.N * p.D : 0) + (a.w_part ? p.V * p.D + p.V : 0);
+        mpcnn::rows_direct_sum_kernel<T><<<(unsigned)std::min<int64_t>(8192, (n + 255) / 256), 256, 0, st>>>(a);
+    }
     HIP_TRY(hipGetLastError());
     return MPCNN_OK;
 }

@@ -155,8 +155,6 @@ struct JoinArgs {
     int padded;                            // places of lse, weight and label: those behind the last row are filled as for rows that add nothing
     float* lse_out;
     double* loss_part;                     // per workgroup, or null
-    unsigned* tickets;                     // to be zero afterwards
-    int n_tickets;
 };
 // ROWS rows per workgroup, the tiles dealt to 256 / ROWS threads each: 4 while that leaves compute units without work, 32 beyond (whole lines)
 constexpr int kJoinFew = 4, kJoinMany = 32, kJoinFewMost = 1024;
@@ -167,7 +165,6 @@ __global__ __launch_bounds__(256) void rows_join_kernel(JoinArgs a)
     constexpr int DEALS = 256 / ROWS;
     __shared__ float2 red[DEALS][ROWS];
     __shared__ double sums[ROWS];
-    for (int i = blockIdx.x * 256 + threadIdx.x; i < a.n_tickets; i += gridDim.x * 256) a.tickets[i] = 0;
     const int own = threadIdx.x % ROWS, deal = threadIdx.x / ROWS;
     const int n = blockIdx.x * ROWS + own;
     constexpr float kNone = -__builtin_inff();
