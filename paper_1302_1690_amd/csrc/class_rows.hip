@@ -55,7 +55,7 @@ Tiling tiling_of(int64_t M, int64_t N, int64_t blocks, int64_t most_splits)
 }
 
 // Three launches (kernels_rows_direct.hpp) instead of a dozen
-constexpr int64_t kDirectWork = 3000000000, kDirectRows = 64;   // rows x features x classes; whatever the work
+constexpr int64_t kDirectWork = 1500000000, kDirectRows = 64;   // rows x features x classes; whatever the work
 
 struct Plan {
     bool halves, train, keep, few, direct;
@@ -63,7 +63,6 @@ struct Plan {
     int64_t score_each, grad_each;       // and their classes
     int score_deal, score_v, score_n;    // direct: waves that share a tile's sum, tiles along classes and rows
     struct { int deal, m, along, splits, each; } gx, gw;   // of the gradients: tiles along rows or classes and along features, parts of the sum, their length
-    size_t label;
     int N, D;
     int64_t V, Np;                       // Np: rows, padded to whole blocks
     int64_t d_bytes, n_bytes;            // a row of blocks along the features, along the rows
@@ -137,13 +136,13 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
             p->label_score = take(4 * rows);
             p->lse = take(4 * p->Np);
             p->weight = take(4 * p->Np);
-            p->label = take(4 * p->Np);
             p->loss_part = take(8 * (p->Np + 1));
             if (train) {
                 p->score = take(4 * classes * p->Np);
+                p->delta_rows = p->halves ? p->score : take(2 * classes * p->Np);
                 p->dx_part = take(p->gx.splits > 1 ? 4 * p->gx.splits * rows * features : 0);
                 p->dw_part = take(p->gw.splits > 1 ? 4 * p->gw.splits * classes * features : 0);
-                p->db_part = take(p->gw.splits > 1 ? 4 * p->gw.splits * classes : 0);
+                p->db_part = take(4 * classes * ((rows + 63) / 64));
             }
             p->total = at;
             return true;
@@ -288,32 +287,53 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
     a.N = p.N; a.D = p.D; a.V = (int)p.V; a.bias = c.bias;
     a.mask = mpcnn::RowMask{c.labels, c.roww, (int)p.V};
     a.stats = (float2*)(ws + p.stats); a.label_score = (float*)(ws + p.label_score);
-    a.score_row = p.Np; a.score_deal = p.score_deal;
+    a.score_row = p.Np; a.score_deal = p.score_deal; a.tiles = p.score_v;
     if (p.train) a.scores = (float*)(ws + p.score);
     mpcnn::rows_direct_scores_kernel<T><<<dim3((unsigned)p.score_v, (unsigned)p.score_n), 256, 0, st>>>(a);
-    mpcnn::JoinArgs j{};
-    j.stats = a.stats; j.tiles = p.score_v; j.N = p.N; j.label_score = a.label_score; j.mask = a.mask;
-    j.lse = (float*)(ws + p.lse); j.weight = (float*)(ws + p.weight); j.lse_out = c.lse; j.rowloss = c.rowloss;
-    j.label = (int*)(ws + p.label); j.padded = (int)p.Np;
-    const int groups = join_groups_of((int)p.Np);
-    j.loss_part = groups == 1 && c.loss ? c.loss : (double*)(ws + p.loss_part);
-    launch_join(j, st);
-    a.loss = groups > 1 ? c.loss : nullptr; a.loss_part = j.loss_part; a.loss_parts = groups;
+    // statistics joined with the derivative where there are few tiles of classes, by a launch of their own otherwise
+    const bool joined = p.score_v > mpcnn::kDeltaFewTiles;
+    a.lse = (float*)(ws + p.lse); a.weight = (float*)(ws + p.weight);
+    double* const shares = (double*)(ws + p.loss_part);
+    // (a workgroup takes several tiles of rows where that leaves four workgroups per compute unit: fewer sums over the rows to add up)
+    constexpr int side = mpcnn::kDeltaSide;
+    const int64_t v_tiles = p.train ? (p.V + side - 1) / side : 1, n_tiles = (p.N + side - 1) / side;
+    a.batch = (int)std::max<int64_t>(1, std::min<int64_t>(n_tiles, v_tiles * n_tiles / (4 * kCUs)));
+    const int along = (int)((n_tiles + a.batch - 1) / a.batch);
+    int groups = along;
+    if (joined) {
+        mpcnn::JoinArgs j{};
+        j.stats = a.stats; j.tiles = p.score_v; j.N = p.N; j.label_score = a.label_score; j.mask = a.mask;
+        j.lse = a.lse; j.weight = a.weight; j.lse_out = c.lse; j.rowloss = c.rowloss;
+        groups = join_groups_of(p.N);
+        j.loss_part = groups == 1 && c.loss ? c.loss : shares;
+        launch_join(j, st);
+    } else {
+        a.rowloss = c.rowloss; a.lse_out = c.lse;
+        a.shares = groups == 1 && c.loss ? c.loss : shares;
+    }
+    a.loss = groups > 1 ? c.loss : nullptr; a.loss_part = shares; a.loss_parts = groups;
+    if (p.train && (c.dx || c.dw || c.db)) a.delta = ws + p.delta_rows;
+    if (a.delta || !joined) {
+        a.db = c.db;
+        if (c.db && along > 1) { a.db_part = (float*)(ws + p.db_part); a.db_parts = along; }
+        mpcnn::rows_direct_delta_kernel<T><<<dim3((unsigned)along, (unsigned)(a.delta ? v_tiles : 1)), 256, 0, st>>>(a);
+    }
     if (p.train) {
-        a.lse = j.lse; a.weight = j.weight; a.label = j.label;
-        a.dx = c.dx; a.dx_pitch = c.dx_pitch; a.dw = c.dw; a.db = c.db;
+        a.dx = c.dx; a.dx_pitch = c.dx_pitch; a.dw = c.dw;
+        a.masked = 1;
         a.x_deal = p.gx.deal; a.w_deal = p.gw.deal; a.x_along = p.gx.along; a.w_along = p.gw.along;
         a.x_splits = p.gx.splits; a.x_each = p.gx.each; a.w_splits = p.gw.splits; a.w_each = p.gw.each;
         a.x_groups = c.dx ? p.gx.m * p.gx.along * p.gx.splits : 0;
-        a.w_groups = c.dw || c.db ? p.gw.m * p.gw.along * p.gw.splits : 0;
+        a.w_groups = c.dw ? p.gw.m * p.gw.along * p.gw.splits : 0;
         if (c.dx && p.gx.splits > 1) a.x_part = (float*)(ws + p.dx_part);
-        if (a.w_groups && p.gw.splits > 1) { a.w_part = (float*)(ws + p.dw_part); a.db_part = (float*)(ws + p.db_part); }
+        if (c.dw && p.gw.splits > 1) a.w_part = (float*)(ws + p.dw_part);
     }
     const int64_t all = (int64_t)a.x_groups + a.w_groups;
     if (all || a.loss) mpcnn::rows_direct_grads_kernel<T><<<(unsigned)std::max<int64_t>(1, all), 256, 0, st>>>(a);
-    if (a.x_part || a.w_part) {
-        const int64_t n = (a.x_part ? (int64_t)p.N * p.D : 0) + (a.w_part ? p.V * p.D + p.V : 0);
-        mpcnn::rows_direct_sum_kernel<T><<<(unsigned)std::min<int64_t>(8192, (n + 255) / 256), 256, 0, st>>>(a);
+    if (a.x_part || a.w_part || a.db_part) {
+        const int64_t n = (a.x_part ? (int64_t)p.N * p.D : 0) + (a.w_part ? p.V * p.D : 0);
+        a.db_groups = a.db_part ? (int)((p.V + 31) / 32) : 0;
+        mpcnn::rows_direct_sum_kernel<T><<<(unsigned)(a.db_groups + std::min<int64_t>(8192, (n + 255) / 256)), 256, 0, st>>>(a);
     }
     HIP_TRY(hipGetLastError());
     return MPCNN_OK;

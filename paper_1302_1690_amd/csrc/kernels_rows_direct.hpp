@@ -2,9 +2,9 @@
 // where they are, at any pitch and address, without being brought into blocks first, and without a stop in LDS.
 //
 //   rows_direct_scores   scores with their bias, stored [class][row], and per row and tile of classes the largest and the sum of exponentials
-//   (rows_join_kernel    joins them; kernels_rows_parts.hpp)
-//   rows_direct_grads    tiles of dx and of dw: the derivative is made from the scores on the way into the product.  A long sum is split over
-//                        workgroups, which leave partial sums, and
+//   rows_direct_delta    joins them (where there are few tiles; else rows_join_kernel has) and turns the scores into the loss's derivative times
+//                        the row's weight: made once, not by every tile of features (20 instructions each, which bound the gradients)
+//   rows_direct_grads    tiles of dx and of dw.  A long sum is split over workgroups, which leave partial sums, and
 //   rows_direct_sum      adds them up in their order.
 //
 // Products on v_mfma_f32_32x32x16_bf16: bf16 numbers as they are, fp32 ones as three bf16 parts (x = h + m + l, 24 bits) and the six largest
@@ -36,17 +36,24 @@ struct DirectArgs {
     float2* stats;                         // [tiles of classes][N]
     float* label_score;
     int score_deal, x_deal, w_deal;        // waves that deal a tile's sum among them: 4 (tiles of 32 x 32) or 1 (64 x 64)
+    // derivative
+    float *lse, *weight;                   // [N]; lse null: joined here
+    float *rowloss, *lse_out;              // results of the join (null: not asked for)
+    int tiles, batch;                      // of the statistics; of the derivative: times 64 rows per workgroup
+    double* shares;                        // of the loss, one per workgroup along the rows, or null
+    void* delta;                           // [V][score_row] of the storage type (fp32: in the scores' place), zeros for rows that add nothing
     // gradients
-    const float *lse, *weight;             // [Np], whole steps: weight 0 and
-    const int* label;                      // label kNoLabel for rows that add nothing and behind the last
     void* dx;
     long dx_pitch;
     void* dw;
     float* db;
+    int masked;                            // some rows may add nothing: their features do not count
     int x_along, w_along;                  // tiles along the features
     int x_splits, x_each, w_splits, w_each;   // parts of the sums over classes and over rows, and their lengths (multiples of kDirectK)
     int x_groups, w_groups;                // workgroups of dx, of dw (0: not asked for)
-    float *x_part, *w_part, *db_part;      // [split][N][D], [split][V][D], [split][V]: where splits > 1
+    float *x_part, *w_part;                // [split][N][D], [split][V][D]: where splits > 1
+    float* db_part;                        // [db_parts][V]: where the derivative's rows are taken by several workgroups
+    int db_parts, db_groups;               // and the workgroups that add them up
     const double* loss_part;
     int loss_parts;
     double* loss;
@@ -213,6 +220,97 @@ __device__ __forceinline__ float direct_delta(float score, float lse, bool live,
     return live ? (hot ? p - 1.f : p) : 0.f;
 }
 
+// 64 classes x `batch` times 64 rows per workgroup: a lane a row, a wave every fourth class
+constexpr int kDeltaSide = 64, kDeltaFewTiles = 32;
+template <typename T>
+__global__ __launch_bounds__(256) void rows_direct_delta_kernel(DirectArgs a)
+{
+    __shared__ float2 red[4][kDeltaSide];
+    __shared__ float tile[kDeltaSide][kDeltaSide + 1];
+    __shared__ double shares[kDeltaSide];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int v0 = blockIdx.y * kDeltaSide;
+    constexpr float kNone = -__builtin_inff();
+    float db = 0.f;
+    double share = 0.0;
+    for (int i = 0; i < a.batch; ++i) {
+        const int n = (blockIdx.x * a.batch + i) * kDeltaSide + lane, at = n < a.N ? n : a.N - 1;
+        if (n - lane >= a.N) break;                      // (uniform)
+        float x[16];
+        if (a.delta)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int v = v0 + wave + 4 * k;
+                x[k] = a.scores[(v < a.V ? v : a.V - 1) * a.score_row + at];
+            }
+        const float w = row_weight(a.mask, at), weight = n < a.N ? w : 0.f;
+        const int label = weight != 0.f ? a.mask.labels[at] : kNoLabel;
+        float lse;
+        if (a.tiles > kDeltaFewTiles) {                  // joined before
+            lse = a.lse[at];
+        } else {
+            float2 t[kDeltaFewTiles / 4], s{kNone, 0.f};
+#pragma unroll
+            for (int q = 0; q < kDeltaFewTiles / 4; ++q) {
+                const int of = wave + 4 * q;
+                t[q] = a.stats[(long)(of < a.tiles ? of : 0) * a.N + at];
+            }
+#pragma unroll
+            for (int q = 0; q < kDeltaFewTiles / 4; ++q)
+                if (wave + 4 * q < a.tiles) s = direct_join(s, t[q]);
+            red[wave][lane] = s;
+            __syncthreads();
+            s = red[0][lane];
+#pragma unroll
+            for (int q = 1; q < 4; ++q) s = direct_join(s, red[q][lane]);
+            lse = s.x == kNone ? kNone : s.x + logf(s.y);
+            if (blockIdx.y == 0 && wave == 0 && n < a.N) {
+                float loss = 0.f;
+                if (weight != 0.f) {
+                    const float score = a.label_score[n];
+                    loss = weight * (score == kNone ? __builtin_inff() : lse - score);   // (a class that is switched off)
+                }
+                if (a.rowloss) a.rowloss[n] = loss;
+                if (a.lse_out) a.lse_out[n] = weight != 0.f ? lse : 0.f;
+                if (a.weight) a.weight[n] = weight;
+                share += (double)loss;
+            }
+        }
+        if (!a.delta) continue;                          // (the loss alone; nobody reads `red` before its next barrier but this wave's lanes)
+        T* const delta = (T*)a.delta;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int v = v0 + wave + 4 * k;
+            const float g = direct_delta(x[k], lse, label != kNoLabel, label == v) * weight, put = weight != 0.f ? g : 0.f;
+            tile[wave + 4 * k][lane] = put;
+            if (v < a.V) store1(delta + v * a.score_row + n, put);
+        }
+        __syncthreads();
+        if (a.db) {                                      // four threads a class
+            float s = 0.f;
+#pragma unroll
+            for (int z = 0; z < 16; ++z) s += tile[tid >> 2][16 * (tid & 3) + z];
+            db += s;
+        }
+        __syncthreads();
+    }
+    if (a.db) {
+        db += __shfl_xor(db, 1, 64);
+        db += __shfl_xor(db, 2, 64);
+        const int v = v0 + (tid >> 2);
+        if ((tid & 3) == 0 && v < a.V) (a.db_part ? a.db_part + (long)blockIdx.x * a.V : a.db)[v] = db;
+    }
+    if (blockIdx.y == 0 && a.shares) {
+        if (wave == 0) shares[lane] = share;
+        __syncthreads();
+        if (tid == 0) {
+            double s = 0.0;
+            for (int q = 0; q < kDeltaSide; ++q) s += shares[q];
+            a.shares[blockIdx.x] = s;
+        }
+    }
+}
+
 template <typename T>
 __global__ __launch_bounds__(256) void rows_direct_grads_kernel(DirectArgs a)
 {
@@ -242,36 +340,55 @@ __global__ __launch_bounds__(256) void rows_direct_grads_kernel(DirectArgs a)
     const int mt = tile / along, dt = tile - mt * along;
     const int side = deal ? 32 : 64;
     const int m0 = mt * side + (deal ? 0 : 32 * (wave >> 1)), d0 = dt * side + (deal ? 0 : 32 * (wave & 1)), k0 = split * each;
-    const int len = K - k0 < each ? K - k0 : each, steps = (len + kDirectK - 1) / kDirectK;
+    const int len = K - k0 < each ? K - k0 : each, steps = (len + kDirectK - 1) / kDirectK, full = len / kDirectK;
     const int first = deal ? wave : 0, by = deal ? 4 : 1;
     v16f acc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[r] = 0.f;
     const int d = d0 + row < a.D ? d0 + row : a.D - 1;
     const int m = m0 + row < M ? m0 + row : M - 1;
-    float bias = 0.f;
-    if (dx) {
-        const float lse = a.lse[m];
-        const int label = a.label[m];
-        const T* const w = (const T*)a.w + d;
-        const float* const sc = a.scores + m;
-        float u[16];
-        T y[16];
-        auto fetch = [&](int s) {                        // scores [class][row], weights [class][feature]: lanes side by side, 8 k's one below the other
+    // fetches across the rows of memory (weights, features, and the derivative for dx): lanes side by side, 8 k's one below the other
+    const T* const b = dx ? (const T*)a.w : (const T*)a.x;
+    const long b_pitch = dx ? a.w_pitch : a.x_pitch;
+    const T* const bp = b + (k0 + 8 * half) * b_pitch + d;
+    auto fetch_b = [&](T (&y)[16], int s) {
+        if (s < full) {
+            const T* const p = bp + s * kDirectK * b_pitch;
+#pragma unroll
+            for (int z = 0; z < 16; ++z) y[z] = p[(16 * (z >> 3) + (z & 7)) * b_pitch];
+        } else {
 #pragma unroll
             for (int z = 0; z < 16; ++z) {
-                const int v = k0 + s * kDirectK + 16 * (z >> 3) + 8 * half + (z & 7), at = v < a.V ? v : a.V - 1;
-                u[z] = sc[at * a.score_row];
-                y[z] = w[at * a.w_pitch];
+                const int k = k0 + s * kDirectK + 16 * (z >> 3) + 8 * half + (z & 7);
+                y[z] = b[(k < K ? k : K - 1) * b_pitch + d];
             }
+        }
+    };
+    if (dx) {
+        const T* const ap = (const T*)a.delta + (k0 + 8 * half) * a.score_row + m;
+        T u[16], y[16];
+        auto fetch = [&](int s) {
+            if (s < full) {
+                const T* const p = ap + s * kDirectK * a.score_row;
+#pragma unroll
+                for (int z = 0; z < 16; ++z) u[z] = p[(16 * (z >> 3) + (z & 7)) * a.score_row];
+            } else {
+#pragma unroll
+                for (int z = 0; z < 16; ++z) {
+                    const int k = k0 + s * kDirectK + 16 * (z >> 3) + 8 * half + (z & 7);
+                    u[z] = ((const T*)a.delta)[(k < K ? k : K - 1) * a.score_row + m];
+                }
+            }
+            fetch_b(y, s);
         };
         if (first < steps) fetch(first);
         for (int s = first; s < steps; s += by) {
             v8f p[2], q[2];
+            const int left = len - s * kDirectK;
 #pragma unroll
             for (int z = 0; z < 16; ++z) {
-                const int v = k0 + s * kDirectK + 16 * (z >> 3) + 8 * half + (z & 7);
-                p[z >> 3][z & 7] = direct_delta(u[z], lse, label != kNoLabel && v < a.V, v == label);
+                const int k = 16 * (z >> 3) + 8 * half + (z & 7);
+                p[z >> 3][z & 7] = k < left ? (float)u[z] : 0.f;
                 q[z >> 3][z & 7] = (float)y[z];          // (beyond the last class times a derivative of zero: finite or not finite anyway)
             }
             if (s + by < steps) fetch(s + by);
@@ -279,84 +396,88 @@ __global__ __launch_bounds__(256) void rows_direct_grads_kernel(DirectArgs a)
             direct_product<T>(acc, p[1], q[1]);
         }
     } else {
-        const float* const sc = a.scores + m * a.score_row;
-        const T* const x = (const T*)a.x + d;
-        v8f u[2], l[2], w8[2];
-        v4i t[4];
+        const T* const ap = (const T*)a.delta + m * a.score_row;
+        Raw8<T> u[2];
         T y[16];
         auto fetch = [&](int s) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int n = k0 + s * kDirectK + 16 * k + 8 * half;    // (scores, lse, weight and label are padded to whole steps)
-                u[k] = load8(sc + n);
-                l[k] = load8(a.lse + n);
-                w8[k] = load8(a.weight + n);
-                t[2 * k] = *reinterpret_cast<const v4i*>(a.label + n);
-                t[2 * k + 1] = *reinterpret_cast<const v4i*>(a.label + n + 4);
-            }
-#pragma unroll
-            for (int z = 0; z < 16; ++z) {
-                const int n = k0 + s * kDirectK + 16 * (z >> 3) + 8 * half + (z & 7);
-                y[z] = x[(n < a.N ? n : a.N - 1) * a.x_pitch];
-            }
+            for (int k = 0; k < 2; ++k) u[k] = raw8(ap + k0 + s * kDirectK + 16 * k + 8 * half);   // (padded to whole steps with zeros)
+            fetch_b(y, s);
         };
         if (first < steps) fetch(first);
         for (int s = first; s < steps; s += by) {
             v8f p[2], q[2];
 #pragma unroll
-            for (int z = 0; z < 16; ++z) {
-                const int k = z >> 3, label = t[z >> 2][z & 3];
-                const bool live = label != kNoLabel;
-                const float g = direct_delta(u[k][z & 7], l[k][z & 7], live, label == m) * w8[k][z & 7];
-                p[k][z & 7] = g;
-                bias += g;
-                q[k][z & 7] = live ? (float)y[z] : 0.f;
+            for (int k = 0; k < 2; ++k) {
+                p[k] = widen(u[k]);
+#pragma unroll
+                for (int z = 0; z < 8; ++z) q[k][z] = (float)y[8 * k + z];
+            }
+            if (a.masked) {                              // rows that add nothing may hold anything
+#pragma unroll
+                for (int z = 0; z < 16; ++z) {
+                    const int n = k0 + s * kDirectK + 16 * (z >> 3) + 8 * half + (z & 7);
+                    if (a.weight[n < K ? n : K - 1] == 0.f) q[z >> 3][z & 7] = 0.f;
+                }
             }
             if (s + by < steps) fetch(s + by);
             direct_product<T>(acc, p[0], q[0]);
             direct_product<T>(acc, p[1], q[1]);
         }
-        bias += __shfl_xor(bias, 32, 64);
     }
 
-    const bool whole = splits == 1;
     auto put = [&](int m, int d, float v) {
         if (m >= M || d >= a.D) return;
-        if (!whole) {
+        if (splits > 1) {
             (dx ? a.x_part : a.w_part)[((long)split * M + m) * a.D + d] = v;
         } else if (dx) {
-            const float scale = a.weight[m];
-            store1((T*)a.dx + m * a.dx_pitch + d, scale == 0.f ? 0.f : v * scale);
-        } else if (a.dw) {
+            store1((T*)a.dx + m * a.dx_pitch + d, a.weight[m] == 0.f ? 0.f : v);
+        } else {
             store1((T*)a.dw + (long)m * a.D + d, v);
         }
     };
-    float* const to_db = whole ? a.db : a.db_part + (long)split * a.V;
     if (deal) {
         const v4f s = direct_fold(acc, fold);
 #pragma unroll
         for (int q = 0; q < 4; ++q) put(m0 + 4 * (tid >> 5) + q, d0 + (tid & 31), s[q]);
-        if (!dx && dt == 0 && a.db) {
-            __syncthreads();
-            if (half == 0) fold[wave][0][row] = bias;
-            __syncthreads();
-            if (tid < 32 && m0 + tid < a.V) to_db[m0 + tid] = ((fold[0][0][tid] + fold[1][0][tid]) + fold[2][0][tid]) + fold[3][0][tid];
-        }
         return;
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) put(m0 + 8 * (r >> 2) + 4 * half + (r & 3), d0 + row, acc[r]);
-    if (!dx && dt == 0 && a.db && (wave & 1) == 0 && half == 0 && m0 + row < a.V) to_db[m0 + row] = bias;
 }
 
 template <typename T>
 __global__ __launch_bounds__(256) void rows_direct_sum_kernel(DirectArgs a)
 {
-    const long nx = a.x_part ? (long)a.N * a.D : 0, nw = a.w_part && a.dw ? (long)a.V * a.D : 0, nb = a.db_part && a.db ? a.V : 0;
-    for (long e = (long)blockIdx.x * 256 + threadIdx.x; e < nx + nw + nb; e += (long)gridDim.x * 256) {
-        const bool of_x = e < nx, of_w = !of_x && e < nx + nw;
-        const long at = of_x ? e : of_w ? e - nx : e - nx - nw, by = of_x ? nx : of_w ? (long)a.V * a.D : a.V;
-        const float* const part = (of_x ? a.x_part : of_w ? a.w_part : a.db_part) + at;
+    const long nx = a.x_part ? (long)a.N * a.D : 0, nw = a.w_part ? (long)a.V * a.D : 0;
+    if (blockIdx.x < (unsigned)a.db_groups) {            // bias gradients: 32 classes, the parts dealt to eight threads each
+        __shared__ float red[8][32];
+        const int own = threadIdx.x & 31, deal = threadIdx.x >> 5;
+        const long v = (long)blockIdx.x * 32 + own;
+        float s = 0.f;
+        if (v < a.V) {
+            int i = deal;
+            for (; i + 56 < a.db_parts; i += 64) {
+                float u[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) u[q] = a.db_part[(long)(i + 8 * q) * a.V + v];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) s += u[q];
+            }
+            for (; i < a.db_parts; i += 8) s += a.db_part[(long)i * a.V + v];
+        }
+        red[deal][own] = s;
+        __syncthreads();
+        if (deal == 0 && v < a.V) {
+            for (int q = 1; q < 8; ++q) s += red[q][own];
+            a.db[v] = s;
+        }
+        return;
+    }
+    for (long e = (long)(blockIdx.x - a.db_groups) * 256 + threadIdx.x; e < nx + nw; e += (long)(gridDim.x - a.db_groups) * 256) {
+        const bool of_x = e < nx;
+        const long at = of_x ? e : e - nx, by = of_x ? nx : nw;
+        const float* const part = (of_x ? a.x_part : a.w_part) + at;
         const int splits = of_x ? a.x_splits : a.w_splits;
         float s = 0.f;
         int i = 0;
@@ -370,12 +491,9 @@ __global__ __launch_bounds__(256) void rows_direct_sum_kernel(DirectArgs a)
         for (; i < splits; ++i) s += part[i * by];
         if (of_x) {
             const long n = at / a.D;
-            const float scale = a.weight[n];
-            store1((T*)a.dx + n * a.dx_pitch + (at - n * a.D), scale == 0.f ? 0.f : s * scale);
-        } else if (of_w) {
-            store1((T*)a.dw + at, s);
+            store1((T*)a.dx + n * a.dx_pitch + (at - n * a.D), a.weight[n] == 0.f ? 0.f : s);
         } else {
-            a.db[at] = s;
+            store1((T*)a.dw + at, s);
         }
     }
 }

@@ -148,7 +148,7 @@ def _stream_handle(stream) -> int:
 
 
 def _ptr(t) -> Optional[int]:
-    return None if t is None else int(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 class Net:
@@ -417,19 +417,22 @@ def _check_norm(norm, device):
 class _On:
     """The tensors' GPU and the stream a call goes to (None: that GPU's current one), made current: memory that
     is allocated inside belongs to that stream, as the work on it does."""
+    __slots__ = ("handle", "ctx")
 
     def __init__(self, device, stream):
         import torch
+        self.ctx = None
         if stream is None:
-            self.handle = torch.cuda.current_stream(device).cuda_stream
-            self.ctx = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+            self.handle = torch._C._cuda_getCurrentRawStream(device.index)
+            if device.index != torch.cuda.current_device():
+                self.ctx = torch.cuda.device(device)
         else:
             self.handle = int(getattr(stream, "cuda_stream", stream))
             if not hasattr(stream, "cuda_stream"):
                 stream = torch.cuda.ExternalStream(self.handle, device=device)
-            self.ctx = torch.cuda.stream(stream)
             if stream.device != device:
                 _refuse("the stream belongs to %s, the tensors to %s" % (stream.device, device))
+            self.ctx = torch.cuda.stream(stream)
 
     def __enter__(self):
         if self.ctx is not None:
@@ -527,60 +530,63 @@ def class_workspace_bytes(rows: int, features: int, classes: int, dtype: int, tr
 
 
 def _rows_of(name, t, device, dtype):
-    """A matrix whose rows are dense -> its pitch in elements."""
-    if t.dim() != 2 or t.device != device or t.dtype != dtype:
+    """A matrix whose rows are dense -> its rows, columns and pitch in elements."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or t.dtype != dtype or t.device != device:
         _refuse("%s: a %s matrix on %s is wanted" % (name, dtype, device))
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    rows, columns = shape
+    if columns > 1 and stride[1] != 1:
         _refuse("%s: the numbers of a row have to be consecutive" % name)
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    return rows, columns, stride[0] if rows > 1 else max(columns, stride[0])
 
 
 def _vector(name, t, n, dtype, device):
-    if t.dtype != dtype or t.device != device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != (n,) or t.device != device or not t.is_contiguous():
         _refuse("%s: %d numbers %s on %s are wanted, consecutive" % (name, n, dtype, device))
     return t.data_ptr()
 
 
-class _ClassCall:
-    """Arguments of class_loss and class_backward, checked."""
+def _class_call(x, w, labels, bias, roww):
+    """The arguments that class_loss and class_backward share, checked; and the tensors' GPU."""
+    import torch
+    device, dtype = x.device, x.dtype
+    if device.type != "cuda":
+        _refuse("x: a tensor on a GPU is wanted")
+    kind = _dtype_of(x)
+    rows, features, x_pitch = _rows_of("x", x, device, dtype)
+    classes, columns, w_pitch = _rows_of("w", w, device, dtype)
+    if columns != features:
+        _refuse("x has %d features, w %d" % (features, columns))
+    f32 = torch.float32
+    return device, (x.data_ptr(), x_pitch, w.data_ptr(), w_pitch, _vector("bias", bias, classes, f32, device),
+                    _vector("labels", labels, rows, torch.int32, device), _vector("roww", roww, rows, f32, device),
+                    rows, features, classes, kind)
 
-    def __init__(self, x, w, labels, bias, roww):
-        import torch
-        if not x.is_cuda:
-            _refuse("x: a tensor on a GPU is wanted")
-        self.device, self.dtype = x.device, _dtype_of(x)
-        self.x_pitch = _rows_of("x", x, x.device, x.dtype)
-        self.w_pitch = _rows_of("w", w, x.device, x.dtype)
-        self.rows, self.features, self.classes = x.shape[0], x.shape[1], w.shape[0]
-        if w.shape[1] != self.features:
-            _refuse("x has %d features, w %d" % (self.features, w.shape[1]))
-        self.args = (x.data_ptr(), self.x_pitch, w.data_ptr(), self.w_pitch,
-                     None if bias is None else _vector("bias", bias, self.classes, torch.float32, x.device),
-                     _vector("labels", labels, self.rows, torch.int32, x.device),
-                     None if roww is None else _vector("roww", roww, self.rows, torch.float32, x.device),
-                     self.rows, self.features, self.classes, self.dtype)
 
-    def output(self, name, given, shape, dtype):
-        """Given (checked), allocated (None) or not asked for (False) -> the tensor or None."""
+def _output(name, given, shape, dtype, device):
+    """Given (checked), allocated (None) or not asked for (False) -> the tensor or None."""
+    if given is None:
         import torch
-        if given is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        if given is False:
-            return None
-        if given.dtype != dtype or given.device != self.device or tuple(given.shape) != shape:
-            _refuse("%s: %s of shape %s on %s is wanted" % (name, dtype, shape, self.device))
-        if not given.is_contiguous() and name != "dx":
-            _refuse("%s has to be contiguous" % name)
-        return given
+        return torch.empty(shape, dtype=dtype, device=device)
+    if given is False:
+        return None
+    if given.dtype != dtype or given.device != device or given.shape != shape:
+        _refuse("%s: %s of shape %s on %s is wanted" % (name, dtype, shape, device))
+    if name != "dx" and not given.is_contiguous():
+        _refuse("%s has to be contiguous" % name)
+    return given
 
-    def workspace(self, ws, training):
-        import torch
-        need = class_workspace_bytes(self.rows, self.features, self.classes, self.dtype, training)
-        if ws is None:
-            return torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
-        if ws.device != self.device or not ws.is_contiguous():
-            _refuse("ws: contiguous memory on %s is wanted" % self.device)
-        return ws
+
+def _class_workspace(ws, args, training, device):
+    """Address and bytes of the workspace, and what keeps it."""
+    import torch
+    if ws is None:
+        ws = torch.empty(max(256, lib().mpcnn_workspace_bytes_class(*args[7:], training)), dtype=torch.uint8, device=device)
+    elif ws.device != device or not ws.is_contiguous():
+        _refuse("ws: contiguous memory on %s is wanted" % device)
+    return ws.data_ptr(), ws.numel() * ws.element_size(), ws
 
 
 def class_loss(x, w, labels, bias=None, roww=None, rowloss=None, lse=None, loss=None, ws=None, stream=None):
@@ -590,13 +596,13 @@ def class_loss(x, w, labels, bias=None, roww=None, rowloss=None, lse=None, loss=
     and roww [rows] fp32 or None.  -> (loss, rowloss, lse): the summed loss (one fp64), w * -log p[label] and
     log sum exp of the scores per row (fp32), put into the tensors given, allocated for None, left out for False."""
     import torch
-    c = _ClassCall(x, w, labels, bias, roww)
-    with _On(c.device, stream) as st:
-        loss = c.output("loss", loss, (1,), torch.float64)
-        rowloss = c.output("rowloss", rowloss, (c.rows,), torch.float32)
-        lse = c.output("lse", lse, (c.rows,), torch.float32)
-        ws = c.workspace(ws, False)
-        _check(lib().mpcnn_class_loss(*c.args, _ptr(rowloss), _ptr(lse), _ptr(loss), ws.data_ptr(), ws.numel() * ws.element_size(), st))
+    device, args = _class_call(x, w, labels, bias, roww)
+    with _On(device, stream) as st:
+        loss = _output("loss", loss, (1,), torch.float64, device)
+        rowloss = _output("rowloss", rowloss, (args[7],), torch.float32, device)
+        lse = _output("lse", lse, (args[7],), torch.float32, device)
+        at, size, _kept = _class_workspace(ws, args, 0, device)
+        _check(lib().mpcnn_class_loss(*args, _ptr(rowloss), _ptr(lse), _ptr(loss), at, size, st))
     return loss, rowloss, lse
 
 
@@ -604,15 +610,20 @@ def class_backward(x, w, labels, bias=None, roww=None, rowloss=None, loss=None, 
     """class_loss and its gradients -> (loss, rowloss, dx, dw, db); dx and dw have x's type, db (None without
     a bias) is fp32.  Each is put into the tensor given (dx: its rows dense), allocated for None, left out for False."""
     import torch
-    c = _ClassCall(x, w, labels, bias, roww)
-    with _On(c.device, stream) as st:
-        loss = c.output("loss", loss, (1,), torch.float64)
-        rowloss = c.output("rowloss", rowloss, (c.rows,), torch.float32)
-        dx = c.output("dx", dx, (c.rows, c.features), x.dtype)
-        dw = c.output("dw", dw, (c.classes, c.features), x.dtype)
-        db = c.output("db", False if bias is None and db is None else db, (c.classes,), torch.float32)
-        ws = c.workspace(ws, True)
-        pitch = c.features if dx is None else _rows_of("dx", dx, c.device, x.dtype)
-        _check(lib().mpcnn_class_backward(*c.args, _ptr(rowloss), _ptr(loss), _ptr(dx), pitch, _ptr(dw), _ptr(db),
-                                          ws.data_ptr(), ws.numel() * ws.element_size(), st))
+    device, args = _class_call(x, w, labels, bias, roww)
+    rows, features, classes = args[7:10]
+    with _On(device, stream) as st:
+        loss = _output("loss", loss, (1,), torch.float64, device)
+        rowloss = _output("rowloss", rowloss, (rows,), torch.float32, device)
+        pitch = features
+        if dx is None:
+            dx = torch.empty((rows, features), dtype=x.dtype, device=device)
+        else:
+            dx = _output("dx", dx, (rows, features), x.dtype, device)
+            if dx is not None:
+                pitch = _rows_of("dx", dx, device, x.dtype)[2]
+        dw = _output("dw", dw, (classes, features), x.dtype, device)
+        db = _output("db", False if bias is None and db is None else db, (classes,), torch.float32, device)
+        at, size, _kept = _class_workspace(ws, args, 1, device)
+        _check(lib().mpcnn_class_backward(*args, _ptr(rowloss), _ptr(loss), _ptr(dx), pitch, _ptr(dw), _ptr(db), at, size, st))
     return loss, rowloss, dx, dw, db
