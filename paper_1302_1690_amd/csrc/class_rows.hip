@@ -33,28 +33,37 @@ inline int64_t up_to(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
 
 struct Tiling { bool big; int tiles_m, tiles_n, splits, per_split; };
 
-// Tiles of 256 x 256 where they give most compute units one, of 128 x 128 (two of their workgroups share a compute unit) otherwise.  Where few
-// of either, the sum over k is split, no further than kLeast blocks.
-Tiling tiling_of(int64_t M, int64_t N, int64_t blocks, int64_t most_splits)
+// Tiles of 256 x 256 (a workgroup per compute unit) or of 128 x 128 (two), the sum over k whole or split so that the parts fill one to four
+// rounds of workgroups: whichever should take least.  A step of k (128 bytes of a row) of a tile takes 1.9 us (measured: 1.15 PFLOP/s on
+// 256 x 256) or, two side by side, 1.3; fp32 storage's steps half as long again; a split costs the partial sums' way to memory and
+// back (12 bytes of traffic at 5 TB/s each) and a launch.
+Tiling tiling_of(int64_t M, int64_t N, int64_t blocks, int64_t most_splits, bool halves)
 {
-    constexpr int kLeast = 8;
-    Tiling t{};
     M = std::max<int64_t>(M, 1); N = std::max<int64_t>(N, 1);   // (no rows: nothing is launched)
-    const int64_t big = (M + 255) / 256 * ((N + 255) / 256), small = (M + 127) / 128 * ((N + 127) / 128);
-    int64_t splits = 1;
-    const int64_t can = std::max<int64_t>(1, std::min(most_splits, blocks / kLeast));
-    t.big = big * can >= kCUs * 3 / 4;
-    if (t.big) splits = std::min(can, std::max<int64_t>(1, kCUs / big));
-    else splits = std::min(can, std::max<int64_t>(1, 2 * kCUs / small));
-    const int64_t side = t.big ? 256 : 128;
-    t.tiles_m = (int)((M + side - 1) / side);
-    t.tiles_n = (int)((N + side - 1) / side);
-    t.per_split = (int)((blocks + splits - 1) / splits);
-    t.splits = (int)((blocks + t.per_split - 1) / t.per_split);
-    return t;
+    Tiling best{};
+    double least = 0.0;
+    for (int big = 0; big < 2; ++big) {
+        const int64_t side = big ? 256 : 128, slots = big ? kCUs : 2 * kCUs;
+        const int64_t tiles = (M + side - 1) / side * ((N + side - 1) / side);
+        for (int round = 0; round <= 4; ++round) {
+            const int64_t splits = round ? round * slots / tiles : 1;
+            if (round && (splits < 2 || splits > most_splits || blocks / splits < 4)) continue;
+            Tiling t{};
+            t.big = big != 0;
+            t.tiles_m = (int)((M + side - 1) / side);
+            t.tiles_n = (int)((N + side - 1) / side);
+            t.per_split = (int)((blocks + splits - 1) / splits);
+            t.splits = (int)((blocks + t.per_split - 1) / t.per_split);
+            const int64_t rounds = (tiles * t.splits + slots - 1) / slots;
+            const double us = (double)rounds * (3.0 + t.per_split * (big ? 1.9 : 1.3) * (halves ? 1.5 : 1.0)) +
+                              (t.splits > 1 ? 4.0 + 12e-6 * (double)M * (double)N * t.splits / 5.0 : 0.0);
+            if (!best.splits || us < least) { best = t; least = us; }
+        }
+    }
+    return best;
 }
 
-// Three launches (kernels_rows_direct.hpp) instead of a dozen
+// Three to five launches (kernels_rows_direct.hpp) instead of a dozen
 constexpr int64_t kDirectWork = 1500000000, kDirectRows = 64;   // rows x features x classes; whatever the work
 
 struct Plan {
@@ -167,8 +176,8 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     p->x_rows = take(N * p->d_bytes);
     p->w_rows = take(piece * p->d_bytes);
     if (train) {
-        p->dx = tiling_of(N, D, v_bytes / mpcnn::kBlockBytes, std::max<int64_t>(1, kPartRoom / (4 * N * D + 1)));
-        p->dw = tiling_of(piece, D, p->n_bytes / mpcnn::kBlockBytes, std::max<int64_t>(1, kPartRoom / (4 * piece * D)));
+        p->dx = tiling_of(N, D, v_bytes / mpcnn::kBlockBytes, std::min<int64_t>(64, std::max<int64_t>(1, kPartRoom / (4 * N * D + 1))), p->halves);
+        p->dw = tiling_of(piece, D, p->n_bytes / mpcnn::kBlockBytes, std::min<int64_t>(64, std::max<int64_t>(1, kPartRoom / (4 * piece * D))), p->halves);
         p->x_cols = take(D * p->n_bytes);
         p->w_cols = take(D * v_bytes);
         p->score = take((p->keep ? classes : piece) * p->Np * 4);
@@ -205,7 +214,7 @@ template <bool HALVES, int RESULT>
 mpcnn_status launch_product(mpcnn::ProductArgs a, const Tiling& t, hipStream_t st)
 {
     a.tiles_m = t.tiles_m; a.tiles_n = t.tiles_n; a.splits = t.splits; a.per_split = t.per_split;
-    return t.big ? launch_instance<2, 2, 4, 4, HALVES, RESULT>(a, st) : launch_instance<2, 2, 2, 2, HALVES, RESULT>(a, st);
+    return t.big ? launch_instance<2, 4, 4, 2, HALVES, RESULT>(a, st) : launch_instance<2, 2, 2, 2, HALVES, RESULT>(a, st);
 }
 
 struct Call {
@@ -356,20 +365,23 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
     unsigned* const x_peak = (unsigned*)(ws + p.peaks);
     unsigned *const w_peak = x_peak + mpcnn::kPeakGroups, *const roww_peak = w_peak + mpcnn::kPeakGroups;
     if constexpr (H) {
+        mpcnn::PeakSet set{};
+        int n = 0;
         auto peak = [&](const void* src, int64_t pitch, int64_t rows, int64_t cols, const mpcnn::RowMask& m, unsigned* words) {
-            mpcnn::PeakArgs a{(const float*)src, pitch, rows, (int)cols, m, words};
-            mpcnn::rows_peak_kernel<<<mpcnn::kPeakGroups, 256, 0, st>>>(a);
+            set.of[n++] = mpcnn::PeakArgs{(const float*)src, pitch, rows, (int)cols, m, words};
         };
         peak(c.x, c.x_pitch, p.N, p.D, mask, x_peak);
         peak(c.w, c.w_pitch, p.V, p.D, every, w_peak);
         if (p.train && c.roww) peak(c.roww, 1, p.N, 1, mask, roww_peak);
+        mpcnn::rows_peak_kernel<<<dim3(mpcnn::kPeakGroups, (unsigned)n), 1024, 0, st>>>(set);
     }
     auto pack = [&](const void* src, int64_t pitch, int64_t R, char* rows, char* cols, int64_t col_bytes, const mpcnn::RowMask& m, const unsigned* words) {
         mpcnn::PackRowsArgs a{};
         a.src = src; a.pitch = pitch; a.R = (int)R; a.C = p.D;
         a.rows = rows; a.cols = cols; a.row_bytes = p.d_bytes; a.col_bytes = col_bytes;
         a.mask = m; a.peak = words;
-        mpcnn::rows_pack_kernel<T><<<dim3((unsigned)((R + 63) / 64), (unsigned)((p.D + 63) / 64)), 256, 0, st>>>(a);
+        const dim3 grid((unsigned)(H ? (R + 63) / 64 : (R + 127) / 128), (unsigned)((p.D + 63) / 64));
+        (H ? mpcnn::rows_pack_kernel : mpcnn::rows_pack16_kernel)<<<grid, 256, 0, st>>>(a);
     };
     // operands as they are: whole blocks at aligned addresses
     auto direct = [&](const void* m, int64_t pitch) { return !H && p.D % 64 == 0 && (uintptr_t)m % 16 == 0 && pitch % 8 == 0 && pitch * 512 < (1ll << 31); };
@@ -389,7 +401,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         a.bias = c.bias ? c.bias + v0 : nullptr;
         a.labels = c.labels; a.stats = stats; a.label_score = (float*)(ws + p.label_score);
         a.scores = out; a.score_row = p.Np; a.class0 = (int)v0;
-        const Tiling t = tiling_of(n_classes, p.N, d_blocks, 1);
+        const Tiling t = tiling_of(n_classes, p.N, d_blocks, 1, H);
         if (tiles) *tiles = t.tiles_m;
         return launch_product<H, mpcnn::kScores>(a, t, st);
     };
@@ -446,7 +458,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         d.db_part = c.db ? (float*)(ws + p.db_part) : nullptr;
         mpcnn::rows_delta_kernel<H><<<dim3((unsigned)(p.Np / 64), (unsigned)((n + 63) / 64)), 256, 0, st>>>(d);
         fin.db_part = d.db_part; fin.tiles = (int)(p.Np / 64); fin.classes = n; fin.db = c.db ? c.db + v0 : nullptr;
-        if (fin.db || fin.loss) mpcnn::rows_finish_kernel<<<fin.db ? (unsigned)((n + 255) / 256) : 1, 256, 0, st>>>(fin);
+        if (fin.db || fin.loss) mpcnn::rows_finish_kernel<<<fin.db ? (unsigned)((n + 31) / 32) : 1, 256, 0, st>>>(fin);
         fin.loss = nullptr;
         if (c.dx) {
             mpcnn::ProductArgs a{};

@@ -2,8 +2,8 @@
 // are and transposed; the softmax's statistics joined; scores turned into the loss's derivative; partial sums added up.
 // All of it is bound by memory: 64 x 64 tiles through LDS, each number read once and written in both orders where both are needed.
 #pragma once
+#include "any_address.hpp"
 #include "ranges.hpp"
-#include "storage.hpp"
 
 namespace mpcnn {
 
@@ -33,38 +33,43 @@ struct PeakArgs {
     RowMask mask;                          // labels null: every row
     unsigned* words;                       // [kPeakGroups]
 };
-__global__ __launch_bounds__(256) void rows_peak_kernel(PeakArgs a)
+struct PeakSet { PeakArgs of[3]; };        // blockIdx.y: which
+__global__ __launch_bounds__(1024) void rows_peak_kernel(PeakSet set)
 {
-    __shared__ unsigned red[4];
+    __shared__ unsigned red[16];
+    const PeakArgs& a = set.of[blockIdx.y];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     unsigned peak = 0;
-    auto add = [&](float x) {
-        const unsigned b = bits_of(x) & 0x7fffffffu;
-        peak = b < kNoPeak && b > peak ? b : peak;
+    auto add = [&](const v8f& x, bool counts) {
+#pragma unroll
+        for (int z = 0; z < 8; ++z) {
+            const unsigned b = bits_of(x[z]) & 0x7fffffffu;
+            peak = counts && b < kNoPeak && b > peak ? b : peak;
+        }
     };
-    if (a.pitch == a.cols && !a.mask.labels) {           // one stretch
-        const long n = a.rows * a.cols, step = (long)gridDim.x * 256;
-        long e = (long)blockIdx.x * 256 + threadIdx.x;
-        for (; e + 7 * step < n; e += 8 * step) {        // eight loads in flight
-            float v[8];
+    // eight numbers of a row at a time, four times eight in flight; rows without gaps are one
+    const bool one = a.pitch == a.cols && !a.mask.labels && a.rows * a.cols < 0x7fffffff;
+    const long cols = one ? a.rows * a.cols : a.cols, rows = one ? 1 : a.rows;
+    const long octets = (cols + 7) / 8, all = rows * octets, step = (long)gridDim.x * 1024;
+    for (long e = (long)blockIdx.x * 1024 + threadIdx.x; e < all; e += 4 * step) {
+        v8f v[4];
+        bool counts[4];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = a.src[e + q * step];
+        for (int q = 0; q < 4; ++q) {
+            const long at = e + q * step < all ? e + q * step : e;
+            const long r = all == octets ? 0 : at / octets, c = 8 * (at - r * octets);
+            v[q] = load8_of(a.src + r * a.pitch, (int)c, (int)cols);
+            counts[q] = !a.mask.labels || row_weight(a.mask, (int)r) != 0.f;
+        }
 #pragma unroll
-            for (int q = 0; q < 8; ++q) add(v[q]);
-        }
-        for (; e < n; e += step) add(a.src[e]);
-    } else {
-        for (long r = (long)blockIdx.x * 4 + wave; r < a.rows; r += (long)gridDim.x * 4) {
-            if (a.mask.labels && row_weight(a.mask, (int)r) == 0.f) continue;
-            for (int c = lane; c < a.cols; c += 64) add(a.src[r * a.pitch + c]);
-        }
+        for (int q = 0; q < 4; ++q) add(v[q], counts[q]);
     }
     peak = wave_largest(peak);
     if (lane == 0) red[wave] = peak;
     __syncthreads();
     if (threadIdx.x == 0) {
         unsigned m = red[0];
-        for (int w = 1; w < 4; ++w) m = red[w] > m ? red[w] : m;
+        for (int w = 1; w < 16; ++w) m = red[w] > m ? red[w] : m;
         a.words[blockIdx.x] = m;
     }
 }
@@ -107,41 +112,86 @@ struct PackRowsArgs {
     RowMask mask;                          // labels null: every row
     const unsigned* peak;                  // fp32: [kPeakGroups], what the numbers are raised by
 };
-template <typename T>
+// fp32, two parts
 __global__ __launch_bounds__(256) void rows_pack_kernel(PackRowsArgs a)
 {
-    constexpr bool HALVES = sizeof(T) == 4;
-    constexpr int kPieces = HALVES ? 16 : 8;
+    constexpr int kPieces = 16;
     __shared__ float tile[64][65];
     const int c0 = 64 * blockIdx.y, r0 = 64 * blockIdx.x;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    float up = 1.f;
-    if constexpr (HALVES) up = power_of_two(raise_of(peak_of(a.peak, kPeakGroups), 0));
-    const T* src = (const T*)a.src;
-    float v[16];
+    const float up = power_of_two(raise_of(peak_of(a.peak, kPeakGroups), 0));
+    v8f v[2];
+    bool there[2];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int r = r0 + wave + 4 * i, c = c0 + lane;
-        const bool there = r < a.R && c < a.C && (!a.mask.labels || row_weight(a.mask, r) != 0.f);
-        v[i] = there ? load1(src + (long)r * a.pitch + c) : 0.f;
+    for (int i = 0; i < 2; ++i) {                        // 8 lanes a row, 8 numbers each
+        const int r = r0 + 32 * i + (threadIdx.x >> 3), at = r < a.R ? r : a.R - 1;
+        v[i] = load8_of((const float*)a.src + at * a.pitch, c0 + 8 * (threadIdx.x & 7), a.C);
+        there[i] = r < a.R && (!a.mask.labels || row_weight(a.mask, at) != 0.f);
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) tile[wave + 4 * i][lane] = v[i] * up;
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int z = 0; z < 8; ++z) tile[32 * i + (threadIdx.x >> 3)][8 * (threadIdx.x & 7) + z] = there[i] ? v[i][z] * up : 0.f;
     __syncthreads();
     if (a.rows)
         for (int q = threadIdx.x; q < 64 * kPieces; q += 256) {
             const int r = q / kPieces, p = q % kPieces;
             const long at = (long)blockIdx.y * (kPieces * 16) + 16 * p;
             if (r0 + r >= a.R || at >= a.row_bytes) continue;
-            *reinterpret_cast<v4f*>(a.rows + (long)(r0 + r) * a.row_bytes + at) = piece_of<HALVES>(p, [&](int i) { return tile[r][i]; });
+            *reinterpret_cast<v4f*>(a.rows + (long)(r0 + r) * a.row_bytes + at) = piece_of<true>(p, [&](int i) { return tile[r][i]; });
         }
     if (a.cols)
         for (int q = threadIdx.x; q < 64 * kPieces; q += 256) {
             const int c = q / kPieces, p = q % kPieces;
             const long at = (long)blockIdx.x * (kPieces * 16) + 16 * p;
             if (c0 + c >= a.C || at >= a.col_bytes) continue;
-            *reinterpret_cast<v4f*>(a.cols + (long)(c0 + c) * a.col_bytes + at) = piece_of<HALVES>(p, [&](int i) { return tile[i][c]; });
+            *reinterpret_cast<v4f*>(a.cols + (long)(c0 + c) * a.col_bytes + at) = piece_of<true>(p, [&](int i) { return tile[i][c]; });
         }
+}
+// bf16: as they are, 128 rows per workgroup.  LDS holds pairs of columns; a thread reads 8 rows of a pair and leaves a piece of either column.
+__global__ __launch_bounds__(256) void rows_pack16_kernel(PackRowsArgs a)
+{
+    typedef unsigned v4u __attribute__((ext_vector_type(4)));
+    __shared__ unsigned tile[128][33];
+    const int c0 = 64 * blockIdx.y, r0 = 128 * blockIdx.x;
+    v4u v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                        // 8 lanes a row, 8 numbers each
+        const int r = r0 + 32 * i + (threadIdx.x >> 3), at = r < a.R ? r : a.R - 1;
+        const Raw8<bf16> u = raw8_of((const bf16*)a.src + at * a.pitch, c0 + 8 * (threadIdx.x & 7), a.C);
+        const bool there = r < a.R && (!a.mask.labels || row_weight(a.mask, at) != 0.f);
+        v[i] = there ? __builtin_bit_cast(v4u, u.a) : v4u{0, 0, 0, 0};
+    }
+    if (a.rows)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = r0 + 32 * i + (threadIdx.x >> 3);
+            const long at = (long)blockIdx.y * 128 + 16 * (threadIdx.x & 7);
+            if (r < a.R && at < a.row_bytes) *reinterpret_cast<v4u*>(a.rows + (long)r * a.row_bytes + at) = v[i];
+        }
+    if (!a.cols) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) tile[32 * i + (threadIdx.x >> 3)][4 * (threadIdx.x & 7) + z] = v[i][z];
+    __syncthreads();
+    const int oct = threadIdx.x & 15;
+    const long at = (long)blockIdx.x * 256 + 16 * oct;
+    if (at >= a.col_bytes) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int pair = 16 * i + (threadIdx.x >> 4), c = c0 + 2 * pair;
+        unsigned x[8];
+#pragma unroll
+        for (int z = 0; z < 8; ++z) x[z] = tile[8 * oct + z][pair];
+        v4u even, odd;
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+            even[z] = (x[2 * z] & 0xffffu) | x[2 * z + 1] << 16;
+            odd[z] = x[2 * z] >> 16 | (x[2 * z + 1] & 0xffff0000u);
+        }
+        if (c < a.C) *reinterpret_cast<v4u*>(a.cols + (long)c * a.col_bytes + at) = even;
+        if (c + 1 < a.C) *reinterpret_cast<v4u*>(a.cols + (long)(c + 1) * a.col_bytes + at) = odd;
+    }
 }
 
 // ---- per row: the statistics of all tiles of classes joined; the loss; per workgroup its share of the summed loss
@@ -369,19 +419,27 @@ __global__ __launch_bounds__(256) void rows_finish_kernel(FinishArgs a)
         if (threadIdx.x == 0) *a.loss = red[0];
     }
     if (!a.db) return;
-    const long v = (long)blockIdx.x * 256 + threadIdx.x;
-    if (v >= a.classes) return;
-    double s0 = 0.0, s1 = 0.0;
-    int t = 0;
-    for (; t + 3 < a.tiles; t += 4) {
-        float u[4];
+    __syncthreads();
+    // 32 classes, the tiles dealt to eight threads each, eight loads in flight
+    const int own = threadIdx.x & 31, deal = threadIdx.x >> 5;
+    const long v = (long)blockIdx.x * 32 + own;
+    double s = 0.0;
+    if (v < a.classes) {
+        int t = deal;
+        for (; t + 56 < a.tiles; t += 64) {
+            float u[8];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) u[q] = a.db_part[(t + q) * a.classes + v];
-        s0 += (double)u[0] + (double)u[1];
-        s1 += (double)u[2] + (double)u[3];
+            for (int q = 0; q < 8; ++q) u[q] = a.db_part[(long)(t + 8 * q) * a.classes + v];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s += (double)u[q];
+        }
+        for (; t < a.tiles; t += 8) s += (double)a.db_part[(long)t * a.classes + v];
     }
-    for (; t < a.tiles; ++t) s0 += (double)a.db_part[t * a.classes + v];
-    a.db[v] = (float)(s0 + s1);
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (deal != 0 || v >= a.classes) return;
+    for (int q = 1; q < 8; ++q) s += red[32 * q + own];
+    a.db[v] = (float)s;
 }
 
 }  // namespace mpcnn

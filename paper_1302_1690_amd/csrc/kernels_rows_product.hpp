@@ -8,14 +8,16 @@
 //
 // A workgroup computes a tile of 32 WM MT x 32 WN NT results, each wave MT x NT of the instruction's, in accumulators.  Both operands' next
 // blocks come from memory straight into the LDS buffer that is not being multiplied (128 bits per lane, a barrier per block).  An LDS row is a
-// block (128 bytes); its 16-byte pieces lie permuted by the row's number, so that the lanes of an operand's fetch, which read one piece
-// each of 32 rows, find them on different banks.  The permutation is made by the addresses in memory that the lanes fetch from.
+// block (128 bytes); its 16-byte pieces lie permuted by half the row's number (two rows are the 256 bytes of the banks), so that the lanes of an
+// operand's fetch, which read one piece each of 32 rows, find them on different banks.  The permutation is made by the addresses in memory that the lanes fetch from.
 //
 // Results: the classes' scores with their bias (m = class, n = row), of which only each row's largest and sum of exponentials over the
 // tile's classes leave the kernel (and the score of its label), or which are stored too; or products, stored rounded; or partial sums.
 #pragma once
+#include <type_traits>
+
+#include "any_address.hpp"
 #include "ranges.hpp"
-#include "storage.hpp"
 
 namespace mpcnn {
 
@@ -61,7 +63,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
     constexpr int BM = 32 * WM * MT, BN = 32 * WN * NT, kWaves = WM * WN;
     constexpr int kStage = (BM + BN) * kBlockBytes;
     constexpr int AI = BM / 8 / kWaves, BI = BN / 8 / kWaves;   // a wave's fetches of 8 rows' blocks
-    static_assert(AI * 8 * kWaves == BM && BI * 8 * kWaves == BN, "the waves share the rows evenly");
+    static_assert(AI * 8 * kWaves == BM && BI * 8 * kWaves == BN && AI % 2 == 0 && BI % 2 == 0, "the waves share the rows evenly");
     extern __shared__ __attribute__((aligned(256))) char lds_raw[];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -86,17 +88,17 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
         __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(a.A + (long)m0 * a.a_row + (long)first * kBlockBytes), 0, 0x7fffffff, 0x00020000);
     const __amdgpu_buffer_rsrc_t rb =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(a.B + (long)n0 * a.b_row + (long)first * kBlockBytes), 0, 0x7fffffff, 0x00020000);
-    const unsigned piece = 16u * ((lane & 7) ^ (lane >> 3));
+    const unsigned piece[2] = {16u * ((lane & 7) ^ (lane >> 4)), 16u * ((lane & 7) ^ (lane >> 4) ^ 4)};   // even, odd q
     unsigned va[AI], vb[BI];
 #pragma unroll
     for (int i = 0; i < AI; ++i) {
         const int r = 8 * (wave * AI + i) + (lane >> 3), left = a.M - 1 - m0;
-        va[i] = (unsigned)(r < left ? r : left) * (unsigned)a.a_row + piece;
+        va[i] = (unsigned)(r < left ? r : left) * (unsigned)a.a_row + piece[i & 1];
     }
 #pragma unroll
     for (int i = 0; i < BI; ++i) {
         const int r = 8 * (wave * BI + i) + (lane >> 3), left = a.N - 1 - n0;
-        vb[i] = (unsigned)(r < left ? r : left) * (unsigned)a.b_row + piece;
+        vb[i] = (unsigned)(r < left ? r : left) * (unsigned)a.b_row + piece[i & 1];
     }
     auto fetch = [&](int block, char* stage) {
 #pragma unroll
@@ -118,10 +120,11 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
 
     // an operand's 16 k's, piece pair s of the block: lane l feeds row l % 32, k's 8 (l / 32) ..
     const int row = lane & 31, half = lane >> 5;
-    const int at_a = (32 * MT * wm + row) * kBlockBytes, at_b = (BM + 32 * NT * wn + row) * kBlockBytes, mix = row & 7;
+    const int at_a = (32 * MT * wm + row) * kBlockBytes, at_b = (BM + 32 * NT * wn + row) * kBlockBytes, mix = row >> 1 & 7;
     auto multiply = [&](const char* stage) {
         auto read = [&](int at, int s) { return *reinterpret_cast<const v4f*>(stage + at + 16 * ((2 * s + half) ^ mix)); };
         auto product = [&](v4f (&x)[MT], v4f (&y)[NT]) {
+            __builtin_amdgcn_s_setprio(1);     // (before the other wave's fetches and reads)
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -130,28 +133,38 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
                         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x[i]), __builtin_bit_cast(f16x8, y[j]), acc[i][j], 0, 0, 0);
                     else
                         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[i]), __builtin_bit_cast(bf16x8, y[j]), acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_s_setprio(0);
         };
+        // a step's operands are read while the one before it is multiplied
         if constexpr (HALVES) {
+            v4f xh[2][MT], yh[2][NT], xl[2][MT], yl[2][NT];
+            auto load = [&](int t, int s) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) { xl[t][i] = read(at_a + i * 32 * kBlockBytes, s + 2); xh[t][i] = read(at_a + i * 32 * kBlockBytes, s); }
+#pragma unroll
+                for (int j = 0; j < NT; ++j) { yh[t][j] = read(at_b + j * 32 * kBlockBytes, s); yl[t][j] = read(at_b + j * 32 * kBlockBytes, s + 2); }
+            };
+            load(0, 0);
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                v4f xh[MT], yh[NT], xl[MT], yl[NT];
-#pragma unroll
-                for (int i = 0; i < MT; ++i) { xh[i] = read(at_a + i * 32 * kBlockBytes, s); xl[i] = read(at_a + i * 32 * kBlockBytes, s + 2); }
-#pragma unroll
-                for (int j = 0; j < NT; ++j) { yh[j] = read(at_b + j * 32 * kBlockBytes, s); yl[j] = read(at_b + j * 32 * kBlockBytes, s + 2); }
-                product(xl, yh);
-                product(xh, yl);
-                product(xh, yh);
+                if (s == 0) load(1, 1);
+                product(xl[s], yh[s]);
+                product(xh[s], yl[s]);
+                product(xh[s], yh[s]);
             }
         } else {
+            v4f x[2][MT], y[2][NT];
+            auto load = [&](int t, int s) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) x[t][i] = read(at_a + i * 32 * kBlockBytes, s);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) y[t][j] = read(at_b + j * 32 * kBlockBytes, s);
+            };
+            load(0, 0);
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                v4f x[MT], y[NT];
-#pragma unroll
-                for (int i = 0; i < MT; ++i) x[i] = read(at_a + i * 32 * kBlockBytes, s);
-#pragma unroll
-                for (int j = 0; j < NT; ++j) y[j] = read(at_b + j * 32 * kBlockBytes, s);
-                product(x, y);
+                if (s < 3) load((s + 1) & 1, s + 1);
+                product(x[s & 1], y[s & 1]);
             }
         }
     };
@@ -239,32 +252,61 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
             a.stats[(long)tm * a.N + n0 + i] = s;
         }
     } else {
-        const int mw = m0 + 32 * MT * wm + 4 * half, nw = n0 + 32 * NT * wn + row;
+        // A wave's results by way of LDS (a place of its own), 32 rows of 32 NT at a time: whole lines to memory, 8 results a lane
+        constexpr int W = 32 * NT, kPitch = W + 4;           // floats; 128-bit words, rows on different banks
+        static_assert(kWaves * 32 * kPitch * 4 <= 2 * kStage, "the ring holds them");
+        float* const mine = reinterpret_cast<float*>(lds_raw) + wave * 32 * kPitch;
+        __syncthreads();                                     // (the last block is read by nobody any more)
+        const int nw = n0 + W * wn;
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int m = mw + 32 * i + 8 * (r >> 2) + (r & 3);
-                if (m >= a.M) continue;
-                float scale = 1.f;
-                if constexpr (RESULT != kPart)
-                    if (a.row_scale) scale = a.row_scale[m];   // (0: nothing of the row, whatever it is multiplied with)
+            for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    const int n = nw + 32 * j;
-                    if (n >= a.N) continue;
-                    float v = acc[i][j][r];
-                    if constexpr (RESULT == kPart) {
-                        float* p = a.part + ((long)split * a.M + m) * a.N + n;
-                        *p = a.add ? *p + v : v;
+                for (int r = 0; r < 16; ++r) mine[(8 * (r >> 2) + 4 * half + (r & 3)) * kPitch + 32 * j + row] = acc[i][j][r];
+            asm volatile("" ::: "memory");                   // (a wave's LDS instructions are served in order)
+#pragma unroll
+            for (int q = 0; q < W / 16; ++q) {               // 64 lanes: W / 8 a row
+                const int of = (64 * q + lane) / (W / 8), c = 8 * ((64 * q + lane) % (W / 8));
+                const int m = m0 + 32 * (MT * wm + i) + of, n = nw + c;
+                const v4f lo = *reinterpret_cast<const v4f*>(mine + of * kPitch + c), hi = *reinterpret_cast<const v4f*>(mine + of * kPitch + c + 4);
+                v8f v{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                if (m >= a.M || n >= a.N) continue;
+                const int left = a.N - n;
+                if constexpr (RESULT == kPart) {
+                    float* const p = a.part + ((long)split * a.M + m) * a.N + n;
+                    if (left >= 8) {
+                        if (a.add) {
+                            const v8f o = load8(p);
+#pragma unroll
+                            for (int z = 0; z < 8; ++z) v[z] += o[z];
+                        }
+                        store8(p, v);
                     } else {
-                        if constexpr (HALVES) v = v * f.first * f.second;
-                        v = scale == 0.f ? 0.f : v * scale;
-                        if constexpr (RESULT == kStoreF32) ((float*)a.out)[(long)m * a.out_row + n] = v;
-                        else ((bf16*)a.out)[(long)m * a.out_row + n] = (bf16)v;
+#pragma unroll
+                        for (int z = 0; z < 8; ++z)
+                            if (z < left) p[z] = a.add ? p[z] + v[z] : v[z];
+                    }
+                } else {
+                    const float scale = a.row_scale ? a.row_scale[m] : 1.f;   // (0: nothing of the row, whatever it is multiplied with)
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) {
+                        if constexpr (HALVES) v[z] = v[z] * f.first * f.second;
+                        v[z] = scale == 0.f ? 0.f : v[z] * scale;
+                    }
+                    using T = std::conditional_t<RESULT == kStoreF32, float, bf16>;
+                    T* const p = (T*)a.out + (long)m * a.out_row + n;
+                    if (left >= 8) {
+                        store8(p, v);
+                    } else {
+#pragma unroll
+                        for (int z = 0; z < 8; ++z)
+                            if (z < left) store1(p + z, v[z]);
                     }
                 }
             }
+            asm volatile("" ::: "memory");
+        }
     }
 }
 
