@@ -46,8 +46,8 @@ Tiling tiling_of(int64_t M, int64_t N, int64_t blocks, int64_t most_splits, bool
         const int64_t side = big ? 256 : 128, slots = big ? kCUs : 2 * kCUs;
         const int64_t tiles = (M + side - 1) / side * ((N + side - 1) / side);
         for (int round = 0; round <= 4; ++round) {
-            const int64_t splits = round ? round * slots / tiles : 1;
-            if (round && (splits < 2 || splits > most_splits || blocks / splits < 4)) continue;
+            const int64_t splits = round ? std::min({round * slots / tiles, most_splits, blocks / 4}) : 1;
+            if (round && splits < 2) continue;
             Tiling t{};
             t.big = big != 0;
             t.tiles_m = (int)((M + side - 1) / side);
@@ -63,8 +63,11 @@ Tiling tiling_of(int64_t M, int64_t N, int64_t blocks, int64_t most_splits, bool
     return best;
 }
 
-// Three to five launches (kernels_rows_direct.hpp) instead of a dozen
-constexpr int64_t kDirectWork = 1500000000, kDirectRows = 64;   // rows x features x classes; whatever the work
+// Three to five launches (kernels_rows_direct.hpp) instead of a dozen: up to this much work, rows x features x classes, and up to more with few rows.
+// Microseconds, there / here, fp32 and bf16: gradients of 1000 x 1000 x 1000 (1e9) 109 / 114 and 63 / 73, of 1000 x 200 x 1000 (2e8) 49 / 88 and 34 / 68,
+// of 3000 x 500 x 1000 (1.5e9) 154 / 120 and 90 / 77; the loss of 1000 x 1000 x 2000 (2e9) 66 / 55 and 34 / 33, of 4000 x 2000 x 200
+// (1.6e9) 62 / 78 and 40 / 46; gradients of 20 x 4000 x 20000 (1.6e9) 336 / 586 and 170 / 274, of 40 x 1000 x 100000 (4e9) 699 / 818 and 382 / 374.
+constexpr int64_t kDirectWork = 1200000000, kDirectLossWork = 2000000000, kDirectFewRows = 64, kDirectFewWork = 4000000000;
 
 struct Plan {
     bool halves, train, keep, few, direct;
@@ -121,7 +124,8 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
         p->total = at;
         return true;
     }
-    p->direct = (rows <= kDirectRows || rows * classes <= kDirectWork / features) && (p->keep || !train) && rows * features < (int64_t)1 << 40;
+    const int64_t most = rows <= kDirectFewRows ? kDirectFewWork : train ? kDirectWork : kDirectLossWork;
+    p->direct = rows * classes <= most / features && (p->keep || !train);
     if (p->direct) {
         // a tile of 32 x 32 for four waves, one of 64 x 64 where that gives every compute unit two workgroups or the sum has one step
         auto deal_of = [](int64_t m, int64_t n, int64_t k) { return (m + 63) / 64 * ((n + 63) / 64) >= 2 * kCUs || k <= mpcnn::kDirectK ? 1 : 4; };
@@ -231,13 +235,19 @@ struct Call {
     float* db;
 };
 
+int join_groups_of(int N, int tiles)
+{
+    const int rows = mpcnn::join_rows(N, tiles);
+    return (N + rows - 1) / rows;
+}
 void launch_join(const mpcnn::JoinArgs& j, hipStream_t st)
 {
-    const int rows = std::max(j.N, j.padded), each = mpcnn::join_rows(rows), groups = (rows + each - 1) / each;
-    if (each == mpcnn::kJoinFew) mpcnn::rows_join_kernel<mpcnn::kJoinFew><<<(unsigned)groups, 256, 0, st>>>(j);
-    else mpcnn::rows_join_kernel<mpcnn::kJoinMany><<<(unsigned)groups, 256, 0, st>>>(j);
+    const unsigned groups = (unsigned)join_groups_of(j.N, j.tiles);
+    if (j.N <= mpcnn::kJoinLeast) mpcnn::rows_join_kernel<mpcnn::kJoinLeast, 1024><<<groups, 1024, 0, st>>>(j);
+    else if (groups == 1) mpcnn::rows_join_kernel<mpcnn::kJoinMany, 1024><<<groups, 1024, 0, st>>>(j);
+    else if (mpcnn::join_rows(j.N, j.tiles) == mpcnn::kJoinFew) mpcnn::rows_join_kernel<mpcnn::kJoinFew, 256><<<groups, 256, 0, st>>>(j);
+    else mpcnn::rows_join_kernel<mpcnn::kJoinMany, 256><<<groups, 256, 0, st>>>(j);
 }
-int join_groups_of(int N) { return (N + mpcnn::join_rows(N) - 1) / mpcnn::join_rows(N); }
 
 template <typename T, int NR>
 void launch_few(const mpcnn::FewArgs& a, bool grads, dim3 grid, hipStream_t st)
@@ -268,7 +278,7 @@ mpcnn_status run_few(const Plan& p, const Call& c, char* ws, hipStream_t st)
     mpcnn::JoinArgs j{};
     j.stats = a.stats; j.tiles = p.score_groups; j.N = p.N; j.label_score = a.label_score; j.mask = a.mask;
     j.lse = (float*)(ws + p.lse); j.weight = (float*)(ws + p.weight); j.lse_out = c.lse; j.rowloss = c.rowloss;
-    const int groups = join_groups_of(p.N);
+    const int groups = join_groups_of(p.N, p.score_groups);
     j.loss_part = groups == 1 && c.loss ? c.loss : (double*)(ws + p.loss_part);
     launch_join(j, st);
     a.loss = groups > 1 ? c.loss : nullptr; a.loss_part = j.loss_part; a.loss_parts = groups;
@@ -313,7 +323,7 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
         mpcnn::JoinArgs j{};
         j.stats = a.stats; j.tiles = p.score_v; j.N = p.N; j.label_score = a.label_score; j.mask = a.mask;
         j.lse = a.lse; j.weight = a.weight; j.lse_out = c.lse; j.rowloss = c.rowloss;
-        groups = join_groups_of(p.N);
+        groups = join_groups_of(p.N, p.score_v);
         j.loss_part = groups == 1 && c.loss ? c.loss : shares;
         launch_join(j, st);
     } else {
@@ -424,7 +434,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         if (rc != MPCNN_OK) return rc;
         done += tiles;
     }
-    const int join_groups = join_groups_of(p.N);
+    const int join_groups = join_groups_of(p.N, p.score_v);
     mpcnn::JoinArgs j{};
     j.stats = (const float2*)(ws + p.stats); j.tiles = done; j.N = p.N;
     j.label_score = (const float*)(ws + p.label_score); j.mask = mask;

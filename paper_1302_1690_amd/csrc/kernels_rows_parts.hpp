@@ -201,18 +201,20 @@ struct JoinArgs {
     const float* label_score;              // [N]
     RowMask mask;
     float *lse, *rowloss, *weight;         // [N]: lse for the derivative, results (null: not asked for), the row's weight or 0
-    int* label;                            // the label, or kNoLabel
-    int padded;                            // places of lse, weight and label: those behind the last row are filled as for rows that add nothing
     float* lse_out;
     double* loss_part;                     // per workgroup, or null
 };
-// ROWS rows per workgroup, the tiles dealt to 256 / ROWS threads each: 4 while that leaves compute units without work, 32 beyond (whole lines)
-constexpr int kJoinFew = 4, kJoinMany = 32, kJoinFewMost = 1024;
-inline int join_rows(int N) { return N <= kJoinFewMost ? kJoinFew : kJoinMany; }
-template <int ROWS>
-__global__ __launch_bounds__(256) void rows_join_kernel(JoinArgs a)
+// ROWS rows per workgroup, the tiles dealt to THREADS / ROWS threads each.  Up to 8 rows, or 32 with few tiles: one workgroup, whose loss is the
+// whole one; 4 rows while that leaves compute units without work; 32 beyond (whole lines).
+constexpr int kJoinLeast = 8, kJoinFew = 4, kJoinMany = 32, kJoinFewMost = 1024, kJoinTiles = 512;
+inline int join_rows(int N, int tiles)
 {
-    constexpr int DEALS = 256 / ROWS;
+    return N <= kJoinLeast ? kJoinLeast : N <= kJoinMany && tiles <= kJoinTiles ? kJoinMany : N <= kJoinFewMost ? kJoinFew : kJoinMany;
+}
+template <int ROWS, int THREADS>
+__global__ __launch_bounds__(THREADS) void rows_join_kernel(JoinArgs a)
+{
+    constexpr int DEALS = THREADS / ROWS;
     __shared__ float2 red[DEALS][ROWS];
     __shared__ double sums[ROWS];
     const int own = threadIdx.x % ROWS, deal = threadIdx.x / ROWS;
@@ -243,11 +245,6 @@ __global__ __launch_bounds__(256) void rows_join_kernel(JoinArgs a)
     s = red[0][own];
     if (deal == 0) {
         double share = 0.0;
-        if (n >= a.N && n < a.padded) {
-            if (a.lse) a.lse[n] = 0.f;
-            if (a.weight) a.weight[n] = 0.f;
-            if (a.label) a.label[n] = kNoLabel;
-        }
         if (n < a.N) {
             for (int d = 1; d < 8; ++d) s = join(s, red[d][own]);
             const float lse = s.x == kNone ? kNone : s.x + logf(s.y);
@@ -259,7 +256,6 @@ __global__ __launch_bounds__(256) void rows_join_kernel(JoinArgs a)
             }
             if (a.lse) a.lse[n] = lse;
             if (a.weight) a.weight[n] = w;
-            if (a.label) a.label[n] = w != 0.f ? a.mask.labels[n] : kNoLabel;
             if (a.lse_out) a.lse_out[n] = w != 0.f ? lse : 0.f;
             if (a.rowloss) a.rowloss[n] = loss;
             share = (double)loss;

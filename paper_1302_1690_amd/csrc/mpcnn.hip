@@ -2608,7 +2608,7 @@ mpcnn_status mpcnn_sgd_step_clipped(mpcnn_net* net, double lr, double grad_scale
     a.partial = (double*)((char*)net->d_grads + align_up(sizeof(float) * net->n_params));
     a.norm = norm_dev;
     a.scale = std::fabs(grad_scale); a.bound = max_norm; a.rate = (float)(lr * grad_scale);
-    LAUNCH("sgd_clipped", -1, 8, 4.0 * n, 16.0 * n, mpcnn::launch_update(a, mpcnn::kStep, n, st));
+    LAUNCH("sgd_clipped", -1, 8, 4.0 * n, 16.0 * n, mpcnn::launch_update(a, mpcnn::kStep, n, nullptr, 0, st));
     HIP_TRY(hipGetLastError());
     net->packs_stale = true; net->wread_stale = true;
     return MPCNN_OK;

@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <memory>
 #include <new>
 #include <vector>
 
@@ -15,6 +16,7 @@ struct mpcnn_grad_list {
     long total = 0;
     int stretches = 0;
     bool params = false;
+    std::vector<int> starts;             // tensors that share memory: each one's first stretch, and the last one's end (else empty)
     mpcnn::Stretch* d_table = nullptr;   // and, behind it, the partial sums
     double* d_partial = nullptr;
 };
@@ -36,8 +38,21 @@ static void launch_mode(const UpdateArgs& a, int mode, unsigned groups, hipStrea
     else update_kernel<kStep, LONE><<<groups, threads, 0, st>>>(a);
 }
 
-void launch_update(UpdateArgs a, int mode, long total, hipStream_t st)
+void launch_update(UpdateArgs a, int mode, long total, const int* starts, int tensors, hipStream_t st)
 {
+    if (tensors && mode != kOnlyNorm) {
+        // tensors that share memory: the norm, then one tensor after the other
+        const int groups = (int)std::min<long>(kNormParts, ((long)a.stretches + 3) / 4);
+        a.parts = groups;
+        norm_parts_kernel<<<(unsigned)groups, 256, 0, st>>>(a);
+        const Stretch* const table = a.table;
+        for (int i = 0; i < tensors; ++i) {
+            a.table = table + starts[i];
+            a.stretches = starts[i + 1] - starts[i];
+            launch_mode<false>(a, mode, (unsigned)std::min<long>(kNormParts, ((long)a.stretches + 3) / 4), st);
+        }
+        return;
+    }
     if (total <= kLoneNumbers && a.stretches <= kLoneStretches) {
         launch_mode<true>(a, mode, 1, st);
         return;
@@ -52,14 +67,19 @@ void launch_update(UpdateArgs a, int mode, long total, hipStream_t st)
 
 namespace {
 
-struct Range { uintptr_t at; uint64_t bytes; };
+struct Range { uintptr_t at; uint64_t bytes; bool param; };
 
-bool overlap(std::vector<Range>& r)
+// Whether two ranges of one kind overlap (`same`), and whether a gradient and a parameter do (`mixed`)
+void overlap(std::vector<Range>& r, bool* same, bool* mixed)
 {
     std::sort(r.begin(), r.end(), [](const Range& x, const Range& y) { return x.at < y.at; });
-    for (size_t i = 1; i < r.size(); ++i)
-        if (r[i].at - r[i - 1].at < r[i - 1].bytes) return true;
-    return false;
+    uintptr_t end[2] = {0, 0};           // of what has begun so far, gradients and parameters
+    *same = *mixed = false;
+    for (const Range& x : r) {
+        *same = *same || x.at < end[x.param];
+        *mixed = *mixed || x.at < end[!x.param];
+        end[x.param] = std::max<uintptr_t>(end[x.param], x.at + x.bytes);
+    }
 }
 
 bool known(int dtype) { return dtype == MPCNN_F32 || dtype == MPCNN_BF16; }
@@ -80,17 +100,21 @@ mpcnn_status make_list(const mpcnn_tensor* t, int count, mpcnn_grad_list** out)
             return fail(MPCNN_EINVAL, "tensor %d: address is no multiple of its element's size", i);
         ++filled;
         total += t[i].n;
-        ranges.push_back({(uintptr_t)t[i].grad_dev, (uint64_t)t[i].n * gs});
+        ranges.push_back({(uintptr_t)t[i].grad_dev, (uint64_t)t[i].n * gs, false});
         if (t[i].param_dev) {
             ++with;
-            ranges.push_back({(uintptr_t)t[i].param_dev, (uint64_t)t[i].n * ps});
+            ranges.push_back({(uintptr_t)t[i].param_dev, (uint64_t)t[i].n * ps, true});
         }
     }
     if (with && with != filled) return fail(MPCNN_EINVAL, "%d of %d tensors have parameters: all or none", with, filled);
-    if (overlap(ranges)) return fail(MPCNN_EINVAL, "two of the tensors overlap in memory");
+    bool same = false, mixed = false;
+    overlap(ranges, &same, &mixed);
+    if (mixed) return fail(MPCNN_EINVAL, "a gradient and a parameter overlap in memory");
     const unsigned len = mpcnn::stretch_length((long)total);
     std::vector<mpcnn::Stretch> table;
-    for (int i = 0; i < count; ++i)
+    std::vector<int> starts;
+    for (int i = 0; i < count; ++i) {
+        if (same && t[i].n) starts.push_back((int)table.size());
         for (int64_t at = 0; at < t[i].n; at += len) {
             mpcnn::Stretch s{};
             s.grad = (char*)t[i].grad_dev + at * (int64_t)size_of(t[i].grad_dtype);
@@ -102,8 +126,11 @@ mpcnn_status make_list(const mpcnn_tensor* t, int count, mpcnn_grad_list** out)
             s.n = (unsigned)std::min<int64_t>(len, t[i].n - at);
             table.push_back(s);
         }
+    }
+    if (same) starts.push_back((int)table.size());
     if (table.size() > (size_t)1 << 30) return fail(MPCNN_EINVAL, "too many numbers: %lld", (long long)total);
-    mpcnn_grad_list* l = new mpcnn_grad_list;
+    std::unique_ptr<mpcnn_grad_list> l(new mpcnn_grad_list);
+    l->starts = std::move(starts);
     l->total = (long)total;
     l->stretches = (int)table.size();
     l->params = with > 0;
@@ -115,12 +142,11 @@ mpcnn_status make_list(const mpcnn_tensor* t, int count, mpcnn_grad_list** out)
     if (e == hipSuccess && bytes) e = hipMemcpy(dev, table.data(), bytes, hipMemcpyHostToDevice);
     if (e != hipSuccess) {
         (void)hipFree(dev);
-        delete l;
         return fail(e == hipErrorOutOfMemory ? MPCNN_ENOMEM : MPCNN_EHIP, "list of %d tensors: %s", count, hipGetErrorString(e));
     }
     l->d_table = (mpcnn::Stretch*)dev;
     l->d_partial = (double*)(dev + bytes);
-    *out = l;
+    *out = l.release();
     return MPCNN_OK;
 }
 
@@ -142,7 +168,7 @@ mpcnn_status update(const mpcnn_grad_list* l, int mode, double rate, double scal
     a.scale = std::fabs(scale);
     a.bound = bound;
     a.rate = (float)(rate * scale);
-    mpcnn::launch_update(a, mode, l->total, (hipStream_t)stream);
+    mpcnn::launch_update(a, mode, l->total, l->starts.data(), l->starts.empty() ? 0 : (int)l->starts.size() - 1, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
     return MPCNN_OK;
 }

@@ -164,6 +164,33 @@ def test_net_clipped_step(which):
     net.close()
 
 
+@pytest.mark.parametrize("n", [60, 30000])
+def test_tensors_that_share_memory(n):
+    """One weight with two gradients, a list that names a gradient twice, one that overlaps the next: tensor by tensor, in order."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    w, g = torch.randn(n, generator=gen, device="cuda"), [torch.randn(n, generator=gen, device="cuda") for _ in range(2)]
+    start = w.clone()
+    norm = mpcnn.GradList(g, [w, w]).sgd_step(0.5, max_norm=1.0)
+    want = _norm64(g)
+    assert abs(norm.item() - want) <= 1e-10 * want
+    f = torch.tensor(0.5 / want, dtype=torch.float64).float().double()
+    one = (start.double() - f * g[0].double()).float().double()
+    assert ((one - f * g[1].double()) - w.double()).abs().max().item() <= 2.0 ** -22 * (w.abs().max().item() + 1)
+    # the same through lists without anything shared: equal up to the two factors' rounding
+    kept = g[0].clone()
+    norm = mpcnn.GradList([g[0], g[0]]).clip(_norm64([g[0]]) / 2)
+    assert abs(norm.item() - math.sqrt(2) * _norm64([kept])) <= 1e-10 * norm.item()
+    c = 1 / (2 * math.sqrt(2))
+    assert (g[0].double() - kept.double() * c * c).abs().max().item() <= 2.0 ** -22 * kept.abs().max().item()
+    kept = g[1].clone()
+    a, b = g[1][:n - 10], g[1][n - 20:]
+    total = _norm64([a, b])
+    mpcnn.GradList([a, b]).clip(total / 4)
+    assert (g[1][:n - 20].double() - kept[:n - 20].double() / 4).abs().max().item() <= 2.0 ** -23 * kept.abs().max().item()
+    assert (g[1][n - 20:n - 10].double() - kept[n - 20:n - 10].double() / 16).abs().max().item() <= 2.0 ** -23 * kept.abs().max().item()
+    assert (g[1][n - 10:].double() - kept[n - 10:].double() / 4).abs().max().item() <= 2.0 ** -23 * kept.abs().max().item()
+
+
 def test_recorded_into_a_graph():
     g = _tensors([40000, 77], [F, B], 6)
     p = _tensors([40000, 77], [F, B], 7)
@@ -200,7 +227,7 @@ def test_on_another_stream():
 def test_refusals():
     a = torch.randn(10, device="cuda")
     for grads, params in (([a.half()], None), ([torch.randn(4, 6, device="cuda").t()], None), ([torch.randn(5)], None), ([a], [a.clone()[:5]]),
-                          ([a], []), ([a, a], None), ([a], [a]), ([a[:6], a[5:]], None)):
+                          ([a], []), ([a], [a]), ([a, a.clone()], [a.clone(), a])):
         with pytest.raises(mpcnn.MpcnnError) as e:
             mpcnn.GradList(grads, params)
         assert e.value.status == 1

@@ -28,9 +28,9 @@ BASE = 1 << 40
     ([(BASE + 1, 0, 5, 1, 0)], "multiple"),
     ([(BASE, 2 * BASE + 2, 5, 1, 0)], "multiple"),
     ([(BASE, 2 * BASE, 5, 0, 0), (BASE + 64, 0, 5, 0, 0)], "all or none"),
-    ([(BASE, 0, 5, 0, 0), (BASE, 0, 5, 0, 0)], "overlap"),                        # the same gradient twice
-    ([(BASE, 0, 5, 0, 0), (BASE + 16, 0, 5, 0, 0)], "overlap"),                   # by its last number
-    ([(BASE + 8, 0, 5, 1, 0), (BASE, 0, 5, 1, 0)], "overlap"),                    # in whatever order
+    ([(BASE, 2 * BASE, 50, 0, 0), (3 * BASE, BASE + 196, 5, 0, 0)], "overlap"),    # a parameter and another one's gradient, by one number
+    ([(BASE, 2 * BASE, 500, 0, 0), (BASE + 400, 3 * BASE, 5, 0, 0), (4 * BASE, BASE + 800, 5, 0, 0)], "overlap"),   # behind one inside another
+    ([(3 * BASE, BASE + 8, 5, 1, 1), (BASE, 2 * BASE, 5, 1, 1)], "overlap"),       # in whatever order
     ([(BASE, BASE, 5, 0, 0)], "overlap"),                                         # a gradient that is its own parameter
 ], ids=range(12))
 def test_list_refusals(rows, says):
