@@ -28,32 +28,53 @@ __device__ __forceinline__ void store8(bf16* p, v8f v)
     *reinterpret_cast<b8_any*>(p) = __builtin_convertvector(v, b8_any);
 }
 
-// The same eight as they lie in memory (half the registers for bf16): raw8 fetches, widen converts
-template <typename T> struct Raw8;
-template <> struct Raw8<float> { f4_any a, b; };
-template <> struct Raw8<bf16> { b8_any a; };
-__device__ __forceinline__ Raw8<float> raw8(const float* p) { return {*reinterpret_cast<const f4_any*>(p), *reinterpret_cast<const f4_any*>(p + 4)}; }
-__device__ __forceinline__ Raw8<bf16> raw8(const bf16* p) { return {*reinterpret_cast<const b8_any*>(p)}; }
-__device__ __forceinline__ v8f widen(const Raw8<float>& r) { return v8f{r.a[0], r.a[1], r.a[2], r.a[3], r.b[0], r.b[1], r.b[2], r.b[3]}; }
-__device__ __forceinline__ v8f widen(const Raw8<bf16>& r) { return __builtin_convertvector(r.a, v8f); }
-__device__ __forceinline__ void set_raw(Raw8<float>& r, int z, float v) { if (z < 4) r.a[z] = v; else r.b[z - 4] = v; }
-__device__ __forceinline__ void set_raw(Raw8<bf16>& r, int z, bf16 v) { r.a[z] = v; }
-
-// Numbers row[at .. at + 7] of a row of n, zeros beyond its end (at may be beyond it too).  The loads of a row's end are not conditional,
-// only their addresses and results are chosen: eight branches with a load in each would wait for memory eight times.
-template <typename T>
-__device__ __forceinline__ Raw8<T> raw8_of(const T* row, int at, int n)
+// E (4 or 8) numbers as they lie in memory (half the registers for bf16): raw_any fetches, widen converts
+typedef __bf16 b4_any __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T, int E> struct Raw;
+template <> struct Raw<float, 8> { f4_any a, b; };
+template <> struct Raw<float, 4> { f4_any a; };
+template <> struct Raw<bf16, 8> { b8_any a; };
+template <> struct Raw<bf16, 4> { b4_any a; };
+template <typename T> using Raw8 = Raw<T, 8>;
+template <int E, typename T>
+__device__ __forceinline__ Raw<T, E> raw_any(const T* p)
 {
-    if (at + 8 <= n) return raw8(row + at);
-    T u[8];
-    Raw8<T> r;
-#pragma unroll
-    for (int z = 0; z < 8; ++z) u[z] = row[at + z < n ? at + z : n - 1];
-#pragma unroll
-    for (int z = 0; z < 8; ++z) set_raw(r, z, at + z < n ? u[z] : (T)0.f);
+    Raw<T, E> r;
+    if constexpr (sizeof(T) == 4 && E == 8) {
+        r.a = *reinterpret_cast<const f4_any*>(p);
+        r.b = *reinterpret_cast<const f4_any*>(p + 4);
+    } else {
+        r.a = *reinterpret_cast<const decltype(r.a)*>(p);
+    }
     return r;
 }
-template <typename T>
-__device__ __forceinline__ v8f load8_of(const T* row, int at, int n) { return widen(raw8_of(row, at, n)); }
+template <typename T> __device__ __forceinline__ Raw8<T> raw8(const T* p) { return raw_any<8>(p); }
+__device__ __forceinline__ v8f widen(const Raw<float, 8>& r) { return v8f{r.a[0], r.a[1], r.a[2], r.a[3], r.b[0], r.b[1], r.b[2], r.b[3]}; }
+__device__ __forceinline__ v4f widen(const Raw<float, 4>& r) { return r.a; }
+__device__ __forceinline__ v8f widen(const Raw<bf16, 8>& r) { return __builtin_convertvector(r.a, v8f); }
+__device__ __forceinline__ v4f widen(const Raw<bf16, 4>& r) { return __builtin_convertvector(r.a, v4f); }
+__device__ __forceinline__ void set_raw(Raw<float, 8>& r, int z, float v) { if (z < 4) r.a[z] = v; else r.b[z - 4] = v; }
+template <typename T, int E> __device__ __forceinline__ void set_raw(Raw<T, E>& r, int z, T v) { r.a[z] = v; }
+__device__ __forceinline__ void store_any(float* p, v8f v) { store8(p, v); }
+__device__ __forceinline__ void store_any(bf16* p, v8f v) { store8(p, v); }
+__device__ __forceinline__ void store_any(float* p, v4f v) { *reinterpret_cast<f4_any*>(p) = v; }
+__device__ __forceinline__ void store_any(bf16* p, v4f v) { *reinterpret_cast<b4_any*>(p) = __builtin_convertvector(v, b4_any); }
+
+// Numbers row[at .. at + E - 1] of a row of n, zeros beyond its end (at may be beyond it too).  The loads of a row's end are not conditional,
+// only their addresses and results are chosen: branches with a load in each would wait for memory one after the other.
+template <int E, typename T>
+__device__ __forceinline__ Raw<T, E> raw_of(const T* row, int at, int n)
+{
+    if (at + E <= n) return raw_any<E>(row + at);
+    T u[E];
+    Raw<T, E> r;
+#pragma unroll
+    for (int z = 0; z < E; ++z) u[z] = row[at + z < n ? at + z : n - 1];
+#pragma unroll
+    for (int z = 0; z < E; ++z) set_raw(r, z, at + z < n ? u[z] : (T)0.f);
+    return r;
+}
+template <typename T> __device__ __forceinline__ Raw8<T> raw8_of(const T* row, int at, int n) { return raw_of<8>(row, at, n); }
+template <typename T> __device__ __forceinline__ v8f load8_of(const T* row, int at, int n) { return widen(raw8_of(row, at, n)); }
 
 }  // namespace mpcnn

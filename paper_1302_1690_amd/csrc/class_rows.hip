@@ -13,7 +13,7 @@
 #include <cstdint>
 
 #include "kernels_rows_direct.hpp"
-#include "kernels_rows_few.hpp"
+#include "rows_few.hpp"
 #include "kernels_rows_parts.hpp"
 #include "kernels_rows_product.hpp"
 #include "status.hpp"
@@ -66,13 +66,14 @@ Tiling tiling_of(int64_t M, int64_t N, int64_t blocks, int64_t most_splits, bool
 // Three to five launches (kernels_rows_direct.hpp) instead of a dozen: up to this much work, rows x features x classes, and up to more with few rows.
 // Microseconds, there / here, fp32 and bf16: gradients of 1000 x 1000 x 1000 (1e9) 109 / 114 and 63 / 73, of 1000 x 200 x 1000 (2e8) 49 / 88 and 34 / 68,
 // of 3000 x 500 x 1000 (1.5e9) 154 / 120 and 90 / 77; the loss of 1000 x 1000 x 2000 (2e9) 66 / 55 and 34 / 33, of 4000 x 2000 x 200
-// (1.6e9) 62 / 78 and 40 / 46; gradients of 20 x 4000 x 20000 (1.6e9) 336 / 586 and 170 / 274, of 40 x 1000 x 100000 (4e9) 699 / 818 and 382 / 374.
-constexpr int64_t kDirectWork = 1200000000, kDirectLossWork = 2000000000, kDirectFewRows = 64, kDirectFewWork = 4000000000;
+// (1.6e9) 62 / 78 and 40 / 46; gradients of 20 x 4000 x 20000 (1.6e9) 336 / 586 and 170 / 274, of 40 x 1000 x 100000 (4e9) 699 / 818
+// and 382 / 374, of 64 x 4096 x 8000 (2e9) 203 / 335 and 149 / 124.
+constexpr int64_t kDirectWork = 1200000000, kDirectLossWork = 2000000000, kDirectFewRows = 64, kDirectFewWork[2] = {4000000000, 1600000000};
 
 struct Plan {
-    bool halves, train, keep, few, direct;
-    int score_groups, grad_groups;       // few: workgroups along the classes, of the scores and of the gradients
-    int64_t score_each, grad_each;       // and their classes
+    bool halves, train, keep, direct, few, few_scores;
+    int grad_groups;                     // few: workgroups along the classes,
+    int64_t score_each, grad_each;       // their classes, and those of the scores' workgroups
     int score_deal, score_v, score_n;    // direct: waves that share a tile's sum, tiles along classes and rows
     struct { int deal, m, along, splits, each; } gx, gw;   // of the gradients: tiles along rows or classes and along features, parts of the sum, their length
     int N, D;
@@ -100,38 +101,34 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     size_t at = 0;
     auto take = [&](int64_t bytes) { const size_t o = at; at += (size_t)up_to(bytes, 256); return o; };
     p->keep = train && classes <= kRoom / p->Np;
-    p->few = rows <= mpcnn::kFewRows && rows > 0;
-    if (p->few) {
-        const int64_t rounds = (classes + mpcnn::kFewRound - 1) / mpcnn::kFewRound;
-        auto share = [&](int64_t least, int64_t most, int* groups, int64_t* each) {
-            const int64_t n = std::max<int64_t>(1, std::min(most, classes / least));
-            *each = (classes + n - 1) / n;
-            *groups = (int)((classes + *each - 1) / *each);
-        };
-        p->score_each = (rounds + 8 * kCUs - 1) / (8 * kCUs) * mpcnn::kFewRound;   // whole rounds
-        p->score_groups = (int)((classes + p->score_each - 1) / p->score_each);
-        share(8, 2 * kCUs, &p->grad_groups, &p->grad_each);
-        p->Np = up_to(classes, 64);      // the scores' rows
-        p->stats = take(8 * (int64_t)p->score_groups * rows);
-        p->label_score = take(4 * rows);
-        p->lse = take(4 * rows);
-        p->weight = take(4 * rows);
-        p->loss_part = take(8 * (rows + 1));
-        if (train) {
-            p->score = take(4 * rows * p->Np);
-            p->dx_part = take(4 * (int64_t)p->grad_groups * rows * features);
-        }
-        p->total = at;
-        return true;
+    const int64_t most = rows <= kDirectFewRows ? kDirectFewWork[p->halves ? 0 : 1] : train ? kDirectWork : kDirectLossWork;
+    p->direct = (rows <= mpcnn::kFewRows || rows * classes <= most / features) && (p->keep || !train);
+    // few rows and many classes: the gradients, and the scores of still fewer, on the vector ALU (kernels_rows_few.hpp has the times)
+    p->few = p->direct && train && rows > 0 && rows <= mpcnn::kFewRows && classes >= (rows <= 4 ? 1024 : 4096);
+    if (p->direct && rows > 0) {
+        const int64_t least = rows <= 2 ? (p->halves ? 1024 : 24576) : p->halves && rows <= mpcnn::kFewScoreRows ? 24576 : kMaxClasses + 1;
+        p->few_scores = classes >= least;
     }
-    const int64_t most = rows <= kDirectFewRows ? kDirectFewWork : train ? kDirectWork : kDirectLossWork;
-    p->direct = rows * classes <= most / features && (p->keep || !train);
     if (p->direct) {
         // a tile of 32 x 32 for four waves, one of 64 x 64 where that gives every compute unit two workgroups or the sum has one step
         auto deal_of = [](int64_t m, int64_t n, int64_t k) { return (m + 63) / 64 * ((n + 63) / 64) >= 2 * kCUs || k <= mpcnn::kDirectK ? 1 : 4; };
         auto tiles = [](int64_t n, int deal) { return (int)((n + (deal == 4 ? 31 : 63)) / (deal == 4 ? 32 : 64)); };
         p->score_deal = deal_of(classes, rows, features);
         p->score_v = tiles(classes, p->score_deal); p->score_n = tiles(rows, p->score_deal);
+        if (p->few_scores) {
+            const int64_t round = mpcnn::kFewRound;
+            p->score_each = ((classes + round - 1) / round + 8 * kCUs - 1) / (8 * kCUs) * round;   // whole rounds
+            p->score_v = (int)((classes + p->score_each - 1) / p->score_each);
+        }
+        if (p->few) {
+            // shares of dx: 512 workgroups, fewer where their shares' way to memory and back would be more than an eighth of the class weights' passes
+            const int64_t each = mpcnn::few_columns((int)rows) * mpcnn::kFewThreads, along = (features + each - 1) / each;
+            const int64_t by_traffic = classes * (p->halves ? 4 : 2) * 3 / (64 * rows);
+            const int64_t n = std::max<int64_t>(1, std::min(classes / 8, std::max(512 / along, std::min<int64_t>(512, by_traffic))));
+            p->grad_each = (classes + n - 1) / n;
+            p->grad_groups = (int)((classes + p->grad_each - 1) / p->grad_each);
+            p->Np = up_to(rows, 4);
+        }
         auto grads = [&](auto& g, int64_t m, int64_t K) {
             g.deal = deal_of(m, features, K);
             g.m = tiles(m, g.deal); g.along = tiles(features, g.deal);
@@ -150,9 +147,11 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
             p->lse = take(4 * p->Np);
             p->weight = take(4 * p->Np);
             p->loss_part = take(8 * (p->Np + 1));
-            if (train) {
+            if (p->few) {
                 p->score = take(4 * classes * p->Np);
-                p->delta_rows = p->halves ? p->score : take(2 * classes * p->Np);
+                p->dx_part = take(4 * (int64_t)p->grad_groups * rows * features);
+            } else if (train) {
+                p->score = take(4 * classes * p->Np);
                 p->dx_part = take(p->gx.splits > 1 ? 4 * p->gx.splits * rows * features : 0);
                 p->dw_part = take(p->gw.splits > 1 ? 4 * p->gw.splits * classes * features : 0);
                 p->db_part = take(4 * classes * ((rows + 63) / 64));
@@ -221,6 +220,16 @@ mpcnn_status launch_product(mpcnn::ProductArgs a, const Tiling& t, hipStream_t s
     return t.big ? launch_instance<2, 4, 4, 2, HALVES, RESULT>(a, st) : launch_instance<2, 2, 2, 2, HALVES, RESULT>(a, st);
 }
 
+// Whether a product reads a matrix as it is: bf16, whole blocks at aligned addresses
+template <typename T>
+bool direct_operand(const void* m, int64_t pitch, int64_t features)
+{
+    return sizeof(T) == 2 && features % 64 == 0 && (uintptr_t)m % 16 == 0 && pitch % 8 == 0 && pitch * 512 < (1ll << 31);
+}
+// From so many class weights on the scores of little work are the block product's too, where it reads them as they are: 64 x 4096 x 32000 bf16
+// 147 -> 68 us, 8 x 4096 x 128000 357 -> 197; 16 x 1024 x 32000 26 / 27
+constexpr int64_t kBlockWeights = 40000000;
+
 struct Call {
     const void *x, *w;
     int64_t x_pitch, w_pitch;
@@ -249,55 +258,6 @@ void launch_join(const mpcnn::JoinArgs& j, hipStream_t st)
     else mpcnn::rows_join_kernel<mpcnn::kJoinMany, 256><<<groups, 256, 0, st>>>(j);
 }
 
-template <typename T, int NR>
-void launch_few(const mpcnn::FewArgs& a, bool grads, dim3 grid, hipStream_t st)
-{
-    if (grads) mpcnn::rows_few_grads_kernel<T, NR><<<grid, mpcnn::kFewThreads, 0, st>>>(a);
-    else mpcnn::rows_few_scores_kernel<T, NR><<<grid, mpcnn::kFewThreads, 0, st>>>(a);
-}
-template <typename T>
-void launch_few(const mpcnn::FewArgs& a, bool grads, dim3 grid, hipStream_t st)
-{
-    switch (a.N) {
-#define CASE(n) case n: launch_few<T, n>(a, grads, grid, st); break;
-        CASE(1) CASE(2) CASE(3) CASE(4) CASE(5) CASE(6) CASE(7) CASE(8)
-#undef CASE
-    }
-}
-template <typename T>
-mpcnn_status run_few(const Plan& p, const Call& c, char* ws, hipStream_t st)
-{
-    mpcnn::FewArgs a{};
-    a.x = c.x; a.w = c.w; a.x_pitch = c.x_pitch; a.w_pitch = c.w_pitch;
-    a.N = p.N; a.D = p.D; a.V = p.V; a.score_row = p.Np; a.bias = c.bias;
-    a.mask = mpcnn::RowMask{c.labels, c.roww, (int)p.V};
-    a.stats = (float2*)(ws + p.stats); a.label_score = (float*)(ws + p.label_score);
-    a.each = p.score_each;
-    if (p.train) a.scores = (float*)(ws + p.score);
-    launch_few<T>(a, false, dim3((unsigned)p.score_groups), st);
-    mpcnn::JoinArgs j{};
-    j.stats = a.stats; j.tiles = p.score_groups; j.N = p.N; j.label_score = a.label_score; j.mask = a.mask;
-    j.lse = (float*)(ws + p.lse); j.weight = (float*)(ws + p.weight); j.lse_out = c.lse; j.rowloss = c.rowloss;
-    const int groups = join_groups_of(p.N, p.score_groups);
-    j.loss_part = groups == 1 && c.loss ? c.loss : (double*)(ws + p.loss_part);
-    launch_join(j, st);
-    a.loss = groups > 1 ? c.loss : nullptr; a.loss_part = j.loss_part; a.loss_parts = groups;
-    if (p.train) {
-        a.lse = j.lse; a.weight = j.weight;
-        a.dw = c.dw; a.db = c.db; a.each = p.grad_each;
-        a.part = c.dx ? (float*)(ws + p.dx_part) : nullptr;
-        a.columns = 16;
-        while (a.columns < mpcnn::kFewThreads && 8 * a.columns < p.D) a.columns *= 2;
-        if (c.dx || c.dw || c.db)
-            launch_few<T>(a, true, dim3((unsigned)p.grad_groups, (unsigned)((p.D + 8 * a.columns - 1) / (8 * a.columns))), st);
-        a.parts = p.grad_groups; a.dx = c.dx; a.dx_pitch = c.dx_pitch;
-    }
-    if (a.part || a.loss)
-        mpcnn::rows_few_sum_kernel<T><<<a.part ? (unsigned)(((int64_t)p.N * p.D + 63) / 64) : 1, 1024, 0, st>>>(a);
-    HIP_TRY(hipGetLastError());
-    return MPCNN_OK;
-}
-
 template <typename T>
 mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
 {
@@ -308,9 +268,29 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
     a.stats = (float2*)(ws + p.stats); a.label_score = (float*)(ws + p.label_score);
     a.score_row = p.Np; a.score_deal = p.score_deal; a.tiles = p.score_v;
     if (p.train) a.scores = (float*)(ws + p.score);
-    mpcnn::rows_direct_scores_kernel<T><<<dim3((unsigned)p.score_v, (unsigned)p.score_n), 256, 0, st>>>(a);
+    mpcnn::FewArgs few{};
+    if (p.few || p.few_scores) {
+        few.x = c.x; few.w = c.w; few.x_pitch = c.x_pitch; few.w_pitch = c.w_pitch;
+        few.N = p.N; few.D = p.D; few.V = p.V; few.score_row = p.Np;
+        few.bias = c.bias; few.mask = a.mask; few.scores = a.scores; few.stats = a.stats; few.label_score = a.label_score;
+    }
+    if (p.few_scores) {
+        few.each = p.score_each;
+        mpcnn::launch_rows_few_scores<T>(few, (unsigned)p.score_v, st);
+    } else if (sizeof(T) == 2 && p.V * p.D >= kBlockWeights && direct_operand<T>(c.x, c.x_pitch, p.D) && direct_operand<T>(c.w, c.w_pitch, p.D)) {
+        mpcnn::ProductArgs b{};
+        b.A = (const char*)c.w; b.a_row = c.w_pitch * 2; b.B = (const char*)c.x; b.b_row = c.x_pitch * 2;
+        b.M = a.V; b.N = p.N; b.blocks = p.D * 2 / mpcnn::kBlockBytes;
+        b.bias = c.bias; b.labels = c.labels; b.stats = a.stats; b.label_score = a.label_score; b.scores = a.scores; b.score_row = p.Np;
+        const Tiling t = tiling_of(p.V, p.N, b.blocks, 1, false);
+        a.tiles = t.tiles_m;
+        const mpcnn_status rc = launch_product<false, mpcnn::kScores>(b, t, st);
+        if (rc != MPCNN_OK) return rc;
+    } else {
+        mpcnn::rows_direct_scores_kernel<T><<<dim3((unsigned)p.score_v, (unsigned)p.score_n), 256, 0, st>>>(a);
+    }
     // statistics joined with the derivative where there are few tiles of classes, by a launch of their own otherwise
-    const bool joined = p.score_v > mpcnn::kDeltaFewTiles;
+    const bool joined = a.tiles > mpcnn::kDeltaFewTiles || p.few;
     a.lse = (float*)(ws + p.lse); a.weight = (float*)(ws + p.weight);
     double* const shares = (double*)(ws + p.loss_part);
     // (a workgroup takes several tiles of rows where that leaves four workgroups per compute unit: fewer sums over the rows to add up)
@@ -321,9 +301,9 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
     int groups = along;
     if (joined) {
         mpcnn::JoinArgs j{};
-        j.stats = a.stats; j.tiles = p.score_v; j.N = p.N; j.label_score = a.label_score; j.mask = a.mask;
+        j.stats = a.stats; j.tiles = a.tiles; j.N = p.N; j.label_score = a.label_score; j.mask = a.mask;
         j.lse = a.lse; j.weight = a.weight; j.lse_out = c.lse; j.rowloss = c.rowloss;
-        groups = join_groups_of(p.N, p.score_v);
+        groups = join_groups_of(p.N, a.tiles);
         j.loss_part = groups == 1 && c.loss ? c.loss : shares;
         launch_join(j, st);
     } else {
@@ -331,11 +311,27 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
         a.shares = groups == 1 && c.loss ? c.loss : shares;
     }
     a.loss = groups > 1 ? c.loss : nullptr; a.loss_part = shares; a.loss_parts = groups;
-    if (p.train && (c.dx || c.dw || c.db)) a.delta = ws + p.delta_rows;
+    if (p.few) {
+        few.lse = a.lse; few.weight = a.weight;
+        few.dw = c.dw; few.db = c.db; few.each = p.grad_each;
+        few.part = c.dx ? (float*)(ws + p.dx_part) : nullptr;
+        const int each = mpcnn::few_columns(p.N);            // features of a thread
+        few.columns = 16;
+        while (few.columns < mpcnn::kFewThreads && each * few.columns < p.D) few.columns *= 2;
+        if (c.dx || c.dw || c.db)
+            mpcnn::launch_rows_few_grads<T>(few, dim3((unsigned)p.grad_groups, (unsigned)((p.D + each * few.columns - 1) / (each * few.columns))), st);
+        few.parts = p.grad_groups; few.dx = c.dx; few.dx_pitch = c.dx_pitch;
+        few.loss = a.loss; few.loss_part = a.loss_part; few.loss_parts = groups;
+        if (few.part || few.loss)
+            mpcnn::launch_rows_few_sum<T>(few, few.part ? (unsigned)(((int64_t)p.N * p.D + 63) / 64) : 1, st);
+        HIP_TRY(hipGetLastError());
+        return MPCNN_OK;
+    }
+    a.delta = p.train && (c.dx || c.dw || c.db);
     if (a.delta || !joined) {
         a.db = c.db;
         if (c.db && along > 1) { a.db_part = (float*)(ws + p.db_part); a.db_parts = along; }
-        mpcnn::rows_direct_delta_kernel<T><<<dim3((unsigned)along, (unsigned)(a.delta ? v_tiles : 1)), 256, 0, st>>>(a);
+        mpcnn::rows_direct_delta_kernel<<<dim3((unsigned)along, (unsigned)(a.delta ? v_tiles : 1)), 256, 0, st>>>(a);
     }
     if (p.train) {
         a.dx = c.dx; a.dx_pitch = c.dx_pitch; a.dw = c.dw;
@@ -369,7 +365,6 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         HIP_TRY(hipGetLastError());
         return MPCNN_OK;
     }
-    if (p.few) return run_few<T>(p, c, ws, st);
     if (p.direct) return run_direct<T>(p, c, ws, st);
     const mpcnn::RowMask every{}, mask{c.labels, c.roww, (int)p.V};
     unsigned* const x_peak = (unsigned*)(ws + p.peaks);
@@ -393,9 +388,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         const dim3 grid((unsigned)(H ? (R + 63) / 64 : (R + 127) / 128), (unsigned)((p.D + 63) / 64));
         (H ? mpcnn::rows_pack_kernel : mpcnn::rows_pack16_kernel)<<<grid, 256, 0, st>>>(a);
     };
-    // operands as they are: whole blocks at aligned addresses
-    auto direct = [&](const void* m, int64_t pitch) { return !H && p.D % 64 == 0 && (uintptr_t)m % 16 == 0 && pitch % 8 == 0 && pitch * 512 < (1ll << 31); };
-    const bool x_direct = direct(c.x, c.x_pitch), w_direct = direct(c.w, c.w_pitch);
+    const bool x_direct = direct_operand<T>(c.x, c.x_pitch, p.D), w_direct = direct_operand<T>(c.w, c.w_pitch, p.D);
     if (!x_direct || p.train)
         pack(c.x, c.x_pitch, p.N, x_direct ? nullptr : ws + p.x_rows, p.train ? ws + p.x_cols : nullptr, p.n_bytes, mask, x_peak);
 
@@ -434,7 +427,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         if (rc != MPCNN_OK) return rc;
         done += tiles;
     }
-    const int join_groups = join_groups_of(p.N, p.score_v);
+    const int join_groups = join_groups_of(p.N, done);
     mpcnn::JoinArgs j{};
     j.stats = (const float2*)(ws + p.stats); j.tiles = done; j.N = p.N;
     j.label_score = (const float*)(ws + p.label_score); j.mask = mask;

@@ -9,7 +9,8 @@
 //
 // Products on v_mfma_f32_32x32x16_bf16: bf16 numbers as they are, fp32 ones as three bf16 parts (x = h + m + l, 24 bits) and the six largest
 // of nine products: the same exponents as fp32, so no scale has to be found first, which is what two fp16 parts need and what costs
-// two more passes.  A lane fetches its own operand, 8 k's of one row, a step (32 k's) ahead of the products; operands are fetched by every
+// two more passes.  The derivative stays fp32 with either storage; for bf16 storage it is multiplied as two parts (16 bits), so that results
+// are rounded once.  A lane fetches its own operand, 8 k's of one row, a step (32 k's) ahead of the products; operands are fetched by every
 // wave that needs them (first-level cache).  Little work is bound by the trips to memory one after the other, some 0.7 us each, and
 // so a workgroup has one tile of 32 x 32 and its four waves deal the sum's steps among them; where there are tiles enough or the
 // sum has a step or two, each wave has a tile of its own (64 x 64 per workgroup).
@@ -41,7 +42,7 @@ struct DirectArgs {
     float *rowloss, *lse_out;              // results of the join (null: not asked for)
     int tiles, batch;                      // of the statistics; of the derivative: times 64 rows per workgroup
     double* shares;                        // of the loss, one per workgroup along the rows, or null
-    void* delta;                           // [V][score_row] of the storage type (fp32: in the scores' place), zeros for rows that add nothing
+    int delta;                             // whether the derivative takes the scores' place, zeros for rows that add nothing
     // gradients
     void* dx;
     long dx_pitch;
@@ -59,31 +60,32 @@ struct DirectArgs {
     double* loss;
 };
 
-template <typename T> constexpr int kDirectParts = sizeof(T) == 4 ? 3 : 1;
-
-template <typename T>
-__device__ __forceinline__ void direct_parts(d_bf16x8 (&p)[kDirectParts<T>], v8f v)
+template <int P>
+__device__ __forceinline__ void direct_parts(d_bf16x8 (&p)[P], v8f v)
 {
     p[0] = __builtin_convertvector(v, d_bf16x8);
-    if constexpr (kDirectParts<T> == 3) {
+    if constexpr (P > 1) {
         const v8f r = v - __builtin_convertvector(p[0], v8f);
         p[1] = __builtin_convertvector(r, d_bf16x8);
-        p[2] = __builtin_convertvector(r - __builtin_convertvector(p[1], v8f), d_bf16x8);
+        if constexpr (P > 2) p[2] = __builtin_convertvector(r - __builtin_convertvector(p[1], v8f), d_bf16x8);
     }
 }
-// acc += 16 k's
-template <typename T>
+// acc += 16 k's, x in PA parts, y in PB
+template <int PA, int PB>
 __device__ __forceinline__ void direct_product(v16f& acc, v8f x, v8f y)
 {
-    constexpr int P = kDirectParts<T>;
-    d_bf16x8 a[P], b[P];
-    direct_parts<T>(a, x);
-    direct_parts<T>(b, y);
+    constexpr int P = PA > PB ? PA : PB;
+    d_bf16x8 a[PA], b[PB];
+    direct_parts<PA>(a, x);
+    direct_parts<PB>(b, y);
 #pragma unroll
     for (int sum = P - 1; sum >= 0; --sum)              // the smallest products first
 #pragma unroll
-        for (int i = 0; i <= sum; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[sum - i], acc, 0, 0, 0);
+        for (int i = 0; i <= sum; ++i)
+            if (i < PA && sum - i < PB) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[sum - i], acc, 0, 0, 0);
 }
+template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+template <typename T> constexpr int kDeltaParts = sizeof(T) == 4 ? 3 : 2;
 
 // The sums of the four waves' accumulators, in their order: thread t the results [4 (t / 32) + q][t % 32] of the tile
 __device__ __forceinline__ v4f direct_fold(const v16f& acc, float (*fold)[32][33])
@@ -141,8 +143,8 @@ __global__ __launch_bounds__(256) void rows_direct_scores_kernel(DirectArgs a)
     for (int s = first; s < steps; s += by) {
         const v8f a0 = widen(u[0]), a1 = widen(u[1]), b0 = widen(y[0]), b1 = widen(y[1]);
         fetch(s + by);
-        direct_product<T>(acc, a0, b0);
-        direct_product<T>(acc, a1, b1);
+        direct_product<kParts<T>, kParts<T>>(acc, a0, b0);
+        direct_product<kParts<T>, kParts<T>>(acc, a1, b1);
     }
     constexpr float kNone = -__builtin_inff();
     if (deal) {
@@ -222,7 +224,6 @@ __device__ __forceinline__ float direct_delta(float score, float lse, bool live,
 
 // 64 classes x `batch` times 64 rows per workgroup: a lane a row, a wave every fourth class
 constexpr int kDeltaSide = 64, kDeltaFewTiles = 32;
-template <typename T>
 __global__ __launch_bounds__(256) void rows_direct_delta_kernel(DirectArgs a)
 {
     __shared__ float2 red[4][kDeltaSide];
@@ -277,13 +278,12 @@ __global__ __launch_bounds__(256) void rows_direct_delta_kernel(DirectArgs a)
             }
         }
         if (!a.delta) continue;                          // (the loss alone; nobody reads `red` before its next barrier but this wave's lanes)
-        T* const delta = (T*)a.delta;
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             const int v = v0 + wave + 4 * k;
             const float g = direct_delta(x[k], lse, label != kNoLabel, label == v) * weight, put = weight != 0.f ? g : 0.f;
             tile[wave + 4 * k][lane] = put;
-            if (v < a.V) store1(delta + v * a.score_row + n, put);
+            if (v < a.V) a.scores[v * a.score_row + n] = put;
         }
         __syncthreads();
         if (a.db) {                                      // four threads a class
@@ -365,18 +365,19 @@ __global__ __launch_bounds__(256) void rows_direct_grads_kernel(DirectArgs a)
         }
     };
     if (dx) {
-        const T* const ap = (const T*)a.delta + (k0 + 8 * half) * a.score_row + m;
-        T u[16], y[16];
+        const float* const ap = a.scores + (k0 + 8 * half) * a.score_row + m;
+        float u[16];
+        T y[16];
         auto fetch = [&](int s) {
             if (s < full) {
-                const T* const p = ap + s * kDirectK * a.score_row;
+                const float* const p = ap + s * kDirectK * a.score_row;
 #pragma unroll
                 for (int z = 0; z < 16; ++z) u[z] = p[(16 * (z >> 3) + (z & 7)) * a.score_row];
             } else {
 #pragma unroll
                 for (int z = 0; z < 16; ++z) {
                     const int k = k0 + s * kDirectK + 16 * (z >> 3) + 8 * half + (z & 7);
-                    u[z] = ((const T*)a.delta)[(k < K ? k : K - 1) * a.score_row + m];
+                    u[z] = a.scores[(k < K ? k : K - 1) * a.score_row + m];
                 }
             }
             fetch_b(y, s);
@@ -388,20 +389,20 @@ __global__ __launch_bounds__(256) void rows_direct_grads_kernel(DirectArgs a)
 #pragma unroll
             for (int z = 0; z < 16; ++z) {
                 const int k = 16 * (z >> 3) + 8 * half + (z & 7);
-                p[z >> 3][z & 7] = k < left ? (float)u[z] : 0.f;
+                p[z >> 3][z & 7] = k < left ? u[z] : 0.f;
                 q[z >> 3][z & 7] = (float)y[z];          // (beyond the last class times a derivative of zero: finite or not finite anyway)
             }
             if (s + by < steps) fetch(s + by);
-            direct_product<T>(acc, p[0], q[0]);
-            direct_product<T>(acc, p[1], q[1]);
+            direct_product<kDeltaParts<T>, kParts<T>>(acc, p[0], q[0]);
+            direct_product<kDeltaParts<T>, kParts<T>>(acc, p[1], q[1]);
         }
     } else {
-        const T* const ap = (const T*)a.delta + m * a.score_row;
-        Raw8<T> u[2];
+        const float* const ap = a.scores + m * a.score_row;
+        v8f u[2];
         T y[16];
         auto fetch = [&](int s) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) u[k] = raw8(ap + k0 + s * kDirectK + 16 * k + 8 * half);   // (padded to whole steps with zeros)
+            for (int k = 0; k < 2; ++k) u[k] = load8(ap + k0 + s * kDirectK + 16 * k + 8 * half);   // (padded to whole steps with zeros)
             fetch_b(y, s);
         };
         if (first < steps) fetch(first);
@@ -409,7 +410,7 @@ __global__ __launch_bounds__(256) void rows_direct_grads_kernel(DirectArgs a)
             v8f p[2], q[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                p[k] = widen(u[k]);
+                p[k] = u[k];
 #pragma unroll
                 for (int z = 0; z < 8; ++z) q[k][z] = (float)y[8 * k + z];
             }
@@ -421,8 +422,8 @@ __global__ __launch_bounds__(256) void rows_direct_grads_kernel(DirectArgs a)
                 }
             }
             if (s + by < steps) fetch(s + by);
-            direct_product<T>(acc, p[0], q[0]);
-            direct_product<T>(acc, p[1], q[1]);
+            direct_product<kDeltaParts<T>, kParts<T>>(acc, p[0], q[0]);
+            direct_product<kDeltaParts<T>, kParts<T>>(acc, p[1], q[1]);
         }
     }
 

@@ -1,49 +1,22 @@
-// The class layer on at most eight rows of features (class_rows.hip): bound by the passes over the class weights (read for the scores, read
-// for the rows' gradient, their own gradient written), so everything is done on the vector ALU in fp32, with 128-bit fetches and stores
-// at whatever address the numbers have, and nothing is fetched for rows that do not exist.
-//
+// The class layer's gradients on at most sixteen rows of features, and scores on at most eight (class_rows.hip): bound by the passes over the
+// class weights (read for the scores, read for the rows' gradient, their own gradient written), so everything is done on the vector
+// ALU in fp32, with 128-bit fetches and stores at whatever address the numbers have, and nothing is fetched for rows that do not exist.
 // A kernel instance per number of rows.
 //
 //   rows_few_scores   16 lanes share a class, 8 features a lane and step; a group has 4 classes at once, so that a row's features, which
-//                     every group reads from LDS, are used 4 times.  64 classes per round of a workgroup; scores stored
-//                     [row][class]; per workgroup and row the largest and the sum of exponentials of all its classes.
-//   rows_few_grads    a thread keeps 8 features of every row and their gradients over a stretch of the classes: one fetch of the class's
-//                     weights, 8 multiplications per row for dx and 8 for dw, one store.
+//                     every group reads from LDS, are used 4 times.  64 classes per round of a workgroup; scores stored [class][row];
+//                     per workgroup and row the largest and the sum of exponentials of all its classes.  (The matrix instruction's
+//                     scores, kernels_rows_direct.hpp, fetch 16 bytes of each of 32 classes at once and reach 2.1-2.9 TB/s on large weights, this
+//                     kernel up to 5; it has less to do at once with few classes, and more arithmetic per row.  us, here / there: 1 x
+//                     4096 x 128000 fp32 404 / 729, bf16 213 / 360; 1 x 1000 x 16000 fp32 20 / 24, bf16 15 / 14; 8 x 1024 x 32000 fp32 33 / 39.)
+//   rows_few_grads    a thread keeps 8 features (4 with more than eight rows) of every row and their gradients over a stretch of the classes:
+//                     one fetch of the class's weights, as many multiplications per row for dx and for dw, one store.
 //   rows_few_sum      adds the workgroups' shares of dx, in a fixed order.
 #pragma once
 #include "any_address.hpp"
-#include "kernels_rows_parts.hpp"
+#include "rows_few.hpp"
 
 namespace mpcnn {
-
-constexpr int kFewRows = 8, kFewRound = 64;      // rows, classes of a round
-constexpr int kFewThreads = 256;
-constexpr int kFewSteps = 8;                     // of 128 features, whose rows LDS holds at once
-
-struct FewArgs {
-    const void *x, *w;
-    long x_pitch, w_pitch;
-    int N, D;
-    long V, score_row;
-    const float* bias;
-    RowMask mask;
-    float* scores;                               // [N][score_row], or null
-    float2* stats;                               // [workgroups][N]
-    float* label_score;
-    long each;                                   // classes of a workgroup
-    // gradients
-    const float *lse, *weight;
-    void* dw;
-    float *db, *part;                            // part: [workgroups][N][D] shares of dx, or null
-    int columns;                                 // threads that share a class's features: 16 .. 256, a power of two
-    // sum
-    int parts;
-    void* dx;
-    long dx_pitch;
-    const double* loss_part;
-    int loss_parts;
-    double* loss;
-};
 
 // The sum over 16 lanes side by side, in all of them
 template <int CTRL>
@@ -63,6 +36,7 @@ template <typename T, int NR>
 __global__ __launch_bounds__(kFewThreads) void rows_few_scores_kernel(FewArgs a)
 {
     constexpr int C = 4;                         // classes of a group of 16 lanes
+    constexpr int kFewSteps = 8;                 // of 128 features, whose rows LDS holds at once
     constexpr float kNone = -__builtin_inff();
     __shared__ float sc[NR][kFewRound];
     __shared__ __attribute__((aligned(32))) float xl[NR][128 * kFewSteps];
@@ -143,7 +117,7 @@ __global__ __launch_bounds__(kFewThreads) void rows_few_scores_kernel(FewArgs a)
             if (n >= NR) continue;               // (uniform)
             const float s = v < end ? sc[n][lane] + b : kNone;
             if (v < end) {
-                if (a.scores) a.scores[n * a.score_row + v] = s;
+                if (a.scores) a.scores[v * a.score_row + n] = s;
                 if (v == a.mask.labels[n]) a.label_score[n] = s;
             }
             // every lane keeps its own classes' statistics until the end
@@ -172,27 +146,29 @@ __global__ __launch_bounds__(kFewThreads) void rows_few_scores_kernel(FewArgs a)
 template <typename T, int NR>
 __global__ __launch_bounds__(kFewThreads) void rows_few_grads_kernel(FewArgs a)
 {
+    constexpr int E = few_columns(NR);
+    typedef float vef __attribute__((ext_vector_type(E)));
     __shared__ float delta[NR][kFewRound];       // times the row's weight
-    __shared__ float fold[kFewThreads][8];
+    __shared__ __attribute__((aligned(32))) float fold[kFewThreads][E];
     const int tid = threadIdx.x;
     const int column = tid & (a.columns - 1), deal = tid / a.columns, deals = kFewThreads / a.columns;
-    const int d = 8 * (blockIdx.y * a.columns + column), left = a.D - d;
+    const int d = E * (blockIdx.y * a.columns + column), left = a.D - d;
     const T* const w = (const T*)a.w;
-    v8f x[NR], dx[NR];
+    vef x[NR], dx[NR];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-        const v8f u = load8_of((const T*)a.x + n * a.x_pitch, d, a.D);
-        x[n] = a.weight[n] != 0.f ? u : v8f{};
-        dx[n] = v8f{};
+        const vef u = widen(raw_of<E>((const T*)a.x + n * a.x_pitch, d, a.D));
+        x[n] = a.weight[n] != 0.f ? u : vef{};
+        dx[n] = vef{};
     }
     const long begin = (long)blockIdx.x * a.each, end = begin + a.each < a.V ? begin + a.each : a.V;
     for (long v0 = begin; v0 < end; v0 += kFewRound) {
         const int count = end - v0 < kFewRound ? (int)(end - v0) : kFewRound;
         for (int i = tid; i < NR * kFewRound; i += kFewThreads) {
-            const int n = i / kFewRound, k = i % kFewRound;
+            const int k = i / NR, n = i % NR;
             float g = 0.f;
             if (k < count) {
-                const float weight = a.weight[n], s = a.scores[n * a.score_row + v0 + k];
+                const float weight = a.weight[n], s = a.scores[(v0 + k) * a.score_row + n];
                 if (weight != 0.f) {
                     g = s == -__builtin_inff() ? 0.f : expf(s - a.lse[n]);
                     if (v0 + k == a.mask.labels[n]) g -= 1.f;
@@ -211,33 +187,33 @@ __global__ __launch_bounds__(kFewThreads) void rows_few_grads_kernel(FewArgs a)
         if (left > 0) {
             constexpr int U = 8;                 // classes in flight
             for (int k0 = deal; k0 < count; k0 += U * deals) {
-                Raw8<T> u[U];
+                Raw<T, E> u[U];
 #pragma unroll
                     for (int q = 0; q < U; ++q) {
                         const int k = k0 + q * deals;
-                        u[q] = raw8_of(w + (v0 + (k < count ? k : count - 1)) * a.w_pitch, d, a.D);
+                        u[q] = raw_of<E>(w + (v0 + (k < count ? k : count - 1)) * a.w_pitch, d, a.D);
                     }
 #pragma unroll
                 for (int q = 0; q < U; ++q) {
                     const int k = k0 + q * deals;
                     if (k >= count) break;
-                    v8f dw = {};
-                    const v8f v = widen(u[q]);
+                    vef dw = {};
+                    const vef v = widen(u[q]);
 #pragma unroll
                     for (int n = 0; n < NR; ++n) {
                         const float g = delta[n][k];
 #pragma unroll
-                            for (int z = 0; z < 8; ++z) dx[n][z] = fmaf(g, v[z], dx[n][z]);
+                            for (int z = 0; z < E; ++z) dx[n][z] = fmaf(g, v[z], dx[n][z]);
 #pragma unroll
-                        for (int z = 0; z < 8; ++z) dw[z] = fmaf(g, x[n][z], dw[z]);
+                        for (int z = 0; z < E; ++z) dw[z] = fmaf(g, x[n][z], dw[z]);
                     }
                     if (a.dw) {
                         T* const to = (T*)a.dw + (v0 + k) * a.D + d;
-                        if (left >= 8) {
-                            store8(to, dw);
+                        if (left >= E) {
+                            store_any(to, dw);
                         } else {
 #pragma unroll
-                            for (int z = 0; z < 8; ++z)
+                            for (int z = 0; z < E; ++z)
                                 if (z < left) store1(to + z, dw[z]);
                         }
                     }
@@ -249,18 +225,18 @@ __global__ __launch_bounds__(kFewThreads) void rows_few_grads_kernel(FewArgs a)
     if (!a.part) return;
 #pragma unroll
     for (int n = 0; n < NR; ++n) {               // the deals of a class's features, in their order
-        *reinterpret_cast<v8f*>(fold[tid]) = dx[n];
+        *reinterpret_cast<vef*>(fold[tid]) = dx[n];
         __syncthreads();
         if (deal == 0 && left > 0) {
-            v8f s = dx[n];
+            vef s = dx[n];
             for (int q = 1; q < deals; ++q) {
-                const v8f o = *reinterpret_cast<const v8f*>(fold[q * a.columns + column]);
+                const vef o = *reinterpret_cast<const vef*>(fold[q * a.columns + column]);
 #pragma unroll
-                for (int z = 0; z < 8; ++z) s[z] += o[z];
+                for (int z = 0; z < E; ++z) s[z] += o[z];
             }
             float* const to = a.part + ((long)blockIdx.x * a.N + n) * a.D + d;
 #pragma unroll
-            for (int z = 0; z < 8; ++z)
+            for (int z = 0; z < E; ++z)
                 if (z < left) to[z] = s[z];
         }
         __syncthreads();

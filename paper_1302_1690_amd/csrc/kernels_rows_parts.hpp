@@ -4,25 +4,11 @@
 #pragma once
 #include "any_address.hpp"
 #include "ranges.hpp"
+#include "rows_mask.hpp"
 
 namespace mpcnn {
 
 constexpr int kPeakGroups = 256;           // words of a peak
-
-// Rows that add something: a label among the classes and a weight that is not zero
-struct RowMask {
-    const int* labels;
-    const float* weights;                  // null: 1
-    int classes;
-};
-__device__ __forceinline__ float row_weight(const RowMask& m, int n)
-{
-    const int t = m.labels[n];
-    if (t < 0 || t >= m.classes) return 0.f;
-    return m.weights ? m.weights[n] : 1.f;
-}
-
-constexpr int kNoLabel = -1;               // in the library's own copy of the labels: a row that adds nothing
 
 // ---- the largest magnitude of a matrix, as bits (one word per workgroup); what is not finite is passed over
 struct PeakArgs {
