@@ -23,7 +23,7 @@ using mpcnn::fail;
 namespace {
 
 constexpr int64_t kMaxRows = 1 << 20, kMaxFeatures = 1 << 20, kMaxClasses = 0x7fffffff - 1024;   // (32-bit offsets inside a tile)
-constexpr int64_t kRoom = (int64_t)1 << 27;            // scores of a piece: 0.5 GB in fp32, and as much of derivatives in both orders
+constexpr int64_t kRoom = (int64_t)1 << 27;            // scores of a piece: 0.5 GB in fp32, and half as much of derivatives (as much with fp32 storage)
 constexpr int64_t kWeightRoom = (int64_t)512 << 20;    // bytes of a piece's class weights, brought into blocks
 constexpr int64_t kPartRoom = (int64_t)256 << 20;      // bytes of a product's partial sums
 constexpr int kMaxPiece = 1 << 20;
@@ -82,9 +82,10 @@ struct Plan {
     int64_t piece;                       // classes
     int64_t stat_tiles;
     Tiling dx, dw;                       // of a whole piece
-    size_t peaks, stats, label_score, lse, weight, loss_part, x_rows, x_cols, w_rows, w_cols, score, delta_rows, delta_cols, db_part,
+    size_t peaks, stats, label_score, lse, weight, loss_part, x_rows, x_cols, w_rows, score, delta, db_part,
         dx_part, dw_part, total;
     int64_t bytes_along(int64_t n) const { return halves ? up_to(n, 32) * 4 : up_to(n, 64) * 2; }
+    int64_t v_blocks(int64_t n) const { return (n + (halves ? 31 : 63)) / (halves ? 32 : 64); }   // of the sum over n classes
     bool dx_parts() const { return dx.splits > 1 || piece < V; }
 };
 
@@ -167,7 +168,6 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     if (train) bound(kRoom / p->Np);
     p->piece = piece;
     const int64_t pieces = (classes + piece - 1) / piece;
-    const int64_t v_bytes = p->bytes_along(piece);
     p->stat_tiles = (classes + 127) / 128 + pieces;
     const int64_t N = p->N, D = p->D;
     p->peaks = take(4 * 3 * mpcnn::kPeakGroups);
@@ -179,13 +179,11 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     p->x_rows = take(N * p->d_bytes);
     p->w_rows = take(piece * p->d_bytes);
     if (train) {
-        p->dx = tiling_of(N, D, v_bytes / mpcnn::kBlockBytes, std::min<int64_t>(64, std::max<int64_t>(1, kPartRoom / (4 * N * D + 1))), p->halves);
+        p->dx = tiling_of(N, D, p->v_blocks(piece), std::min<int64_t>(64, std::max<int64_t>(1, kPartRoom / (4 * N * D + 1))), p->halves);
         p->dw = tiling_of(piece, D, p->n_bytes / mpcnn::kBlockBytes, std::min<int64_t>(64, std::max<int64_t>(1, kPartRoom / (4 * piece * D))), p->halves);
         p->x_cols = take(D * p->n_bytes);
-        p->w_cols = take(D * v_bytes);
         p->score = take((p->keep ? classes : piece) * p->Np * 4);
-        p->delta_rows = take(N * v_bytes);
-        p->delta_cols = take(piece * p->n_bytes);
+        p->delta = take(piece * p->n_bytes);
         p->db_part = take(p->Np / 64 * piece * 4);
         if (p->dx_parts()) p->dx_part = take(4 * (int64_t)p->dx.splits * N * D);
         if (p->dw.splits > 1) p->dw_part = take(4 * (int64_t)p->dw.splits * piece * D);
@@ -195,11 +193,11 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
 }
 
 // ---- launches of the product
-template <int WM, int WN, int MT, int NT, bool HALVES, int RESULT>
+template <int WM, int WN, int MT, int NT, bool HALVES, int RESULT, bool ACROSS>
 mpcnn_status launch_instance(const mpcnn::ProductArgs& a, hipStream_t st)
 {
     constexpr int lds = 2 * 32 * (WM * MT + WN * NT) * mpcnn::kBlockBytes;
-    auto* kernel = &mpcnn::rows_product_kernel<WM, WN, MT, NT, HALVES, RESULT>;
+    auto* kernel = &mpcnn::rows_product_kernel<WM, WN, MT, NT, HALVES, RESULT, ACROSS>;
     if constexpr (lds > 64 * 1024) {       // must be said once per device
         static std::atomic<uint64_t> said{0};
         int dev = 0;
@@ -213,11 +211,11 @@ mpcnn_status launch_instance(const mpcnn::ProductArgs& a, hipStream_t st)
     kernel<<<(unsigned)up_to(all, 8), 64 * WM * WN, lds, st>>>(a);
     return MPCNN_OK;
 }
-template <bool HALVES, int RESULT>
+template <bool HALVES, int RESULT, bool ACROSS = false>
 mpcnn_status launch_product(mpcnn::ProductArgs a, const Tiling& t, hipStream_t st)
 {
     a.tiles_m = t.tiles_m; a.tiles_n = t.tiles_n; a.splits = t.splits; a.per_split = t.per_split;
-    return t.big ? launch_instance<2, 4, 4, 2, HALVES, RESULT>(a, st) : launch_instance<2, 2, 2, 2, HALVES, RESULT>(a, st);
+    return t.big ? launch_instance<2, 4, 4, 2, HALVES, RESULT, ACROSS>(a, st) : launch_instance<2, 2, 2, 2, HALVES, RESULT, ACROSS>(a, st);
 }
 
 // Whether a product reads a matrix as it is: bf16, whole blocks at aligned addresses
@@ -368,23 +366,23 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
     if (p.direct) return run_direct<T>(p, c, ws, st);
     const mpcnn::RowMask every{}, mask{c.labels, c.roww, (int)p.V};
     unsigned* const x_peak = (unsigned*)(ws + p.peaks);
-    unsigned *const w_peak = x_peak + mpcnn::kPeakGroups, *const roww_peak = w_peak + mpcnn::kPeakGroups;
+    unsigned *const w_peak = x_peak + mpcnn::kPeakGroups, *const wx_peak = c.roww ? w_peak + mpcnn::kPeakGroups : x_peak;   // wx: of the weighted features
     if constexpr (H) {
         mpcnn::PeakSet set{};
         int n = 0;
-        auto peak = [&](const void* src, int64_t pitch, int64_t rows, int64_t cols, const mpcnn::RowMask& m, unsigned* words) {
-            set.of[n++] = mpcnn::PeakArgs{(const float*)src, pitch, rows, (int)cols, m, words};
+        auto peak = [&](const void* src, int64_t pitch, int64_t rows, const mpcnn::RowMask& m, int weighted, unsigned* words) {
+            set.of[n++] = mpcnn::PeakArgs{(const float*)src, pitch, rows, p.D, m, weighted, words};
         };
-        peak(c.x, c.x_pitch, p.N, p.D, mask, x_peak);
-        peak(c.w, c.w_pitch, p.V, p.D, every, w_peak);
-        if (p.train && c.roww) peak(c.roww, 1, p.N, 1, mask, roww_peak);
+        peak(c.x, c.x_pitch, p.N, mask, 0, x_peak);
+        peak(c.w, c.w_pitch, p.V, every, 0, w_peak);
+        if (p.train && c.roww) peak(c.x, c.x_pitch, p.N, mask, 1, wx_peak);
         mpcnn::rows_peak_kernel<<<dim3(mpcnn::kPeakGroups, (unsigned)n), 1024, 0, st>>>(set);
     }
     auto pack = [&](const void* src, int64_t pitch, int64_t R, char* rows, char* cols, int64_t col_bytes, const mpcnn::RowMask& m, const unsigned* words) {
         mpcnn::PackRowsArgs a{};
         a.src = src; a.pitch = pitch; a.R = (int)R; a.C = p.D;
         a.rows = rows; a.cols = cols; a.row_bytes = p.d_bytes; a.col_bytes = col_bytes;
-        a.mask = m; a.peak = words;
+        a.mask = m; a.peak = words; a.col_peak = wx_peak;
         const dim3 grid((unsigned)(H ? (R + 63) / 64 : (R + 127) / 128), (unsigned)((p.D + 63) / 64));
         (H ? mpcnn::rows_pack_kernel : mpcnn::rows_pack16_kernel)<<<grid, 256, 0, st>>>(a);
     };
@@ -408,20 +406,19 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         if (tiles) *tiles = t.tiles_m;
         return launch_product<H, mpcnn::kScores>(a, t, st);
     };
-    auto weights_of = [&](int64_t v0, int64_t n_classes, bool rows, bool cols, int64_t v_bytes) {   // (and whether blocks along the features are in memory already)
-        if ((!rows || w_direct) && !cols) return;
-        pack((const char*)c.w + v0 * c.w_pitch * (int64_t)sizeof(T), c.w_pitch, n_classes, rows && !w_direct ? ws + p.w_rows : nullptr,
-             cols ? ws + p.w_cols : nullptr, v_bytes, every, w_peak);
+    // a piece's weights in blocks along the features, where they are not read as they are
+    auto weights_of = [&](int64_t v0, int64_t n_classes) {
+        if (!w_direct) pack((const char*)c.w + v0 * c.w_pitch * (int64_t)sizeof(T), c.w_pitch, n_classes, ws + p.w_rows, nullptr, 0, every, w_peak);
     };
     auto rows_at = [&](int64_t v0) { return w_direct ? (const char*)c.w + v0 * c.w_pitch * 2 : (const char*)(ws + p.w_rows); };
     const int64_t w_row = w_direct ? c.w_pitch * 2 : p.d_bytes;
 
     float* const score = p.train ? (float*)(ws + p.score) : nullptr;
-    const bool one_piece = p.train && p.V <= piece;      // its weights are brought into both orders at once
+    const bool one_piece = p.V <= piece;                 // (its weights' blocks are there in the second round)
     int done = 0;
     for (int64_t v0 = 0; v0 < p.V; v0 += piece) {
         const int64_t n = std::min(piece, p.V - v0);
-        weights_of(v0, n, true, one_piece && c.dx, p.bytes_along(n));
+        weights_of(v0, n);
         int tiles = 0;
         const mpcnn_status rc = scores(v0, n, rows_at(v0), w_row, (float2*)(ws + p.stats) + (int64_t)done * p.N, p.keep ? score + v0 * p.Np : nullptr, &tiles);
         if (rc != MPCNN_OK) return rc;
@@ -444,9 +441,9 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         return MPCNN_OK;
     }
     for (int64_t v0 = 0; v0 < p.V; v0 += piece) {
-        const int64_t n = std::min(piece, p.V - v0), v_bytes = p.bytes_along(n);
+        const int64_t n = std::min(piece, p.V - v0);
         const bool last = v0 + n == p.V;
-        if (!one_piece) weights_of(v0, n, !p.keep, c.dx != nullptr, v_bytes);
+        if (!one_piece && (!p.keep || c.dx)) weights_of(v0, n);
         float* const s = p.keep ? score + v0 * p.Np : score;
         if (!p.keep) {
             const mpcnn_status rc = scores(v0, n, rows_at(v0), w_row, nullptr, s, nullptr);
@@ -455,9 +452,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         mpcnn::DeltaArgs d{};
         d.scores = s; d.score_row = p.Np; d.classes = (int)n; d.class0 = (int)v0; d.N = p.N;
         d.labels = c.labels; d.lse = j.lse; d.weight = j.weight;
-        if (c.dx) { d.rows = ws + p.delta_rows; d.row_bytes = v_bytes; }
-        if (c.dw) { d.cols = ws + p.delta_cols; d.col_bytes = p.n_bytes; }
-        d.weight_peak = H && c.roww ? roww_peak : nullptr;
+        if (c.dx || c.dw) { d.out = ws + p.delta; d.out_bytes = p.n_bytes; }
         d.db_part = c.db ? (float*)(ws + p.db_part) : nullptr;
         mpcnn::rows_delta_kernel<H><<<dim3((unsigned)(p.Np / 64), (unsigned)((n + 63) / 64)), 256, 0, st>>>(d);
         fin.db_part = d.db_part; fin.tiles = (int)(p.Np / 64); fin.classes = n; fin.db = c.db ? c.db + v0 : nullptr;
@@ -465,33 +460,33 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         fin.loss = nullptr;
         if (c.dx) {
             mpcnn::ProductArgs a{};
-            a.A = ws + p.delta_rows; a.a_row = v_bytes; a.B = ws + p.w_cols; a.b_row = v_bytes;
-            a.M = p.N; a.N = p.D; a.blocks = (int)(v_bytes / mpcnn::kBlockBytes);
+            a.A = ws + p.delta; a.a_row = p.n_bytes; a.a_bytes = n * p.n_bytes;
+            a.B = rows_at(v0); a.b_row = w_row; a.b_bytes = (n - 1) * w_row + (w_direct ? 2 * (int64_t)p.D : p.d_bytes);
+            a.M = p.N; a.N = p.D; a.blocks = (int)p.v_blocks(n);
             a.a_up = 14; a.b_peak = H ? w_peak : nullptr; a.b_words = mpcnn::kPeakGroups;
-            a.out = c.dx; a.out_row = c.dx_pitch; a.row_scale = j.weight;
+            a.out = c.dx; a.out_row = c.dx_pitch; a.row_scale = j.weight; a.row_mask = !H;
             Tiling t = p.dx;
             t.per_split = (int)((a.blocks + t.splits - 1) / t.splits);
             mpcnn_status rc;
             if (p.dx_parts()) {
                 a.part = (float*)(ws + p.dx_part); a.add = v0 > 0;
-                rc = launch_product<H, mpcnn::kPart>(a, t, st);
+                rc = launch_product<H, mpcnn::kPart, true>(a, t, st);
                 if (last) {
                     mpcnn::SumArgs sum{};
                     sum.part = a.part; sum.splits = t.splits; sum.M = p.N; sum.N = p.D; sum.out_row = c.dx_pitch;
-                    sum.a_up = 14; sum.b_peak = a.b_peak; sum.halves = H; sum.row_scale = j.weight; sum.out = c.dx; sum.out_bf16 = !H;
+                    sum.a_up = 14; sum.b_peak = a.b_peak; sum.halves = H; sum.row_scale = j.weight; sum.row_mask = !H; sum.out = c.dx; sum.out_bf16 = !H;
                     mpcnn::rows_sum_kernel<<<(unsigned)std::min<int64_t>(4096, ((int64_t)p.N * p.D + 255) / 256), 256, 0, st>>>(sum);
                 }
             } else {
-                rc = launch_product<H, kStore>(a, t, st);
+                rc = launch_product<H, kStore, true>(a, t, st);
             }
             if (rc != MPCNN_OK) return rc;
         }
         if (c.dw) {
             mpcnn::ProductArgs a{};
-            a.A = ws + p.delta_cols; a.a_row = p.n_bytes; a.B = ws + p.x_cols; a.b_row = p.n_bytes;
+            a.A = ws + p.delta; a.a_row = p.n_bytes; a.B = ws + p.x_cols; a.b_row = p.n_bytes;
             a.M = (int)n; a.N = p.D; a.blocks = (int)(p.n_bytes / mpcnn::kBlockBytes);
-            a.a_peak = d.weight_peak; a.a_words = mpcnn::kPeakGroups; a.a_up = 14;
-            a.b_peak = H ? x_peak : nullptr; a.b_words = mpcnn::kPeakGroups;
+            a.a_up = 14; a.b_peak = H ? wx_peak : nullptr; a.b_words = mpcnn::kPeakGroups;
             a.out = (char*)c.dw + v0 * p.D * (int64_t)sizeof(T); a.out_row = p.D;
             Tiling t = p.dw;
             t.tiles_m = (int)((n + (t.big ? 255 : 127)) / (t.big ? 256 : 128));
@@ -501,7 +496,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
                 rc = launch_product<H, mpcnn::kPart>(a, t, st);
                 mpcnn::SumArgs sum{};
                 sum.part = a.part; sum.splits = t.splits; sum.M = n; sum.N = p.D; sum.out_row = p.D;
-                sum.a_peak = a.a_peak; sum.a_up = 14; sum.b_peak = a.b_peak; sum.halves = H; sum.out = a.out; sum.out_bf16 = !H;
+                sum.a_up = 14; sum.b_peak = a.b_peak; sum.halves = H; sum.out = a.out; sum.out_bf16 = !H;
                 mpcnn::rows_sum_kernel<<<(unsigned)std::min<int64_t>(4096, (n * p.D + 255) / 256), 256, 0, st>>>(sum);
             } else {
                 rc = launch_product<H, kStore>(a, t, st);

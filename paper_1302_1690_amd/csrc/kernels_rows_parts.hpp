@@ -17,6 +17,7 @@ struct PeakArgs {
     long rows;
     int cols;
     RowMask mask;                          // labels null: every row
+    int weighted;                          // numbers times their row's weight
     unsigned* words;                       // [kPeakGroups]
 };
 struct PeakSet { PeakArgs of[3]; };        // blockIdx.y: which
@@ -26,11 +27,11 @@ __global__ __launch_bounds__(1024) void rows_peak_kernel(PeakSet set)
     const PeakArgs& a = set.of[blockIdx.y];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     unsigned peak = 0;
-    auto add = [&](const v8f& x, bool counts) {
+    auto add = [&](const v8f& x, float weight) {
 #pragma unroll
         for (int z = 0; z < 8; ++z) {
-            const unsigned b = bits_of(x[z]) & 0x7fffffffu;
-            peak = counts && b < kNoPeak && b > peak ? b : peak;
+            const unsigned b = bits_of(x[z] * (a.weighted ? weight : 1.f)) & 0x7fffffffu;
+            peak = weight != 0.f && b < kNoPeak && b > peak ? b : peak;
         }
     };
     // eight numbers of a row at a time, four times eight in flight; rows without gaps are one
@@ -39,16 +40,16 @@ __global__ __launch_bounds__(1024) void rows_peak_kernel(PeakSet set)
     const long octets = (cols + 7) / 8, all = rows * octets, step = (long)gridDim.x * 1024;
     for (long e = (long)blockIdx.x * 1024 + threadIdx.x; e < all; e += 4 * step) {
         v8f v[4];
-        bool counts[4];
+        float weight[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const long at = e + q * step < all ? e + q * step : e;
             const long r = all == octets ? 0 : at / octets, c = 8 * (at - r * octets);
             v[q] = load8_of(a.src + r * a.pitch, (int)c, (int)cols);
-            counts[q] = !a.mask.labels || row_weight(a.mask, (int)r) != 0.f;
+            weight[q] = a.mask.labels ? row_weight(a.mask, (int)r) : 1.f;
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) add(v[q], counts[q]);
+        for (int q = 0; q < 4; ++q) add(v[q], weight[q]);
     }
     peak = wave_largest(peak);
     if (lane == 0) red[wave] = peak;
@@ -96,7 +97,7 @@ struct PackRowsArgs {
     char *rows, *cols;
     long row_bytes, col_bytes;
     RowMask mask;                          // labels null: every row
-    const unsigned* peak;                  // fp32: [kPeakGroups], what the numbers are raised by
+    const unsigned *peak, *col_peak;       // fp32: [kPeakGroups], what the numbers are raised by; along the columns they are times their row's weight
 };
 // fp32, two parts
 __global__ __launch_bounds__(256) void rows_pack_kernel(PackRowsArgs a)
@@ -104,34 +105,41 @@ __global__ __launch_bounds__(256) void rows_pack_kernel(PackRowsArgs a)
     constexpr int kPieces = 16;
     __shared__ float tile[64][65];
     const int c0 = 64 * blockIdx.y, r0 = 64 * blockIdx.x;
+    __shared__ float weight[64];
     const float up = power_of_two(raise_of(peak_of(a.peak, kPeakGroups), 0));
     v8f v[2];
-    bool there[2];
+    float w[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {                        // 8 lanes a row, 8 numbers each
         const int r = r0 + 32 * i + (threadIdx.x >> 3), at = r < a.R ? r : a.R - 1;
         v[i] = load8_of((const float*)a.src + at * a.pitch, c0 + 8 * (threadIdx.x & 7), a.C);
-        there[i] = r < a.R && (!a.mask.labels || row_weight(a.mask, at) != 0.f);
+        const float of = a.mask.labels ? row_weight(a.mask, at) : 1.f;
+        w[i] = r < a.R ? of : 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i) {
+        const int r = 32 * i + (threadIdx.x >> 3);
 #pragma unroll
-        for (int z = 0; z < 8; ++z) tile[32 * i + (threadIdx.x >> 3)][8 * (threadIdx.x & 7) + z] = there[i] ? v[i][z] * up : 0.f;
+        for (int z = 0; z < 8; ++z) tile[r][8 * (threadIdx.x & 7) + z] = w[i] != 0.f ? v[i][z] : 0.f;
+        if ((threadIdx.x & 7) == 0) weight[r] = w[i];
+    }
     __syncthreads();
     if (a.rows)
         for (int q = threadIdx.x; q < 64 * kPieces; q += 256) {
             const int r = q / kPieces, p = q % kPieces;
             const long at = (long)blockIdx.y * (kPieces * 16) + 16 * p;
             if (r0 + r >= a.R || at >= a.row_bytes) continue;
-            *reinterpret_cast<v4f*>(a.rows + (long)(r0 + r) * a.row_bytes + at) = piece_of<true>(p, [&](int i) { return tile[r][i]; });
+            *reinterpret_cast<v4f*>(a.rows + (long)(r0 + r) * a.row_bytes + at) = piece_of<true>(p, [&](int i) { return tile[r][i] * up; });
         }
-    if (a.cols)
+    if (a.cols) {
+        const float up_c = power_of_two(raise_of(peak_of(a.col_peak, kPeakGroups), 0));
         for (int q = threadIdx.x; q < 64 * kPieces; q += 256) {
             const int c = q / kPieces, p = q % kPieces;
             const long at = (long)blockIdx.x * (kPieces * 16) + 16 * p;
             if (c0 + c >= a.C || at >= a.col_bytes) continue;
-            *reinterpret_cast<v4f*>(a.cols + (long)(c0 + c) * a.col_bytes + at) = piece_of<true>(p, [&](int i) { return tile[i][c]; });
+            *reinterpret_cast<v4f*>(a.cols + (long)(c0 + c) * a.col_bytes + at) = piece_of<true>(p, [&](int i) { return tile[i][c] * weight[i] * up_c; });
         }
+    }
 }
 // bf16: as they are, 128 rows per workgroup.  LDS holds pairs of columns; a thread reads 8 rows of a pair and leaves a piece of either column.
 __global__ __launch_bounds__(256) void rows_pack16_kernel(PackRowsArgs a)
@@ -257,18 +265,17 @@ __global__ __launch_bounds__(THREADS) void rows_join_kernel(JoinArgs a)
     }
 }
 
-// ---- scores [classes][score_row] of a piece of the classes into the derivative p - [class = label], in blocks: along the classes as it is
-// (`rows`: [N][row_bytes], the data gradient's operand; the row's weight follows behind the product) and along the rows times the row's
-// weight (`cols`: [classes][col_bytes], the weight gradient's).  db_part: per tile of 64 rows the sums over them.
+// ---- scores [classes][score_row] of a piece of the classes into the derivative p - [class = label], in blocks along the rows ([classes][out_bytes]):
+// with bf16 storage times the row's weight (rounded once), with fp32 storage raised by 2^14 (the weight follows: with the features, or behind the
+// product).  db_part: per tile of 64 rows the sums over them, weighted.
 struct DeltaArgs {
     const float* scores;
     long score_row;
     int classes, class0, N;
     const int* labels;
     const float *lse, *weight;             // [N]
-    char *rows, *cols;
-    long row_bytes, col_bytes;
-    const unsigned* weight_peak;           // fp32: the weights' (null: all are 1)
+    char* out;                             // or null
+    long out_bytes;
     float* db_part;                        // [tiles of rows][classes], or null
 };
 template <bool HALVES>
@@ -297,35 +304,24 @@ __global__ __launch_bounds__(256) void rows_delta_kernel(DeltaArgs a)
         if (v < a.classes && w != 0.f) {
             g = x[i] == -__builtin_inff() ? 0.f : expf(x[i] - lse);
             if (v == label) g -= 1.f;
+            if constexpr (!HALVES) g *= w;
         }
         tile[wave + 4 * i][lane] = g;
     }
-    if (wave == 0) weight[lane] = w;
+    if (wave == 0) weight[lane] = HALVES ? w : 1.f;
     __syncthreads();
-    float up_r = 1.f, up_c = 1.f;
-    if constexpr (HALVES) {
-        up_r = power_of_two(14);
-        up_c = power_of_two(a.weight_peak ? raise_of(peak_of(a.weight_peak, kPeakGroups), 0) : 14);
-    }
     if (a.db_part) {
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s += tile[lane][16 * wave + i] * weight[16 * wave + i];
         sums[wave][lane] = s;
     }
-    if (a.rows)
-        for (int q = threadIdx.x; q < 64 * kPieces; q += 256) {
-            const int r = q / kPieces, p = q % kPieces;
-            const long at = (long)blockIdx.y * (kPieces * 16) + 16 * p;
-            if (n0 + r >= a.N || at >= a.row_bytes) continue;
-            *reinterpret_cast<v4f*>(a.rows + (long)(n0 + r) * a.row_bytes + at) = piece_of<HALVES>(p, [&](int i) { return tile[i][r] * up_r; });
-        }
-    if (a.cols)
+    if (a.out)
         for (int q = threadIdx.x; q < 64 * kPieces; q += 256) {
             const int c = q / kPieces, p = q % kPieces;
             const long at = (long)blockIdx.x * (kPieces * 16) + 16 * p;
-            if (v0 + c >= a.classes || at >= a.col_bytes) continue;
-            *reinterpret_cast<v4f*>(a.cols + (long)(v0 + c) * a.col_bytes + at) = piece_of<HALVES>(p, [&](int i) { return tile[c][i] * weight[i] * up_c; });
+            if (v0 + c >= a.classes || at >= a.out_bytes) continue;
+            *reinterpret_cast<v4f*>(a.out + (long)(v0 + c) * a.out_bytes + at) = piece_of<HALVES>(p, [&](int i) { return HALVES ? tile[c][i] * 0x1p14f : tile[c][i]; });
         }
     if (a.db_part) {
         __syncthreads();
@@ -342,6 +338,7 @@ struct SumArgs {
     const unsigned *a_peak, *b_peak;       // as in ProductArgs
     int a_up, b_up, halves;
     const float* row_scale;
+    int row_mask;
     void* out;
     int out_bf16;
 };
@@ -358,7 +355,8 @@ __global__ __launch_bounds__(256) void rows_sum_kernel(SumArgs a)
         double s = 0.0;
         for (int i = 0; i < a.splits; ++i) s += (double)a.part[i * all + e];
         const long m = e / a.N, n = e - m * a.N;
-        const float scale = a.row_scale ? a.row_scale[m] : 1.f;
+        float scale = a.row_scale ? a.row_scale[m] : 1.f;
+        scale = a.row_mask && scale != 0.f ? 1.f : scale;
         const float v = scale == 0.f ? 0.f : (float)s * f.first * f.second * scale;
         if (a.out_bf16) ((bf16*)a.out)[m * a.out_row + n] = (bf16)v;
         else ((float*)a.out)[m * a.out_row + n] = v;

@@ -1,5 +1,5 @@
-// The matrix product of the class layer on rows of features (class_rows.hip): C[m][n] = sum_k A[m][k] B[n][k], both operands with k
-// running fastest, 16-bit numbers on v_mfma_f32_32x32x16, sums in fp32.
+// The matrix product of the class layer on rows of features (class_rows.hip): C[m][n] = sum_k A[m][k] B[n][k], 16-bit numbers on
+// v_mfma_f32_32x32x16, sums in fp32; both operands with k running fastest, or (ACROSS) both with k as the rows of memory, A[k][m], B[k][n].
 //
 // Operands.  bf16 storage: as they are.  fp32 storage: two fp16 parts per number (x 2^e = h + l, ranges.hpp), which lie in turn,
 // 32 numbers' first parts and their second parts, so that one 128-byte block of a row is 64 bf16 numbers or 32 fp32 ones and the kernel's
@@ -10,6 +10,11 @@
 // blocks come from memory straight into the LDS buffer that is not being multiplied (128 bits per lane, a barrier per block).  An LDS row is a
 // block (128 bytes); its 16-byte pieces lie permuted by half the row's number (two rows are the 256 bytes of the banks), so that the lanes of an
 // operand's fetch, which read one piece each of 32 rows, find them on different banks.  The permutation is made by the addresses in memory that the lanes fetch from.
+//
+// ACROSS: a block is 64 k's (32 of fp32 storage) of the tile's columns, an LDS row a k's 512 bytes (for 128 columns 256, of fp32 storage twice
+// that).  The instruction wants 8 k's of one column per lane: ds_read_b64_tr_b16 turns 4 k's x 16 columns around within 16 lanes (lane r names
+// 4 columns, r % 4, of k r / 4 and receives column r at all 4), so two of them are an operand.  The 4 k's 64 bytes, which 32 lanes fetch
+// together, lie permuted by k (64-byte groups), on different banks.  Rows of k beyond the last come as zeros (the descriptor's bound).
 //
 // Results: the classes' scores with their bias (m = class, n = row), of which only each row's largest and sum of exponentials over the
 // tile's classes leave the kernel (and the score of its label), or which are stored too; or products, stored rounded; or partial sums.
@@ -30,6 +35,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 struct ProductArgs {
     const char *A, *B;                     // rows of blocks
     long a_row, b_row;                     // bytes
+    long a_bytes, b_bytes;                 // ACROSS: of the operands in all
     int M, N;
     int blocks, per_split;                 // along k: in all, of a workgroup
     int tiles_m, tiles_n, splits;
@@ -46,7 +52,8 @@ struct ProductArgs {
     // products
     void* out;                             // [M][out_row]
     long out_row;
-    const float* row_scale;                // [M], or null
+    const float* row_scale;                // [M], or null (0: nothing of the row, whatever it is multiplied with)
+    int row_mask;                          // only that
     float* part;                           // [splits][M][N]: partial sums instead (added to what is there: add)
     int add;
 };
@@ -57,7 +64,45 @@ __device__ __forceinline__ int raised_by(const unsigned* peak, int words, int up
     return peak ? raise_of(peak_of(peak, words), 0) : up;
 }
 
-template <int WM, int WN, int MT, int NT, bool HALVES, int RESULT>
+// ACROSS: operands x and y of one step of the instruction, A's from the LDS addresses pa + KA and KA + JA on, B's likewise.  (The builtin for this
+// instruction waits for all fetches into LDS, also those into the other buffer: 1144 us against 958 for a product of 8192 x 4096 x 16000.)
+template <int KA, int JA, int KB, int JB>
+__device__ __forceinline__ void read_turned(v4f (&x)[4], v4f (&y)[2], const unsigned (&pa)[4], const unsigned (&pb)[2])
+{
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    v2f a0, a1, b0, b1, c0, c1, d0, d1, e0, e1, f0, f1;
+    asm volatile("ds_read_b64_tr_b16 %0, %12 offset:%18\n\tds_read_b64_tr_b16 %1, %12 offset:%19\n\t"
+                 "ds_read_b64_tr_b16 %2, %13 offset:%18\n\tds_read_b64_tr_b16 %3, %13 offset:%19\n\t"
+                 "ds_read_b64_tr_b16 %4, %14 offset:%18\n\tds_read_b64_tr_b16 %5, %14 offset:%19\n\t"
+                 "ds_read_b64_tr_b16 %6, %15 offset:%18\n\tds_read_b64_tr_b16 %7, %15 offset:%19\n\t"
+                 "ds_read_b64_tr_b16 %8, %16 offset:%20\n\tds_read_b64_tr_b16 %9, %16 offset:%21\n\t"
+                 "ds_read_b64_tr_b16 %10, %17 offset:%20\n\tds_read_b64_tr_b16 %11, %17 offset:%21\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(a0), "=&v"(a1), "=&v"(b0), "=&v"(b1), "=&v"(c0), "=&v"(c1), "=&v"(d0), "=&v"(d1), "=&v"(e0), "=&v"(e1), "=&v"(f0), "=&v"(f1)
+                 : "v"(pa[0]), "v"(pa[1]), "v"(pa[2]), "v"(pa[3]), "v"(pb[0]), "v"(pb[1]), "n"(KA), "n"(KA + JA), "n"(KB), "n"(KB + JB)
+                 : "memory");
+    x[0] = v4f{a0[0], a0[1], a1[0], a1[1]}; x[1] = v4f{b0[0], b0[1], b1[0], b1[1]};
+    x[2] = v4f{c0[0], c0[1], c1[0], c1[1]}; x[3] = v4f{d0[0], d0[1], d1[0], d1[1]};
+    y[0] = v4f{e0[0], e0[1], e1[0], e1[1]}; y[1] = v4f{f0[0], f0[1], f1[0], f1[1]};
+}
+template <int KA, int JA, int KB, int JB>
+__device__ __forceinline__ void read_turned(v4f (&x)[2], v4f (&y)[2], const unsigned (&pa)[2], const unsigned (&pb)[2])
+{
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    v2f a0, a1, b0, b1, e0, e1, f0, f1;
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %4, %10 offset:%14\n\tds_read_b64_tr_b16 %5, %10 offset:%15\n\t"
+                 "ds_read_b64_tr_b16 %6, %11 offset:%14\n\tds_read_b64_tr_b16 %7, %11 offset:%15\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(a0), "=&v"(a1), "=&v"(b0), "=&v"(b1), "=&v"(e0), "=&v"(e1), "=&v"(f0), "=&v"(f1)
+                 : "v"(pa[0]), "v"(pa[1]), "v"(pb[0]), "v"(pb[1]), "n"(KA), "n"(KA + JA), "n"(KB), "n"(KB + JB)
+                 : "memory");
+    x[0] = v4f{a0[0], a0[1], a1[0], a1[1]}; x[1] = v4f{b0[0], b0[1], b1[0], b1[1]};
+    y[0] = v4f{e0[0], e0[1], e1[0], e1[1]}; y[1] = v4f{f0[0], f0[1], f1[0], f1[1]};
+}
+
+template <int WM, int WN, int MT, int NT, bool HALVES, int RESULT, bool ACROSS>
 __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductArgs a)
 {
     constexpr int BM = 32 * WM * MT, BN = 32 * WN * NT, kWaves = WM * WN;
@@ -80,8 +125,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
     const int tn = in / deep, tm = 8 * group + in - tn * deep;
     const int m0 = tm * BM, n0 = tn * BN;
 
-    // ---- fetches: rows 8 q .. 8 q + 7 of a block, lane l the piece l % 8 of row 8 q + l / 8 as it lies in LDS
+    // ---- fetches: rows 8 q .. 8 q + 7 of a block, lane l the piece l % 8 of row 8 q + l / 8 as it lies in LDS; ACROSS: as many bytes of its rows of k
     typedef __attribute__((address_space(3))) void* lds_ptr;
+    constexpr int kSize = HALVES ? 4 : 2, kRows = 64 * 2 / kSize, kARow = BM * kSize, kBRow = BN * kSize;   // ACROSS: bytes of a number, k's of a block, an LDS row
     const int first = split * a.per_split;
     const int count = a.blocks - first < a.per_split ? a.blocks - first : a.per_split;
     const __amdgpu_buffer_rsrc_t ra =
@@ -92,22 +138,49 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
     unsigned va[AI], vb[BI];
 #pragma unroll
     for (int i = 0; i < AI; ++i) {
-        const int r = 8 * (wave * AI + i) + (lane >> 3), left = a.M - 1 - m0;
-        va[i] = (unsigned)(r < left ? r : left) * (unsigned)a.a_row + piece[i & 1];
+        if constexpr (ACROSS) {
+            const unsigned at = (unsigned)((wave * AI + i) * 1024 + 16 * lane), k = at / kARow;
+            va[i] = k * (unsigned)a.a_row + 16u * ((at % kARow / 16) ^ 4 * (k & 3));
+        } else {
+            const int r = 8 * (wave * AI + i) + (lane >> 3), left = a.M - 1 - m0;
+            va[i] = (unsigned)(r < left ? r : left) * (unsigned)a.a_row + piece[i & 1];
+        }
     }
 #pragma unroll
     for (int i = 0; i < BI; ++i) {
-        const int r = 8 * (wave * BI + i) + (lane >> 3), left = a.N - 1 - n0;
-        vb[i] = (unsigned)(r < left ? r : left) * (unsigned)a.b_row + piece[i & 1];
+        if constexpr (ACROSS) {
+            const unsigned at = (unsigned)((wave * BI + i) * 1024 + 16 * lane), k = at / kBRow;
+            vb[i] = k * (unsigned)a.b_row + 16u * ((at % kBRow / 16) ^ 4 * (k & 3));
+        } else {
+            const int r = 8 * (wave * BI + i) + (lane >> 3), left = a.N - 1 - n0;
+            vb[i] = (unsigned)(r < left ? r : left) * (unsigned)a.b_row + piece[i & 1];
+        }
     }
+    // ACROSS: an operand from a block's first k on (the bound does not see a scalar offset, so each block has a descriptor of its own)
+    auto from = [&](const char* operand, long bytes, long offset) {
+        const long left = bytes - offset;
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(operand + (left > 0 ? offset : 0)), 0,
+                                                 left <= 0 ? 0 : left < 0x7fffffff ? (int)left : 0x7fffffff, 0x00020000);
+    };
     auto fetch = [&](int block, char* stage) {
+        if constexpr (ACROSS) {
+            const __amdgpu_buffer_rsrc_t pa = from(a.A, a.a_bytes, (long)(first + block) * kRows * a.a_row + (long)m0 * kSize);
+            const __amdgpu_buffer_rsrc_t pb = from(a.B, a.b_bytes, (long)(first + block) * kRows * a.b_row + (long)n0 * kSize);
 #pragma unroll
-        for (int i = 0; i < AI; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(stage + (wave * AI + i) * 1024), 16, (int)va[i], block * kBlockBytes, 0, 0);
+            for (int i = 0; i < AI; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(pa, (lds_ptr)(stage + (wave * AI + i) * 1024), 16, (int)va[i], 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < BI; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(stage + BM * kBlockBytes + (wave * BI + i) * 1024), 16, (int)vb[i],
-                                                     block * kBlockBytes, 0, 0);
+            for (int i = 0; i < BI; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(pb, (lds_ptr)(stage + BM * kBlockBytes + (wave * BI + i) * 1024), 16, (int)vb[i], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < AI; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(stage + (wave * AI + i) * 1024), 16, (int)va[i], block * kBlockBytes, 0, 0);
+#pragma unroll
+            for (int i = 0; i < BI; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(stage + BM * kBlockBytes + (wave * BI + i) * 1024), 16, (int)vb[i],
+                                                         block * kBlockBytes, 0, 0);
+        }
     };
 
     v16f acc[MT][NT];
@@ -121,8 +194,17 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
     // an operand's 16 k's, piece pair s of the block: lane l feeds row l % 32, k's 8 (l / 32) ..
     const int row = lane & 31, half = lane >> 5;
     const int at_a = (32 * MT * wm + row) * kBlockBytes, at_b = (BM + 32 * NT * wn + row) * kBlockBytes, mix = row >> 1 & 7;
+    // ACROSS: lane l names 4 columns of k 8 (l / 32) + (l % 16) / 4 of the step's 16, and of the k 4 on
+    const int turn = (lane & 15) >> 2, of_row = 8 * half + turn, of_col = 32 * (lane >> 4 & 1) + 8 * (lane & 3);
+    int group_a[MT], group_b[NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) group_a[i] = of_row * kARow + of_col + 64 * ((MT * wm + i) * (HALVES ? 2 : 1) ^ turn);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) group_b[j] = BM * kBlockBytes + of_row * kBRow + of_col + 64 * ((NT * wn + j) * (HALVES ? 2 : 1) ^ turn);
     auto multiply = [&](const char* stage) {
         auto read = [&](int at, int s) { return *reinterpret_cast<const v4f*>(stage + at + 16 * ((2 * s + half) ^ mix)); };
+        auto read_a = [&](int i, int s) { return read(at_a + i * 32 * kBlockBytes, s); };
+        auto read_b = [&](int j, int s) { return read(at_b + j * 32 * kBlockBytes, s); };
         auto product = [&](v4f (&x)[MT], v4f (&y)[NT]) {
             __builtin_amdgcn_s_setprio(1);     // (before the other wave's fetches and reads)
 #pragma unroll
@@ -135,14 +217,46 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
                         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[i]), __builtin_bit_cast(bf16x8, y[j]), acc[i][j], 0, 0, 0);
             __builtin_amdgcn_s_setprio(0);
         };
-        // a step's operands are read while the one before it is multiplied
-        if constexpr (HALVES) {
+        if constexpr (ACROSS) {
+            // the second parts' 64 bytes are the group beside the first parts': the other one of a pair, whatever the permutation
+            const unsigned base = (unsigned)(uintptr_t)(lds_ptr)stage;
+            unsigned pa[MT], pb[NT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) pa[i] = base + group_a[i];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) pb[j] = base + group_b[j];
+            auto step = [&](auto at) {
+                constexpr int kA = 16 * decltype(at)::value * kARow, kB = 16 * decltype(at)::value * kBRow;
+                v4f x[MT], y[NT];
+                read_turned<kA, 4 * kARow, kB, 4 * kBRow>(x, y, pa, pb);
+                if constexpr (HALVES) {
+                    v4f xl[MT], yl[NT];
+                    unsigned la[MT], lb[NT];
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) la[i] = pa[i] ^ 64;
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) lb[j] = pb[j] ^ 64;
+                    product(x, y);
+                    read_turned<kA, 4 * kARow, kB, 4 * kBRow>(xl, yl, la, lb);
+                    product(xl, y);
+                    product(x, yl);
+                } else {
+                    product(x, y);
+                }
+            };
+            step(std::integral_constant<int, 0>{});
+            step(std::integral_constant<int, 1>{});
+            if constexpr (!HALVES) {
+                step(std::integral_constant<int, 2>{});
+                step(std::integral_constant<int, 3>{});
+            }
+        } else if constexpr (HALVES) {   // a step's operands are read while the one before it is multiplied
             v4f xh[2][MT], yh[2][NT], xl[2][MT], yl[2][NT];
             auto load = [&](int t, int s) {
 #pragma unroll
-                for (int i = 0; i < MT; ++i) { xl[t][i] = read(at_a + i * 32 * kBlockBytes, s + 2); xh[t][i] = read(at_a + i * 32 * kBlockBytes, s); }
+                for (int i = 0; i < MT; ++i) { xl[t][i] = read_a(i, s + 2); xh[t][i] = read_a(i, s); }
 #pragma unroll
-                for (int j = 0; j < NT; ++j) { yh[t][j] = read(at_b + j * 32 * kBlockBytes, s); yl[t][j] = read(at_b + j * 32 * kBlockBytes, s + 2); }
+                for (int j = 0; j < NT; ++j) { yh[t][j] = read_b(j, s); yl[t][j] = read_b(j, s + 2); }
             };
             load(0, 0);
 #pragma unroll
@@ -156,9 +270,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
             v4f x[2][MT], y[2][NT];
             auto load = [&](int t, int s) {
 #pragma unroll
-                for (int i = 0; i < MT; ++i) x[t][i] = read(at_a + i * 32 * kBlockBytes, s);
+                for (int i = 0; i < MT; ++i) x[t][i] = read_a(i, s);
 #pragma unroll
-                for (int j = 0; j < NT; ++j) y[t][j] = read(at_b + j * 32 * kBlockBytes, s);
+                for (int j = 0; j < NT; ++j) y[t][j] = read_b(j, s);
             };
             load(0, 0);
 #pragma unroll
@@ -288,7 +402,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
                             if (z < left) p[z] = a.add ? p[z] + v[z] : v[z];
                     }
                 } else {
-                    const float scale = a.row_scale ? a.row_scale[m] : 1.f;   // (0: nothing of the row, whatever it is multiplied with)
+                    float scale = a.row_scale ? a.row_scale[m] : 1.f;
+                    scale = a.row_mask && scale != 0.f ? 1.f : scale;
 #pragma unroll
                     for (int z = 0; z < 8; ++z) {
                         if constexpr (HALVES) v[z] = v[z] * f.first * f.second;
