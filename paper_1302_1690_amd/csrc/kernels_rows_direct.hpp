@@ -277,7 +277,10 @@ __global__ __launch_bounds__(256) void rows_direct_delta_kernel(DirectArgs a)
                 share += (double)loss;
             }
         }
-        if (!a.delta) continue;                          // (the loss alone; nobody reads `red` before its next barrier but this wave's lanes)
+        if (!a.delta) {                                  // the loss alone
+            __syncthreads();                             // (`red` has been read)
+            continue;
+        }
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             const int v = v0 + wave + 4 * k;

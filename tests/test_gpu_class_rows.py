@@ -230,6 +230,13 @@ def test_very_many_classes():
     _check(x, w, bias, labels, roww, "many")
 
 
+@pytest.mark.parametrize("dtype", [F, B], ids=["f32", "bf16"])
+def test_very_many_rows(dtype):
+    """So many rows that a workgroup takes several tiles of them, up to the most that there may be."""
+    for rows in (300001, 1 << 20):
+        _check(*_inputs(rows, 5, 6, dtype, 6), "rows")
+
+
 def test_no_rows():
     w, bias = torch.randn(50, 8, device="cuda"), torch.randn(50, device="cuda")
     x, labels = torch.empty(0, 8, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
