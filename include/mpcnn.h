@@ -256,7 +256,8 @@ mpcnn_status mpcnn_sgd_step(mpcnn_net* net, float lr, float grad_scale, void* hi
  * parameter), c = min(1, max_norm / norm), theta -= lr * grad_scale * c * g.  max_norm > 0, infinity for
  * no bound.  norm_dev: one fp64 on the device that receives norm (before the bound), or NULL.  A norm
  * that is not finite leaves the parameters as they are.  Squares and sums are fp64, in a fixed order.
- * Errors: EINVAL (also: lr or grad_scale not finite, max_norm not above zero), EHIP.
+ * Errors: EINVAL (also: lr, grad_scale or, as an fp32 number, their product not finite, max_norm not above
+ * zero, norm_dev no multiple of 8), EHIP.
  */
 mpcnn_status mpcnn_sgd_step_clipped(mpcnn_net* net, double lr, double grad_scale, double max_norm, double* norm_dev,
                                     void* hip_stream);

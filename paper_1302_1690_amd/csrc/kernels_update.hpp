@@ -152,10 +152,10 @@ __global__ __launch_bounds__(LONE ? 1024 : 256) void update_kernel(UpdateArgs a)
     if (!(norm < __builtin_inf())) return;                   // (NaN too)
     const double c = norm > a.bound ? a.bound / norm : 1.0;
     if (MODE == kClip && c == 1.0) return;
-    const float f = MODE == kClip ? (float)c : (float)(c * (double)a.rate);   // one rounding; the product with a gradient is the next
+    const float f = MODE == kClip ? (float)c : (float)(c * a.rate);   // one rounding; the product with a gradient is the next
     const int first = (int)blockIdx.x * WAVES + wave, by = (int)gridDim.x * WAVES;
     for (int i = first; i < a.stretches; i += by) {
-        const Stretch t = stretch_at(a, a.back ? a.stretches - 1 - i : i);
+        const Stretch t = stretch_at(a, i);
         if constexpr (MODE == kClip) {
             if (t.grad_bf16) scale_down((bf16*)t.grad, t.n, lane, f);
             else scale_down((float*)t.grad, t.n, lane, f);

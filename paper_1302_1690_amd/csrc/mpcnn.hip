@@ -2597,7 +2597,8 @@ mpcnn_status mpcnn_sgd_step_clipped(mpcnn_net* net, double lr, double grad_scale
 {
     if (!net) return fail(MPCNN_EINVAL, "null net");
     if (!net->d_params) return fail(MPCNN_EINVAL, "parameters were never set");
-    if (!std::isfinite(lr) || !std::isfinite(grad_scale)) return fail(MPCNN_EINVAL, "scale %g, rate %g", grad_scale, lr);
+    if ((uintptr_t)norm_dev % sizeof(double)) return fail(MPCNN_EINVAL, "norm's address is no multiple of its size");
+    if (!mpcnn::rate_fits(lr, grad_scale)) return fail(MPCNN_EINVAL, "scale %g, rate %g", grad_scale, lr);
     if (!(max_norm > 0.0)) return fail(MPCNN_EINVAL, "max_norm = %g", max_norm);
     const long n = (long)net->n_params;
     hipStream_t st = (hipStream_t)hip_stream;
@@ -2607,7 +2608,7 @@ mpcnn_status mpcnn_sgd_step_clipped(mpcnn_net* net, double lr, double grad_scale
     a.stretches = (int)((n + a.flat_len - 1) / a.flat_len);
     a.partial = (double*)((char*)net->d_grads + align_up(sizeof(float) * net->n_params));
     a.norm = norm_dev;
-    a.scale = std::fabs(grad_scale); a.bound = max_norm; a.rate = (float)(lr * grad_scale);
+    a.scale = std::fabs(grad_scale); a.bound = max_norm; a.rate = lr * grad_scale;
     LAUNCH("sgd_clipped", -1, 8, 4.0 * n, 16.0 * n, mpcnn::launch_update(a, mpcnn::kStep, n, nullptr, 0, st));
     HIP_TRY(hipGetLastError());
     net->packs_stale = true; net->wread_stale = true;

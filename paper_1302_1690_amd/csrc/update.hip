@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <limits>
 #include <memory>
 #include <new>
 #include <vector>
@@ -22,6 +23,11 @@ struct mpcnn_grad_list {
 };
 
 namespace mpcnn {
+
+bool rate_fits(double rate, double scale)
+{
+    return std::isfinite(scale) && std::isfinite(rate) && std::fabs(rate * scale) <= (double)std::numeric_limits<float>::max();
+}
 
 unsigned stretch_length(long total)
 {
@@ -100,6 +106,7 @@ mpcnn_status make_list(const mpcnn_tensor* t, int count, mpcnn_grad_list** out)
             return fail(MPCNN_EINVAL, "tensor %d: address is no multiple of its element's size", i);
         ++filled;
         total += t[i].n;
+        if (total > (int64_t)1 << 40) return fail(MPCNN_EINVAL, "too many numbers: over 2^40");
         ranges.push_back({(uintptr_t)t[i].grad_dev, (uint64_t)t[i].n * gs, false});
         if (t[i].param_dev) {
             ++with;
@@ -128,7 +135,7 @@ mpcnn_status make_list(const mpcnn_tensor* t, int count, mpcnn_grad_list** out)
         }
     }
     if (same) starts.push_back((int)table.size());
-    if (table.size() > (size_t)1 << 30) return fail(MPCNN_EINVAL, "too many numbers: %lld", (long long)total);
+    if (table.size() > (size_t)1 << 30) return fail(MPCNN_EINVAL, "too many tensors: %d", count);
     std::unique_ptr<mpcnn_grad_list> l(new mpcnn_grad_list);
     l->starts = std::move(starts);
     l->total = (long)total;
@@ -154,7 +161,8 @@ mpcnn_status update(const mpcnn_grad_list* l, int mode, double rate, double scal
 {
     if (!l) return fail(MPCNN_EINVAL, "null list");
     if (mode == mpcnn::kOnlyNorm && !norm) return fail(MPCNN_EINVAL, "null argument");
-    if (!std::isfinite(scale) || !std::isfinite(rate)) return fail(MPCNN_EINVAL, "scale %g, rate %g", scale, rate);
+    if ((uintptr_t)norm % sizeof(double)) return fail(MPCNN_EINVAL, "norm's address is no multiple of its size");
+    if (!mpcnn::rate_fits(rate, scale)) return fail(MPCNN_EINVAL, "scale %g, rate %g", scale, rate);
     if (!(bound > 0.0)) return fail(MPCNN_EINVAL, "max_norm = %g", bound);
     if (mode == mpcnn::kStep && l->stretches && !l->params) return fail(MPCNN_EINVAL, "the list has no parameters");
     int dev = -1;
@@ -167,7 +175,7 @@ mpcnn_status update(const mpcnn_grad_list* l, int mode, double rate, double scal
     a.norm = norm;
     a.scale = std::fabs(scale);
     a.bound = bound;
-    a.rate = (float)(rate * scale);
+    a.rate = rate * scale;
     mpcnn::launch_update(a, mode, l->total, l->starts.data(), l->starts.empty() ? 0 : (int)l->starts.size() - 1, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
     return MPCNN_OK;

@@ -25,12 +25,12 @@ struct UpdateArgs {
     double* partial;        // [parts]
     double* norm;           // result, or null
     double scale, bound;    // |s|, largest norm
-    float rate;             // signed: rate * s
-    int back;               // stretches from the list's end on: what the norm's pass read last comes first
+    double rate;            // signed: rate * s
 };
 enum { kOnlyNorm = 0, kClip = 1, kStep = 2 };
 
-
+// Whether a step can be taken with these numbers: each finite, and so the product, as an fp32 number too
+bool rate_fits(double rate, double scale);
 // Stretch length for so many numbers in all: enough stretches for every wave that can run, none shorter than one fetch
 unsigned stretch_length(long total);
 // mode: kOnlyNorm, kClip, kStep; fills in a.parts.  `total`: numbers in all.  Tensors that share memory are updated one after the other, in the

@@ -212,6 +212,20 @@ def test_recorded_into_a_graph():
         assert norm.item() == e_norm.item()
 
 
+def test_a_tensor_of_more_than_2_to_the_32_numbers():
+    n = (1 << 32) + 5
+    g, p = (torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    g[0], g[n - 1] = 3.0, 4.0
+    l = mpcnn.GradList([g], [p])
+    assert l.norm().item() == 5.0
+    l.sgd_step(1.0, max_norm=2.5)
+    assert p[0].item() == -1.5 and p[n - 1].item() == -2.0 and int(torch.count_nonzero(p)) == 2
+    l.clip(1.25)
+    assert g[0].item() == 0.75 and g[n - 1].item() == 1.0 and int(torch.count_nonzero(g)) == 2
+    del l, g, p
+    torch.cuda.empty_cache()
+
+
 def test_on_another_stream():
     s = torch.cuda.Stream()
     g = torch.randn(300000, device="cuda")
@@ -238,3 +252,13 @@ def test_refusals():
         with pytest.raises(mpcnn.MpcnnError) as e:
             call()
         assert e.value.status == 1
+    kept = a.clone()
+    step = mpcnn.GradList([a], [kept])
+    norm = torch.zeros(2, dtype=torch.float64, device="cuda")
+    shifted = norm.view(torch.uint8)[4:12]
+    for call in (lambda: step.sgd_step(1e30, grad_scale=1e30), lambda: step.sgd_step(1e300, grad_scale=1e300), lambda: step.sgd_step(1e39),
+                 lambda: mpcnn._check(mpcnn.lib().mpcnn_grad_norm(l._h, 1.0, shifted.data_ptr(), None))):
+        with pytest.raises(mpcnn.MpcnnError) as e:
+            call()
+        assert e.value.status == 1
+    assert torch.equal(kept, a) and (norm == 0).all()

@@ -38,6 +38,11 @@ def test_list_refusals(rows, says):
     assert st == EINVAL and says in text, text
 
 
+def test_too_many_numbers():
+    st, text = _create([(BASE, 0, 1 << 40, 0, 0), (8 * BASE, 0, 1 << 40, 0, 0)])
+    assert st == EINVAL and "2^40" in text
+
+
 def test_null_arguments():
     assert _create([], count=2)[0] == EINVAL
     assert _create([], count=-1)[0] == EINVAL
