@@ -333,7 +333,6 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
     }
     if (p.train) {
         a.dx = c.dx; a.dx_pitch = c.dx_pitch; a.dw = c.dw;
-        a.masked = 1;
         a.x_deal = p.gx.deal; a.w_deal = p.gw.deal; a.x_along = p.gx.along; a.w_along = p.gw.along;
         a.x_splits = p.gx.splits; a.x_each = p.gx.each; a.w_splits = p.gw.splits; a.w_each = p.gw.each;
         a.x_groups = c.dx ? p.gx.m * p.gx.along * p.gx.splits : 0;

@@ -48,7 +48,6 @@ struct DirectArgs {
     long dx_pitch;
     void* dw;
     float* db;
-    int masked;                            // some rows may add nothing: their features do not count
     int x_along, w_along;                  // tiles along the features
     int x_splits, x_each, w_splits, w_each;   // parts of the sums over classes and over rows, and their lengths (multiples of kDirectK)
     int x_groups, w_groups;                // workgroups of dx, of dw (0: not asked for)
@@ -417,12 +416,10 @@ __global__ __launch_bounds__(256) void rows_direct_grads_kernel(DirectArgs a)
 #pragma unroll
                 for (int z = 0; z < 8; ++z) q[k][z] = (float)y[8 * k + z];
             }
-            if (a.masked) {                              // rows that add nothing may hold anything
 #pragma unroll
-                for (int z = 0; z < 16; ++z) {
-                    const int n = k0 + s * kDirectK + 16 * (z >> 3) + 8 * half + (z & 7);
-                    if (a.weight[n < K ? n : K - 1] == 0.f) q[z >> 3][z & 7] = 0.f;
-                }
+            for (int z = 0; z < 16; ++z) {               // rows that add nothing may hold anything
+                const int n = k0 + s * kDirectK + 16 * (z >> 3) + 8 * half + (z & 7);
+                if (a.weight[n < K ? n : K - 1] == 0.f) q[z >> 3][z & 7] = 0.f;
             }
             if (s + by < steps) fetch(s + by);
             direct_product<kDeltaParts<T>, kParts<T>>(acc, p[0], q[0]);

@@ -17,6 +17,6 @@ __device__ __forceinline__ float row_weight(const RowMask& m, int n)
     return m.weights ? m.weights[n] : 1.f;
 }
 
-constexpr int kNoLabel = -1;               // in the library's own copy of the labels: a row that adds nothing
+constexpr int kNoLabel = -1;               // in the place of the label of a row that adds nothing
 
 }  // namespace mpcnn
