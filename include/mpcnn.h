@@ -304,7 +304,7 @@ mpcnn_status mpcnn_sgd_step_list(const mpcnn_grad_list* list, double lr, double 
  *   scores s[n][v] = x[n] . w[v] + bias[v],   p = softmax over v,   L = sum over n of w[n] * -log p[n][t[n]]
  * with t = labels, w = roww (1 if roww_dev is NULL); rows with t < 0, t >= classes or w = 0 add nothing,
  * whatever their features hold.  The scores are taken in pieces of the classes and are not kept; where
- * all of them fit the room of a piece (2^27) they are computed once.
+ * all of them fit the room of a piece (2^28) they may be, so that they are computed once.
  *   x_dev      [rows][x_pitch], w_dev [classes][w_pitch], both `dtype`; pitches in elements, at least
  *              `features`.  Any address that is a multiple of its element's size; whole blocks of 64
  *              features at 16-byte aligned rows are read in place with MPCNN_BF16, others copied.

@@ -6,8 +6,9 @@
 //   dx[n] = weight[n] sum_v delta[n][v] w[v],   dw[v] = sum_n weight[n] delta[n][v] x[n],   db[v] = sum_n weight[n] delta[n][v]
 //
 // The classes are taken in pieces.  A first round over them leaves, per row, each tile's largest score and sum of exponentials, and no scores.
-// The second computes a piece's scores again, turns them into the derivative and multiplies that with the weights and the features
-// (kernels_rows_product.hpp).  Where the scores of all classes fit the room that a piece's take (kRoom), they are kept from the first round.
+// The second computes a piece's scores again, as the derivative, which it multiplies with the weights and the features
+// (kernels_rows_product.hpp).  Where the scores of all classes fit the room that a piece's take (kRoom) and are more work than traffic
+// (kKeepFeatures), they are kept from the first round.
 #include <algorithm>
 #include <atomic>
 #include <cstdint>
@@ -23,7 +24,12 @@ using mpcnn::fail;
 namespace {
 
 constexpr int64_t kMaxRows = 1 << 20, kMaxFeatures = 1 << 20, kMaxClasses = 0x7fffffff - 1024;   // (32-bit offsets inside a tile)
-constexpr int64_t kRoom = (int64_t)1 << 27;            // scores of a piece: 0.5 GB in fp32, and half as much of derivatives (as much with fp32 storage)
+constexpr int64_t kRoom = (int64_t)1 << 28;            // derivatives of a piece: 0.5 GB (1 GB with fp32 storage), and scores that are kept: 1 GB
+// Scores that fit are kept where computing them again takes longer than their way to memory and back: with so many features and more, fp32 and
+// bf16.  us, kept / computed again: 8000 x 8000 with 64 features 375 / 349 and 267 / 219, with 128 405 / 410 and 290 / 242, with 256
+// 536 / 564 and 335 / 301, with 512 770 / 874 and 423 / 433, with 1024 1233 / 1467 and 544 / 605; 12000 x 20000 with 256 1676 / 1737 and 996 / 915,
+// with 1024 4351 / 5288 and 2077 / 2284; 4000 x 4000 with 64 168 / 169 and 132 / 131.
+constexpr int kKeepFeatures[2] = {128, 512};
 constexpr int64_t kWeightRoom = (int64_t)512 << 20;    // bytes of a piece's class weights, brought into blocks
 constexpr int64_t kPartRoom = (int64_t)256 << 20;      // bytes of a product's partial sums
 constexpr int kMaxPiece = 1 << 20;
@@ -101,9 +107,10 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     p->n_bytes = p->bytes_along(p->Np);
     size_t at = 0;
     auto take = [&](int64_t bytes) { const size_t o = at; at += (size_t)up_to(bytes, 256); return o; };
-    p->keep = train && classes <= kRoom / p->Np;
+    const bool fits = classes <= kRoom / p->Np;
+    p->keep = train && fits && features >= kKeepFeatures[p->halves ? 0 : 1];
     const int64_t most = rows <= kDirectFewRows ? kDirectFewWork[p->halves ? 0 : 1] : train ? kDirectWork : kDirectLossWork;
-    p->direct = (rows <= mpcnn::kFewRows || rows * classes <= most / features) && (p->keep || !train);
+    p->direct = (rows <= mpcnn::kFewRows || rows * classes <= most / features) && (fits || !train);
     // few rows and many classes: the gradients, and the scores of still fewer, on the vector ALU (kernels_rows_few.hpp has the times)
     p->few = p->direct && train && rows > 0 && rows <= mpcnn::kFewRows && classes >= (rows <= 4 ? 1024 : 4096);
     if (p->direct && rows > 0) {
@@ -182,7 +189,7 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
         p->dx = tiling_of(N, D, p->v_blocks(piece), std::min<int64_t>(64, std::max<int64_t>(1, kPartRoom / (4 * N * D + 1))), p->halves);
         p->dw = tiling_of(piece, D, p->n_bytes / mpcnn::kBlockBytes, std::min<int64_t>(64, std::max<int64_t>(1, kPartRoom / (4 * piece * D))), p->halves);
         p->x_cols = take(D * p->n_bytes);
-        p->score = take((p->keep ? classes : piece) * p->Np * 4);
+        if (p->keep) p->score = take(classes * p->Np * 4);
         p->delta = take(piece * p->n_bytes);
         p->db_part = take(p->Np / 64 * piece * 4);
         if (p->dx_parts()) p->dx_part = take(4 * (int64_t)p->dx.splits * N * D);
@@ -389,21 +396,20 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
     if (!x_direct || p.train)
         pack(c.x, c.x_pitch, p.N, x_direct ? nullptr : ws + p.x_rows, p.train ? ws + p.x_cols : nullptr, p.n_bytes, mask, x_peak);
 
-    // a piece's scores
+    // a piece's scores, or what becomes of them
     const int64_t piece = !p.train && w_direct ? std::min<int64_t>(p.V, kMaxPiece) : p.piece;
     const int d_blocks = (int)(p.d_bytes / mpcnn::kBlockBytes);
-    auto scores = [&](int64_t v0, int64_t n_classes, const char* w_rows, int64_t w_row, float2* stats, float* out, int* tiles) {
-        mpcnn::ProductArgs a{};
+    int done = 0;                                        // tiles of classes
+    auto scores = [&](int64_t v0, int64_t n_classes, const char* w_rows, int64_t w_row, mpcnn::ProductArgs a, bool delta) {
         a.A = w_rows; a.a_row = w_row;
         a.B = x_direct ? (const char*)c.x : ws + p.x_rows; a.b_row = x_direct ? c.x_pitch * 2 : p.d_bytes;
         a.M = (int)n_classes; a.N = p.N; a.blocks = d_blocks;
         a.a_peak = H ? w_peak : nullptr; a.b_peak = H ? x_peak : nullptr; a.a_words = a.b_words = mpcnn::kPeakGroups;
         a.bias = c.bias ? c.bias + v0 : nullptr;
-        a.labels = c.labels; a.stats = stats; a.label_score = (float*)(ws + p.label_score);
-        a.scores = out; a.score_row = p.Np; a.class0 = (int)v0;
+        a.labels = c.labels; a.class0 = (int)v0;
         const Tiling t = tiling_of(n_classes, p.N, d_blocks, 1, H);
-        if (tiles) *tiles = t.tiles_m;
-        return launch_product<H, mpcnn::kScores>(a, t, st);
+        if (!delta) done += t.tiles_m;
+        return delta ? launch_product<H, mpcnn::kDelta>(a, t, st) : launch_product<H, mpcnn::kScores>(a, t, st);
     };
     // a piece's weights in blocks along the features, where they are not read as they are
     auto weights_of = [&](int64_t v0, int64_t n_classes) {
@@ -412,16 +418,16 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
     auto rows_at = [&](int64_t v0) { return w_direct ? (const char*)c.w + v0 * c.w_pitch * 2 : (const char*)(ws + p.w_rows); };
     const int64_t w_row = w_direct ? c.w_pitch * 2 : p.d_bytes;
 
-    float* const score = p.train ? (float*)(ws + p.score) : nullptr;
+    float* const score = p.keep ? (float*)(ws + p.score) : nullptr;
     const bool one_piece = p.V <= piece;                 // (its weights' blocks are there in the second round)
-    int done = 0;
     for (int64_t v0 = 0; v0 < p.V; v0 += piece) {
         const int64_t n = std::min(piece, p.V - v0);
         weights_of(v0, n);
-        int tiles = 0;
-        const mpcnn_status rc = scores(v0, n, rows_at(v0), w_row, (float2*)(ws + p.stats) + (int64_t)done * p.N, p.keep ? score + v0 * p.Np : nullptr, &tiles);
+        mpcnn::ProductArgs a{};
+        a.stats = (float2*)(ws + p.stats) + (int64_t)done * p.N; a.label_score = (float*)(ws + p.label_score);
+        a.scores = p.keep ? score + v0 * p.Np : nullptr; a.score_row = p.Np;
+        const mpcnn_status rc = scores(v0, n, rows_at(v0), w_row, a, false);
         if (rc != MPCNN_OK) return rc;
-        done += tiles;
     }
     const int join_groups = join_groups_of(p.N, done);
     mpcnn::JoinArgs j{};
@@ -443,18 +449,21 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         const int64_t n = std::min(piece, p.V - v0);
         const bool last = v0 + n == p.V;
         if (!one_piece && (!p.keep || c.dx)) weights_of(v0, n);
-        float* const s = p.keep ? score + v0 * p.Np : score;
-        if (!p.keep) {
-            const mpcnn_status rc = scores(v0, n, rows_at(v0), w_row, nullptr, s, nullptr);
+        char* const delta = c.dx || c.dw ? ws + p.delta : nullptr;
+        float* const db_part = c.db ? (float*)(ws + p.db_part) : nullptr;
+        if (p.keep) {
+            mpcnn::DeltaArgs d{};
+            d.scores = score + v0 * p.Np; d.score_row = p.Np; d.classes = (int)n; d.class0 = (int)v0; d.N = p.N;
+            d.labels = c.labels; d.lse = j.lse; d.weight = j.weight;
+            d.out = delta; d.out_bytes = p.n_bytes; d.db_part = db_part;
+            mpcnn::rows_delta_kernel<H><<<dim3((unsigned)(p.Np / 64), (unsigned)((n + 63) / 64)), 256, 0, st>>>(d);
+        } else {
+            mpcnn::ProductArgs a{};
+            a.lse = j.lse; a.weight = j.weight; a.delta = delta; a.delta_bytes = p.n_bytes; a.padded = (int)p.Np; a.db_part = db_part;
+            const mpcnn_status rc = scores(v0, n, rows_at(v0), w_row, a, true);
             if (rc != MPCNN_OK) return rc;
         }
-        mpcnn::DeltaArgs d{};
-        d.scores = s; d.score_row = p.Np; d.classes = (int)n; d.class0 = (int)v0; d.N = p.N;
-        d.labels = c.labels; d.lse = j.lse; d.weight = j.weight;
-        if (c.dx || c.dw) { d.out = ws + p.delta; d.out_bytes = p.n_bytes; }
-        d.db_part = c.db ? (float*)(ws + p.db_part) : nullptr;
-        mpcnn::rows_delta_kernel<H><<<dim3((unsigned)(p.Np / 64), (unsigned)((n + 63) / 64)), 256, 0, st>>>(d);
-        fin.db_part = d.db_part; fin.tiles = (int)(p.Np / 64); fin.classes = n; fin.db = c.db ? c.db + v0 : nullptr;
+        fin.db_part = db_part; fin.tiles = (int)(p.Np / 64); fin.classes = n; fin.db = c.db ? c.db + v0 : nullptr;
         if (fin.db || fin.loss) mpcnn::rows_finish_kernel<<<fin.db ? (unsigned)((n + 31) / 32) : 1, 256, 0, st>>>(fin);
         fin.loss = nullptr;
         if (c.dx) {

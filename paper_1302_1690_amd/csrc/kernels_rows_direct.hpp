@@ -21,7 +21,6 @@
 namespace mpcnn {
 
 constexpr int kDirectK = 32;
-constexpr float kLog2eHigh = 1.4426950408889634f, kLog2eLow = 1.925963033500212e-08f;   // log2 e in two fp32 numbers
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef __bf16 d_bf16x8 __attribute__((ext_vector_type(8)));
@@ -210,17 +209,6 @@ __global__ __launch_bounds__(256) void rows_direct_scores_kernel(DirectArgs a)
     if (tid < 64 && nt < a.N) a.stats[(long)blockIdx.x * a.N + nt] = direct_join(red[0][tid], red[1][tid]);
 }
 
-// exp(score - lse) - hot; nothing for rows that are not live.  exp by the hardware's exp2, whose argument's rounding is made good: x log2 e = t + r
-// to twice fp32's bits, 2^(t + r) = 2^t (1 + r ln 2) for |r| below a 2^-24th of t.
-__device__ __forceinline__ float direct_delta(float score, float lse, bool live, bool hot)
-{
-    const float x = score == -__builtin_inff() ? -1e30f : score - lse;     // (a class that is switched off, and a row that has no other)
-    const float t = x * kLog2eHigh, r = fmaf(x, kLog2eHigh, -t) + x * kLog2eLow;
-    const float e = __builtin_amdgcn_exp2f(t);
-    const float p = e > 0.f ? fmaf(e, r * 0.6931471805599453f, e) : e;
-    return live ? (hot ? p - 1.f : p) : 0.f;
-}
-
 // 64 classes x `batch` times 64 rows per workgroup: a lane a row, a wave every fourth class
 constexpr int kDeltaSide = 64, kDeltaFewTiles = 32;
 __global__ __launch_bounds__(256) void rows_direct_delta_kernel(DirectArgs a)
@@ -283,7 +271,7 @@ __global__ __launch_bounds__(256) void rows_direct_delta_kernel(DirectArgs a)
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             const int v = v0 + wave + 4 * k;
-            const float g = direct_delta(x[k], lse, label != kNoLabel, label == v) * weight, put = weight != 0.f ? g : 0.f;
+            const float g = class_delta(x[k], lse, label != kNoLabel, label == v) * weight, put = weight != 0.f ? g : 0.f;
             tile[wave + 4 * k][lane] = put;
             if (v < a.V) a.scores[v * a.score_row + n] = put;
         }

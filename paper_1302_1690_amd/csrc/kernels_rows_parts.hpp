@@ -302,8 +302,7 @@ __global__ __launch_bounds__(256) void rows_delta_kernel(DeltaArgs a)
         const int v = v0 + wave + 4 * i;
         float g = 0.f;
         if (v < a.classes && w != 0.f) {
-            g = x[i] == -__builtin_inff() ? 0.f : expf(x[i] - lse);
-            if (v == label) g -= 1.f;
+            g = class_delta(x[i], lse, true, v == label);
             if constexpr (!HALVES) g *= w;
         }
         tile[wave + 4 * i][lane] = g;

@@ -17,12 +17,14 @@
 // together, lie permuted by k (64-byte groups), on different banks.  Rows of k beyond the last come as zeros (the descriptor's bound).
 //
 // Results: the classes' scores with their bias (m = class, n = row), of which only each row's largest and sum of exponentials over the
-// tile's classes leave the kernel (and the score of its label), or which are stored too; or products, stored rounded; or partial sums.
+// tile's classes leave the kernel (and the score of its label), or which are stored too; or the loss's derivative in the place of the scores, as
+// the gradients' products want it; or products, stored rounded; or partial sums.
 #pragma once
 #include <type_traits>
 
 #include "any_address.hpp"
 #include "ranges.hpp"
+#include "rows_mask.hpp"
 
 namespace mpcnn {
 
@@ -49,6 +51,12 @@ struct ProductArgs {
     float* scores;                         // [M][score_row], or null
     long score_row;
     int class0;                            // the first class of A
+    // derivative
+    const float *lse, *weight;             // [N]
+    char* delta;                           // [M][delta_bytes] blocks along the rows, or null
+    long delta_bytes;
+    int padded;                            // rows, with those of the last block of 64
+    float* db_part;                        // [padded / 64][M]: sums over 64 rows, or null
     // products
     void* out;                             // [M][out_row]
     long out_row;
@@ -57,7 +65,7 @@ struct ProductArgs {
     float* part;                           // [splits][M][N]: partial sums instead (added to what is there: add)
     int add;
 };
-enum { kScores = 0, kStoreF32 = 1, kStoreBf16 = 2, kPart = 3 };
+enum { kScores = 0, kStoreF32 = 1, kStoreBf16 = 2, kPart = 3, kDelta = 4 };
 
 __device__ __forceinline__ int raised_by(const unsigned* peak, int words, int up)
 {
@@ -364,6 +372,73 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
                 s = float2{top, s.y * __builtin_amdgcn_exp2f((s.x - base) * kLog2e) + o.y * __builtin_amdgcn_exp2f((o.x - base) * kLog2e)};
             }
             a.stats[(long)tm * a.N + n0 + i] = s;
+        }
+    } else if constexpr (RESULT == kDelta) {
+        // By way of LDS as below: a lane has 8 rows of a class
+        constexpr int W = 32 * NT, kPitch = W + 4;
+        static_assert(W == 64 && (kWaves * 32 * kPitch + BM) * 4 <= 2 * kStage, "a wave's columns are a sum's 64 rows; the ring holds them");
+        float* const mine = reinterpret_cast<float*>(lds_raw) + wave * 32 * kPitch;
+        float* const bias_l = reinterpret_cast<float*>(lds_raw) + kWaves * 32 * kPitch;
+        __syncthreads();
+        for (int i = tid; i < BM; i += 64 * kWaves) bias_l[i] = a.bias && m0 + i < a.M ? a.bias[m0 + i] : 0.f;
+        const int nw = n0 + W * wn, c = 8 * (lane & 7), n = nw + c;
+        float lse[8], weight[8];
+        int label[8];
+#pragma unroll
+        for (int z = 0; z < 8; ++z) {
+            const int at = n + z < a.N ? n + z : a.N - 1;
+            const float w = a.weight[at];
+            lse[z] = a.lse[at];
+            weight[z] = n + z < a.N ? w : 0.f;
+            label[z] = a.labels[at] - a.class0;
+        }
+        __syncthreads();
+        if (nw >= a.padded) return;                          // (a wave's own places in LDS from here on)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mine[(8 * (r >> 2) + 4 * half + (r & 3)) * kPitch + 32 * j + row] = acc[i][j][r];
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int of = 8 * q + (lane >> 3), at = 32 * (MT * wm + i) + of, m = m0 + at;
+                const v4f lo = *reinterpret_cast<const v4f*>(mine + of * kPitch + c), hi = *reinterpret_cast<const v4f*>(mine + of * kPitch + c + 4);
+                v8f v{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                const float bias = bias_l[at];
+                float sum = 0.f;
+#pragma unroll
+                for (int z = 0; z < 8; ++z) {
+                    if constexpr (HALVES) v[z] = v[z] * f.first * f.second;
+                    const float g = class_delta(v[z] + bias, lse[z], weight[z] != 0.f, label[z] == m);
+                    const float weighted = weight[z] != 0.f ? g * weight[z] : 0.f;
+                    sum += weighted;
+                    v[z] = HALVES ? g * 0x1p14f : weighted;
+                }
+                if (a.db_part) {
+                    sum += __shfl_xor(sum, 1, 64);
+                    sum += __shfl_xor(sum, 2, 64);
+                    sum += __shfl_xor(sum, 4, 64);
+                    if ((lane & 7) == 0 && m < a.M) a.db_part[(long)(nw >> 6) * a.M + m] = sum;
+                }
+                if (!a.delta || m >= a.M) continue;
+                char* const to = a.delta + (long)m * a.delta_bytes;
+                if constexpr (HALVES) {
+                    f16x8 h, l;
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) {
+                        h[z] = (_Float16)v[z];
+                        l[z] = (_Float16)(v[z] - (float)h[z]);
+                    }
+                    char* const at32 = to + (n >> 5) * kBlockBytes + 2 * (n & 31);
+                    *reinterpret_cast<f16x8*>(at32) = h;
+                    *reinterpret_cast<f16x8*>(at32 + kBlockBytes / 2) = l;
+                } else {
+                    *reinterpret_cast<bf16x8*>(to + 2 * n) = __builtin_convertvector(v, bf16x8);
+                }
+            }
+            asm volatile("" ::: "memory");
         }
     } else {
         // A wave's results by way of LDS (a place of its own), 32 rows of 32 NT at a time: whole lines to memory, 8 results a lane

@@ -134,7 +134,8 @@ def test_sizes(rows, features, classes, dtype):
 
 # on both sides of where another kernel takes over: few rows with many classes, scores of few rows, large weights read as they are, much work
 PATHS = [(1, 70, 1100), (2, 100, 1023), (2, 64, 24577), (3, 129, 1024), (4, 31, 4097), (5, 33, 4096), (8, 40, 24576), (9, 72, 24600), (15, 1025, 4100),
-         (16, 40, 5000), (17, 40, 5000), (16, 2048, 19600), (64, 1024, 39100), (65, 256, 20000), (300, 320, 13000), (257, 70, 70001), (1500, 1000, 801)]
+         (16, 40, 5000), (17, 40, 5000), (16, 2048, 19600), (64, 1024, 39100), (65, 256, 20000), (300, 320, 13000), (257, 70, 70001), (1500, 1000, 801),
+         (700, 127, 20011), (700, 128, 20011), (1030, 511, 5003), (1030, 512, 5003)]
 
 
 @pytest.mark.parametrize("dtype", [F, B], ids=["f32", "bf16"])
@@ -229,8 +230,8 @@ def test_magnitudes(dtype):
 
 @pytest.mark.parametrize("dtype", [F, B], ids=["f32", "bf16"])
 def test_classes_in_pieces(dtype):
-    """More scores than a piece holds: they are computed twice."""
-    rows, features, classes = 8192, 24, 20003
+    """More scores than a piece holds."""
+    rows, features, classes = 8192, 24, 40003
     _check(*_inputs(rows, features, classes, dtype, 4, weights=dtype == F), "pieces")
 
 
@@ -328,8 +329,8 @@ def test_strides_and_addresses_with_more_classes(rows, features, classes, dtype)
 
 
 def test_pieces_of_weights_that_are_read_as_they_are():
-    x, w, bias, labels, roww = _inputs(8192, 64, 20003, B, 4)
-    flat = torch.full((20003, 128), math.nan, dtype=B, device="cuda")
+    x, w, bias, labels, roww = _inputs(8192, 64, 40003, B, 4)
+    flat = torch.full((40003, 128), math.nan, dtype=B, device="cuda")
     flat[:, 32:96] = w
     want = _check(x, w, bias, labels, roww)
     loss, rowloss, dx, dw, db = mpcnn.class_backward(x, flat[:, 32:96], labels, bias=bias, roww=roww)
