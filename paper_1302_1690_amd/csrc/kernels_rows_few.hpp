@@ -10,7 +10,8 @@
 //                     kernel up to 5; it has less to do at once with few classes, and more arithmetic per row.  us, here / there: 1 x
 //                     4096 x 128000 fp32 404 / 729, bf16 213 / 360; 1 x 1000 x 16000 fp32 20 / 24, bf16 15 / 14; 8 x 1024 x 32000 fp32 33 / 39.)
 //   rows_few_grads    a thread keeps 8 features (4 with more than eight rows) of every row and their gradients over a stretch of the classes:
-//                     one fetch of the class's weights, as many multiplications per row for dx and for dw, one store.
+//                     one fetch of the class's weights, as many multiplications per row for dx and for dw, one store.  5 x 1000 x 30011 bf16
+//                     30 us, 4.0 TB/s of weights read and gradients written.
 //   rows_few_sum      adds the workgroups' shares of dx, in a fixed order.
 #pragma once
 #include "any_address.hpp"

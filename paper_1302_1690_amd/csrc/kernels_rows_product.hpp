@@ -19,6 +19,11 @@
 // Results: the classes' scores with their bias (m = class, n = row), of which only each row's largest and sum of exponentials over the
 // tile's classes leave the kernel (and the score of its label), or which are stored too; or the loss's derivative in the place of the scores, as
 // the gradients' products want it; or products, stored rounded; or partial sums.
+//
+// Bound by the matrix instruction at the clock that its power leaves (a library's plain bf16 product reaches 1.21-1.29 PFLOP/s, this layer's fp32
+// products a third of that).  8192 x 4096 x 32000 bf16, 2.1e12 operations: scores' statistics 1.78 ms (1.21 PFLOP/s), derivative 1.92 ms (1.12), features'
+// gradient 1.82 ms (1.18), class weights' gradient 1.72 ms (1.25).  4100 x 768 x 16001 fp32, 1.0e11: scores, stored, 384 us (262 TFLOP/s), gradients
+// 349 (289) and 332 (303).  256 x 256 results on eight waves: half the fetches of 128 x 128, which has more workgroups where there is less work.
 #pragma once
 #include <type_traits>
 

@@ -11,7 +11,10 @@
 // A norm that is not finite (an infinity or NaN among the gradients) changes nothing: gradients and parameters stay as they were.
 //
 // Bound by the passes over memory: one for the norm, two more for clipping (none where the norm is within the bound: the gradients
-// are what they were), three more for a step.
+// are what they were), three more for a step.  5e8 numbers of both types in 300 tensors: norm 237 us, 5.6 TB/s.  4e8 fp32 numbers in 300 tensors: step
+// 1205 us, 5.3 TB/s over four passes.  80e6 bf16 numbers in 150 tensors: clipping 141 us with the copy that brings the gradients.  3e6 in 1000 tensors:
+// 11 us, two launches.  The update goes through the list from its end on: what the norm's pass read last is in the last-level cache (steps on
+// 1e8 fp32 numbers 327 -> 307 us, on 4e8 1230 -> 1205, on 1.5e8 bf16 250 -> 237).
 #pragma once
 #include "any_address.hpp"
 #include "update.hpp"
@@ -155,7 +158,7 @@ __global__ __launch_bounds__(LONE ? 1024 : 256) void update_kernel(UpdateArgs a)
     const float f = MODE == kClip ? (float)c : (float)(c * a.rate);   // one rounding; the product with a gradient is the next
     const int first = (int)blockIdx.x * WAVES + wave, by = (int)gridDim.x * WAVES;
     for (int i = first; i < a.stretches; i += by) {
-        const Stretch t = stretch_at(a, i);
+        const Stretch t = stretch_at(a, LONE ? i : a.stretches - 1 - i);   // (from the end on)
         if constexpr (MODE == kClip) {
             if (t.grad_bf16) scale_down((bf16*)t.grad, t.n, lane, f);
             else scale_down((float*)t.grad, t.n, lane, f);
