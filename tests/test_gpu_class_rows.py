@@ -8,6 +8,7 @@ Tolerances, with u = 2^-24 (half a step of fp32) and sums bounded by the number 
   p = exp(s - lse) has a relative error of 2 e_s + 8 u (|s - lse| + 2) =: e_p (in exponents, times 2 where it is small: expm1(x) < 2 x);
   delta is rounded to bf16 (2^-8 of itself) or to two fp16 parts (2^-22 of itself, 2^-38 of 1): e_d = e_p p + r |delta|;
   dx is a sum over the classes of delta w (their errors, classes u), dw one over the rows; both are rounded (u or 2^-8)."""
+import gc
 import math
 
 import pytest
@@ -16,6 +17,14 @@ import torch
 from paper_1302_1690_amd import mpcnn
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _nothing_is_left():
+    """Tensors that caught exceptions keep in reference cycles go now, not while another test watches the allocator."""
+    yield
+    gc.collect()
+
 
 F, B = torch.float32, torch.bfloat16
 U = 2.0 ** -24

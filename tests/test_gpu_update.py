@@ -4,6 +4,7 @@ Tolerances.  The norm is summed in fp64: n additions of one sign are off by less
 comparison's own sum as much.  A clipped gradient is g fl(c): c rounded to fp32 (half a step, 2^-24), the product rounded to the tensor's
 type (2^-24, or fp32 and then bf16: 2^-24 + 2^-8).  A step p - f g is one fused operation with f rounded to fp32 (2^-24 of |f g|), rounded
 once to fp32 (2^-24 of the result) and, for bf16 parameters, once more (2^-8)."""
+import gc
 import math
 
 import numpy as np
@@ -13,6 +14,14 @@ import torch
 from paper_1302_1690_amd import mpcnn, workloads as wl
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _nothing_is_left():
+    """Tensors that caught exceptions keep in reference cycles go now, not while another test watches the allocator."""
+    yield
+    gc.collect()
+
 
 F, B = torch.float32, torch.bfloat16
 HALF = {F: 2.0 ** -24, B: 2.0 ** -8 + 2.0 ** -24}
