@@ -347,12 +347,12 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
         if (c.dx && p.gx.splits > 1) a.x_part = (float*)(ws + p.dx_part);
         if (c.dw && p.gw.splits > 1) a.w_part = (float*)(ws + p.dw_part);
     }
-    const int64_t all = (int64_t)a.x_groups + a.w_groups;
+    a.db_groups = a.db_part ? (int)((p.V + 31) / 32) : 0;
+    const int64_t all = (int64_t)a.x_groups + a.w_groups + a.db_groups;
     if (all || a.loss) mpcnn::rows_direct_grads_kernel<T><<<(unsigned)std::max<int64_t>(1, all), 256, 0, st>>>(a);
-    if (a.x_part || a.w_part || a.db_part) {
+    if (a.x_part || a.w_part) {
         const int64_t n = (a.x_part ? (int64_t)p.N * p.D : 0) + (a.w_part ? p.V * p.D : 0);
-        a.db_groups = a.db_part ? (int)((p.V + 31) / 32) : 0;
-        mpcnn::rows_direct_sum_kernel<T><<<(unsigned)(a.db_groups + std::min<int64_t>(8192, (n + 255) / 256)), 256, 0, st>>>(a);
+        mpcnn::rows_direct_sum_kernel<T><<<(unsigned)std::min<int64_t>(8192, (n + 255) / 256), 256, 0, st>>>(a);
     }
     HIP_TRY(hipGetLastError());
     return MPCNN_OK;

@@ -4,8 +4,8 @@
 //   rows_direct_scores   scores with their bias, stored [class][row], and per row and tile of classes the largest and the sum of exponentials
 //   rows_direct_delta    joins them (where there are few tiles; else rows_join_kernel has) and turns the scores into the loss's derivative times
 //                        the row's weight: made once, not by every tile of features (20 instructions each, which bound the gradients)
-//   rows_direct_grads    tiles of dx and of dw.  A long sum is split over workgroups, which leave partial sums, and
-//   rows_direct_sum      adds them up in their order.
+//   rows_direct_grads    tiles of dx and of dw, and the bias gradients' sums.  A long sum is split over workgroups, which leave partial sums, and
+//   rows_direct_sum      adds them up in their order (where there are any).
 //
 // Products on v_mfma_f32_32x32x16_bf16: bf16 numbers as they are, fp32 ones as three bf16 parts (x = h + m + l, 24 bits) and the six largest
 // of nine products: the same exponents as fp32, so no scale has to be found first, which is what two fp16 parts need and what costs
@@ -322,7 +322,32 @@ __global__ __launch_bounds__(256) void rows_direct_grads_kernel(DirectArgs a)
     }
     const bool dx = id < a.x_groups;
     if (!dx) id -= a.x_groups;
-    if (!dx && id >= a.w_groups) return;                 // (a launch for the loss alone)
+    if (!dx && id >= a.w_groups) {                       // bias gradients: 32 classes, the parts dealt to eight threads each
+        id -= a.w_groups;
+        if (id >= a.db_groups) return;                   // (a launch for the loss alone)
+        float (*const db_red)[32] = reinterpret_cast<float (*)[32]>(fold);
+        const int own = tid & 31, deal = tid >> 5;
+        const long v = (long)id * 32 + own;
+        float s = 0.f;
+        if (v < a.V) {
+            int i = deal;
+            for (; i + 56 < a.db_parts; i += 64) {
+                float u[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) u[q] = a.db_part[(long)(i + 8 * q) * a.V + v];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) s += u[q];
+            }
+            for (; i < a.db_parts; i += 8) s += a.db_part[(long)i * a.V + v];
+        }
+        db_red[deal][own] = s;
+        __syncthreads();
+        if (deal == 0 && v < a.V) {
+            for (int q = 1; q < 8; ++q) s += db_red[q][own];
+            a.db[v] = s;
+        }
+        return;
+    }
     const bool deal = (dx ? a.x_deal : a.w_deal) == 4;
     const int splits = dx ? a.x_splits : a.w_splits, each = dx ? a.x_each : a.w_each, along = dx ? a.x_along : a.w_along;
     const int K = dx ? a.V : a.N, M = dx ? a.N : a.V;
@@ -439,31 +464,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void rows_direct_sum_kernel(DirectArgs a)
 {
     const long nx = a.x_part ? (long)a.N * a.D : 0, nw = a.w_part ? (long)a.V * a.D : 0;
-    if (blockIdx.x < (unsigned)a.db_groups) {            // bias gradients: 32 classes, the parts dealt to eight threads each
-        __shared__ float red[8][32];
-        const int own = threadIdx.x & 31, deal = threadIdx.x >> 5;
-        const long v = (long)blockIdx.x * 32 + own;
-        float s = 0.f;
-        if (v < a.V) {
-            int i = deal;
-            for (; i + 56 < a.db_parts; i += 64) {
-                float u[8];
-#pragma unroll
-                for (int q = 0; q < 8; ++q) u[q] = a.db_part[(long)(i + 8 * q) * a.V + v];
-#pragma unroll
-                for (int q = 0; q < 8; ++q) s += u[q];
-            }
-            for (; i < a.db_parts; i += 8) s += a.db_part[(long)i * a.V + v];
-        }
-        red[deal][own] = s;
-        __syncthreads();
-        if (deal == 0 && v < a.V) {
-            for (int q = 1; q < 8; ++q) s += red[q][own];
-            a.db[v] = s;
-        }
-        return;
-    }
-    for (long e = (long)(blockIdx.x - a.db_groups) * 256 + threadIdx.x; e < nx + nw; e += (long)(gridDim.x - a.db_groups) * 256) {
+    for (long e = (long)blockIdx.x * 256 + threadIdx.x; e < nx + nw; e += (long)gridDim.x * 256) {
         const bool of_x = e < nx;
         const long at = of_x ? e : e - nx, by = of_x ? nx : nw;
         const float* const part = (of_x ? a.x_part : a.w_part) + at;

@@ -569,7 +569,7 @@ def _output(name, given, shape, dtype, device):
     """Given (checked), allocated (None) or not asked for (False) -> the tensor or None."""
     if given is None:
         import torch
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(*shape, dtype=dtype, device=device)
     if given is False:
         return None
     if given.dtype != dtype or given.device != device or given.shape != shape:
@@ -617,7 +617,7 @@ def class_backward(x, w, labels, bias=None, roww=None, rowloss=None, loss=None, 
         rowloss = _output("rowloss", rowloss, (rows,), torch.float32, device)
         pitch = features
         if dx is None:
-            dx = torch.empty((rows, features), dtype=x.dtype, device=device)
+            dx = torch.empty(rows, features, dtype=x.dtype, device=device)
         else:
             dx = _output("dx", dx, (rows, features), x.dtype, device)
             if dx is not None:
