@@ -77,4 +77,31 @@ __device__ __forceinline__ Raw<T, E> raw_of(const T* row, int at, int n)
 template <typename T> __device__ __forceinline__ Raw8<T> raw8_of(const T* row, int at, int n) { return raw_of<8>(row, at, n); }
 template <typename T> __device__ __forceinline__ v8f load8_of(const T* row, int at, int n) { return widen(raw8_of(row, at, n)); }
 
+// Eight bf16 numbers at addresses of which some are no multiple of four, as the words that they lie in (each holds one of them at least), and turned
+// by 16 bits where they begin in the middle of one.  The memory pipeline takes 128-bit fetches at such addresses apart.
+struct Odd8 {
+    typedef unsigned u4_any __attribute__((ext_vector_type(4), aligned(4)));
+    u4_any a;
+    unsigned b;
+};
+__device__ __forceinline__ Odd8 odd8(const bf16* p)
+{
+    const unsigned* const q = reinterpret_cast<const unsigned*>((uintptr_t)p & ~(uintptr_t)3);
+    return Odd8{*reinterpret_cast<const Odd8::u4_any*>(q), q[(uintptr_t)p & 2 ? 4 : 0]};
+}
+__device__ __forceinline__ Odd8 odd8_of(const bf16* row, int at, int n)
+{
+    const Odd8::u4_any r = __builtin_bit_cast(Odd8::u4_any, raw8_of(row, at, n).a);
+    if (!((uintptr_t)(row + at) & 2)) return Odd8{r, 0};
+    return Odd8{Odd8::u4_any{r[0] << 16, r[0] >> 16 | r[1] << 16, r[1] >> 16 | r[2] << 16, r[2] >> 16 | r[3] << 16}, r[3] >> 16};
+}
+__device__ __forceinline__ v8f widen(const Odd8& o, const bf16* p)       // p: where they were fetched, or anything as far from a multiple of four
+{
+    const unsigned by = 8 * ((unsigned)(uintptr_t)p & 2);
+    Raw8<bf16> r;
+    r.a = __builtin_bit_cast(b8_any, Odd8::u4_any{__builtin_amdgcn_alignbit(o.a[1], o.a[0], by), __builtin_amdgcn_alignbit(o.a[2], o.a[1], by),
+                                                  __builtin_amdgcn_alignbit(o.a[3], o.a[2], by), __builtin_amdgcn_alignbit(o.b, o.a[3], by)});
+    return widen(r);
+}
+
 }  // namespace mpcnn

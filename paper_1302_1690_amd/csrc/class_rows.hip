@@ -292,7 +292,11 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
         const mpcnn_status rc = launch_product<false, mpcnn::kScores>(b, t, st);
         if (rc != MPCNN_OK) return rc;
     } else {
-        mpcnn::rows_direct_scores_kernel<T><<<dim3((unsigned)p.score_v, (unsigned)p.score_n), 256, 0, st>>>(a);
+        const dim3 grid((unsigned)p.score_v, (unsigned)p.score_n);
+        // rows of bf16 that begin between words (one row has no pitch)
+        const bool odd = sizeof(T) == 2 && (((uintptr_t)c.x | (uintptr_t)c.w | 2 * (uint64_t)(p.N > 1 ? c.x_pitch : 0) | 2 * (uint64_t)(p.V > 1 ? c.w_pitch : 0)) & 2);
+        if (odd) mpcnn::rows_direct_scores_kernel<T, sizeof(T) == 2><<<grid, 256, 0, st>>>(a);
+        else mpcnn::rows_direct_scores_kernel<T, false><<<grid, 256, 0, st>>>(a);
     }
     // statistics joined with the derivative where there are few tiles of classes, by a launch of their own otherwise
     const bool joined = a.tiles > mpcnn::kDeltaFewTiles || p.few;

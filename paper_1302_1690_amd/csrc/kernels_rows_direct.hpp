@@ -107,7 +107,9 @@ __device__ __forceinline__ float2 direct_join(float2 s, float2 o)
     return float2{t, s.y * __expf(s.x - b) + o.y * __expf(o.x - b)};
 }
 
-template <typename T>
+// ODD: of bf16 rows some begin at addresses that are no multiple of four (any_address.hpp).  The loss of 23 x 2541 x 10715: 48 us without, 30 with it;
+// of 23 x 2544 x 10715: 18 us.
+template <typename T, bool ODD>
 __global__ __launch_bounds__(256) void rows_direct_scores_kernel(DirectArgs a)
 {
     __shared__ float fold[4][32][33];
@@ -124,22 +126,24 @@ __global__ __launch_bounds__(256) void rows_direct_scores_kernel(DirectArgs a)
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[r] = 0.f;
     const int steps = (a.D + kDirectK - 1) / kDirectK, whole = a.D / kDirectK, first = deal ? wave : 0, by = deal ? 4 : 1;
-    Raw8<T> u[2], y[2];
+    std::conditional_t<ODD, Odd8, Raw8<T>> u[2], y[2];
     auto fetch = [&](int s) {
-        if (s < whole) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) { u[k] = raw8(pa + kDirectK * s + 16 * k + 8 * half); y[k] = raw8(pb + kDirectK * s + 16 * k + 8 * half); }
-        } else if (s < steps) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                u[k] = raw8_of(pa, kDirectK * s + 16 * k + 8 * half, a.D);
-                y[k] = raw8_of(pb, kDirectK * s + 16 * k + 8 * half, a.D);
+        for (int k = 0; k < 2; ++k) {
+            const int at = kDirectK * s + 16 * k + 8 * half;
+            if (s < whole) {
+                if constexpr (ODD) { u[k] = odd8(pa + at); y[k] = odd8(pb + at); }
+                else { u[k] = raw8(pa + at); y[k] = raw8(pb + at); }
+            } else if (s < steps) {
+                if constexpr (ODD) { u[k] = odd8_of(pa, at, a.D); y[k] = odd8_of(pb, at, a.D); }
+                else { u[k] = raw8_of(pa, at, a.D); y[k] = raw8_of(pb, at, a.D); }
             }
         }
     };
+    auto wide = [&](const auto& v, const T* row) { if constexpr (ODD) return widen(v, row); else return widen(v); };   // (steps are whole words)
     fetch(first);
     for (int s = first; s < steps; s += by) {
-        const v8f a0 = widen(u[0]), a1 = widen(u[1]), b0 = widen(y[0]), b1 = widen(y[1]);
+        const v8f a0 = wide(u[0], pa), a1 = wide(u[1], pa), b0 = wide(y[0], pb), b1 = wide(y[1], pb);
         fetch(s + by);
         direct_product<kParts<T>, kParts<T>>(acc, a0, b0);
         direct_product<kParts<T>, kParts<T>>(acc, a1, b1);
