@@ -88,7 +88,8 @@ struct Plan {
     int64_t piece;                       // classes
     int64_t stat_tiles;
     Tiling dx, dw;                       // of a whole piece
-    size_t peaks, stats, label_score, lse, weight, loss_part, x_rows, x_cols, w_rows, score, delta, db_part,
+    Tiling sc;                           // of the scores, where there is one piece
+    size_t peaks, stats, label_score, lse, weight, loss_part, x_rows, x_cols, w_rows, score, score_part, delta, db_part,
         dx_part, dw_part, total;
     int64_t bytes_along(int64_t n) const { return halves ? up_to(n, 32) * 4 : up_to(n, 64) * 2; }
     int64_t v_blocks(int64_t n) const { return (n + (halves ? 31 : 63)) / (halves ? 32 : 64); }   // of the sum over n classes
@@ -175,8 +176,12 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     if (train) bound(kRoom / p->Np);
     p->piece = piece;
     const int64_t pieces = (classes + piece - 1) / piece;
-    p->stat_tiles = (classes + 127) / 128 + pieces;
     const int64_t N = p->N, D = p->D;
+    // The scores' sums over the features are split, too, where their tiles leave compute units without work.  us, split and summed / whole, bf16 1000 x 4096
+    // x 2000 36 / 44, 200 x 4000 x 3000 26 / 46, 100 x 4096 x 20000 46 / 54; fp32 2469 x 3084 x 776 69 / 75, 1000 x 2048 x 2000 45 / 54.
+    p->sc = tiling_of(classes, N, p->d_bytes / mpcnn::kBlockBytes, pieces == 1 ? 16 : 1, p->halves);
+    p->stat_tiles = std::max((classes + 127) / 128 + pieces, (classes + mpcnn::kScoresSum - 1) / mpcnn::kScoresSum * (p->sc.splits > 1));
+    p->score_part = take(p->sc.splits > 1 ? 4 * p->sc.splits * classes * N : 0);
     p->peaks = take(4 * 3 * mpcnn::kPeakGroups);
     p->stats = take(8 * p->stat_tiles * N);
     p->label_score = take(4 * N);
@@ -411,6 +416,16 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         a.a_peak = H ? w_peak : nullptr; a.b_peak = H ? x_peak : nullptr; a.a_words = a.b_words = mpcnn::kPeakGroups;
         a.bias = c.bias ? c.bias + v0 : nullptr;
         a.labels = c.labels; a.class0 = (int)v0;
+        if (!delta && p.sc.splits > 1) {
+            a.part = (float*)(ws + p.score_part);
+            const mpcnn_status rc = launch_product<H, mpcnn::kPart>(a, p.sc, st);
+            mpcnn::ScoresSumArgs s{};
+            s.part = a.part; s.splits = p.sc.splits; s.M = a.M; s.N = a.N; s.a_peak = a.a_peak; s.b_peak = a.b_peak;
+            s.bias = a.bias; s.labels = a.labels; s.stats = a.stats; s.label_score = a.label_score; s.scores = a.scores; s.score_row = a.score_row;
+            done = (a.M + mpcnn::kScoresSum - 1) / mpcnn::kScoresSum;
+            mpcnn::rows_scores_sum_kernel<H><<<dim3((unsigned)((a.N + 63) / 64), (unsigned)done), 256, 0, st>>>(s);
+            return rc;
+        }
         const Tiling t = tiling_of(n_classes, p.N, d_blocks, 1, H);
         if (!delta) done += t.tiles_m;
         return delta ? launch_product<H, mpcnn::kDelta>(a, t, st) : launch_product<H, mpcnn::kScores>(a, t, st);

@@ -190,6 +190,79 @@ __global__ __launch_bounds__(256) void rows_pack16_kernel(PackRowsArgs a)
     }
 }
 
+// ---- scores from the partial sums of their product: their statistics over 32 classes, their label's, and the scores themselves where they are kept
+struct ScoresSumArgs {
+    const float* part;                     // [splits][M][N]
+    int splits, M, N;
+    const unsigned *a_peak, *b_peak;       // fp32 storage: what the operands were raised by
+    const float* bias;                     // [M] or null
+    const int* labels;                     // [N]
+    float2* stats;                         // [tiles of 32 classes][N]
+    float* label_score;                    // [N]
+    float* scores;                         // [M][score_row], or null
+    long score_row;
+};
+constexpr int kScoresSum = 32;            // classes of a workgroup, eight a wave
+template <bool HALVES>
+__global__ __launch_bounds__(256) void rows_scores_sum_kernel(ScoresSumArgs a)
+{
+    constexpr float kNone = -__builtin_inff();
+    __shared__ float2 red[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = 64 * blockIdx.x + lane, at = n < a.N ? n : a.N - 1, m0 = kScoresSum * blockIdx.y + wave;
+    Lower f{1.f, 1.f};
+    if constexpr (HALVES) f = lower_by(raise_of(peak_of(a.a_peak, kPeakGroups), 0) + raise_of(peak_of(a.b_peak, kPeakGroups), 0));
+    float s[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s[k] = 0.f;
+    const float* p[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) p[k] = a.part + (long)(m0 + 4 * k < a.M ? m0 + 4 * k : a.M - 1) * a.N + at;
+    const long by = (long)a.M * a.N;
+    int i = 0;
+    for (; i + 4 <= a.splits; i += 4) {                  // 32 loads in flight
+        float v[4][8];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[q][k] = p[k][(i + q) * by];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s[k] += v[q][k];
+    }
+    for (; i < a.splits; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[k] += p[k][i * by];
+    const int label = n < a.N ? a.labels[n] : -1;
+    float top = kNone;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int m = m0 + 4 * k;
+        if constexpr (HALVES) s[k] = s[k] * f.first * f.second;
+        s[k] = m < a.M ? s[k] + (a.bias ? a.bias[m] : 0.f) : kNone;
+        top = fmaxf(top, s[k]);
+        if (m >= a.M || n >= a.N) continue;
+        if (a.scores) a.scores[m * a.score_row + n] = s[k];
+        if (m == label) a.label_score[n] = s[k];
+    }
+    const float base = top == kNone ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += __expf(s[k] - base);
+    red[wave][lane] = float2{top, sum};
+    __syncthreads();
+    if (wave != 0 || n >= a.N) return;
+    float2 t = red[0][lane];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        const float2 o = red[w][lane];
+        const float all = fmaxf(t.x, o.x), b = all == kNone ? 0.f : all;
+        t = float2{all, t.y * __expf(t.x - b) + o.y * __expf(o.x - b)};
+    }
+    a.stats[(long)blockIdx.y * a.N + n] = t;
+}
+
 // ---- per row: the statistics of all tiles of classes joined; the loss; per workgroup its share of the summed loss
 struct JoinArgs {
     const float2* stats;                   // [tiles][N]
