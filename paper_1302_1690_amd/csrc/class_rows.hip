@@ -76,6 +76,10 @@ Tiling tiling_of(int64_t M, int64_t N, int64_t blocks, int64_t most_splits, bool
 // and 382 / 374, of 64 x 4096 x 8000 (2e9) 203 / 335 and 149 / 124.
 constexpr int64_t kDirectWork = 1200000000, kDirectLossWork = 2000000000, kDirectFewRows = 64, kDirectFewWork[2] = {4000000000, 1600000000};
 
+// bf16 class weights from which on the scores of up to 4 and of up to 12 rows are the vector ALU's, too (fewer come from the last-level cache fast enough;
+// times in kernels_rows_few.hpp)
+constexpr int64_t kFewWeights[2] = {70000000, 150000000};
+
 struct Plan {
     bool halves, train, keep, direct, few, few_scores;
     int grad_groups;                     // few: workgroups along the classes,
@@ -115,8 +119,9 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     // few rows and many classes: the gradients, and the scores of still fewer, on the vector ALU (kernels_rows_few.hpp has the times)
     p->few = p->direct && train && rows > 0 && rows <= mpcnn::kFewRows && classes >= (rows <= 4 ? 1024 : 4096);
     if (p->direct && rows > 0) {
-        const int64_t least = rows <= 2 ? (p->halves ? 1024 : 24576) : p->halves && rows <= mpcnn::kFewScoreRows ? 24576 : kMaxClasses + 1;
-        p->few_scores = classes >= least;
+        if (p->halves) p->few_scores = rows <= mpcnn::kFewScoreRows && classes >= (rows <= 3 ? 1024 : 24576);
+        else if (rows <= 2) p->few_scores = classes >= 24576;
+        else p->few_scores = rows <= mpcnn::kFewScoreRows && classes >= kFewWeights[rows <= 4 ? 0 : 1] / features;
     }
     if (p->direct) {
         // a tile of 32 x 32 for four waves, one of 64 x 64 where that gives every compute unit two workgroups or the sum has one step
@@ -150,7 +155,7 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
         };
         const int64_t groups = grads(p->gx, rows, classes) + grads(p->gw, classes, rows);
         if (groups < 0x7fffffff) {
-            p->stat_tiles = p->score_v;
+            p->stat_tiles = std::max<int64_t>(p->score_v, (classes + 127) / 128);   // (of the block product at most)
             p->stats = take(8 * p->stat_tiles * rows);
             p->label_score = take(4 * rows);
             p->lse = take(4 * p->Np);
@@ -284,10 +289,11 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
         few.N = p.N; few.D = p.D; few.V = p.V; few.score_row = p.Np;
         few.bias = c.bias; few.mask = a.mask; few.scores = a.scores; few.stats = a.stats; few.label_score = a.label_score;
     }
-    if (p.few_scores) {
+    const bool blocks = sizeof(T) == 2 && p.V * p.D >= kBlockWeights && direct_operand<T>(c.x, c.x_pitch, p.D) && direct_operand<T>(c.w, c.w_pitch, p.D);
+    if (p.few_scores && !(blocks && p.N > 2)) {
         few.each = p.score_each;
         mpcnn::launch_rows_few_scores<T>(few, (unsigned)p.score_v, st);
-    } else if (sizeof(T) == 2 && p.V * p.D >= kBlockWeights && direct_operand<T>(c.x, c.x_pitch, p.D) && direct_operand<T>(c.w, c.w_pitch, p.D)) {
+    } else if (blocks) {
         mpcnn::ProductArgs b{};
         b.A = (const char*)c.w; b.a_row = c.w_pitch * 2; b.B = (const char*)c.x; b.b_row = c.x_pitch * 2;
         b.M = a.V; b.N = p.N; b.blocks = p.D * 2 / mpcnn::kBlockBytes;

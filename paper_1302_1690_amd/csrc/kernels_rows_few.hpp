@@ -1,4 +1,4 @@
-// The class layer's gradients on at most sixteen rows of features, and scores on at most eight (class_rows.hip): bound by the passes over the
+// The class layer's gradients on at most sixteen rows of features, and scores on at most twelve (class_rows.hip): bound by the passes over the
 // class weights (read for the scores, read for the rows' gradient, their own gradient written), so everything is done on the vector
 // ALU in fp32, with 128-bit fetches and stores at whatever address the numbers have, and nothing is fetched for rows that do not exist.
 // A kernel instance per number of rows.
@@ -8,7 +8,9 @@
 //                     per workgroup and row the largest and the sum of exponentials of all its classes.  (The matrix instruction's
 //                     scores, kernels_rows_direct.hpp, fetch 16 bytes of each of 32 classes at once and reach 2.1-2.9 TB/s on large weights, this
 //                     kernel up to 5; it has less to do at once with few classes, and more arithmetic per row.  us, here / there: 1 x
-//                     4096 x 128000 fp32 404 / 729, bf16 213 / 360; 1 x 1000 x 16000 fp32 20 / 24, bf16 15 / 14; 8 x 1024 x 32000 fp32 33 / 39.)
+//                     4096 x 128000 fp32 404 / 729, bf16 213 / 360; 1 x 1000 x 16000 fp32 20 / 24, bf16 15 / 14; 8 x 1024 x 32000 fp32 33 / 39.  Whole calls of the loss:
+//                     fp32 12 x 2912 x 73000 270 / 460, 3 x 2912 x 10000 40 / 58, 8 x 1000 x 10000 34 / 31; bf16 3 x 2912 x 73000 119 / 220, 3 x 2912 x 25000
+//                     45 / 49, 12 x 2912 x 73000 217 / 242, 8 x 2912 x 25000 59 / 49, 12 x 2913 x 73000 220 / 353.)
 //   rows_few_grads    a thread keeps 8 features (4 with more than eight rows) of every row and their gradients over a stretch of the classes:
 //                     one fetch of the class's weights, as many multiplications per row for dx and for dw, one store.  5 x 1000 x 30011 bf16
 //                     30 us, 4.0 TB/s of weights read and gradients written.
@@ -37,7 +39,7 @@ template <typename T, int NR>
 __global__ __launch_bounds__(kFewThreads) void rows_few_scores_kernel(FewArgs a)
 {
     constexpr int C = 4;                         // classes of a group of 16 lanes
-    constexpr int kFewSteps = 8;                 // of 128 features, whose rows LDS holds at once
+    constexpr int kFewSteps = NR <= 8 ? 8 : 4;   // of 128 features, whose rows LDS holds at once
     constexpr float kNone = -__builtin_inff();
     __shared__ float sc[NR][kFewRound];
     __shared__ __attribute__((aligned(32))) float xl[NR][128 * kFewSteps];

@@ -6,14 +6,10 @@ namespace mpcnn {
 template <typename T>
 void launch_rows_few_scores(const FewArgs& a, unsigned groups, hipStream_t st)
 {
-    static_assert(kFewScoreRows == 8, "a case each");
+    static_assert(kFewScoreRows == 12, "a case each");
     switch (a.N) {
 #define CASE(n) case n: rows_few_scores_kernel<T, n><<<groups, kFewThreads, 0, st>>>(a); break;
-        CASE(1) CASE(2)
-        default:
-            if constexpr (sizeof(T) == 4) {                // (bf16: two rows at most)
-                switch (a.N) { CASE(3) CASE(4) CASE(5) CASE(6) CASE(7) CASE(8) }
-            }
+        CASE(1) CASE(2) CASE(3) CASE(4) CASE(5) CASE(6) CASE(7) CASE(8) CASE(9) CASE(10) CASE(11) CASE(12)
 #undef CASE
     }
 }

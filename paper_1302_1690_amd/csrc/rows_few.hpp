@@ -4,7 +4,7 @@
 
 namespace mpcnn {
 
-constexpr int kFewRows = 16, kFewScoreRows = 8, kFewRound = 64;      // rows, classes of a round
+constexpr int kFewRows = 16, kFewScoreRows = 12, kFewRound = 64;      // rows, classes of a round
 constexpr int kFewThreads = 256;
 // Features of a thread of rows_few_grads: what a thread keeps of every row and of its gradient fits its registers
 __host__ __device__ constexpr int few_columns(int rows) { return rows <= 8 ? 8 : 4; }

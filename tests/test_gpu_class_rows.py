@@ -145,7 +145,8 @@ def test_sizes(rows, features, classes, dtype):
 PATHS = [(1, 70, 1100), (2, 100, 1023), (2, 64, 24577), (3, 129, 1024), (4, 31, 4097), (5, 33, 4096), (8, 40, 24576), (9, 72, 24600), (15, 1025, 4100),
          (16, 40, 5000), (17, 40, 5000), (16, 2048, 19600), (64, 1024, 39100), (65, 256, 20000), (300, 320, 13000), (257, 70, 70001), (1500, 1000, 801),
          (700, 127, 20011), (700, 128, 20011), (1030, 511, 5003), (1030, 512, 5003),
-         (200, 4000, 3001), (129, 4096, 5003)]
+         (200, 4000, 3001), (129, 4096, 5003),
+         (3, 50, 1024), (12, 100, 24576), (13, 100, 24576), (4, 700, 100000), (12, 1501, 100003), (12, 1504, 100003), (11, 1536, 100003), (13, 1501, 100003)]
 
 
 @pytest.mark.parametrize("dtype", [F, B], ids=["f32", "bf16"])
