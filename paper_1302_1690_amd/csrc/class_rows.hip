@@ -80,8 +80,13 @@ constexpr int64_t kDirectWork = 1200000000, kDirectLossWork = 2000000000, kDirec
 // times in kernels_rows_few.hpp)
 constexpr int64_t kFewWeights[2] = {70000000, 150000000};
 
+// fp32 class weights from which on the scores of up to 32 and of up to so many rows are rows_wide_scores_kernel's.  us, with it / before (rows_direct_scores
+// or, with more work, weights brought into blocks): 16 x 4096 x 50000 331 / 432, 32 x 4096 x 50000 325 / 869, 64 x 4096 x 50000 324 / 866, 128 x 4096 x 50000
+// 538 / 894, 32 x 1000 x 20000 56 / 48, 64 x 1000 x 20000 57 / 68, 64 x 4096 x 3000 58 / 66, 64 x 1000 x 5000 38 / 37.
+constexpr int64_t kWideRows = 128, kWideWeights[2] = {50000000, 12000000};
+
 struct Plan {
-    bool halves, train, keep, direct, few, few_scores;
+    bool halves, train, keep, direct, few, few_scores, wide;
     int grad_groups;                     // few: workgroups along the classes,
     int64_t score_each, grad_each;       // their classes, and those of the scores' workgroups
     int score_deal, score_v, score_n;    // direct: waves that share a tile's sum, tiles along classes and rows
@@ -93,7 +98,7 @@ struct Plan {
     int64_t stat_tiles;
     Tiling dx, dw;                       // of a whole piece
     Tiling sc;                           // of the scores, where there is one piece
-    size_t peaks, stats, label_score, lse, weight, loss_part, x_rows, x_cols, w_rows, score, score_part, delta, db_part,
+    size_t peaks, stats, label_score, lse, weight, loss_part, x_rows, x_cols, w_rows, x_split, score, score_part, delta, db_part,
         dx_part, dw_part, total;
     int64_t bytes_along(int64_t n) const { return halves ? up_to(n, 32) * 4 : up_to(n, 64) * 2; }
     int64_t v_blocks(int64_t n) const { return (n + (halves ? 31 : 63)) / (halves ? 32 : 64); }   // of the sum over n classes
@@ -115,7 +120,8 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     const bool fits = classes <= kRoom / p->Np;
     p->keep = train && fits && features >= kKeepFeatures[p->halves ? 0 : 1];
     const int64_t most = rows <= kDirectFewRows ? kDirectFewWork[p->halves ? 0 : 1] : train ? kDirectWork : kDirectLossWork;
-    p->direct = (rows <= mpcnn::kFewRows || rows * classes <= most / features) && (fits || !train);
+    p->wide = p->halves && rows > mpcnn::kFewScoreRows && rows <= kWideRows && classes >= kWideWeights[rows <= 32 ? 0 : 1] / features;
+    p->direct = (rows <= mpcnn::kFewRows || rows * classes <= most / features || (p->wide && !train)) && (fits || !train);
     // few rows and many classes: the gradients, and the scores of still fewer, on the vector ALU (kernels_rows_few.hpp has the times)
     p->few = p->direct && train && rows > 0 && rows <= mpcnn::kFewRows && classes >= (rows <= 4 ? 1024 : 4096);
     if (p->direct && rows > 0) {
@@ -129,6 +135,7 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
         auto tiles = [](int64_t n, int deal) { return (int)((n + (deal == 4 ? 31 : 63)) / (deal == 4 ? 32 : 64)); };
         p->score_deal = deal_of(classes, rows, features);
         p->score_v = tiles(classes, p->score_deal); p->score_n = tiles(rows, p->score_deal);
+        if (p->wide) p->score_v = tiles(classes, 4);
         if (p->few_scores) {
             const int64_t round = mpcnn::kFewRound;
             p->score_each = ((classes + round - 1) / round + 8 * kCUs - 1) / (8 * kCUs) * round;   // whole rounds
@@ -161,6 +168,7 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
             p->lse = take(4 * p->Np);
             p->weight = take(4 * p->Np);
             p->loss_part = take(8 * (p->Np + 1));
+            if (p->wide) p->x_split = take(up_to(rows, 32 * mpcnn::kWideTiles) * up_to(features, mpcnn::kDirectK) * 6);
             if (p->few) {
                 p->score = take(4 * classes * p->Np);
                 p->dx_part = take(4 * (int64_t)p->grad_groups * rows * features);
@@ -302,6 +310,14 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
         a.tiles = t.tiles_m;
         const mpcnn_status rc = launch_product<false, mpcnn::kScores>(b, t, st);
         if (rc != MPCNN_OK) return rc;
+    } else if (sizeof(T) == 4 && p.wide) {
+        mpcnn::SplitArgs s{};
+        s.x = (const float*)c.x; s.x_pitch = c.x_pitch; s.N = p.N; s.D = p.D; s.out = ws + p.x_split;
+        s.tiles = (int)(up_to(p.N, 32 * mpcnn::kWideTiles) / 32);
+        const int64_t n = (int64_t)s.tiles * ((p.D + mpcnn::kDirectK - 1) / mpcnn::kDirectK) * 128;
+        mpcnn::rows_split_kernel<<<(unsigned)std::min<int64_t>(4096, (n + 255) / 256), 256, 0, st>>>(s);
+        a.x_split = s.out; a.x_tiles = s.tiles;
+        mpcnn::rows_wide_scores_kernel<<<(unsigned)(p.score_v * (s.tiles / mpcnn::kWideTiles)), 256, 0, st>>>(a);
     } else {
         const dim3 grid((unsigned)p.score_v, (unsigned)p.score_n);
         // rows of bf16 that begin between words (one row has no pitch)

@@ -35,6 +35,8 @@ struct DirectArgs {
     long score_row;
     float2* stats;                         // [tiles of classes][N]
     float* label_score;
+    const char* x_split;                   // features as operands (rows_split_kernel)
+    int x_tiles;                           // of 32 rows, a multiple of kWideTiles
     int score_deal, x_deal, w_deal;        // waves that deal a tile's sum among them: 4 (tiles of 32 x 32) or 1 (64 x 64)
     // derivative
     float *lse, *weight;                   // [N]; lse null: joined here
@@ -211,6 +213,117 @@ __global__ __launch_bounds__(256) void rows_direct_scores_kernel(DirectArgs a)
     __syncthreads();
     const int nt = blockIdx.y * 64 + tid;
     if (tid < 64 && nt < a.N) a.stats[(long)blockIdx.x * a.N + nt] = direct_join(red[0][tid], red[1][tid]);
+}
+
+// ---- fp32 scores of some tens of rows over many classes: bound by the pass over the class weights, which a wave takes from memory into its operands
+// and splits once for 64 rows.  The features are split before (rows_split_kernel), into operands as the lanes want them: [step of 32 k's][16 k's][part]
+// [tile of 32 rows][lane], and come from the second-level cache.  The waves deal the sum's steps among them.
+struct SplitArgs {
+    const float* x;
+    long x_pitch;
+    int N, D, tiles;                       // of 32 rows
+    char* out;
+};
+__global__ __launch_bounds__(256) void rows_split_kernel(SplitArgs a)
+{
+    const long all = (long)(a.D + kDirectK - 1) / kDirectK * 2 * a.tiles * 64;
+    for (long e = (long)blockIdx.x * 256 + threadIdx.x; e < all; e += (long)gridDim.x * 256) {
+        const int lane = (int)(e & 63), tile = (int)((e >> 6) % a.tiles);
+        const long k16 = (e >> 6) / a.tiles;
+        const int n = 32 * tile + (lane & 31);
+        const v8f v = load8_of(a.x + (long)(n < a.N ? n : a.N - 1) * a.x_pitch, (int)(16 * k16) + 8 * (lane >> 5), a.D);
+        d_bf16x8 p[3];
+        direct_parts<3>(p, v);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) *reinterpret_cast<d_bf16x8*>(a.out + (((k16 * 3 + i) * a.tiles + tile) * 64 + lane) * 16) = p[i];
+    }
+}
+constexpr int kWideTiles = 2;              // of 32 rows, of a wave
+__global__ __launch_bounds__(256) void rows_wide_scores_kernel(DirectArgs a)
+{
+    constexpr float kNone = -__builtin_inff();
+    __shared__ float fold[4][32][33];
+    __shared__ float2 red[8][64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int groups_n = a.x_tiles / kWideTiles;         // (side by side: they read the same class weights)
+    const int vt = blockIdx.x / groups_n, t0 = kWideTiles * (blockIdx.x - vt * groups_n), v0 = 32 * vt;
+    const int row = lane & 31, half = lane >> 5;
+    const float* const pw = (const float*)a.w + (long)(v0 + row < a.V ? v0 + row : a.V - 1) * a.w_pitch;
+    const int steps = (a.D + kDirectK - 1) / kDirectK, whole = a.D / kDirectK;
+    v16f acc[kWideTiles];
+#pragma unroll
+    for (int j = 0; j < kWideTiles; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
+    Raw8<float> u[2];
+    d_bf16x8 x[2][3][kWideTiles];
+    auto fetch_w = [&](int s) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int at = kDirectK * s + 16 * k + 8 * half;
+            if (s < whole) u[k] = raw8(pw + at);
+            else if (s < steps) u[k] = raw8_of(pw, at, a.D);
+        }
+    };
+    auto fetch_x = [&](int s) {
+        if (s >= steps) return;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+#pragma unroll
+                for (int j = 0; j < kWideTiles; ++j)
+                    x[k][i][j] = *reinterpret_cast<const d_bf16x8*>(a.x_split + (((long)(2 * s + k) * 3 + i) * a.x_tiles + t0 + j) * 1024 + 16 * lane);
+    };
+    fetch_w(wave);
+    fetch_x(wave);
+    for (int s = wave; s < steps; s += 4) {
+        d_bf16x8 w[2][3];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) direct_parts<3>(w[k], widen(u[k]));
+        fetch_w(s + 4);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int j = 0; j < kWideTiles; ++j)
+#pragma unroll
+                for (int sum = 2; sum >= 0; --sum)       // the smallest products first
+#pragma unroll
+                    for (int i = 0; i <= sum; ++i) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[k][i], x[k][sum - i][j], acc[j], 0, 0, 0);
+        fetch_x(s + 4);
+    }
+#pragma unroll
+    for (int j = 0; j < kWideTiles; ++j) {
+        v4f s = direct_fold(acc[j], fold);
+        const int n0 = 32 * (t0 + j), n = n0 + (tid & 31), m0 = v0 + 4 * (tid >> 5);
+        const bool real = n < a.N;
+        const int label = real ? a.mask.labels[n] : -1;
+        float top = kNone;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int m = m0 + q;
+            const float b = a.bias ? a.bias[m < a.V ? m : a.V - 1] : 0.f;
+            s[q] = m < a.V ? s[q] + b : kNone;
+            top = fmaxf(top, s[q]);
+            if (m < a.V && real) {
+                if (a.scores) a.scores[m * a.score_row + n] = s[q];
+                if (m == label) a.label_score[n] = s[q];
+            }
+        }
+        const float base = top == kNone ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum += __expf(s[q] - base);
+        red[tid >> 5][tid & 31] = float2{top, sum};
+        __syncthreads();                                 // (and the fold has been read)
+        if (tid < 32 && n0 + tid < a.N) {
+            float2 t = red[0][tid];
+#pragma unroll
+            for (int q = 1; q < 8; ++q) t = direct_join(t, red[q][tid]);
+            a.stats[(long)vt * a.N + n0 + tid] = t;
+        }
+        __syncthreads();
+    }
 }
 
 // 64 classes x `batch` times 64 rows per workgroup: a lane a row, a wave every fourth class

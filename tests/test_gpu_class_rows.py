@@ -115,8 +115,9 @@ def _check(x, w, bias, labels, roww, what=""):
     want = _want(x, w, bias, labels, roww)
     loss, rowloss, lse = mpcnn.class_loss(x, w, labels, bias=bias, roww=roww)
     loss2, rowloss2, dx, dw, db = mpcnn.class_backward(x, w, labels, bias=bias, roww=roww)
-    # (in between the loss alone and the gradients' loss come from kernels of their own, each as far from the formula as it may be)
-    if not 1.2e9 < x.shape[0] * w.numel() <= 2e9:
+    # (there the loss alone and the gradients' loss come from kernels of their own, each as far from the formula as it may be)
+    work = x.shape[0] * w.numel()
+    if not (1.2e9 < work <= 2e9 or (x.dtype == F and x.shape[0] <= 128 and work > 1.2e9)):
         assert torch.equal(rowloss, rowloss2)
     _near("rowloss", rowloss2, want["rowloss"])
     for l, r in ((loss, rowloss), (loss2, rowloss2)):
@@ -146,7 +147,8 @@ PATHS = [(1, 70, 1100), (2, 100, 1023), (2, 64, 24577), (3, 129, 1024), (4, 31, 
          (16, 40, 5000), (17, 40, 5000), (16, 2048, 19600), (64, 1024, 39100), (65, 256, 20000), (300, 320, 13000), (257, 70, 70001), (1500, 1000, 801),
          (700, 127, 20011), (700, 128, 20011), (1030, 511, 5003), (1030, 512, 5003),
          (200, 4000, 3001), (129, 4096, 5003),
-         (3, 50, 1024), (12, 100, 24576), (13, 100, 24576), (4, 700, 100000), (12, 1501, 100003), (12, 1504, 100003), (11, 1536, 100003), (13, 1501, 100003)]
+         (3, 50, 1024), (12, 100, 24576), (13, 100, 24576), (4, 700, 100000), (12, 1501, 100003), (12, 1504, 100003), (11, 1536, 100003), (13, 1501, 100003),
+         (13, 999, 10011), (33, 1001, 9991), (64, 33, 303031), (65, 1031, 9700), (128, 1031, 9700), (129, 1031, 9700), (100, 4096, 20001)]
 
 
 @pytest.mark.parametrize("dtype", [F, B], ids=["f32", "bf16"])
