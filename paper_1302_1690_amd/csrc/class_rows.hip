@@ -80,10 +80,11 @@ constexpr int64_t kDirectWork = 1200000000, kDirectLossWork = 2000000000, kDirec
 // times in kernels_rows_few.hpp)
 constexpr int64_t kFewWeights[2] = {70000000, 150000000};
 
-// fp32 class weights from which on the scores of up to 32 and of up to so many rows are rows_wide_scores_kernel's.  us, with it / before (rows_direct_scores
-// or, with more work, weights brought into blocks): 16 x 4096 x 50000 331 / 432, 32 x 4096 x 50000 325 / 869, 64 x 4096 x 50000 324 / 866, 128 x 4096 x 50000
-// 538 / 894, 32 x 1000 x 20000 56 / 48, 64 x 1000 x 20000 57 / 68, 64 x 4096 x 3000 58 / 66, 64 x 1000 x 5000 38 / 37.
-constexpr int64_t kWideRows = 128, kWideWeights[2] = {50000000, 12000000};
+// fp32 class weights from which on the scores of 9 to so many rows are rows_wide_scores_kernel's (but for those that are rows_few_scores').  us, with it /
+// before (rows_direct_scores or, with more work, weights brought into blocks): 16 x 4096 x 50000 260 / 455, 32 x 4096 x 50000 265 / 870,
+// 64 x 4096 x 50000 333 / 860, 100 x 4096 x 20000 225 / 320, 128 x 4096 x 50000 538 / 894, 32 x 1000 x 20000 44 / 47, 64 x 1000 x 20000 57 / 68,
+// 32 x 4096 x 3000 50 / 65, 64 x 4096 x 3000 58 / 66, 64 x 1000 x 5000 38 / 37.
+constexpr int64_t kWideRows = 128, kWideWeights = 12000000;
 
 struct Plan {
     bool halves, train, keep, direct, few, few_scores, wide;
@@ -120,7 +121,7 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     const bool fits = classes <= kRoom / p->Np;
     p->keep = train && fits && features >= kKeepFeatures[p->halves ? 0 : 1];
     const int64_t most = rows <= kDirectFewRows ? kDirectFewWork[p->halves ? 0 : 1] : train ? kDirectWork : kDirectLossWork;
-    p->wide = p->halves && rows > mpcnn::kFewScoreRows && rows <= kWideRows && classes >= kWideWeights[rows <= 32 ? 0 : 1] / features;
+    p->wide = p->halves && rows > 8 && rows <= kWideRows && classes >= kWideWeights / features && (rows > mpcnn::kFewScoreRows || classes < 24576);
     p->direct = (rows <= mpcnn::kFewRows || rows * classes <= most / features || (p->wide && !train)) && (fits || !train);
     // few rows and many classes: the gradients, and the scores of still fewer, on the vector ALU (kernels_rows_few.hpp has the times)
     p->few = p->direct && train && rows > 0 && rows <= mpcnn::kFewRows && classes >= (rows <= 4 ? 1024 : 4096);
@@ -168,7 +169,7 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
             p->lse = take(4 * p->Np);
             p->weight = take(4 * p->Np);
             p->loss_part = take(8 * (p->Np + 1));
-            if (p->wide) p->x_split = take(up_to(rows, 32 * mpcnn::kWideTiles) * up_to(features, mpcnn::kDirectK) * 6);
+            if (p->wide) p->x_split = take(up_to(rows, rows <= 32 ? 32 : 64) * up_to(features, mpcnn::kDirectK) * 6);
             if (p->few) {
                 p->score = take(4 * classes * p->Np);
                 p->dx_part = take(4 * (int64_t)p->grad_groups * rows * features);
@@ -313,11 +314,12 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
     } else if (sizeof(T) == 4 && p.wide) {
         mpcnn::SplitArgs s{};
         s.x = (const float*)c.x; s.x_pitch = c.x_pitch; s.N = p.N; s.D = p.D; s.out = ws + p.x_split;
-        s.tiles = (int)(up_to(p.N, 32 * mpcnn::kWideTiles) / 32);
+        s.tiles = p.N <= 32 ? 1 : (int)(up_to(p.N, 64) / 32);
         const int64_t n = (int64_t)s.tiles * ((p.D + mpcnn::kDirectK - 1) / mpcnn::kDirectK) * 128;
         mpcnn::rows_split_kernel<<<(unsigned)std::min<int64_t>(4096, (n + 255) / 256), 256, 0, st>>>(s);
         a.x_split = s.out; a.x_tiles = s.tiles;
-        mpcnn::rows_wide_scores_kernel<<<(unsigned)(p.score_v * (s.tiles / mpcnn::kWideTiles)), 256, 0, st>>>(a);
+        if (s.tiles == 1) mpcnn::rows_wide_scores_kernel<1><<<(unsigned)p.score_v, 256, 0, st>>>(a);
+        else mpcnn::rows_wide_scores_kernel<2><<<(unsigned)(p.score_v * (s.tiles / 2)), 256, 0, st>>>(a);
     } else {
         const dim3 grid((unsigned)p.score_v, (unsigned)p.score_n);
         // rows of bf16 that begin between words (one row has no pitch)

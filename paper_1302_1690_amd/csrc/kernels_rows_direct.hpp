@@ -36,7 +36,7 @@ struct DirectArgs {
     float2* stats;                         // [tiles of classes][N]
     float* label_score;
     const char* x_split;                   // features as operands (rows_split_kernel)
-    int x_tiles;                           // of 32 rows, a multiple of kWideTiles
+    int x_tiles;                           // of 32 rows, a multiple of the kernel's
     int score_deal, x_deal, w_deal;        // waves that deal a tile's sum among them: 4 (tiles of 32 x 32) or 1 (64 x 64)
     // derivative
     float *lse, *weight;                   // [N]; lse null: joined here
@@ -216,8 +216,10 @@ __global__ __launch_bounds__(256) void rows_direct_scores_kernel(DirectArgs a)
 }
 
 // ---- fp32 scores of some tens of rows over many classes: bound by the pass over the class weights, which a wave takes from memory into its operands
-// and splits once for 64 rows.  The features are split before (rows_split_kernel), into operands as the lanes want them: [step of 32 k's][16 k's][part]
-// [tile of 32 rows][lane], and come from the second-level cache.  The waves deal the sum's steps among them.
+// and splits once for up to 64 rows.  The features are split before (rows_split_kernel), into operands as the lanes want them: [step of 32 k's][16 k's][part]
+// [tile of 32 rows][lane], and come from the second-level cache, for 64 rows three times the class
+// weights' bytes.  The waves deal the sum's steps among them.  64 x 4096 x 50000: 313 us, 2.6 TB/s of weights.  (Two steps of weights ahead: 8 % slower; two
+// waves of other classes beside each other, which read the same features: 8 % slower.)
 struct SplitArgs {
     const float* x;
     long x_pitch;
@@ -238,25 +240,25 @@ __global__ __launch_bounds__(256) void rows_split_kernel(SplitArgs a)
         for (int i = 0; i < 3; ++i) *reinterpret_cast<d_bf16x8*>(a.out + (((k16 * 3 + i) * a.tiles + tile) * 64 + lane) * 16) = p[i];
     }
 }
-constexpr int kWideTiles = 2;              // of 32 rows, of a wave
+template <int NT>                          // tiles of 32 rows of a wave: 1 or 2
 __global__ __launch_bounds__(256) void rows_wide_scores_kernel(DirectArgs a)
 {
     constexpr float kNone = -__builtin_inff();
     __shared__ float fold[4][32][33];
     __shared__ float2 red[8][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int groups_n = a.x_tiles / kWideTiles;         // (side by side: they read the same class weights)
-    const int vt = blockIdx.x / groups_n, t0 = kWideTiles * (blockIdx.x - vt * groups_n), v0 = 32 * vt;
+    const int groups_n = a.x_tiles / NT;                 // (side by side: they read the same class weights)
+    const int vt = blockIdx.x / groups_n, t0 = NT * (blockIdx.x - vt * groups_n), v0 = 32 * vt;
     const int row = lane & 31, half = lane >> 5;
     const float* const pw = (const float*)a.w + (long)(v0 + row < a.V ? v0 + row : a.V - 1) * a.w_pitch;
     const int steps = (a.D + kDirectK - 1) / kDirectK, whole = a.D / kDirectK;
-    v16f acc[kWideTiles];
+    v16f acc[NT];
 #pragma unroll
-    for (int j = 0; j < kWideTiles; ++j)
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
     Raw8<float> u[2];
-    d_bf16x8 x[2][3][kWideTiles];
+    d_bf16x8 x[2][3][NT];
     auto fetch_w = [&](int s) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -272,7 +274,7 @@ __global__ __launch_bounds__(256) void rows_wide_scores_kernel(DirectArgs a)
 #pragma unroll
             for (int i = 0; i < 3; ++i)
 #pragma unroll
-                for (int j = 0; j < kWideTiles; ++j)
+                for (int j = 0; j < NT; ++j)
                     x[k][i][j] = *reinterpret_cast<const d_bf16x8*>(a.x_split + (((long)(2 * s + k) * 3 + i) * a.x_tiles + t0 + j) * 1024 + 16 * lane);
     };
     fetch_w(wave);
@@ -285,7 +287,7 @@ __global__ __launch_bounds__(256) void rows_wide_scores_kernel(DirectArgs a)
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int j = 0; j < kWideTiles; ++j)
+            for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int sum = 2; sum >= 0; --sum)       // the smallest products first
 #pragma unroll
@@ -293,7 +295,7 @@ __global__ __launch_bounds__(256) void rows_wide_scores_kernel(DirectArgs a)
         fetch_x(s + 4);
     }
 #pragma unroll
-    for (int j = 0; j < kWideTiles; ++j) {
+    for (int j = 0; j < NT; ++j) {
         v4f s = direct_fold(acc[j], fold);
         const int n0 = 32 * (t0 + j), n = n0 + (tid & 31), m0 = v0 + 4 * (tid >> 5);
         const bool real = n < a.N;
