@@ -13,7 +13,7 @@
 // are rounded once.  A lane fetches its own operand, 8 k's of one row, a step (32 k's) ahead of the products; operands are fetched by every
 // wave that needs them (first-level cache).  Little work is bound by the trips to memory one after the other, some 0.7 us each, and
 // so a workgroup has one tile of 32 x 32 and its four waves deal the sum's steps among them; where there are tiles enough or the
-// sum has a step or two, each wave has a tile of its own (64 x 64 per workgroup).  213 x 100 x 37 fp32: 7.0 + 6.7 + 6.3 + 1.9 us.
+// sum has a step or two, each wave has a tile of its own (64 x 64 per workgroup).  213 x 100 x 37 fp32: 7.0 + 6.7 + 6.3 us.
 #pragma once
 #include "any_address.hpp"
 #include "kernels_rows_parts.hpp"
