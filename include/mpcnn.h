@@ -318,7 +318,8 @@ mpcnn_status mpcnn_sgd_step_list(const mpcnn_grad_list* list, double lr, double 
  *   dx_dev     [rows][dx_pitch] `dtype` (0 for rows that add nothing), dw_dev [classes][features]
  *              `dtype`, db_dev [classes] fp32.
  * Sums, scores and statistics are fp32 or wider; MPCNN_F32 products are made of fp16 parts (two per
- * number, three products: 22 bits, fewer of numbers below 2^-16 of their matrix's largest magnitude) or, where
+ * number, three products: 22 bits, fewer of features and class weights below 2^-16 of their matrix's largest
+ * magnitude and of the scores' derivatives p - [v = t] below 2^-28, which are off by up to 2^-49) or, where
  * there is little work, of three bf16 parts (24 bits); with MPCNN_BF16 the scores' derivative is rounded to
  * bf16 before it is multiplied (to two bf16 parts where there is little work), results once more.  Values that are not finite in rows that add something or in w
  * give results that are not finite.  The result does not depend on launch timing.

@@ -67,9 +67,9 @@ __global__ __launch_bounds__(1024) void rows_peak_kernel(PeakSet set)
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
-// Piece p (16 bytes) of the 128 (bf16) or 256 (parts) bytes that 64 numbers take; get(i) is the i-th of them, raised
+// Piece p (16 bytes) of the 128 (bf16) or 256 (parts) bytes that 64 numbers take; get(i) is the i-th of them, raised; second parts by low_up more
 template <bool HALVES, typename F>
-__device__ __forceinline__ v4f piece_of(int p, F get)
+__device__ __forceinline__ v4f piece_of(int p, F get, float low_up = 1.f)
 {
     if constexpr (HALVES) {
         f16x8_t v;
@@ -79,7 +79,7 @@ __device__ __forceinline__ v4f piece_of(int p, F get)
         for (int z = 0; z < 8; ++z) {
             const float x = get(at + z);
             const _Float16 h = (_Float16)x;
-            v[z] = low ? (_Float16)(x - (float)h) : h;
+            v[z] = low ? (_Float16)((x - (float)h) * low_up) : h;
         }
         return __builtin_bit_cast(v4f, v);
     } else {
@@ -341,8 +341,8 @@ __global__ __launch_bounds__(THREADS) void rows_join_kernel(JoinArgs a)
 }
 
 // ---- scores [classes][score_row] of a piece of the classes into the derivative p - [class = label], in blocks along the rows ([classes][out_bytes]):
-// with bf16 storage times the row's weight (rounded once), with fp32 storage raised by 2^14 (the weight follows: with the features, or behind the
-// product).  db_part: per tile of 64 rows the sums over them, weighted.
+// with bf16 storage times the row's weight (rounded once), with fp32 storage raised by 2^14, its second parts by kLowUp more (kernels_rows_product.hpp; the
+// weight follows: with the features, or behind the product).  db_part: per tile of 64 rows the sums over them, weighted.
 struct DeltaArgs {
     const float* scores;
     long score_row;
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(256) void rows_delta_kernel(DeltaArgs a)
             const int c = q / kPieces, p = q % kPieces;
             const long at = (long)blockIdx.x * (kPieces * 16) + 16 * p;
             if (v0 + c >= a.classes || at >= a.out_bytes) continue;
-            *reinterpret_cast<v4f*>(a.out + (long)(v0 + c) * a.out_bytes + at) = piece_of<HALVES>(p, [&](int i) { return HALVES ? tile[c][i] * 0x1p14f : tile[c][i]; });
+            *reinterpret_cast<v4f*>(a.out + (long)(v0 + c) * a.out_bytes + at) = piece_of<HALVES>(p, [&](int i) { return HALVES ? tile[c][i] * 0x1p14f : tile[c][i]; }, kLowUp);
         }
     if (a.db_part) {
         __syncthreads();

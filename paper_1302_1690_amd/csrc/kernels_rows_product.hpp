@@ -3,8 +3,11 @@
 //
 // Operands.  bf16 storage: as they are.  fp32 storage: two fp16 parts per number (x 2^e = h + l, ranges.hpp), which lie in turn,
 // 32 numbers' first parts and their second parts, so that one 128-byte block of a row is 64 bf16 numbers or 32 fp32 ones and the kernel's
-// fetches are the same; the products are h h', h l' and l h' (what is left out, l l', is below 2^-22 of a product).  k is padded with
-// zeros to whole blocks; rows beyond the last are not read (the last one is, again, and its results dropped).
+// fetches are the same; the products are h h', h l' and l h' (what is left out, l l', is below 2^-22 of a product).  The derivative is p for all but
+// the labels' classes, and with many classes most p are far below the scale that suits the labels' (numbers up to 1 are raised by 2^14): its second parts
+// are raised by 2^11 more (kLowUp), and what they are multiplied with, the first parts of the class weights or the features, is lowered by as much in
+// registers.  Then it keeps 22 bits down to 2^-28, and is off by at most 2^-49 below (without: 2^-17, 2^-39; a class that is nobody's label and has p = 1e-9 got a
+// gradient that was off by 1e-3).  k is padded with zeros to whole blocks; rows beyond the last are not read (the last one is, again, and its results dropped).
 //
 // A workgroup computes a tile of 32 WM MT x 32 WN NT results, each wave MT x NT of the instruction's, in accumulators.  Both operands' next
 // blocks come from memory straight into the LDS buffer that is not being multiplied (128 bits per lane, a barrier per block).  An LDS row is a
@@ -214,6 +217,13 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
     for (int i = 0; i < MT; ++i) group_a[i] = of_row * kARow + of_col + 64 * ((MT * wm + i) * (HALVES ? 2 : 1) ^ turn);
 #pragma unroll
     for (int j = 0; j < NT; ++j) group_b[j] = BM * kBlockBytes + of_row * kBRow + of_col + 64 * ((NT * wn + j) * (HALVES ? 2 : 1) ^ turn);
+    // fp32 gradients: by what the partners of A's second parts are lowered, where A is the derivative (else A has a peak of its own)
+    constexpr bool kGradient = HALVES && (RESULT == kStoreF32 || RESULT == kPart);
+    const _Float16 low = (_Float16)(kGradient && (RESULT == kStoreF32 || ACROSS || !a.a_peak) ? kLowDown : 1.f);
+    auto lower = [&](v4f (&y)[NT]) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) y[j] = __builtin_bit_cast(v4f, __builtin_bit_cast(f16x8, y[j]) * low);
+    };
     auto multiply = [&](const char* stage) {
         auto read = [&](int at, int s) { return *reinterpret_cast<const v4f*>(stage + at + 16 * ((2 * s + half) ^ mix)); };
         auto read_a = [&](int i, int s) { return read(at_a + i * 32 * kBlockBytes, s); };
@@ -251,8 +261,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
                     for (int j = 0; j < NT; ++j) lb[j] = pb[j] ^ 64;
                     product(x, y);
                     read_turned<kA, 4 * kARow, kB, 4 * kBRow>(xl, yl, la, lb);
-                    product(xl, y);
                     product(x, yl);
+                    lower(y);
+                    product(xl, y);
                 } else {
                     product(x, y);
                 }
@@ -275,9 +286,16 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 if (s == 0) load(1, 1);
-                product(xl[s], yh[s]);
-                product(xh[s], yl[s]);
-                product(xh[s], yh[s]);
+                if constexpr (kGradient) {     // (lowered in place: there are no registers for a copy)
+                    product(xh[s], yl[s]);
+                    product(xh[s], yh[s]);
+                    lower(yh[s]);
+                    product(xl[s], yh[s]);
+                } else {
+                    product(xl[s], yh[s]);
+                    product(xh[s], yl[s]);
+                    product(xh[s], yh[s]);
+                }
             }
         } else {
             v4f x[2][MT], y[2][NT];
@@ -434,7 +452,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
 #pragma unroll
                     for (int z = 0; z < 8; ++z) {
                         h[z] = (_Float16)v[z];
-                        l[z] = (_Float16)(v[z] - (float)h[z]);
+                        l[z] = (_Float16)((v[z] - (float)h[z]) * kLowUp);
                     }
                     char* const at32 = to + (n >> 5) * kBlockBytes + 2 * (n & 31);
                     *reinterpret_cast<f16x8*>(at32) = h;
