@@ -190,10 +190,11 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     if (train) bound(kRoom / p->Np);
     p->piece = piece;
     const int64_t pieces = (classes + piece - 1) / piece;
-    const int64_t N = p->N, D = p->D;
+    // (Np, not N, in what is planned from here on: the same for all rows of a block of 64, as most_bytes wants it)
+    const int64_t N = p->N, Np = p->Np, D = p->D;
     // The scores' sums over the features are split, too, where their tiles leave compute units without work.  us, split and summed / whole, bf16 1000 x 4096
     // x 2000 36 / 44, 200 x 4000 x 3000 26 / 46, 100 x 4096 x 20000 46 / 54; fp32 2469 x 3084 x 776 69 / 75, 1000 x 2048 x 2000 45 / 54.
-    p->sc = tiling_of(classes, N, p->d_bytes / mpcnn::kBlockBytes, pieces == 1 ? 16 : 1, p->halves);
+    p->sc = tiling_of(classes, Np, p->d_bytes / mpcnn::kBlockBytes, pieces == 1 ? 16 : 1, p->halves);
     p->stat_tiles = std::max((classes + 127) / 128 + pieces, (classes + mpcnn::kScoresSum - 1) / mpcnn::kScoresSum * (p->sc.splits > 1));
     p->score_part = take(p->sc.splits > 1 ? 4 * p->sc.splits * classes * N : 0);
     p->peaks = take(4 * 3 * mpcnn::kPeakGroups);
@@ -205,7 +206,7 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     p->x_rows = take(N * p->d_bytes);
     p->w_rows = take(piece * p->d_bytes);
     if (train) {
-        p->dx = tiling_of(N, D, p->v_blocks(piece), std::min<int64_t>(64, std::max<int64_t>(1, kPartRoom / (4 * N * D + 1))), p->halves);
+        p->dx = tiling_of(Np, D, p->v_blocks(piece), std::min<int64_t>(64, std::max<int64_t>(1, kPartRoom / (4 * Np * D))), p->halves);
         p->dw = tiling_of(piece, D, p->n_bytes / mpcnn::kBlockBytes, std::min<int64_t>(64, std::max<int64_t>(1, kPartRoom / (4 * piece * D))), p->halves);
         p->x_cols = take(D * p->n_bytes);
         if (p->keep) p->score = take(classes * p->Np * 4);
@@ -216,6 +217,27 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     }
     p->total = at;
     return true;
+}
+
+// What is enough for every call with at most so many rows.  The sizes of a plan do not only grow with the rows: at 17 a way ends that leaves shares of the
+// features' gradient, at the rows whose scores fill kRoom the scores are dropped (1000 features x 30011 classes, bf16: 35 MB for 16 rows, 10 MB for 17; 768 x 50257:
+// 1.7 GB for 5106, 0.7 GB for 6207).  So every plan that may be the largest is made: up to 64 rows each; beyond, the choices are the same for all
+// rows of a block of 32 (tiles of 32 rows, sums split in steps of 32, with little work) or of 64 (blocks and tiles, with much), and the sizes grow with the rows inside
+// one, so each block's last is looked at, and the last rows of little work.  20-50 us for 8192 rows.
+size_t most_bytes(int64_t rows, int64_t features, int64_t classes, int dtype, bool train)
+{
+    Plan p;
+    size_t most = 0;
+    auto look = [&](int64_t r) {
+        if (make_plan(r, features, classes, dtype, train, &p)) most = std::max(most, p.total);
+    };
+    look(rows);
+    if (!most) return 0;                                 // (bad sizes)
+    for (int64_t r = 0; r < std::min<int64_t>(rows, 65); ++r) look(r);
+    const int64_t little = (train ? kDirectWork : kDirectLossWork) / features / classes;
+    if (little < rows) look(little);
+    for (int64_t r = 96; r < rows; r = r < std::max(little, kWideRows) ? r + 32 : up_to(r + 1, 64)) look(r);
+    return most;
 }
 
 // ---- launches of the product
@@ -599,6 +621,11 @@ mpcnn_status checked(int64_t rows, int64_t features, int64_t classes, mpcnn_dtyp
 extern "C" {
 
 size_t mpcnn_workspace_bytes_class(int64_t rows, int64_t features, int64_t classes, mpcnn_dtype dtype, int training)
+{
+    return dtype == MPCNN_F32 || dtype == MPCNN_BF16 ? most_bytes(rows, features, classes, dtype, training != 0) : 0;
+}
+
+size_t mpcnn_workspace_bytes_class_call(int64_t rows, int64_t features, int64_t classes, mpcnn_dtype dtype, int training)
 {
     Plan p;
     if ((dtype != MPCNN_F32 && dtype != MPCNN_BF16) || !make_plan(rows, features, classes, dtype, training != 0, &p)) return 0;

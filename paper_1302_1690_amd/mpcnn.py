@@ -35,7 +35,7 @@ SYMBOLS = [
     "mpcnn_workspace_bytes_banded", "mpcnn_seg_backward_banded", "mpcnn_seg_forward_static",
     "mpcnn_plan_describe", "mpcnn_sgd_step_clipped", "mpcnn_grad_list_create", "mpcnn_grad_list_destroy",
     "mpcnn_grad_norm", "mpcnn_grad_clip", "mpcnn_sgd_step_list",
-    "mpcnn_workspace_bytes_class", "mpcnn_class_loss", "mpcnn_class_backward",
+    "mpcnn_workspace_bytes_class", "mpcnn_workspace_bytes_class_call", "mpcnn_class_loss", "mpcnn_class_backward",
 ]
 
 
@@ -122,8 +122,9 @@ def lib():
         L.mpcnn_grad_clip.argtypes = [vp, C.c_double, vp, vp]
         L.mpcnn_sgd_step_list.argtypes = [vp, C.c_double, C.c_double, C.c_double, vp, vp]
         l = C.c_int64
-        L.mpcnn_workspace_bytes_class.argtypes = [l, l, l, i, i]
-        L.mpcnn_workspace_bytes_class.restype = sz
+        for f in (L.mpcnn_workspace_bytes_class, L.mpcnn_workspace_bytes_class_call):
+            f.argtypes = [l, l, l, i, i]
+            f.restype = sz
         L.mpcnn_class_loss.argtypes = [vp, l, vp, l, vp, vp, vp, l, l, l, i, vp, vp, vp, vp, sz, vp]
         L.mpcnn_class_backward.argtypes = [vp, l, vp, l, vp, vp, vp, l, l, l, i, vp, vp, vp, l, vp, vp, vp, sz, vp]
         L.mpcnn_get_activation.argtypes = [vp, i, vp, sz]
@@ -526,6 +527,7 @@ class GradList:
 
 
 def class_workspace_bytes(rows: int, features: int, classes: int, dtype: int, training: bool) -> int:
+    """Bytes of workspace that are enough for class_loss (training: class_backward) on so many rows or fewer."""
     return lib().mpcnn_workspace_bytes_class(rows, features, classes, dtype, 1 if training else 0)
 
 
@@ -583,7 +585,7 @@ def _class_workspace(ws, args, training, device):
     """Address and bytes of the workspace, and what keeps it."""
     import torch
     if ws is None:
-        ws = torch.empty(max(256, lib().mpcnn_workspace_bytes_class(*args[7:], training)), dtype=torch.uint8, device=device)
+        ws = torch.empty(max(256, lib().mpcnn_workspace_bytes_class_call(*args[7:], training)), dtype=torch.uint8, device=device)
     elif ws.device != device or not ws.is_contiguous():
         _refuse("ws: contiguous memory on %s is wanted" % device)
     return ws.data_ptr(), ws.numel() * ws.element_size(), ws
