@@ -272,8 +272,9 @@ mpcnn_status mpcnn_sgd_step_clipped(mpcnn_net* net, double lr, double grad_scale
  *     MPCNN_F32 or MPCNN_BF16 (gradient and parameter types are independent), at any address that is a
  *     multiple of its element's size; n = 0 is allowed, and so is an empty list.  param_dev: NULL in
  *     all tensors, or in none.  Gradients may share memory with each other, and so may parameters (one
- *     weight used in two places, a gradient from each): such a list is updated tensor by tensor, in its
- *     order, a launch each; the norm counts each tensor.  Errors: EINVAL (null pointer, unknown type, a
+ *     weight used in two places, a gradient from each): tensors that a call writes and that share memory
+ *     are updated one after the other, in the list's order (a launch for each run of tensors that share
+ *     none); the norm counts each tensor.  Errors: EINVAL (null pointer, unknown type, a
  *     gradient that overlaps a parameter), ENOMEM, EHIP.
  *   mpcnn_grad_norm: *norm_dev = |grad_scale| * 2-norm over all gradients together.
  *   mpcnn_grad_clip: gradients *= min(1, max_norm / norm), rounded to their type; *norm_dev (may be

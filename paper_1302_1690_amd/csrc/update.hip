@@ -2,7 +2,9 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <iterator>
 #include <limits>
+#include <map>
 #include <memory>
 #include <new>
 #include <vector>
@@ -17,7 +19,9 @@ struct mpcnn_grad_list {
     long total = 0;
     int stretches = 0;
     bool params = false;
-    std::vector<int> starts;             // tensors that share memory: each one's first stretch, and the last one's end (else empty)
+    // The tensors in runs, in their order: none of a run shares memory with another of it that a call writes.  Each run's first stretch, and the last one's
+    // end, for calls that write the gradients and for those that write the parameters (empty: all tensors are one run).
+    std::vector<int> grad_runs, param_runs;
     mpcnn::Stretch* d_table = nullptr;   // and, behind it, the partial sums
     double* d_partial = nullptr;
 };
@@ -44,15 +48,15 @@ static void launch_mode(const UpdateArgs& a, int mode, unsigned groups, hipStrea
     else update_kernel<kStep, LONE><<<groups, threads, 0, st>>>(a);
 }
 
-void launch_update(UpdateArgs a, int mode, long total, const int* starts, int tensors, hipStream_t st)
+void launch_update(UpdateArgs a, int mode, long total, const int* starts, int runs, hipStream_t st)
 {
-    if (tensors && mode != kOnlyNorm) {
-        // tensors that share memory: the norm, then one tensor after the other
+    if (runs && mode != kOnlyNorm) {
+        // tensors that share memory: the norm, then one run after the other
         const int groups = (int)std::min<long>(kNormParts, ((long)a.stretches + 3) / 4);
         a.parts = groups;
         norm_parts_kernel<<<(unsigned)groups, 256, 0, st>>>(a);
         const Stretch* const table = a.table;
-        for (int i = 0; i < tensors; ++i) {
+        for (int i = 0; i < runs; ++i) {
             a.table = table + starts[i];
             a.stretches = starts[i + 1] - starts[i];
             launch_mode<false>(a, mode, (unsigned)std::min<long>(kNormParts, ((long)a.stretches + 3) / 4), st);
@@ -75,18 +79,32 @@ namespace {
 
 struct Range { uintptr_t at; uint64_t bytes; bool param; };
 
-// Whether two ranges of one kind overlap (`same`), and whether a gradient and a parameter do (`mixed`)
-void overlap(std::vector<Range>& r, bool* same, bool* mixed)
+// Whether two ranges of one kind overlap (same[param]), and whether a gradient and a parameter do (mixed)
+void overlap(std::vector<Range>& r, bool (&same)[2], bool* mixed)
 {
     std::sort(r.begin(), r.end(), [](const Range& x, const Range& y) { return x.at < y.at; });
     uintptr_t end[2] = {0, 0};           // of what has begun so far, gradients and parameters
-    *same = *mixed = false;
+    same[0] = same[1] = *mixed = false;
     for (const Range& x : r) {
-        *same = *same || x.at < end[x.param];
+        same[x.param] = same[x.param] || x.at < end[x.param];
         *mixed = *mixed || x.at < end[!x.param];
         end[x.param] = std::max<uintptr_t>(end[x.param], x.at + x.bytes);
     }
 }
+
+// The ranges of a run so far, which do not overlap, by where they begin
+struct Run {
+    std::map<uintptr_t, uintptr_t> ends;
+    // Whether a tensor at [at, end) has to begin a new run (and, if so, it has)
+    bool cut(uintptr_t at, uintptr_t end)
+    {
+        const auto next = ends.lower_bound(at);
+        const bool meets = (next != ends.end() && next->first < end) || (next != ends.begin() && std::prev(next)->second > at);
+        if (meets) ends.clear();
+        ends.emplace(at, end);
+        return meets;
+    }
+};
 
 bool known(int dtype) { return dtype == MPCNN_F32 || dtype == MPCNN_BF16; }
 uint64_t size_of(int dtype) { return dtype == MPCNN_BF16 ? 2 : 4; }
@@ -114,14 +132,20 @@ mpcnn_status make_list(const mpcnn_tensor* t, int count, mpcnn_grad_list** out)
         }
     }
     if (with && with != filled) return fail(MPCNN_EINVAL, "%d of %d tensors have parameters: all or none", with, filled);
-    bool same = false, mixed = false;
-    overlap(ranges, &same, &mixed);
+    bool same[2], mixed = false;
+    overlap(ranges, same, &mixed);
     if (mixed) return fail(MPCNN_EINVAL, "a gradient and a parameter overlap in memory");
     const unsigned len = mpcnn::stretch_length((long)total);
     std::vector<mpcnn::Stretch> table;
-    std::vector<int> starts;
+    std::vector<int> runs[2];
+    Run run[2];
     for (int i = 0; i < count; ++i) {
-        if (same && t[i].n) starts.push_back((int)table.size());
+        for (int k = 0; k < 2 && t[i].n; ++k) {
+            if (!same[k]) continue;
+            const uintptr_t at = (uintptr_t)(k ? t[i].param_dev : t[i].grad_dev);
+            const bool cut = run[k].cut(at, at + t[i].n * size_of(k ? t[i].param_dtype : t[i].grad_dtype));
+            if (cut || runs[k].empty()) runs[k].push_back((int)table.size());
+        }
         for (int64_t at = 0; at < t[i].n; at += len) {
             mpcnn::Stretch s{};
             s.grad = (char*)t[i].grad_dev + at * (int64_t)size_of(t[i].grad_dtype);
@@ -134,10 +158,12 @@ mpcnn_status make_list(const mpcnn_tensor* t, int count, mpcnn_grad_list** out)
             table.push_back(s);
         }
     }
-    if (same) starts.push_back((int)table.size());
+    for (int k = 0; k < 2; ++k)
+        if (same[k]) runs[k].push_back((int)table.size());
     if (table.size() > (size_t)1 << 30) return fail(MPCNN_EINVAL, "too many tensors: %d", count);
     std::unique_ptr<mpcnn_grad_list> l(new mpcnn_grad_list);
-    l->starts = std::move(starts);
+    l->grad_runs = std::move(runs[0]);
+    l->param_runs = std::move(runs[1]);
     l->total = (long)total;
     l->stretches = (int)table.size();
     l->params = with > 0;
@@ -176,7 +202,8 @@ mpcnn_status update(const mpcnn_grad_list* l, int mode, double rate, double scal
     a.scale = std::fabs(scale);
     a.bound = bound;
     a.rate = rate * scale;
-    mpcnn::launch_update(a, mode, l->total, l->starts.data(), l->starts.empty() ? 0 : (int)l->starts.size() - 1, (hipStream_t)stream);
+    const std::vector<int>& runs = mode == mpcnn::kClip ? l->grad_runs : l->param_runs;
+    mpcnn::launch_update(a, mode, l->total, runs.data(), runs.empty() ? 0 : (int)runs.size() - 1, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
     return MPCNN_OK;
 }

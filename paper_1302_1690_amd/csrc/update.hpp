@@ -33,8 +33,8 @@ enum { kOnlyNorm = 0, kClip = 1, kStep = 2 };
 bool rate_fits(double rate, double scale);
 // Stretch length for so many numbers in all: enough stretches for every wave that can run, none shorter than one fetch
 unsigned stretch_length(long total);
-// mode: kOnlyNorm, kClip, kStep; fills in a.parts.  `total`: numbers in all.  Tensors that share memory are updated one after the other, in the
-// list's order: starts[0 .. tensors] are their stretches (tensors = 0: none do).
-void launch_update(UpdateArgs a, int mode, long total, const int* starts, int tensors, hipStream_t st);
+// mode: kOnlyNorm, kClip, kStep; fills in a.parts.  `total`: numbers in all.  Where tensors that are written share memory, they are updated in runs, one
+// after the other, in the list's order: starts[0 .. runs] are the runs' stretches (runs = 0: no two do).
+void launch_update(UpdateArgs a, int mode, long total, const int* starts, int runs, hipStream_t st);
 
 }  // namespace mpcnn
