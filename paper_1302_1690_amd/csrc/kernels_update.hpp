@@ -8,6 +8,9 @@
 // waves in stretches of at most kStretch numbers of one tensor, dealt out in the list's order.  A tensor may start at any element:
 // lanes fetch 8 numbers as one or two 128-bit words at whatever address they have.
 //
+// The factor c, or rate s c, is rounded to fp32 once.  Below fp32's normal numbers it would lose bits there, or all of them (gradients of 1e38 clipped to a norm of
+// 1): then it is taken as `lift` = 2^-126, by which gradients are multiplied first, exactly where it matters, and what is left of it.
+//
 // A norm that is not finite (an infinity or NaN among the gradients) changes nothing: gradients and parameters stay as they were.
 //
 // Bound by the passes over memory: one for the norm, two more for clipping (none where the norm is within the bound: the gradients
@@ -61,7 +64,7 @@ __device__ __forceinline__ double squares(const G* g, unsigned n, unsigned lane)
 }
 
 template <typename G>
-__device__ __forceinline__ void scale_down(G* g, unsigned n, unsigned lane, float c)
+__device__ __forceinline__ void scale_down(G* g, unsigned n, unsigned lane, float c, float lift)
 {
     unsigned i = 8 * lane;
     for (; i + 3 * 512 + 8 <= n; i += 4 * 512) {
@@ -69,31 +72,31 @@ __device__ __forceinline__ void scale_down(G* g, unsigned n, unsigned lane, floa
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = load8(g + i + 512 * q);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) store8(g + i + 512 * q, v[q] * c);
+        for (int q = 0; q < 4; ++q) store8(g + i + 512 * q, v[q] * lift * c);
     }
-    for (; i + 8 <= n; i += 512) store8(g + i, load8(g + i) * c);
+    for (; i + 8 <= n; i += 512) store8(g + i, load8(g + i) * lift * c);
     const unsigned t = (n & ~7u) + lane;
-    if (t < n) store1(g + t, load1(g + t) * c);
+    if (t < n) store1(g + t, load1(g + t) * lift * c);
 }
 
-__device__ __forceinline__ v8f moved(v8f p, v8f g, float f)
+__device__ __forceinline__ v8f moved(v8f p, v8f g, float f, float lift)
 {
 #pragma unroll
-    for (int z = 0; z < 8; ++z) p[z] = fmaf(-f, g[z], p[z]);
+    for (int z = 0; z < 8; ++z) p[z] = fmaf(-f, g[z] * lift, p[z]);
     return p;
 }
 template <typename G, typename P>
-__device__ __forceinline__ void step_down(const G* g, P* p, unsigned n, unsigned lane, float f)
+__device__ __forceinline__ void step_down(const G* g, P* p, unsigned n, unsigned lane, float f, float lift)
 {
     unsigned i = 8 * lane;
     for (; i + 512 + 8 <= n; i += 2 * 512) {
         const v8f g0 = load8(g + i), g1 = load8(g + i + 512), p0 = load8(p + i), p1 = load8(p + i + 512);
-        store8(p + i, moved(p0, g0, f));
-        store8(p + i + 512, moved(p1, g1, f));
+        store8(p + i, moved(p0, g0, f, lift));
+        store8(p + i + 512, moved(p1, g1, f, lift));
     }
-    for (; i + 8 <= n; i += 512) store8(p + i, moved(load8(p + i), load8(g + i), f));
+    for (; i + 8 <= n; i += 512) store8(p + i, moved(load8(p + i), load8(g + i), f, lift));
     const unsigned t = (n & ~7u) + lane;
-    if (t < n) store1(p + t, fmaf(-f, load1(g + t), load1(p + t)));
+    if (t < n) store1(p + t, fmaf(-f, load1(g + t) * lift, load1(p + t)));
 }
 
 // Sum over the workgroup's threads in a fixed order; the result in every thread
@@ -155,19 +158,21 @@ __global__ __launch_bounds__(LONE ? 1024 : 256) void update_kernel(UpdateArgs a)
     if (!(norm < __builtin_inf())) return;                   // (NaN too)
     const double c = norm > a.bound ? a.bound / norm : 1.0;
     if (MODE == kClip && c == 1.0) return;
-    const float f = MODE == kClip ? (float)c : (float)(c * a.rate);   // one rounding; the product with a gradient is the next
+    const double factor = MODE == kClip ? c : c * a.rate;
+    const bool low = fabs(factor) < 0x1p-126;
+    const float f = (float)(low ? factor * 0x1p126 : factor), lift = low ? 0x1p-126f : 1.f;   // one rounding; the product with a gradient is the next
     const int first = (int)blockIdx.x * WAVES + wave, by = (int)gridDim.x * WAVES;
     for (int i = first; i < a.stretches; i += by) {
         const Stretch t = stretch_at(a, LONE ? i : a.stretches - 1 - i);   // (from the end on)
         if constexpr (MODE == kClip) {
-            if (t.grad_bf16) scale_down((bf16*)t.grad, t.n, lane, f);
-            else scale_down((float*)t.grad, t.n, lane, f);
+            if (t.grad_bf16) scale_down((bf16*)t.grad, t.n, lane, f, lift);
+            else scale_down((float*)t.grad, t.n, lane, f, lift);
         } else if (t.grad_bf16) {
-            if (t.param_bf16) step_down((const bf16*)t.grad, (bf16*)t.param, t.n, lane, f);
-            else step_down((const bf16*)t.grad, (float*)t.param, t.n, lane, f);
+            if (t.param_bf16) step_down((const bf16*)t.grad, (bf16*)t.param, t.n, lane, f, lift);
+            else step_down((const bf16*)t.grad, (float*)t.param, t.n, lane, f, lift);
         } else {
-            if (t.param_bf16) step_down((const float*)t.grad, (bf16*)t.param, t.n, lane, f);
-            else step_down((const float*)t.grad, (float*)t.param, t.n, lane, f);
+            if (t.param_bf16) step_down((const float*)t.grad, (bf16*)t.param, t.n, lane, f, lift);
+            else step_down((const float*)t.grad, (float*)t.param, t.n, lane, f, lift);
         }
     }
 }
