@@ -295,15 +295,23 @@ __global__ __launch_bounds__(THREADS) void rows_join_kernel(JoinArgs a)
     };
     float2 s{kNone, 0.f};
     if (n < a.N) {
+        // (fp64: of hundreds of millions of classes there are a hundred thousand tiles a thread, each below half a step of an fp32 sum that has one likely class)
+        double sum = 0.0;
+        auto add = [&](float2 o) {
+            const float top = fmaxf(s.x, o.x), base = top == kNone ? 0.f : top;
+            sum = fma(sum, (double)__expf(s.x - base), (double)(o.y * __expf(o.x - base)));
+            s.x = top;
+        };
         int t = deal;
         for (; t + 7 * DEALS < a.tiles; t += 8 * DEALS) {
             float2 v[8];
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] = a.stats[(long)(t + DEALS * q) * a.N + n];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) s = join(s, v[q]);
+            for (int q = 0; q < 8; ++q) add(v[q]);
         }
-        for (; t < a.tiles; t += DEALS) s = join(s, a.stats[(long)t * a.N + n]);
+        for (; t < a.tiles; t += DEALS) add(a.stats[(long)t * a.N + n]);
+        s.y = (float)sum;
     }
     red[deal][own] = s;
     __syncthreads();
