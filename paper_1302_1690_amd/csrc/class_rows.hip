@@ -34,6 +34,9 @@ constexpr int64_t kWeightRoom = (int64_t)512 << 20;    // bytes of a piece's cla
 constexpr int64_t kPartRoom = (int64_t)256 << 20;      // bytes of a product's partial sums
 constexpr int kMaxPiece = 1 << 20;
 constexpr int kCUs = 256;
+// A launch has less than 2^32 threads (of workgroups of 256: less than kMostGroups of them) and its grid's second side less than 2^16.  Products of this many
+// results stay below that with tiles of either size (128 x 128: half of it).
+constexpr int64_t kMostGroups = 1 << 24, kMostSide = (1 << 16) - 1, kMostResults = (int64_t)1 << 37;
 
 inline int64_t up_to(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
 
@@ -95,7 +98,7 @@ struct Plan {
     int N, D;
     int64_t V, Np;                       // Np: rows, padded to whole blocks
     int64_t d_bytes, n_bytes;            // a row of blocks along the features, along the rows
-    int64_t piece;                       // classes
+    int64_t piece, most_piece;           // classes; where the class weights are read as they are and no derivative is kept
     int64_t stat_tiles;
     Tiling dx, dw;                       // of a whole piece
     Tiling sc;                           // of the scores, where there is one piece
@@ -130,6 +133,11 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
         else if (rows <= 2) p->few_scores = classes >= 24576;
         else p->few_scores = rows <= mpcnn::kFewScoreRows && classes >= kFewWeights[rows <= 4 ? 0 : 1] / features;
     }
+    // what its launches cannot have is much work's, in pieces: 2^28 fp32 classes (of more than 64 rows; of more than 12, 2^29) or 2^30 bf16 ones, the
+    // derivative of the last few of 2^22
+    const int64_t score_groups = p->wide ? (classes + 31) / 32 * (rows <= 32 ? 1 : up_to(rows, 64) / 64) : (classes + 63) / 64;
+    if (!p->few_scores && score_groups >= kMostGroups) p->direct = false;
+    if (train && !p->few && (classes + mpcnn::kDeltaSide - 1) / mpcnn::kDeltaSide > kMostSide) p->direct = false;
     if (p->direct) {
         // a tile of 32 x 32 for four waves, one of 64 x 64 where that gives every compute unit two workgroups or the sum has one step
         auto deal_of = [](int64_t m, int64_t n, int64_t k) { return (m + 63) / 64 * ((n + 63) / 64) >= 2 * kCUs || k <= mpcnn::kDirectK ? 1 : 4; };
@@ -159,33 +167,32 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
             const int64_t n = std::min(most, std::max<int64_t>(1, 4 * kCUs / std::max<int64_t>(1, all)));
             g.each = (int)up_to(std::max<int64_t>(1, (K + n - 1) / n), step);
             g.splits = (int)std::max<int64_t>(1, (K + g.each - 1) / g.each);
-            return all * g.splits;
         };
-        const int64_t groups = grads(p->gx, rows, classes) + grads(p->gw, classes, rows);
-        if (groups < 0x7fffffff) {
-            p->stat_tiles = std::max<int64_t>(p->score_v, (classes + 127) / 128);   // (of the block product at most)
-            p->stats = take(8 * p->stat_tiles * rows);
-            p->label_score = take(4 * rows);
-            p->lse = take(4 * p->Np);
-            p->weight = take(4 * p->Np);
-            p->loss_part = take(8 * (p->Np + 1));
-            if (p->wide) p->x_split = take(up_to(rows, rows <= 32 ? 32 : 64) * up_to(features, mpcnn::kDirectK) * 6);
-            if (p->few) {
-                p->score = take(4 * classes * p->Np);
-                p->dx_part = take(4 * (int64_t)p->grad_groups * rows * features);
-            } else if (train) {
-                p->score = take(4 * classes * p->Np);
-                p->dx_part = take(p->gx.splits > 1 ? 4 * p->gx.splits * rows * features : 0);
-                p->dw_part = take(p->gw.splits > 1 ? 4 * p->gw.splits * classes * features : 0);
-                p->db_part = take(4 * classes * ((rows + 63) / 64));
-            }
-            p->total = at;
-            return true;
+        grads(p->gx, rows, classes);
+        grads(p->gw, classes, rows);
+        p->stat_tiles = std::max<int64_t>(p->score_v, (classes + 127) / 128);   // (of the block product at most)
+        p->stats = take(8 * p->stat_tiles * rows);
+        p->label_score = take(4 * rows);
+        p->lse = take(4 * p->Np);
+        p->weight = take(4 * p->Np);
+        p->loss_part = take(8 * (p->Np + 1));
+        if (p->wide) p->x_split = take(up_to(rows, rows <= 32 ? 32 : 64) * up_to(features, mpcnn::kDirectK) * 6);
+        if (p->few) {
+            p->score = take(4 * classes * p->Np);
+            p->dx_part = take(4 * (int64_t)p->grad_groups * rows * features);
+        } else if (train) {
+            p->score = take(4 * classes * p->Np);
+            p->dx_part = take(p->gx.splits > 1 ? 4 * p->gx.splits * rows * features : 0);
+            p->dw_part = take(p->gw.splits > 1 ? 4 * p->gw.splits * classes * features : 0);
+            p->db_part = take(4 * classes * ((rows + 63) / 64));
         }
-        p->direct = false;
+        p->total = at;
+        return true;
     }
     int64_t piece = std::min<int64_t>(classes, kMaxPiece);
     auto bound = [&](int64_t most) { if (piece > most) piece = std::max<int64_t>(256, most / 256 * 256); };
+    bound(kMostResults / p->Np);
+    p->most_piece = piece;
     bound(kWeightRoom / p->d_bytes);
     if (train) bound(kRoom / p->Np);
     p->piece = piece;
@@ -452,7 +459,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         pack(c.x, c.x_pitch, p.N, x_direct ? nullptr : ws + p.x_rows, p.train ? ws + p.x_cols : nullptr, p.n_bytes, mask, x_peak);
 
     // a piece's scores, or what becomes of them
-    const int64_t piece = !p.train && w_direct ? std::min<int64_t>(p.V, kMaxPiece) : p.piece;
+    const int64_t piece = !p.train && w_direct ? p.most_piece : p.piece;
     const int d_blocks = (int)(p.d_bytes / mpcnn::kBlockBytes);
     int done = 0;                                        // tiles of classes
     auto scores = [&](int64_t v0, int64_t n_classes, const char* w_rows, int64_t w_row, mpcnn::ProductArgs a, bool delta) {

@@ -1,4 +1,4 @@
-"""The class layer on rows at the most classes that launches can be made for, against the formulas in 64 bits.
+"""The class layer on rows at the most classes and results that launches can be made for, and beyond (work in pieces), against the formulas in 64 bits.
 
 Tolerances, u = 2^-24.  A score s = x . w + bias with S = sum |x w|: (features + 4) u S + 2 u |s|, in fp32 2^-20 S more (parts: 3 2^-22, and 2^-38 of the largest x
 and w times the features).  lse: a number of the sum passes 64 additions in its tile, then those of the joins, of which one of at least 64 threads makes
@@ -29,7 +29,8 @@ def _e_lse(lse, size, features, classes, dtype):
     return ((features + 4) * U + (2.0 ** -20 if dtype == F else 0)) * size + (classes / 128 / 64 + 128) * U + 8 * U * (lse.abs() + 1)
 
 
-@pytest.mark.parametrize("dtype,rows,classes", [(F, 70, (1 << 28) - 64), (B, 14, (1 << 30) - 64)], ids=["f32-70-below", "bf16-14-below"])
+@pytest.mark.parametrize("dtype,rows,classes", [(F, 13, (1 << 29) + 5), (F, 70, (1 << 28) + 5), (F, 70, (1 << 28) - 64), (B, 13, (1 << 30) + 7), (B, 14, (1 << 30) - 64)],
+                         ids=["f32-13", "f32-70", "f32-70-below", "bf16-13", "bf16-14-below"])
 def test_loss_over_hundreds_of_millions_of_classes(dtype, rows, classes):
     gen = torch.Generator(device="cuda").manual_seed(rows)
     w = torch.empty((classes, 1), dtype=dtype, device="cuda").normal_(generator=gen)
@@ -45,4 +46,56 @@ def test_loss_over_hundreds_of_millions_of_classes(dtype, rows, classes):
     assert ((rowloss.double() - nll).abs() <= 2 * e).all()
     assert abs(loss.item() - rowloss.double().sum().item()) <= 1e-12 * rowloss.double().abs().sum().item()
     del w
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [F, B], ids=["f32", "bf16"])
+@pytest.mark.parametrize("classes", [(1 << 22) - 64, (1 << 22) - 63, 1 << 22])
+def test_gradients_over_four_million_classes(classes, dtype):
+    rows, features = 20, 3
+    gen = torch.Generator(device="cuda").manual_seed(classes)
+    x = torch.randn((rows, features), generator=gen, device="cuda").to(dtype)
+    w = (torch.randn((classes, features), generator=gen, device="cuda") * 0.5).to(dtype)
+    labels = torch.randint(0, classes, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    labels[0], labels[1] = 0, classes - 1
+    loss, rowloss, dx, dw, db = mpcnn.class_backward(x, w, labels, db=torch.empty(classes, device="cuda"))
+    lse, size = _lse(x, w)
+    e_lse = _e_lse(lse, size, features, classes, dtype)
+    x64, w64 = x.double(), w.double()
+    nll = lse - (x64 * w64[labels.long()]).sum(1)
+    assert ((rowloss.double() - nll).abs() <= 2 * e_lse).all()
+    p = torch.exp(x64 @ w64.t() - lse[:, None])
+    e_p = 4 * float(e_lse.max()) + 8 * U * 40 + (2.0 ** -22 if dtype == F else 2.0 ** -8)
+    floor = 2.0 ** -49 if dtype == F else 0.0
+    at = torch.arange(rows, device="cuda")
+    g = p.clone()
+    g[at, labels.long()] -= 1
+    rounding = U if dtype == F else 2.0 ** -8
+    # the label's own derivative is p - 1: another u, and what it is rounded to
+    hot = torch.zeros_like(p)
+    hot[at, labels.long()] = 2 * U + (2.0 ** -22 if dtype == F else 2.0 ** -8)
+    e = p * e_p + floor + hot
+    want = g.t() @ x64
+    assert ((dw.double() - want).abs() <= (e + rows * U * g.abs()).t() @ x64.abs() * 1.01 + (rounding + 2.0 ** -21) * (g.abs().t() @ x64.abs())).all()
+    assert ((db.double() - g.sum(0)).abs() <= e.sum(0) + (rows + 2) * U * g.abs().sum(0)).all()
+    # (sums over the classes: an accumulator takes 16 of them at a time, fp32's in three products)
+    want, terms = g @ w64, g.abs() @ w64.abs()
+    assert ((dx.double() - want).abs() <= e @ w64.abs() + (3 * classes / 16 * U + 2.0 ** -21 + rounding) * terms).all()
+
+
+def test_a_million_classes_on_half_a_million_rows():
+    rows, features, classes = (1 << 19) + 77, 64, (1 << 20) + 300
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    x = (torch.randn((rows, features), generator=gen, device="cuda")).to(B)
+    w = (torch.randn((classes, features), generator=gen, device="cuda") * 0.25).to(B)
+    labels = torch.randint(0, classes, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    loss, rowloss, lse = mpcnn.class_loss(x, w, labels)
+    some = torch.cat([torch.arange(40, device="cuda"), torch.randint(0, rows, (100,), generator=gen, device="cuda"), torch.arange(rows - 40, rows, device="cuda")])
+    want, size = _lse(x[some], w)
+    e = _e_lse(want, size, features, classes, B)
+    assert ((lse[some].double() - want).abs() <= e).all()
+    nll = want - (x[some].double() * w[labels[some].long()].double()).sum(1)
+    assert ((rowloss[some].double() - nll).abs() <= 2 * e).all()
+    assert abs(loss.item() - rowloss.double().sum().item()) <= 1e-12 * rowloss.double().abs().sum().item()
+    assert torch.isfinite(lse).all() and float(lse.min()) > 10
     torch.cuda.empty_cache()
