@@ -36,8 +36,8 @@ __global__ __launch_bounds__(1024) void rows_peak_kernel(PeakSet set)
             peak = weight != 0.f && b < kNoPeak && b > peak ? b : peak;
         }
     };
-    // eight numbers of a row at a time, four times eight in flight; rows without gaps are one
-    const bool one = a.pitch == a.cols && !a.mask.labels && a.rows * a.cols < 0x7fffffff;
+    // eight numbers of a row at a time, four times eight in flight; rows without gaps are one (whose last eight numbers' end is a 32-bit number, too)
+    const bool one = a.pitch == a.cols && !a.mask.labels && a.rows * a.cols <= 0x7fffffff - 8;
     const long cols = one ? a.rows * a.cols : a.cols, rows = one ? 1 : a.rows;
     const long octets = (cols + 7) / 8, all = rows * octets, step = (long)gridDim.x * 1024;
     for (long e = (long)blockIdx.x * 1024 + threadIdx.x; e < all; e += 4 * step) {

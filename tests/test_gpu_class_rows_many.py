@@ -99,3 +99,25 @@ def test_a_million_classes_on_half_a_million_rows():
     assert abs(loss.item() - rowloss.double().sum().item()) <= 1e-12 * rowloss.double().abs().sum().item()
     assert torch.isfinite(lse).all() and float(lse.min()) > 10
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("classes", [1073741819, 1073741820, 1073741821])
+def test_weights_of_nearly_2_to_the_31_numbers(classes):
+    """What lies behind them is no part of their largest magnitude."""
+    rows, features = 129, 2
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    flat = torch.empty(classes * features + 64, device="cuda").normal_(generator=gen)
+    flat[classes * features:] = 1e30
+    w = flat[:classes * features].view(classes, features)
+    x = torch.randn((rows, features), generator=gen, device="cuda")
+    labels = torch.randint(0, classes, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    labels[3] = classes - 1
+    loss, rowloss, lse = mpcnn.class_loss(x, w, labels)
+    some = torch.tensor([0, 1, 3, 64, 127, 128], device="cuda")
+    want, size = _lse(x[some], w)
+    e = _e_lse(want, size, features, classes, F)
+    assert ((lse[some].double() - want).abs() <= e).all()
+    nll = want - (x[some].double() * w[labels[some].long()].double()).sum(1)
+    assert ((rowloss[some].double() - nll).abs() <= 2 * e).all()
+    del flat, w
+    torch.cuda.empty_cache()
