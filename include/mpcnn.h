@@ -282,7 +282,8 @@ mpcnn_status mpcnn_sgd_step_clipped(mpcnn_net* net, double lr, double grad_scale
  *   mpcnn_sgd_step_list: parameters -= lr * grad_scale * c * gradient, c as in mpcnn_sgd_step_clipped,
  *     computed in fp32 and rounded once; gradients are not written.
  * Norms, bounds and what is not finite: as in mpcnn_sgd_step_clipped.  One list must not be used from
- * two streams at once.  Errors: EINVAL (also: another device is current, a step without parameters), EHIP.
+ * two streams at once.  Errors: EINVAL (also: another device is current, a step without parameters, norm_dev
+ * inside one of the tensors), EHIP.
  */
 typedef struct {
     void* grad_dev;

@@ -7,6 +7,7 @@
 #include <map>
 #include <memory>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "kernels_update.hpp"
@@ -22,6 +23,7 @@ struct mpcnn_grad_list {
     // The tensors in runs, in their order: none of a run shares memory with another of it that a call writes.  Each run's first stretch, and the last one's
     // end, for calls that write the gradients and for those that write the parameters (empty: all tensors are one run).
     std::vector<int> grad_runs, param_runs;
+    std::vector<std::pair<uintptr_t, uintptr_t>> held;   // the tensors' memory: begins and ends, in order, none meeting the next
     mpcnn::Stretch* d_table = nullptr;   // and, behind it, the partial sums
     double* d_partial = nullptr;
 };
@@ -164,6 +166,10 @@ mpcnn_status make_list(const mpcnn_tensor* t, int count, mpcnn_grad_list** out)
     std::unique_ptr<mpcnn_grad_list> l(new mpcnn_grad_list);
     l->grad_runs = std::move(runs[0]);
     l->param_runs = std::move(runs[1]);
+    for (const Range& r : ranges) {          // (sorted)
+        if (!l->held.empty() && r.at <= l->held.back().second) l->held.back().second = std::max(l->held.back().second, r.at + r.bytes);
+        else l->held.emplace_back(r.at, r.at + r.bytes);
+    }
     l->total = (long)total;
     l->stretches = (int)table.size();
     l->params = with > 0;
@@ -183,11 +189,20 @@ mpcnn_status make_list(const mpcnn_tensor* t, int count, mpcnn_grad_list** out)
     return MPCNN_OK;
 }
 
+// Whether the fp64 number at `norm` lies in the tensors' memory, in part or whole
+bool holds(const mpcnn_grad_list* l, const double* norm)
+{
+    const uintptr_t at = (uintptr_t)norm, end = at + sizeof *norm;
+    const auto next = std::lower_bound(l->held.begin(), l->held.end(), at, [](const auto& r, uintptr_t x) { return r.second <= x; });
+    return next != l->held.end() && next->first < end;
+}
+
 mpcnn_status update(const mpcnn_grad_list* l, int mode, double rate, double scale, double bound, double* norm, void* stream)
 {
     if (!l) return fail(MPCNN_EINVAL, "null list");
     if (mode == mpcnn::kOnlyNorm && !norm) return fail(MPCNN_EINVAL, "null argument");
     if ((uintptr_t)norm % sizeof(double)) return fail(MPCNN_EINVAL, "norm's address is no multiple of its size");
+    if (norm && holds(l, norm)) return fail(MPCNN_EINVAL, "norm lies in one of the tensors");
     if (!mpcnn::rate_fits(rate, scale)) return fail(MPCNN_EINVAL, "scale %g, rate %g", scale, rate);
     if (!(bound > 0.0)) return fail(MPCNN_EINVAL, "max_norm = %g", bound);
     if (mode == mpcnn::kStep && l->stretches && !l->params) return fail(MPCNN_EINVAL, "the list has no parameters");
