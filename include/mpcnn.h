@@ -324,7 +324,8 @@ mpcnn_status mpcnn_sgd_step_list(const mpcnn_grad_list* list, double lr, double 
  * magnitude and of the scores' derivatives p - [v = t] below 2^-28, which are off by up to 2^-49) or, where
  * there is little work, of three bf16 parts (24 bits); with MPCNN_BF16 the scores' derivative is rounded to
  * bf16 before it is multiplied (to two bf16 parts where there is little work), results once more.  Values that are not finite in rows that add something or in w
- * give results that are not finite.  The result does not depend on launch timing.
+ * give results that are not finite.  The result does not depend on launch timing.  The two calls may take
+ * the same rows' scores by different kernels: their losses can differ in the last bits.
  *   ws_dev: 256-byte aligned scratch.  mpcnn_workspace_bytes_class: what is enough for every call with at
  *              most so many rows (it never shrinks when the rows grow; up to 50 us for 8192 rows, 5 ms for 2^20:
  *              ask once).  mpcnn_workspace_bytes_class_call: what a call with exactly so many rows needs,

@@ -72,20 +72,27 @@ Tiling tiling_of(int64_t M, int64_t N, int64_t blocks, int64_t most_splits, bool
     return best;
 }
 
-// Three to five launches (kernels_rows_direct.hpp) instead of a dozen: up to this much work, rows x features x classes, and up to more with few rows.
-// Microseconds, there / here, fp32 and bf16: gradients of 1000 x 1000 x 1000 (1e9) 109 / 114 and 63 / 73, of 1000 x 200 x 1000 (2e8) 49 / 88 and 34 / 68,
+// Two to six launches (kernels_rows_direct.hpp) instead of a dozen: up to this much work, rows x features x classes, and up to more with few rows.
+// Microseconds a call, in few launches / as much work, fp32 and bf16: gradients of 1000 x 1000 x 1000 (1e9) 109 / 114 and 63 / 73, of 1000 x 200 x 1000 (2e8) 49 / 88 and 34 / 68,
 // of 3000 x 500 x 1000 (1.5e9) 154 / 120 and 90 / 77; the loss of 1000 x 1000 x 2000 (2e9) 66 / 55 and 34 / 33, of 4000 x 2000 x 200
 // (1.6e9) 62 / 78 and 40 / 46; gradients of 20 x 4000 x 20000 (1.6e9) 336 / 586 and 170 / 274, of 40 x 1000 x 100000 (4e9) 699 / 818
 // and 382 / 374, of 64 x 4096 x 8000 (2e9) 203 / 335 and 149 / 124.
 constexpr int64_t kDirectWork = 1200000000, kDirectLossWork = 2000000000, kDirectFewRows = 64, kDirectFewWork[2] = {4000000000, 1600000000};
 
+// Classes from which on gradients are rows_few_grads', of up to 4 rows and of up to 16.  us a call, there / in tiles (kernels_rows_direct.hpp), fp32 and bf16:
+// 4 x 1000 x 512 27 / 25 and 27 / 24, x 1024 28 / 29 and 27 / 28, x 2048 30 / 35 and 27 / 30; 5 x 1000 x 4096 38 / 39 and 33 / 32, 8 x 1000 x 2048 36 / 36 and 29 / 30,
+// x 4096 47 / 40 and 38 / 32, x 8192 54 / 51 and 39 / 41, x 16384 69 / 74 and 44 / 58; 12 x 200 x 4096 28 / 31 and 27 / 30; 16 x 1000 x 4096 47 / 40 and 44 / 33, x 16384 69 / 74
+// and 56 / 59; 16 x 4096 x 4096 81 / 87 and 65 / 68.  And classes from which on scores are rows_few_scores': the first of up to 3 fp32 rows, the second of more, and of up to
+// 2 bf16 rows (times in kernels_rows_few.hpp).
+constexpr int64_t kFewClasses[2] = {1024, 4096}, kFewScoreClasses[2] = {1024, 24576};
+
 // bf16 class weights from which on the scores of up to 4 and of up to 12 rows are the vector ALU's, too (fewer come from the last-level cache fast enough;
 // times in kernels_rows_few.hpp)
 constexpr int64_t kFewWeights[2] = {70000000, 150000000};
 
-// fp32 class weights from which on the scores of 9 to so many rows are rows_wide_scores_kernel's (but for those that are rows_few_scores').  us, with it /
-// before (rows_direct_scores or, with more work, weights brought into blocks): 16 x 4096 x 50000 260 / 455, 32 x 4096 x 50000 265 / 870,
-// 64 x 4096 x 50000 333 / 860, 100 x 4096 x 20000 225 / 320, 128 x 4096 x 50000 538 / 894, 32 x 1000 x 20000 44 / 47, 64 x 1000 x 20000 57 / 68,
+// fp32 class weights from which on the scores of 9 to so many rows are rows_wide_scores_kernel's (but for those that are rows_few_scores').  us a call of the
+// loss, with it / without (rows_direct_scores or, with more work, weights brought into blocks): 16 x 4096 x 50000 260 / 455, 32 x 4096 x 50000 265 / 870,
+// 64 x 4096 x 50000 310 / 860, 100 x 4096 x 20000 225 / 320, 128 x 4096 x 50000 538 / 894, 32 x 1000 x 20000 44 / 47, 64 x 1000 x 20000 57 / 68,
 // 32 x 4096 x 3000 50 / 65, 64 x 4096 x 3000 58 / 66, 64 x 1000 x 5000 38 / 37.
 constexpr int64_t kWideRows = 128, kWideWeights = 12000000;
 
@@ -124,13 +131,13 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     const bool fits = classes <= kRoom / p->Np;
     p->keep = train && fits && features >= kKeepFeatures[p->halves ? 0 : 1];
     const int64_t most = rows <= kDirectFewRows ? kDirectFewWork[p->halves ? 0 : 1] : train ? kDirectWork : kDirectLossWork;
-    p->wide = p->halves && rows > 8 && rows <= kWideRows && classes >= kWideWeights / features && (rows > mpcnn::kFewScoreRows || classes < 24576);
+    p->wide = p->halves && rows > 8 && rows <= kWideRows && classes >= kWideWeights / features && (rows > mpcnn::kFewScoreRows || classes < kFewScoreClasses[1]);
     p->direct = (rows <= mpcnn::kFewRows || rows * classes <= most / features || (p->wide && !train)) && (fits || !train);
     // few rows and many classes: the gradients, and the scores of still fewer, on the vector ALU (kernels_rows_few.hpp has the times)
-    p->few = p->direct && train && rows > 0 && rows <= mpcnn::kFewRows && classes >= (rows <= 4 ? 1024 : 4096);
+    p->few = p->direct && train && rows > 0 && rows <= mpcnn::kFewRows && classes >= kFewClasses[rows <= 4 ? 0 : 1];
     if (p->direct && rows > 0) {
-        if (p->halves) p->few_scores = rows <= mpcnn::kFewScoreRows && classes >= (rows <= 3 ? 1024 : 24576);
-        else if (rows <= 2) p->few_scores = classes >= 24576;
+        if (p->halves) p->few_scores = rows <= mpcnn::kFewScoreRows && classes >= kFewScoreClasses[rows <= 3 ? 0 : 1];
+        else if (rows <= 2) p->few_scores = classes >= kFewScoreClasses[1];
         else p->few_scores = rows <= mpcnn::kFewScoreRows && classes >= kFewWeights[rows <= 4 ? 0 : 1] / features;
     }
     // what its launches cannot have is much work's, in pieces: 2^28 fp32 classes (of more than 64 rows; of more than 12, 2^29) or 2^30 bf16 ones, the
@@ -466,7 +473,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
         a.A = w_rows; a.a_row = w_row;
         a.B = x_direct ? (const char*)c.x : ws + p.x_rows; a.b_row = x_direct ? c.x_pitch * 2 : p.d_bytes;
         a.M = (int)n_classes; a.N = p.N; a.blocks = d_blocks;
-        a.a_peak = H ? w_peak : nullptr; a.b_peak = H ? x_peak : nullptr; a.a_words = a.b_words = mpcnn::kPeakGroups;
+        a.a_peak = H ? w_peak : nullptr; a.b_peak = H ? x_peak : nullptr;
         a.bias = c.bias ? c.bias + v0 : nullptr;
         a.labels = c.labels; a.class0 = (int)v0;
         if (!delta && p.sc.splits > 1) {
@@ -543,7 +550,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
             a.A = ws + p.delta; a.a_row = p.n_bytes; a.a_bytes = n * p.n_bytes;
             a.B = rows_at(v0); a.b_row = w_row; a.b_bytes = (n - 1) * w_row + (w_direct ? 2 * (int64_t)p.D : p.d_bytes);
             a.M = p.N; a.N = p.D; a.blocks = (int)p.v_blocks(n);
-            a.a_up = 14; a.b_peak = H ? w_peak : nullptr; a.b_words = mpcnn::kPeakGroups;
+            a.b_peak = H ? w_peak : nullptr;
             a.out = c.dx; a.out_row = c.dx_pitch; a.row_scale = j.weight; a.row_mask = !H;
             Tiling t = p.dx;
             t.per_split = (int)((a.blocks + t.splits - 1) / t.splits);
@@ -554,7 +561,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
                 if (last) {
                     mpcnn::SumArgs sum{};
                     sum.part = a.part; sum.splits = t.splits; sum.M = p.N; sum.N = p.D; sum.out_row = c.dx_pitch;
-                    sum.a_up = 14; sum.b_peak = a.b_peak; sum.halves = H; sum.row_scale = j.weight; sum.row_mask = !H; sum.out = c.dx; sum.out_bf16 = !H;
+                    sum.b_peak = a.b_peak; sum.halves = H; sum.row_scale = j.weight; sum.row_mask = !H; sum.out = c.dx; sum.out_bf16 = !H;
                     mpcnn::rows_sum_kernel<<<(unsigned)std::min<int64_t>(4096, ((int64_t)p.N * p.D + 255) / 256), 256, 0, st>>>(sum);
                 }
             } else {
@@ -566,7 +573,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
             mpcnn::ProductArgs a{};
             a.A = ws + p.delta; a.a_row = p.n_bytes; a.B = ws + p.x_cols; a.b_row = p.n_bytes;
             a.M = (int)n; a.N = p.D; a.blocks = (int)(p.n_bytes / mpcnn::kBlockBytes);
-            a.a_up = 14; a.b_peak = H ? wx_peak : nullptr; a.b_words = mpcnn::kPeakGroups;
+            a.b_peak = H ? wx_peak : nullptr;
             a.out = (char*)c.dw + v0 * p.D * (int64_t)sizeof(T); a.out_row = p.D;
             Tiling t = p.dw;
             t.tiles_m = (int)((n + (t.big ? 255 : 127)) / (t.big ? 256 : 128));
@@ -576,7 +583,7 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
                 rc = launch_product<H, mpcnn::kPart>(a, t, st);
                 mpcnn::SumArgs sum{};
                 sum.part = a.part; sum.splits = t.splits; sum.M = n; sum.N = p.D; sum.out_row = p.D;
-                sum.a_up = 14; sum.b_peak = a.b_peak; sum.halves = H; sum.out = a.out; sum.out_bf16 = !H;
+                sum.b_peak = a.b_peak; sum.halves = H; sum.out = a.out; sum.out_bf16 = !H;
                 mpcnn::rows_sum_kernel<<<(unsigned)std::min<int64_t>(4096, (n * p.D + 255) / 256), 256, 0, st>>>(sum);
             } else {
                 rc = launch_product<H, kStore>(a, t, st);

@@ -22,7 +22,6 @@ namespace mpcnn {
 
 constexpr int kDirectK = 32;
 
-typedef int v4i __attribute__((ext_vector_type(4)));
 typedef __bf16 d_bf16x8 __attribute__((ext_vector_type(8)));
 
 struct DirectArgs {
@@ -218,7 +217,7 @@ __global__ __launch_bounds__(256) void rows_direct_scores_kernel(DirectArgs a)
 // ---- fp32 scores of some tens of rows over many classes: bound by the pass over the class weights, which a wave takes from memory into its operands
 // and splits once for up to 64 rows.  The features are split before (rows_split_kernel), into operands as the lanes want them: [step of 32 k's][16 k's][part]
 // [tile of 32 rows][lane], and come from the second-level cache, for 64 rows three times the class
-// weights' bytes.  The waves deal the sum's steps among them.  64 x 4096 x 50000: 313 us, 2.6 TB/s of weights.  (Two steps of weights ahead: 8 % slower; two
+// weights' bytes.  The waves deal the sum's steps among them.  64 x 4096 x 50000: a call of the loss 310 us, 2.6 TB/s of weights.  (Two steps of weights ahead: 8 % slower; two
 // waves of other classes beside each other, which read the same features: 8 % slower.)
 struct SplitArgs {
     const float* x;

@@ -11,6 +11,7 @@
 namespace mpcnn {
 
 constexpr int kPeakGroups = 256;           // words of a peak
+constexpr int kDeltaRaise = 14;            // what the derivative (up to 1) is raised by
 
 // ---- the largest magnitude of a matrix, as bits (one word per workgroup); what is not finite is passed over
 struct PeakArgs {
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(THREADS) void rows_join_kernel(JoinArgs a)
 }
 
 // ---- scores [classes][score_row] of a piece of the classes into the derivative p - [class = label], in blocks along the rows ([classes][out_bytes]):
-// with bf16 storage times the row's weight (rounded once), with fp32 storage raised by 2^14, its second parts by kLowUp more (kernels_rows_product.hpp; the
+// with bf16 storage times the row's weight (rounded once), with fp32 storage raised by 2^kDeltaRaise, its second parts by kLowUp more (kernels_rows_product.hpp; the
 // weight follows: with the features, or behind the product).  db_part: per tile of 64 rows the sums over them, weighted.
 struct DeltaArgs {
     const float* scores;
@@ -403,7 +404,7 @@ __global__ __launch_bounds__(256) void rows_delta_kernel(DeltaArgs a)
             const int c = q / kPieces, p = q % kPieces;
             const long at = (long)blockIdx.x * (kPieces * 16) + 16 * p;
             if (v0 + c >= a.classes || at >= a.out_bytes) continue;
-            *reinterpret_cast<v4f*>(a.out + (long)(v0 + c) * a.out_bytes + at) = piece_of<HALVES>(p, [&](int i) { return HALVES ? tile[c][i] * 0x1p14f : tile[c][i]; }, kLowUp);
+            *reinterpret_cast<v4f*>(a.out + (long)(v0 + c) * a.out_bytes + at) = piece_of<HALVES>(p, [&](int i) { return HALVES ? tile[c][i] * power_of_two(kDeltaRaise) : tile[c][i]; }, kLowUp);
         }
     if (a.db_part) {
         __syncthreads();
@@ -417,8 +418,8 @@ struct SumArgs {
     const float* part;
     int splits;
     long M, N, out_row;
-    const unsigned *a_peak, *b_peak;       // as in ProductArgs
-    int a_up, b_up, halves;
+    const unsigned* b_peak;                // as in ProductArgs, of the derivative's products
+    int halves;
     const float* row_scale;
     int row_mask;
     void* out;
@@ -427,11 +428,7 @@ struct SumArgs {
 __global__ __launch_bounds__(256) void rows_sum_kernel(SumArgs a)
 {
     Lower f{1.f, 1.f};
-    if (a.halves) {
-        const int ua = a.a_peak ? raise_of(peak_of(a.a_peak, kPeakGroups), 0) : a.a_up;
-        const int ub = a.b_peak ? raise_of(peak_of(a.b_peak, kPeakGroups), 0) : a.b_up;
-        f = lower_by(ua + ub);
-    }
+    if (a.halves) f = lower_by(kDeltaRaise + raise_of(peak_of(a.b_peak, kPeakGroups), 0));
     const long all = a.M * a.N;
     for (long e = (long)blockIdx.x * 256 + threadIdx.x; e < all; e += (long)gridDim.x * 256) {
         double s = 0.0;

@@ -31,8 +31,7 @@
 #include <type_traits>
 
 #include "any_address.hpp"
-#include "ranges.hpp"
-#include "rows_mask.hpp"
+#include "kernels_rows_parts.hpp"
 
 namespace mpcnn {
 
@@ -49,8 +48,7 @@ struct ProductArgs {
     int M, N;
     int blocks, per_split;                 // along k: in all, of a workgroup
     int tiles_m, tiles_n, splits;
-    const unsigned *a_peak, *b_peak;       // fp32 storage: what the operands were raised by (null: by a_up, b_up)
-    int a_words, b_words, a_up, b_up;
+    const unsigned *a_peak, *b_peak;       // fp32 storage: [kPeakGroups], what the operands were raised by (a_peak null: A is the derivative, kDeltaRaise)
     // scores
     const float* bias;                     // [M] or null
     const int* labels;                     // [N]
@@ -74,11 +72,6 @@ struct ProductArgs {
     int add;
 };
 enum { kScores = 0, kStoreF32 = 1, kStoreBf16 = 2, kPart = 3, kDelta = 4 };
-
-__device__ __forceinline__ int raised_by(const unsigned* peak, int words, int up)
-{
-    return peak ? raise_of(peak_of(peak, words), 0) : up;
-}
 
 // ACROSS: operands x and y of one step of the instruction, A's from the LDS addresses pa + KA and KA + JA on, B's likewise.  (The builtin for this
 // instruction waits for all fetches into LDS, also those into the other buffer: 1144 us against 958 for a product of 8192 x 4096 x 16000.)
@@ -326,8 +319,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
     // ---- results
     Lower f{1.f, 1.f};
     if constexpr (HALVES) {
-        const int up = raised_by(a.a_peak, a.a_words, a.a_up) + raised_by(a.b_peak, a.b_words, a.b_up);
-        f = lower_by(up);
+        const int up = a.a_peak ? raise_of(peak_of(a.a_peak, kPeakGroups), 0) : kDeltaRaise;
+        f = lower_by(up + raise_of(peak_of(a.b_peak, kPeakGroups), 0));
     }
     if constexpr (RESULT == kScores) {
         constexpr float kNone = -__builtin_inff();
@@ -341,7 +334,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
         for (int j = 0; j < NT; ++j) {
             const int n = nw + 32 * j;
             const bool real = n < a.N;
-            int label = real && a.stats ? a.labels[n] - a.class0 : -1;
+            int label = real ? a.labels[n] - a.class0 : -1;
             label = label < a.M ? label : -1;
             float top = kNone;
 #pragma unroll
@@ -367,7 +360,6 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
                         if (m < a.M) to[(long)m * a.score_row] = acc[i][j][r];
                     }
             }
-            if (!a.stats) continue;
             const float other = __shfl_xor(top, 32, 64);
             top = fmaxf(top, other);
             const float base = top == kNone ? 0.f : top;
@@ -383,7 +375,6 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
             sum += __shfl_xor(sum, 32, 64);
             if (half == 0) red[wm * BN + 32 * NT * wn + 32 * j + row] = float2{top, sum};
         }
-        if (!a.stats) return;
         __syncthreads();
         for (int i = tid; i < BN; i += 64 * kWaves) {
             if (n0 + i >= a.N) continue;
@@ -437,7 +428,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
                     const float g = class_delta(v[z] + bias, lse[z], weight[z] != 0.f, label[z] == m);
                     const float weighted = weight[z] != 0.f ? g * weight[z] : 0.f;
                     sum += weighted;
-                    v[z] = HALVES ? g * 0x1p14f : weighted;
+                    v[z] = HALVES ? g * power_of_two(kDeltaRaise) : weighted;
                 }
                 if (a.db_part) {
                     sum += __shfl_xor(sum, 1, 64);
