@@ -610,7 +610,8 @@ def class_loss(x, w, labels, bias=None, roww=None, rowloss=None, lse=None, loss=
 
 def class_backward(x, w, labels, bias=None, roww=None, rowloss=None, loss=None, dx=None, dw=None, db=None, ws=None, stream=None):
     """class_loss and its gradients -> (loss, rowloss, dx, dw, db); dx and dw have x's type, db (None without
-    a bias) is fp32.  Each is put into the tensor given (dx: its rows dense), allocated for None, left out for False."""
+    a bias) is fp32.  Each is put into the tensor given (dx: its rows dense), allocated for None, left out for False.
+    Its losses can differ from class_loss's in the last bits."""
     import torch
     device, args = _class_call(x, w, labels, bias, roww)
     rows, features, classes = args[7:10]
