@@ -348,6 +348,56 @@ mpcnn_status mpcnn_class_backward(const void* x_dev, int64_t x_pitch, const void
                                   void* dw_dev, float* db_dev, void* ws_dev, size_t ws_bytes, void* hip_stream);
 
 /*
+ * Rows kept in 8 bits.  Blocks of 32 features share a power of two 2^e, the least for which the block's largest magnitude is at most
+ * 127 * 2^e (MPCNN_I8, two's complement) or 448 * 2^e (MPCNN_E4M3, one sign, four exponent, three mantissa bits, no infinity), and e >= -100; a number is kept as
+ * x * 2^-e, rounded to nearest even (numbers that would read back as infinity, from 2^128 - 2^121 and 2^128 - 2^124 on: as the largest finite one).  So a number is off by at most 1/127 of its block's largest with MPCNN_I8, by 2^-4 of itself (or 2^-17 of its
+ * block's largest) with MPCNN_E4M3, and what is kept reads back as an exact number of either storage type.  A block with a number that is not finite reads back as NaN, all of it.
+ *   values_dev  [rows][features rounded up to 32] bytes, 16-byte aligned; zeros behind the last feature,
+ *   scales_dev  [rows][features rounded up to 32, / 32] bytes: e + 127, or 255 for a block that is not finite.
+ * mpcnn_rows_pack: x_dev [rows][x_pitch] into 8 bits.  mpcnn_rows_unpack: back, rounded to `dtype` (which is exact).
+ * A pitch is in elements, at least `features`; matrices lie at any address that is a multiple of their element's size.  rows = 0 is allowed.
+ * Errors: EINVAL (also: an output that overlaps an input), EUNSUPPORTED (more than 2^31 - 1 rows or 2^20 features), EHIP.
+ */
+typedef enum { MPCNN_I8 = 2, MPCNN_E4M3 = 3 } mpcnn_packing;
+typedef struct {
+    void* values_dev; /* NULL: none */
+    uint8_t* scales_dev;
+    int kind; /* mpcnn_packing */
+} mpcnn_packed;
+mpcnn_status mpcnn_rows_pack(const void* x_dev, int64_t x_pitch, int64_t rows, int64_t features, mpcnn_dtype dtype,
+                             const mpcnn_packed* out, void* hip_stream);
+mpcnn_status mpcnn_rows_unpack(const mpcnn_packed* x, int64_t rows, int64_t features, mpcnn_dtype dtype, void* out_dev,
+                               int64_t out_pitch, void* hip_stream);
+
+/*
+ * Root-mean-square norm of rows of features, as it stands before a class layer, with the residual's addition:
+ *   h = x + residual (x if residual_dev is NULL),  rstd = 1 / sqrt(mean over the features of h^2 + eps),  y = h * rstd * gain
+ * in fp32; y comes from h before it is rounded.
+ *   x_dev, residual_dev  [rows][pitch] `dtype`, gain_dev [features] fp32,
+ *   y_dev, h_dev         `dtype`, y_packed, h_packed: the same in 8 bits, rstd_dev [rows] fp32.  Each may be NULL; y and h may be written in both forms.
+ * y_dev and h_dev may be x_dev or residual_dev itself, with its pitch (a residual stream that is updated where it lies).
+ * A row that is not finite gives one that is not finite; the others are as without it.
+ *
+ * mpcnn_rows_norm_backward: for gradients dy of y and dh of h (NULL: zero), with u = dy * gain, n = h * rstd,
+ *   dx = dh + rstd * (u - n * mean over the features of u * n)   (x's gradient and the residual's),   dgain = sum over the rows of dy * n
+ *   h comes from h_dev or, in 8 bits, from h_packed (one of them is given); rstd_dev as mpcnn_rows_norm left it.
+ *   dx_dev `dtype`, dgain_dev [features] fp32: each may be NULL.  dx_dev may be dy_dev, dh_dev or h_dev itself, with its pitch.
+ *   A row of dy that is zero throughout adds nothing and its dx is dh, whatever its h and rstd hold (rows that mpcnn_class_backward ignores).
+ *   ws_dev: 256-byte aligned, at least mpcnn_workspace_bytes_norm (it never shrinks when the rows grow).  Sums have a fixed order.
+ * Pitches, addresses, sizes and errors as above; EINVAL also for an eps that is negative or not finite; EWORKSPACE.  rows = 0 is allowed (dgain = 0).
+ */
+mpcnn_status mpcnn_rows_norm(const void* x_dev, int64_t x_pitch, const void* residual_dev, int64_t residual_pitch,
+                             const float* gain_dev, int64_t rows, int64_t features, mpcnn_dtype dtype, double eps,
+                             void* y_dev, int64_t y_pitch, const mpcnn_packed* y_packed, void* h_dev, int64_t h_pitch,
+                             const mpcnn_packed* h_packed, float* rstd_dev, void* hip_stream);
+size_t mpcnn_workspace_bytes_norm(int64_t rows, int64_t features);
+mpcnn_status mpcnn_rows_norm_backward(const void* dy_dev, int64_t dy_pitch, const void* h_dev, int64_t h_pitch,
+                                      const mpcnn_packed* h_packed, const float* gain_dev, const float* rstd_dev,
+                                      const void* dh_dev, int64_t dh_pitch, int64_t rows, int64_t features,
+                                      mpcnn_dtype dtype, void* dx_dev, int64_t dx_pitch, float* dgain_dev, void* ws_dev,
+                                      size_t ws_bytes, void* hip_stream);
+
+/*
  * The loss alone, L as in mpcnn_seg_backward for the current parameters: a forward pass that
  * keeps nothing and computes no gradient (the evaluations of a line search).
  *   loss_dev: one fp64 on the device.  ws_dev: at least mpcnn_workspace_bytes(net,B,H,W,0).

@@ -17,9 +17,12 @@
 #include "rows_few.hpp"
 #include "kernels_rows_parts.hpp"
 #include "kernels_rows_product.hpp"
+#include "spans.hpp"
 #include "status.hpp"
 
 using mpcnn::fail;
+using mpcnn::meet;
+using mpcnn::Span;
 
 namespace {
 
@@ -594,9 +597,6 @@ mpcnn_status run(const Plan& p, const Call& c, char* ws, hipStream_t st)
     HIP_TRY(hipGetLastError());
     return MPCNN_OK;
 }
-
-struct Span { uintptr_t at; uint64_t bytes; };
-bool meet(const Span& a, const Span& b) { return a.at && b.at && a.bytes && b.bytes && a.at < b.at + b.bytes && b.at < a.at + a.bytes; }
 
 mpcnn_status checked(int64_t rows, int64_t features, int64_t classes, mpcnn_dtype dtype, const Call& c, bool train, void* ws, size_t ws_bytes, void* stream)
 {

@@ -17,23 +17,10 @@
 //   rows_few_sum      adds the workgroups' shares of dx, in a fixed order.
 #pragma once
 #include "any_address.hpp"
+#include "lanes.hpp"
 #include "rows_few.hpp"
 
 namespace mpcnn {
-
-// The sum over 16 lanes side by side, in all of them
-template <int CTRL>
-__device__ __forceinline__ float add_moved(float s)
-{
-    return s + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, s), CTRL, 0xf, 0xf, true));
-}
-__device__ __forceinline__ float sum16(float s)
-{
-    s = add_moved<0x128>(s);   // row_ror:8, 4, 2, 1
-    s = add_moved<0x124>(s);
-    s = add_moved<0x122>(s);
-    return add_moved<0x121>(s);
-}
 
 template <typename T, int NR>
 __global__ __launch_bounds__(kFewThreads) void rows_few_scores_kernel(FewArgs a)

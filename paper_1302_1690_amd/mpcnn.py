@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libmpcnn.so")
 KIND_C, KIND_MP, KIND_FC = 0, 1, 2
 STATIC_WORKSPACE_BYTES = 64 * 1024 * 1024   # MPCNN_STATIC_WORKSPACE_BYTES
 F32, BF16 = 0, 1
+I8, E4M3 = 2, 3   # mpcnn_packing: kinds of rows in 8 bits
 
 STATUS = {0: "MPCNN_OK", 1: "MPCNN_EINVAL", 2: "MPCNN_ESHAPE", 3: "MPCNN_EWORKSPACE",
           4: "MPCNN_EUNSUPPORTED", 5: "MPCNN_EHIP", 6: "MPCNN_ENOMEM"}
@@ -36,6 +37,7 @@ SYMBOLS = [
     "mpcnn_plan_describe", "mpcnn_sgd_step_clipped", "mpcnn_grad_list_create", "mpcnn_grad_list_destroy",
     "mpcnn_grad_norm", "mpcnn_grad_clip", "mpcnn_sgd_step_list",
     "mpcnn_workspace_bytes_class", "mpcnn_workspace_bytes_class_call", "mpcnn_class_loss", "mpcnn_class_backward",
+    "mpcnn_rows_pack", "mpcnn_rows_unpack", "mpcnn_rows_norm", "mpcnn_workspace_bytes_norm", "mpcnn_rows_norm_backward",
 ]
 
 
@@ -60,6 +62,11 @@ class _Tensor(C.Structure):
     """mpcnn_tensor: a gradient and the parameters it belongs to."""
     _fields_ = [("grad", C.c_void_p), ("param", C.c_void_p), ("n", C.c_int64), ("grad_dtype", C.c_int),
                 ("param_dtype", C.c_int)]
+
+
+class _Packed(C.Structure):
+    """mpcnn_packed: a matrix in 8 bits."""
+    _fields_ = [("values", C.c_void_p), ("scales", C.c_void_p), ("kind", C.c_int)]
 
 
 _lib = None
@@ -127,6 +134,13 @@ def lib():
             f.restype = sz
         L.mpcnn_class_loss.argtypes = [vp, l, vp, l, vp, vp, vp, l, l, l, i, vp, vp, vp, vp, sz, vp]
         L.mpcnn_class_backward.argtypes = [vp, l, vp, l, vp, vp, vp, l, l, l, i, vp, vp, vp, l, vp, vp, vp, sz, vp]
+        pk = C.POINTER(_Packed)
+        L.mpcnn_rows_pack.argtypes = [vp, l, l, l, i, pk, vp]
+        L.mpcnn_rows_unpack.argtypes = [pk, l, l, i, vp, l, vp]
+        L.mpcnn_rows_norm.argtypes = [vp, l, vp, l, vp, l, l, i, C.c_double, vp, l, pk, vp, l, pk, vp, vp]
+        L.mpcnn_workspace_bytes_norm.argtypes = [l, l]
+        L.mpcnn_workspace_bytes_norm.restype = sz
+        L.mpcnn_rows_norm_backward.argtypes = [vp, l, vp, l, pk, vp, vp, vp, l, l, l, i, vp, l, vp, vp, sz, vp]
         L.mpcnn_get_activation.argtypes = [vp, i, vp, sz]
         L.mpcnn_get_argmax.argtypes = [vp, i, vp, sz]
         L.mpcnn_last_error.restype = C.c_char_p
@@ -630,3 +644,174 @@ def class_backward(x, w, labels, bias=None, roww=None, rowloss=None, loss=None, 
         at, size, _kept = _class_workspace(ws, args, 1, device)
         _check(lib().mpcnn_class_backward(*args, _ptr(rowloss), _ptr(loss), _ptr(dx), pitch, _ptr(dw), _ptr(db), at, size, st))
     return loss, rowloss, dx, dw, db
+
+
+# ---- rows beside the class layer: in 8 bits, and their norm
+
+class PackedRows:
+    """Rows of features in 8 bits (mpcnn_packed): `values` [rows, features rounded up to 32], int8 or float8_e4m3fn, zeros behind the
+    last feature, and `scales` [rows, blocks of 32 features] uint8: 127 + the exponent of the block's power of two, 255 for a block that is not finite."""
+    __slots__ = ("values", "scales", "features", "kind", "_c")
+
+    def __init__(self, values, scales, features: int):
+        import torch
+        kind = {torch.int8: I8, torch.float8_e4m3fn: E4M3}.get(values.dtype)
+        if kind is None:
+            _refuse("values: %s: int8 and float8_e4m3fn are supported" % values.dtype)
+        blocks = (features + 31) // 32
+        if features < 1 or values.dim() != 2 or values.shape[1] != 32 * blocks or not values.is_contiguous() or not values.is_cuda:
+            _refuse("values: a contiguous matrix of %d columns on a GPU is wanted" % (32 * blocks))
+        if scales.dtype != torch.uint8 or scales.shape != (values.shape[0], blocks) or not scales.is_contiguous() or scales.device != values.device:
+            _refuse("scales: [%d, %d] uint8 on %s are wanted, contiguous" % (values.shape[0], blocks, values.device))
+        self.values, self.scales, self.features, self.kind = values, scales, features, kind
+        self._c = _Packed(values.data_ptr(), scales.data_ptr(), kind)
+
+    @classmethod
+    def empty(cls, rows: int, features: int, kind: int, device):
+        import torch
+        if kind not in (I8, E4M3) or isinstance(kind, bool):
+            _refuse("unknown kind %r of rows in 8 bits" % (kind,))
+        blocks = (features + 31) // 32
+        return cls(torch.empty(rows, 32 * blocks, dtype=torch.int8 if kind == I8 else torch.float8_e4m3fn, device=device),
+                   torch.empty(rows, blocks, dtype=torch.uint8, device=device), features)
+
+    @property
+    def rows(self) -> int:
+        return self.values.shape[0]
+
+    @property
+    def device(self):
+        return self.values.device
+
+
+def _on_gpu(name, x):
+    """A matrix of rows on a GPU -> (device, kind, rows, features, pitch)."""
+    device = x.device
+    if device.type != "cuda":
+        _refuse("%s: a tensor on a GPU is wanted" % name)
+    return (device, _dtype_of(x)) + _rows_of(name, x, device, x.dtype)
+
+
+def _matrix_out(name, given, rows, features, dtype, device):
+    """A matrix to write, given (its rows dense), allocated (None) or left out (False) -> the tensor or None, its address, its pitch."""
+    import torch
+    if given is None:
+        given = torch.empty(rows, features, dtype=dtype, device=device)
+        return given, given.data_ptr(), features
+    if given is False:
+        return None, None, features
+    if given.shape != (rows, features):
+        _refuse("%s: %d rows of %d features are wanted" % (name, rows, features))
+    return given, given.data_ptr(), _rows_of(name, given, device, dtype)[2]
+
+
+def _packed_out(name, given, rows, features, device):
+    """PackedRows, given or a kind to allocate them in."""
+    if not isinstance(given, PackedRows):
+        return PackedRows.empty(rows, features, given, device)
+    if given.rows != rows or given.features != features or given.device != device:
+        _refuse("%s: %d rows of %d features in 8 bits on %s are wanted" % (name, rows, features, device))
+    return given
+
+
+def _is_kind(v) -> bool:
+    return isinstance(v, PackedRows) or (isinstance(v, int) and not isinstance(v, bool))
+
+
+def _like(name, t, rows, features, dtype, device):
+    """Another input of the same shape, or None -> its address and pitch."""
+    if t is None:
+        return None, features
+    got = _rows_of(name, t, device, dtype)
+    if got[:2] != (rows, features):
+        _refuse("%s: %d rows of %d features are wanted" % (name, rows, features))
+    return t.data_ptr(), got[2]
+
+
+def rows_pack(x, kind=I8, stream=None) -> PackedRows:
+    """Rows of features (fp32 or bf16) into 8 bits, I8 or E4M3, blocks of 32 features with a power of two each; `kind` may be the PackedRows to
+    write into."""
+    device, dtype, rows, features, pitch = _on_gpu("x", x)
+    with _On(device, stream) as st:
+        out = _packed_out("kind", kind, rows, features, device)
+        _check(lib().mpcnn_rows_pack(x.data_ptr(), pitch, rows, features, dtype, C.byref(out._c), st))
+    return out
+
+
+def rows_unpack(packed: PackedRows, out=None, stream=None):
+    """What rows in 8 bits stand for, into `out` (fp32 or bf16, exact in both; None: a new bf16 tensor)."""
+    import torch
+    device, rows, features = packed.device, packed.rows, packed.features
+    with _On(device, stream) as st:
+        dtype = torch.bfloat16 if out is None else out.dtype
+        out, at, pitch = _matrix_out("out", out, rows, features, dtype, device)
+        _check(lib().mpcnn_rows_unpack(C.byref(packed._c), rows, features, _dtype_of(out), at, pitch, st))
+    return out
+
+
+def rows_norm(x, gain, residual=None, eps: float = 1e-6, y=None, h=None, kept=False, rstd=None, stream=None):
+    """Root-mean-square norm of rows, with the residual's addition: h = x + residual, y = h / sqrt(mean h^2 + eps) * gain.
+
+    x [rows, features] fp32 or bf16, rows dense, residual likewise or None; gain [features] fp32.  -> (y, h, kept, rstd).
+    y: a tensor of x's type, or in 8 bits: a kind (I8, E4M3) or PackedRows to write into.  h: the sum in x's type (without a residual only if asked
+    for by a tensor); kept: the sum in 8 bits, a kind or PackedRows.  rstd [rows] fp32.  Each is put into what is given, allocated for None, left out
+    for False.  y and h may be x or residual itself."""
+    import torch
+    device, dtype, rows, features, x_pitch = _on_gpu("x", x)
+    res, res_pitch = _like("residual", residual, rows, features, x.dtype, device)
+    g = _vector("gain", gain, features, torch.float32, device)
+    with _On(device, stream) as st:
+        y_at, y_pitch, y8, h8 = None, features, None, None
+        if _is_kind(y):
+            y = _packed_out("y", y, rows, features, device)
+            y8 = C.byref(y._c)
+        else:
+            y, y_at, y_pitch = _matrix_out("y", y, rows, features, x.dtype, device)
+        h, h_at, h_pitch = _matrix_out("h", False if h is None and residual is None else h, rows, features, x.dtype, device)
+        if kept is not False:
+            kept = _packed_out("kept", I8 if kept is None else kept, rows, features, device)
+            h8 = C.byref(kept._c)
+        else:
+            kept = None
+        rstd = _output("rstd", rstd, (rows,), torch.float32, device)
+        _check(lib().mpcnn_rows_norm(x.data_ptr(), x_pitch, res, res_pitch, g, rows, features, dtype, eps, y_at, y_pitch, y8, h_at, h_pitch, h8,
+                                     _ptr(rstd), st))
+    return y, h, kept, rstd
+
+
+def norm_workspace_bytes(rows: int, features: int) -> int:
+    """Bytes of workspace that are enough for rows_norm_backward on so many rows or fewer."""
+    return lib().mpcnn_workspace_bytes_norm(rows, features)
+
+
+def _workspace(ws, size, device):
+    """The workspace's address and bytes, and what keeps it."""
+    import torch
+    if ws is None:
+        ws = torch.empty(max(256, size), dtype=torch.uint8, device=device)
+    elif ws.device != device or not ws.is_contiguous():
+        _refuse("ws: contiguous memory on %s is wanted" % device)
+    return ws.data_ptr(), ws.numel() * ws.element_size(), ws
+
+
+def rows_norm_backward(dy, h, gain, rstd, dh=None, dx=None, dgain=None, ws=None, stream=None):
+    """Gradients of rows_norm -> (dx, dgain), from the gradients dy of y and dh of h (or None), and h as a tensor or as the PackedRows that were kept.
+    dx (x's gradient and the residual's, dy's type) may be dy, dh or h itself; dgain is fp32.  Each is put into the tensor given, allocated for
+    None, left out for False.  A row of dy that is zero throughout adds nothing, whatever h holds there."""
+    import torch
+    device, dtype, rows, features, dy_pitch = _on_gpu("dy", dy)
+    h_at, h_pitch, h8 = None, features, None
+    if isinstance(h, PackedRows):
+        _packed_out("h", h, rows, features, device)
+        h8 = C.byref(h._c)
+    else:
+        h_at, h_pitch = _like("h", h, rows, features, dy.dtype, device)
+    more, more_pitch = _like("dh", dh, rows, features, dy.dtype, device)
+    g, r = _vector("gain", gain, features, torch.float32, device), _vector("rstd", rstd, rows, torch.float32, device)
+    with _On(device, stream) as st:
+        dx, dx_at, dx_pitch = _matrix_out("dx", dx, rows, features, dy.dtype, device)
+        dgain = _output("dgain", dgain, (features,), torch.float32, device)
+        at, size, _kept = _workspace(ws, lib().mpcnn_workspace_bytes_norm(rows, features) if ws is None else 0, device)
+        _check(lib().mpcnn_rows_norm_backward(dy.data_ptr(), dy_pitch, h_at, h_pitch, h8, g, r, more, more_pitch, rows, features, dtype, dx_at, dx_pitch,
+                                              _ptr(dgain), at, size, st))
+    return dx, dgain
