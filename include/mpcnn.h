@@ -398,6 +398,50 @@ mpcnn_status mpcnn_rows_norm_backward(const void* dy_dev, int64_t dy_pitch, cons
                                       size_t ws_bytes, void* hip_stream);
 
 /*
+ * Beam search over a class layer's classes.  Every sequence has `beams` beams; each offers its continuations by every class:
+ *   s[b][k][v] = score + bias[v] (fp32),  value = totals[b][k] + (s - log sum over v of exp s) in 64 bits
+ * and the `width` largest of a sequence's beams * classes values go on, best first; equal ones by the lower beam, then the lower class.
+ *   scores_dev [sequences * beams][scores_pitch] `dtype`, bias_dev [classes] fp32 or NULL (minus infinity switches a class off, whatever its scores hold),
+ *   totals_dev [sequences][beams] fp32: the beams' log-probabilities so far; minus infinity (or NaN): a dead beam, which offers nothing,
+ *   done_dev   [sequences][beams] bytes or NULL: beams that are finished offer one candidate, the class `end`, at their total.  The scores of
+ *              dead and finished beams are not read.  A beam with a score that is NaN or plus infinity, or with no class on, offers nothing.
+ *   end        the class that ends a sequence, or -1 (then done_dev is NULL).
+ * Out, [sequences][width]: totals_out_dev fp32, parents_dev (the beam) and classes_dev int32, done_out_dev bytes (or NULL): whether the parent was finished or
+ * the class is `end`.  Where fewer candidates are there: minus infinity, -1, -1, 1.
+ * Log sums are fp32 exponentials added up and joined in 64 bits (off by some 1e-7): candidates of one beam are in the order of its scores, exactly, and beams that
+ * hold the same are equals.
+ *   ws_dev: 256-byte aligned, at least mpcnn_workspace_bytes_beam (it never shrinks when the sequences grow).  The result does not depend on launch timing.
+ * Errors: EINVAL (also: outputs or the workspace overlap an input or each other), EUNSUPPORTED (more than 64 beams or 64 wanted, 2^20 beams of
+ * all sequences, 2^31 - 1025 classes), EWORKSPACE, EHIP.  sequences = 0 is allowed.
+ */
+size_t mpcnn_workspace_bytes_beam(int64_t sequences, int64_t beams, int64_t classes);
+mpcnn_status mpcnn_beam_select(const void* scores_dev, int64_t scores_pitch, const float* bias_dev, const float* totals_dev,
+                               const uint8_t* done_dev, int64_t end, int64_t sequences, int64_t beams, int64_t width,
+                               int64_t classes, mpcnn_dtype dtype, float* totals_out_dev, int32_t* parents_dev,
+                               int32_t* classes_dev, uint8_t* done_out_dev, void* ws_dev, size_t ws_bytes,
+                               void* hip_stream);
+
+/*
+ * The beams' states (caches, recurrent states, of any type) put in the order of the beams that go on, where they lie: row b * beams + k of every tensor becomes
+ * what row b * beams + parents[b][k] was.  A row whose parent is itself, -1 or no beam stays, and is neither read nor written.
+ *   A tensor is sequences * beams rows, row_pitch bytes apart, each of `segments` segments, segment_pitch bytes apart, of `units` units of unit_bytes each
+ *   (a cache [rows][heads][positions][inner]: heads segments of positions units; anything else: one segment of one unit).
+ *   mpcnn_beam_states_create: the list, made once, on the current device, which has to be the current one in every call; synchronous.  The tensors stay the
+ *     caller's.  Errors: EINVAL (also: two of them overlap), EUNSUPPORTED (over 65535 tensors, rows above 2^34 bytes, beams as above), ENOMEM, EHIP.
+ *   mpcnn_beam_reorder: parents_dev [sequences][beams] int32; length: only so many units of every segment (below zero: all).  Errors: EINVAL (also: another
+ *     device is current, the parents lie in a state), EHIP.
+ */
+typedef struct {
+    void* data_dev;
+    int64_t row_pitch, segment_pitch, unit_bytes, units, segments;
+} mpcnn_beam_state;
+typedef struct mpcnn_beam_states mpcnn_beam_states;
+mpcnn_status mpcnn_beam_states_create(const mpcnn_beam_state* states_host, int count, int64_t sequences, int64_t beams,
+                                      mpcnn_beam_states** out);
+void mpcnn_beam_states_destroy(mpcnn_beam_states* list); /* waits for the device; NULL is allowed */
+mpcnn_status mpcnn_beam_reorder(const mpcnn_beam_states* list, const int32_t* parents_dev, int64_t length, void* hip_stream);
+
+/*
  * The loss alone, L as in mpcnn_seg_backward for the current parameters: a forward pass that
  * keeps nothing and computes no gradient (the evaluations of a line search).
  *   loss_dev: one fp64 on the device.  ws_dev: at least mpcnn_workspace_bytes(net,B,H,W,0).

@@ -38,6 +38,7 @@ SYMBOLS = [
     "mpcnn_grad_norm", "mpcnn_grad_clip", "mpcnn_sgd_step_list",
     "mpcnn_workspace_bytes_class", "mpcnn_workspace_bytes_class_call", "mpcnn_class_loss", "mpcnn_class_backward",
     "mpcnn_rows_pack", "mpcnn_rows_unpack", "mpcnn_rows_norm", "mpcnn_workspace_bytes_norm", "mpcnn_rows_norm_backward",
+    "mpcnn_workspace_bytes_beam", "mpcnn_beam_select", "mpcnn_beam_states_create", "mpcnn_beam_states_destroy", "mpcnn_beam_reorder",
 ]
 
 
@@ -67,6 +68,12 @@ class _Tensor(C.Structure):
 class _Packed(C.Structure):
     """mpcnn_packed: a matrix in 8 bits."""
     _fields_ = [("values", C.c_void_p), ("scales", C.c_void_p), ("kind", C.c_int)]
+
+
+class _BeamState(C.Structure):
+    """mpcnn_beam_state: a tensor of beams' states."""
+    _fields_ = [("data", C.c_void_p), ("row_pitch", C.c_int64), ("segment_pitch", C.c_int64), ("unit_bytes", C.c_int64), ("units", C.c_int64),
+                ("segments", C.c_int64)]
 
 
 _lib = None
@@ -141,6 +148,13 @@ def lib():
         L.mpcnn_workspace_bytes_norm.argtypes = [l, l]
         L.mpcnn_workspace_bytes_norm.restype = sz
         L.mpcnn_rows_norm_backward.argtypes = [vp, l, vp, l, pk, vp, vp, vp, l, l, l, i, vp, l, vp, vp, sz, vp]
+        L.mpcnn_workspace_bytes_beam.argtypes = [l, l, l]
+        L.mpcnn_workspace_bytes_beam.restype = sz
+        L.mpcnn_beam_select.argtypes = [vp, l, vp, vp, vp, l, l, l, l, l, i, vp, vp, vp, vp, vp, sz, vp]
+        L.mpcnn_beam_states_create.argtypes = [C.POINTER(_BeamState), i, l, l, C.POINTER(vp)]
+        L.mpcnn_beam_states_destroy.argtypes = [vp]
+        L.mpcnn_beam_states_destroy.restype = None
+        L.mpcnn_beam_reorder.argtypes = [vp, vp, l, vp]
         L.mpcnn_get_activation.argtypes = [vp, i, vp, sz]
         L.mpcnn_get_argmax.argtypes = [vp, i, vp, sz]
         L.mpcnn_last_error.restype = C.c_char_p
@@ -815,3 +829,109 @@ def rows_norm_backward(dy, h, gain, rstd, dh=None, dx=None, dgain=None, ws=None,
         _check(lib().mpcnn_rows_norm_backward(dy.data_ptr(), dy_pitch, h_at, h_pitch, h8, g, r, more, more_pitch, rows, features, dtype, dx_at, dx_pitch,
                                               _ptr(dgain), at, size, st))
     return dx, dgain
+
+
+# ---- beam search over a class layer's classes
+
+def beam_workspace_bytes(sequences: int, beams: int, classes: int) -> int:
+    """Bytes of workspace that are enough for beam_select on so many sequences or fewer."""
+    return lib().mpcnn_workspace_bytes_beam(sequences, beams, classes)
+
+
+def _beams(totals, done, device):
+    """Sequences and beams, and the addresses of what is known of the beams."""
+    import torch
+    if totals.dim() != 2 or totals.dtype != torch.float32 or totals.device != device or not totals.is_contiguous():
+        _refuse("totals: [sequences, beams] fp32 on %s are wanted, consecutive" % device)
+    if done is not None and (done.dtype not in (torch.bool, torch.uint8) or done.shape != totals.shape or done.device != device or not done.is_contiguous()):
+        _refuse("done: %s bool on %s are wanted, consecutive" % (tuple(totals.shape), device))
+    return totals.shape[0], totals.shape[1]
+
+
+def _beam_outputs(out, sequences, width, device):
+    """What a selection writes: given as (totals, parents, classes, done), or allocated."""
+    import torch
+    if out is None:
+        shape = (sequences, width)
+        return (torch.empty(shape, dtype=torch.float32, device=device), torch.empty(shape, dtype=torch.int32, device=device),
+                torch.empty(shape, dtype=torch.int32, device=device), torch.empty(shape, dtype=torch.bool, device=device))
+    totals, parents, classes, done = out
+    for name, t, dtype in (("totals", totals, torch.float32), ("parents", parents, torch.int32), ("classes", classes, torch.int32), ("done", done, torch.bool)):
+        _output(name, t, (sequences, width), dtype, device)
+    return out
+
+
+def beam_select(scores, totals, width=None, bias=None, done=None, end: int = -1, out=None, ws=None, stream=None):
+    """The continuations of every sequence's beams that go on -> (totals, parents, classes, done), each [sequences, width], best first.
+
+    scores [sequences * beams, classes] fp32 or bf16, rows dense; totals [sequences, beams] fp32: the beams' log-probabilities so far (minus infinity: dead);
+    bias [classes] fp32 or None (minus infinity: off); done [sequences, beams] bool or None: finished beams, which offer class `end` at their total; width:
+    how many go on (None: as many as there are).  totals fp32, parents (beams of the sequence) and classes int32, done bool; minus infinity, -1, -1
+    and True where there is no candidate.  `out`: four such tensors to write into."""
+    device, kind, rows, classes, pitch = _on_gpu("scores", scores)
+    sequences, beams = _beams(totals, done, device)
+    if rows != sequences * beams:
+        _refuse("scores: %d rows of %d sequences of %d beams" % (rows, sequences, beams))
+    import torch
+    width = beams if width is None else width
+    b = _vector("bias", bias, classes, torch.float32, device)
+    with _On(device, stream) as st:
+        out = _beam_outputs(out, sequences, width, device)
+        at, size, _kept = _workspace(ws, lib().mpcnn_workspace_bytes_beam(sequences, beams, classes) if ws is None else 0, device)
+        _check(lib().mpcnn_beam_select(scores.data_ptr(), pitch, b, totals.data_ptr(), _ptr(done), end, sequences, beams, width, classes, kind,
+                                       *[t.data_ptr() for t in out], at, size, st))
+    return out
+
+
+class BeamStates:
+    """mpcnn_beam_states handle: tensors [sequences * beams, ...] on one GPU, of any types, each row dense, that follow the beams.  With `axis`, reorder can be
+    told to move the first positions along that axis only.  The list keeps the tensors alive and works on their memory."""
+
+    def __init__(self, tensors, sequences: int, beams: int, axis: Optional[int] = None):
+        import torch
+        self._h = None
+        self.tensors, self.sequences, self.beams = list(tensors), sequences, beams
+        self.device = self.tensors[0].device if self.tensors else torch.device("cuda", torch.cuda.current_device())
+        arr = (_BeamState * max(1, len(self.tensors)))()
+        for k, t in enumerate(self.tensors):
+            if not t.is_cuda or t.device != self.device:
+                _refuse("every state has to be on one GPU: %s, %s" % (t.device, self.device))
+            if t.dim() < 1 or t.shape[0] != sequences * beams:
+                _refuse("state %d: %d rows are wanted, the shape is %s" % (k, sequences * beams, tuple(t.shape)))
+            if axis is not None and not 1 <= axis < t.dim():
+                _refuse("state %d: no axis %d in %s" % (k, axis, tuple(t.shape)))
+            if t.numel() and not t[0].is_contiguous():
+                _refuse("state %d: rows have to be dense: strides %s of %s" % (k, tuple(t.stride()), tuple(t.shape)))
+            size = t.element_size()
+            s = arr[k]
+            s.data, s.row_pitch = t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else 0) * size
+            s.segments = 1 if axis is None else int(np.prod(t.shape[1:axis], dtype=np.int64))
+            s.units = 1 if axis is None else t.shape[axis]
+            s.unit_bytes = int(np.prod(t.shape[1:] if axis is None else t.shape[axis + 1:], dtype=np.int64)) * size
+            s.segment_pitch = s.units * s.unit_bytes
+        h = C.c_void_p()
+        with torch.cuda.device(self.device):
+            _check(lib().mpcnn_beam_states_create(arr, len(self.tensors), sequences, beams, C.byref(h)))
+        self._h = h
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().mpcnn_beam_states_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except TypeError:     # interpreter shutdown: the module's globals are already gone
+            pass
+
+    def reorder(self, parents, length: Optional[int] = None, stream=None):
+        """Row b * beams + k of every tensor becomes what row b * beams + parents[b, k] was (int32, -1: it stays); with `length`, in the first `length`
+        positions only."""
+        import torch
+        if parents.dtype != torch.int32 or parents.shape != (self.sequences, self.beams) or parents.device != self.device or not parents.is_contiguous():
+            _refuse("parents: [%d, %d] int32 on %s are wanted, consecutive" % (self.sequences, self.beams, self.device))
+        if length is not None and length < 0:
+            _refuse("length = %d" % length)
+        with _On(self.device, stream) as st:
+            _check(lib().mpcnn_beam_reorder(self._h, parents.data_ptr(), -1 if length is None else length, st))
