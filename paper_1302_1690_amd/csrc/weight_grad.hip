@@ -1,0 +1,121 @@
+// The gradient of a linear layer's weights from rows kept in 8 bits (include/mpcnn.h, mpcnn_rows_weight_grad): the plan, checks and launches.
+#include <algorithm>
+#include <atomic>
+#include <cstdint>
+
+#include "kernels_weight_grad.hpp"
+#include "spans.hpp"
+#include "status.hpp"
+
+using mpcnn::fail;
+using mpcnn::meet;
+using mpcnn::Span;
+
+namespace {
+
+constexpr int64_t kMaxRows = 0x7fffffff - 64, kMaxFeatures = 1 << 20, kMostPitch = (int64_t)1 << 40;
+constexpr int64_t kMostResults = (int64_t)1 << 37;     // tiles of 128 x 128: 2^23 workgroups (a launch has less than 2^32 threads)
+constexpr int64_t kPartRoom = (int64_t)256 << 20;      // bytes of the partial sums
+constexpr int kCUs = 256;
+
+struct Plan { bool big; int tiles_m, tiles_n, blocks, splits, per_split; size_t total; };
+
+bool make_plan(int64_t rows, int64_t outs, int64_t features, int dtype, Plan* p)
+{
+    if (rows < 0 || rows > kMaxRows || outs < 1 || outs > kMaxFeatures || features < 1 || features > kMaxFeatures || outs * features > kMostResults) return false;
+    *p = Plan{};
+    const bool f32 = dtype == MPCNN_F32;
+    const int64_t depth = f32 ? 32 : 64, blocks = (rows + depth - 1) / depth;
+    auto tiles = [&](int64_t side) { return ((outs + side - 1) / side) * ((features + side - 1) / side); };
+    p->big = !f32 && tiles(256) >= kCUs * 3 / 4;
+    const int64_t side = p->big ? 256 : 128, all = tiles(side);
+    const int64_t slots = p->big ? kCUs : 2 * kCUs;
+    const int64_t room = std::max<int64_t>(1, kPartRoom / (4 * outs * features));
+    const int64_t splits = std::max<int64_t>(1, std::min({slots / all, blocks / 4, room, (int64_t)64}));
+    p->tiles_m = (int)((outs + side - 1) / side);
+    p->tiles_n = (int)((features + side - 1) / side);
+    p->blocks = (int)blocks;
+    p->per_split = (int)std::max<int64_t>(1, (blocks + splits - 1) / splits);
+    p->splits = (int)std::max<int64_t>(1, (blocks + p->per_split - 1) / p->per_split);
+    p->total = p->splits > 1 ? (size_t)((4 * p->splits * outs * features + 255) / 256 * 256) : 0;
+    return true;
+}
+
+template <typename T, int WM, int WN, int MT, int NT, int KB>
+mpcnn_status launch(const mpcnn::WeightGradArgs& a, hipStream_t st)
+{
+    constexpr int lds = 2 * KB * 2 * 32 * ((sizeof(T) == 4 ? 3 : 1) * WM * MT + WN * NT);
+    auto* kernel = &mpcnn::weight_grad_kernel<T, WM, WN, MT, NT, KB>;
+    if constexpr (lds > 64 * 1024) {       // must be said once per device
+        static std::atomic<uint64_t> said{0};
+        int dev = 0;
+        HIP_TRY(hipGetDevice(&dev));
+        if (!(said.load(std::memory_order_relaxed) >> (dev & 63) & 1)) {
+            HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+            said.fetch_or(1ull << (dev & 63), std::memory_order_relaxed);
+        }
+    }
+    const int64_t all = (int64_t)a.tiles_m * a.tiles_n * a.splits;
+    kernel<<<(unsigned)((all + 7) / 8 * 8), 64 * WM * WN, lds, st>>>(a);
+    return MPCNN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t mpcnn_workspace_bytes_weight_grad(int64_t rows, int64_t outs, int64_t features, mpcnn_dtype dtype)
+{
+    Plan p;
+    if ((dtype != MPCNN_F32 && dtype != MPCNN_BF16) || !make_plan(rows, outs, features, dtype, &p)) return 0;
+    return std::max<size_t>(256, p.total);
+}
+
+mpcnn_status mpcnn_rows_weight_grad(const void* dy_dev, int64_t dy_pitch, const mpcnn_packed* x, int64_t rows, int64_t outs, int64_t features, mpcnn_dtype dtype,
+                                    void* dw_dev, mpcnn_dtype dw_dtype, void* ws_dev, size_t ws_bytes, void* hip_stream)
+{
+    if (rows < 0 || outs < 1 || features < 1) return fail(MPCNN_EINVAL, "%lld rows, %lld outputs, %lld features", (long long)rows, (long long)outs, (long long)features);
+    if ((dtype != MPCNN_F32 && dtype != MPCNN_BF16) || (dw_dtype != MPCNN_F32 && dw_dtype != MPCNN_BF16))
+        return fail(MPCNN_EINVAL, "unknown type %d or %d", (int)dtype, (int)dw_dtype);
+    if (!dw_dev || !ws_dev || (rows > 0 && (!dy_dev || !x || !x->values_dev || !x->scales_dev))) return fail(MPCNN_EINVAL, "null argument");
+    if (rows > 0 && x->kind != MPCNN_I8 && x->kind != MPCNN_E4M3) return fail(MPCNN_EINVAL, "unknown kind %d", x->kind);
+    if (dy_pitch < outs || dy_pitch > kMostPitch) return fail(MPCNN_EINVAL, "a pitch of %lld with %lld outputs", (long long)dy_pitch, (long long)outs);
+    const int64_t size = dtype == MPCNN_F32 ? 4 : 2, dw_size = dw_dtype == MPCNN_F32 ? 4 : 2;
+    if ((uintptr_t)dy_dev % size || (uintptr_t)dw_dev % dw_size || (rows > 0 && (uintptr_t)x->values_dev % 16))
+        return fail(MPCNN_EINVAL, "an address is no multiple of its element's size, or packed rows' none of 16");
+    Plan p;
+    if (!make_plan(rows, outs, features, dtype, &p))
+        return fail(MPCNN_EUNSUPPORTED, "%lld rows, %lld outputs, %lld features: at most %lld, %lld, %lld, and %lld weights", (long long)rows, (long long)outs, (long long)features,
+                    (long long)kMaxRows, (long long)kMaxFeatures, (long long)kMaxFeatures, (long long)kMostResults);
+    if (ws_bytes < p.total) return fail(MPCNN_EWORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, p.total);
+    if ((uintptr_t)ws_dev & 255u) return fail(MPCNN_EINVAL, "workspace must be 256-byte aligned");
+    const int64_t padded = (features + mpcnn::kBlock - 1) / mpcnn::kBlock * mpcnn::kBlock;
+    const Span dw{(uintptr_t)dw_dev, (uint64_t)(outs * features * dw_size)}, ws{(uintptr_t)ws_dev, p.total}, dy = mpcnn::rows_span(dy_dev, rows, outs, dy_pitch, size);
+    const Span values{rows > 0 ? (uintptr_t)x->values_dev : 0, (uint64_t)(rows * padded)}, scales{rows > 0 ? (uintptr_t)x->scales_dev : 0, (uint64_t)(rows * (padded / mpcnn::kBlock))};
+    for (const Span& in : {dy, values, scales})
+        if (meet(in, dw) || meet(in, ws)) return fail(MPCNN_EINVAL, "an output or the workspace overlaps an input");
+    if (meet(dw, ws)) return fail(MPCNN_EINVAL, "the output and the workspace overlap");
+    const hipStream_t st = (hipStream_t)hip_stream;
+    const int64_t n = outs * features;
+    const unsigned sum_groups = (unsigned)std::min<int64_t>(8192, (n + 255) / 256);
+    if (!rows) {
+        mpcnn::weight_grad_sum_kernel<<<sum_groups, 256, 0, st>>>(nullptr, 0, n, dw_dev, dw_dtype == MPCNN_BF16);
+        HIP_TRY(hipGetLastError());
+        return MPCNN_OK;
+    }
+    mpcnn::WeightGradArgs a{};
+    a.dy = dy_dev; a.dy_pitch = dy_pitch; a.x = mpcnn::Packed{(unsigned char*)x->values_dev, x->scales_dev, x->kind};
+    a.N = (int)rows; a.M = (int)outs; a.D = (int)features; a.padded = (int)padded;
+    a.blocks = p.blocks; a.per_split = p.per_split; a.splits = p.splits; a.tiles_m = p.tiles_m; a.tiles_n = p.tiles_n;
+    a.dw = dw_dev; a.dw_bf16 = dw_dtype == MPCNN_BF16;
+    a.part = p.splits > 1 ? (float*)ws_dev : nullptr;
+    const mpcnn_status rc = dtype == MPCNN_F32 ? launch<float, 2, 2, 2, 2, 32>(a, st)
+                            : p.big            ? launch<mpcnn::bf16, 2, 4, 4, 2, 64>(a, st)
+                                               : launch<mpcnn::bf16, 2, 2, 2, 2, 64>(a, st);
+    if (rc != MPCNN_OK) return rc;
+    if (p.splits > 1) mpcnn::weight_grad_sum_kernel<<<sum_groups, 256, 0, st>>>(a.part, p.splits, n, dw_dev, a.dw_bf16);
+    HIP_TRY(hipGetLastError());
+    return MPCNN_OK;
+}
+
+}  // extern "C"

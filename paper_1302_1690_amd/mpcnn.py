@@ -38,6 +38,7 @@ SYMBOLS = [
     "mpcnn_grad_norm", "mpcnn_grad_clip", "mpcnn_sgd_step_list",
     "mpcnn_workspace_bytes_class", "mpcnn_workspace_bytes_class_call", "mpcnn_class_loss", "mpcnn_class_backward",
     "mpcnn_rows_pack", "mpcnn_rows_unpack", "mpcnn_rows_norm", "mpcnn_workspace_bytes_norm", "mpcnn_rows_norm_backward",
+    "mpcnn_workspace_bytes_weight_grad", "mpcnn_rows_weight_grad",
     "mpcnn_workspace_bytes_beam", "mpcnn_beam_select", "mpcnn_beam_states_create", "mpcnn_beam_states_destroy", "mpcnn_beam_reorder",
 ]
 
@@ -148,6 +149,9 @@ def lib():
         L.mpcnn_workspace_bytes_norm.argtypes = [l, l]
         L.mpcnn_workspace_bytes_norm.restype = sz
         L.mpcnn_rows_norm_backward.argtypes = [vp, l, vp, l, pk, vp, vp, vp, l, l, l, i, vp, l, vp, vp, sz, vp]
+        L.mpcnn_workspace_bytes_weight_grad.argtypes = [l, l, l, i]
+        L.mpcnn_workspace_bytes_weight_grad.restype = sz
+        L.mpcnn_rows_weight_grad.argtypes = [vp, l, pk, l, l, l, i, vp, i, vp, sz, vp]
         L.mpcnn_workspace_bytes_beam.argtypes = [l, l, l]
         L.mpcnn_workspace_bytes_beam.restype = sz
         L.mpcnn_beam_select.argtypes = [vp, l, vp, vp, vp, l, l, l, l, l, i, vp, vp, vp, vp, vp, sz, vp]
@@ -829,6 +833,31 @@ def rows_norm_backward(dy, h, gain, rstd, dh=None, dx=None, dgain=None, ws=None,
         _check(lib().mpcnn_rows_norm_backward(dy.data_ptr(), dy_pitch, h_at, h_pitch, h8, g, r, more, more_pitch, rows, features, dtype, dx_at, dx_pitch,
                                               _ptr(dgain), at, size, st))
     return dx, dgain
+
+
+def weight_grad_workspace_bytes(rows: int, outs: int, features: int, dtype: int) -> int:
+    """Bytes of workspace of rows_weight_grad with these sizes."""
+    return lib().mpcnn_workspace_bytes_weight_grad(rows, outs, features, dtype)
+
+
+def rows_weight_grad(dy, x: PackedRows, dw=None, ws=None, stream=None):
+    """The gradient of a linear layer's weights, dw[o, f] = sum over the rows of dy[n, o] x[n, f], from the layer's input rows in 8 bits.
+
+    dy [rows, outs] fp32 or bf16, rows dense; dw [outs, features]: given (fp32 or bf16) or allocated in dy's type."""
+    import torch
+    device, dtype, rows, outs, pitch = _on_gpu("dy", dy)
+    if not isinstance(x, PackedRows):
+        _refuse("x: PackedRows are wanted")
+    features = x.features
+    _packed_out("x", x, rows, features, device)
+    with _On(device, stream) as st:
+        if dw is None:
+            dw = torch.empty(outs, features, dtype=dy.dtype, device=device)
+        else:
+            _output("dw", dw, (outs, features), dw.dtype, device)
+        at, size, _kept = _workspace(ws, lib().mpcnn_workspace_bytes_weight_grad(rows, outs, features, dtype) if ws is None else 0, device)
+        _check(lib().mpcnn_rows_weight_grad(dy.data_ptr(), pitch, C.byref(x._c), rows, outs, features, dtype, dw.data_ptr(), _dtype_of(dw), at, size, st))
+    return dw
 
 
 # ---- beam search over a class layer's classes
