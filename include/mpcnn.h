@@ -435,6 +435,20 @@ mpcnn_status mpcnn_beam_select(const void* scores_dev, int64_t scores_pitch, con
                                void* hip_stream);
 
 /*
+ * The same from a class layer's rows of features (mpcnn_class_loss): s[b][k][v] = x[b * beams + k] . w[v] + bias[v], as that layer computes scores of
+ * little work (MPCNN_F32: 24-bit products), in fp32 [classes][beams of all sequences, rounded up to 4] in the workspace.
+ *   x_dev [sequences * beams][x_pitch], w_dev [classes][w_pitch], both `dtype`.  Values in w that are not finite give scores that are not finite, also of a class that is off.
+ *   ws_dev: at least mpcnn_workspace_bytes_class_beam (it never shrinks when the sequences grow).
+ * Errors: as above; EUNSUPPORTED also for more than 2^34 scores, 2^20 features or 2^27 classes.
+ */
+size_t mpcnn_workspace_bytes_class_beam(int64_t sequences, int64_t beams, int64_t features, int64_t classes, mpcnn_dtype dtype);
+mpcnn_status mpcnn_class_beam(const void* x_dev, int64_t x_pitch, const void* w_dev, int64_t w_pitch, const float* bias_dev,
+                              const float* totals_dev, const uint8_t* done_dev, int64_t end, int64_t sequences, int64_t beams,
+                              int64_t width, int64_t features, int64_t classes, mpcnn_dtype dtype, float* totals_out_dev,
+                              int32_t* parents_dev, int32_t* classes_dev, uint8_t* done_out_dev, void* ws_dev,
+                              size_t ws_bytes, void* hip_stream);
+
+/*
  * The beams' states (caches, recurrent states, of any type) put in the order of the beams that go on, where they lie: row b * beams + k of every tensor becomes
  * what row b * beams + parents[b][k] was.  A row whose parent is itself, -1 or no beam stays, and is neither read nor written.
  *   A tensor is sequences * beams rows, row_pitch bytes apart, each of `segments` segments, segment_pitch bytes apart, of `units` units of unit_bytes each

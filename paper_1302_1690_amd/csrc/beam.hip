@@ -5,6 +5,7 @@
 #include <new>
 #include <vector>
 
+#include "class_scores.hpp"
 #include "kernels_beam.hpp"
 #include "spans.hpp"
 #include "status.hpp"
@@ -24,11 +25,13 @@ struct mpcnn_beam_states {
 namespace {
 
 constexpr int64_t kMaxRows = 1 << 20, kMaxClasses = 0x7fffffff - 1024, kMostPitch = (int64_t)1 << 40;
+constexpr int64_t kMostScores = (int64_t)1 << 34;      // of a class layer, kept: 2^22 workgroups of four rows' chunks
 constexpr int kCUs = 256;
 
 struct Plan { int64_t rows, chunks, parts, part_chunks; size_t stats, tops, total; };
 
-bool make_plan(int64_t sequences, int64_t beams, int64_t classes, Plan* p)
+// columns: the scores are a class layer's, [class][row], and every chunk of a row a workgroup's
+bool make_plan(int64_t sequences, int64_t beams, int64_t classes, Plan* p, bool columns = false)
 {
     if (sequences < 0 || beams < 1 || beams > mpcnn::kMaxBeams || sequences > kMaxRows / beams || classes < 1 || classes > kMaxClasses) return false;
     *p = Plan{};
@@ -37,10 +40,14 @@ bool make_plan(int64_t sequences, int64_t beams, int64_t classes, Plan* p)
     // four workgroups a compute unit, each wave of which has a chunk at least
     const int64_t wanted = std::max<int64_t>(1, 4 * kCUs / std::max<int64_t>(1, p->rows));
     p->part_chunks = std::max<int64_t>(4, (p->chunks + wanted - 1) / wanted);
+    if (columns) {
+        if (sequences * beams * classes > kMostScores) return false;
+        p->part_chunks = 1;
+    }
     p->parts = (p->chunks + p->part_chunks - 1) / p->part_chunks;
     auto up = [](int64_t n) { return (size_t)((n + 255) / 256 * 256); };
     p->stats = 0;
-    p->tops = up(8 * (p->rows + 4 * kCUs));                              // (parts are at most 4 kCUs / rows + 1)
+    p->tops = up(columns ? 8 * p->rows * p->chunks : 8 * (p->rows + 4 * kCUs));       // (parts are at most 4 kCUs / rows + 1)
     p->total = p->tops + up(4 * p->rows * p->chunks);
     return true;
 }
@@ -61,18 +68,23 @@ struct Call {
     uint8_t* done_out;
 };
 
-mpcnn_status check(const Call& c, Plan* p)
+mpcnn_status check(const Call& c, Plan* p, bool columns = false)
 {
     if (c.sequences < 0 || c.beams < 1 || c.width < 1 || c.classes < 1)
         return fail(MPCNN_EINVAL, "%lld sequences of %lld beams, %lld wanted, %lld classes", (long long)c.sequences, (long long)c.beams, (long long)c.width, (long long)c.classes);
     if (c.end < -1 || c.end >= c.classes || (c.done && c.end < 0)) return fail(MPCNN_EINVAL, "class %lld of %lld ends a sequence", (long long)c.end, (long long)c.classes);
-    if (c.width > mpcnn::kMaxBeams || !make_plan(c.sequences, c.beams, c.classes, p))
+    if (c.width > mpcnn::kMaxBeams || !make_plan(c.sequences, c.beams, c.classes, p, columns))
         return fail(MPCNN_EUNSUPPORTED, "%lld sequences of %lld beams, %lld wanted, %lld classes: at most %d beams, %lld of all sequences, %lld classes", (long long)c.sequences,
                     (long long)c.beams, (long long)c.width, (long long)c.classes, mpcnn::kMaxBeams, (long long)kMaxRows, (long long)kMaxClasses);
     if (c.sequences > 0 && (!c.totals || !c.totals_out || !c.parents || !c.classes_out)) return fail(MPCNN_EINVAL, "null argument");
     if (((uintptr_t)c.bias | (uintptr_t)c.totals | (uintptr_t)c.totals_out | (uintptr_t)c.parents | (uintptr_t)c.classes_out) % 4)
         return fail(MPCNN_EINVAL, "an address is no multiple of its element's size");
     return MPCNN_OK;
+}
+
+mpcnn::ClassScores scores_of(const void* x, int64_t x_pitch, const void* w, int64_t w_pitch, const float* bias, int64_t rows, int64_t features, int64_t classes, int dtype)
+{
+    return mpcnn::ClassScores{x, w, x_pitch, w_pitch, bias, rows, features, classes, dtype};
 }
 
 // Outputs and the workspace may not meet an input or each other
@@ -94,17 +106,25 @@ mpcnn_status apart(const Call& c, const Span& scores, const void* ws, size_t ws_
     return MPCNN_OK;
 }
 
-template <typename T>
-mpcnn_status select(const Plan& p, const Call& c, const void* scores, int64_t pitch, const float* bias, char* ws, hipStream_t st)
+mpcnn::BeamArgs args_of(const Plan& p, const Call& c, const void* scores, int64_t pitch, char* ws)
 {
     mpcnn::BeamArgs a{};
-    a.scores = scores; a.pitch = pitch; a.bias = bias; a.totals = c.totals; a.done = c.done; a.end = (int)c.end;
+    a.scores = scores; a.pitch = pitch; a.totals = c.totals; a.done = c.done; a.end = (int)c.end;
     a.sequences = (int)c.sequences; a.beams = (int)c.beams; a.width = (int)c.width;
     a.V = (int)c.classes; a.chunks = (int)p.chunks; a.parts = (int)p.parts; a.part_chunks = (int)p.part_chunks;
     a.stats = (float2*)(ws + p.stats); a.tops = (float*)(ws + p.tops);
     a.totals_out = c.totals_out; a.parents = c.parents; a.classes = c.classes_out; a.done_out = c.done_out;
+    return a;
+}
+size_t pick_bytes(const Call& c) { return (size_t)(c.width * c.width) * 12; }
+
+template <typename T>
+mpcnn_status select(const Plan& p, const Call& c, const void* scores, int64_t pitch, char* ws, hipStream_t st)
+{
+    mpcnn::BeamArgs a = args_of(p, c, scores, pitch, ws);
+    a.bias = c.bias;
     mpcnn::beam_stats_kernel<T><<<(unsigned)(p.rows * p.parts), 256, 0, st>>>(a);
-    mpcnn::beam_pick_kernel<T><<<(unsigned)c.sequences, mpcnn::kPickThreads, (size_t)(c.width * c.width) * 12, st>>>(a);
+    mpcnn::beam_pick_kernel<mpcnn::BeamRow<T>><<<(unsigned)c.sequences, mpcnn::kPickThreads, pick_bytes(c), st>>>(a);
     HIP_TRY(hipGetLastError());
     return MPCNN_OK;
 }
@@ -182,8 +202,52 @@ mpcnn_status mpcnn_beam_select(const void* scores_dev, int64_t scores_pitch, con
     if ((uintptr_t)scores_dev % size) return fail(MPCNN_EINVAL, "an address is no multiple of its element's size");
     TRY(apart(c, mpcnn::rows_span(scores_dev, p.rows, classes, scores_pitch, size), ws_dev, ws_bytes, p.total));
     if (!sequences) return MPCNN_OK;
-    return dtype == MPCNN_F32 ? select<float>(p, c, scores_dev, scores_pitch, bias_dev, (char*)ws_dev, (hipStream_t)hip_stream)
-                              : select<mpcnn::bf16>(p, c, scores_dev, scores_pitch, bias_dev, (char*)ws_dev, (hipStream_t)hip_stream);
+    return dtype == MPCNN_F32 ? select<float>(p, c, scores_dev, scores_pitch, (char*)ws_dev, (hipStream_t)hip_stream)
+                              : select<mpcnn::bf16>(p, c, scores_dev, scores_pitch, (char*)ws_dev, (hipStream_t)hip_stream);
+}
+
+size_t mpcnn_workspace_bytes_class_beam(int64_t sequences, int64_t beams, int64_t features, int64_t classes, mpcnn_dtype dtype)
+{
+    Plan p;
+    if ((dtype != MPCNN_F32 && dtype != MPCNN_BF16) || !make_plan(sequences, beams, classes, &p, true)) return 0;
+    const size_t scores = mpcnn::class_scores_bytes(scores_of(nullptr, 0, nullptr, 0, nullptr, p.rows, features, classes, dtype));
+    return scores ? p.total + scores : 0;
+}
+
+mpcnn_status mpcnn_class_beam(const void* x_dev, int64_t x_pitch, const void* w_dev, int64_t w_pitch, const float* bias_dev, const float* totals_dev,
+                              const uint8_t* done_dev, int64_t end, int64_t sequences, int64_t beams, int64_t width, int64_t features, int64_t classes,
+                              mpcnn_dtype dtype, float* totals_out_dev, int32_t* parents_dev, int32_t* classes_dev, uint8_t* done_out_dev, void* ws_dev,
+                              size_t ws_bytes, void* hip_stream)
+{
+    const Call c{bias_dev, totals_dev, done_dev, end, sequences, beams, width, classes, totals_out_dev, parents_dev, classes_dev, done_out_dev};
+    Plan p;
+    TRY(check(c, &p, true));
+    if (features < 1) return fail(MPCNN_EINVAL, "%lld features", (long long)features);
+    if (dtype != MPCNN_F32 && dtype != MPCNN_BF16) return fail(MPCNN_EINVAL, "unknown type %d", (int)dtype);
+    if (!w_dev || (sequences > 0 && !x_dev)) return fail(MPCNN_EINVAL, "null argument");
+    if (x_pitch < features || w_pitch < features || x_pitch > kMostPitch || w_pitch > kMostPitch)
+        return fail(MPCNN_EINVAL, "pitches of %lld and %lld with %lld features", (long long)x_pitch, (long long)w_pitch, (long long)features);
+    const int64_t size = dtype == MPCNN_F32 ? 4 : 2;
+    if (((uintptr_t)x_dev | (uintptr_t)w_dev) % size) return fail(MPCNN_EINVAL, "an address is no multiple of its element's size");
+    const mpcnn::ClassScores s = scores_of(x_dev, x_pitch, w_dev, w_pitch, bias_dev, p.rows, features, classes, dtype);
+    const size_t scores_bytes = mpcnn::class_scores_bytes(s);
+    if (!scores_bytes) return fail(MPCNN_EUNSUPPORTED, "%lld rows, %lld features, %lld classes", (long long)p.rows, (long long)features, (long long)classes);
+    const size_t need = p.total + scores_bytes;
+    TRY(apart(c, mpcnn::rows_span(x_dev, p.rows, features, x_pitch, size), ws_dev, ws_bytes, need));
+    const Span w = mpcnn::rows_span(w_dev, classes, features, w_pitch, size);
+    for (const Span& o : {Span{(uintptr_t)ws_dev, need}, Span{(uintptr_t)totals_out_dev, 4 * (uint64_t)(sequences * width)}, Span{(uintptr_t)parents_dev, 4 * (uint64_t)(sequences * width)},
+                          Span{(uintptr_t)classes_dev, 4 * (uint64_t)(sequences * width)}, Span{(uintptr_t)done_out_dev, (uint64_t)(sequences * width)}})
+        if (meet(o, w)) return fail(MPCNN_EINVAL, "an output or the workspace overlaps an input");
+    if (!sequences) return MPCNN_OK;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    float* scores = nullptr;
+    int64_t pitch = 0;
+    TRY(mpcnn::class_scores(s, (char*)ws_dev + p.total, &scores, &pitch, st));
+    const mpcnn::BeamArgs a = args_of(p, c, scores, pitch, (char*)ws_dev);
+    mpcnn::beam_columns_kernel<<<(unsigned)(p.chunks * ((p.rows + 3) / 4)), 256, 0, st>>>(a);
+    mpcnn::beam_pick_kernel<mpcnn::BeamColumn><<<(unsigned)sequences, mpcnn::kPickThreads, pick_bytes(c), st>>>(a);
+    HIP_TRY(hipGetLastError());
+    return MPCNN_OK;
 }
 
 mpcnn_status mpcnn_beam_states_create(const mpcnn_beam_state* states_host, int count, int64_t sequences, int64_t beams, mpcnn_beam_states** out)

@@ -13,6 +13,7 @@
 #include <atomic>
 #include <cstdint>
 
+#include "class_scores.hpp"
 #include "kernels_rows_direct.hpp"
 #include "rows_few.hpp"
 #include "kernels_rows_parts.hpp"
@@ -119,6 +120,37 @@ struct Plan {
     bool dx_parts() const { return dx.splits > 1 || piece < V; }
 };
 
+// Whose the scores of little work are: rows_wide_scores_kernel's, rows_few_scores_kernel's, or rows_direct_scores_kernel's
+bool wide_scores(bool halves, int64_t rows, int64_t features, int64_t classes)
+{
+    return halves && rows > 8 && rows <= kWideRows && classes >= kWideWeights / features && (rows > mpcnn::kFewScoreRows || classes < kFewScoreClasses[1]);
+}
+bool few_scores(bool halves, int64_t rows, int64_t features, int64_t classes)
+{
+    if (halves) return rows <= mpcnn::kFewScoreRows && classes >= kFewScoreClasses[rows <= 3 ? 0 : 1];
+    if (rows <= 2) return classes >= kFewScoreClasses[1];
+    return rows <= mpcnn::kFewScoreRows && classes >= kFewWeights[rows <= 4 ? 0 : 1] / features;
+}
+int64_t score_groups(bool wide, int64_t rows, int64_t classes)
+{
+    return wide ? (classes + 31) / 32 * (rows <= 32 ? 1 : up_to(rows, 64) / 64) : (classes + 63) / 64;
+}
+// a tile of 32 x 32 for four waves, one of 64 x 64 where that gives every compute unit two workgroups or the sum has one step
+int deal_of(int64_t m, int64_t n, int64_t k) { return (m + 63) / 64 * ((n + 63) / 64) >= 2 * kCUs || k <= mpcnn::kDirectK ? 1 : 4; }
+int dealt_tiles(int64_t n, int deal) { return (int)((n + (deal == 4 ? 31 : 63)) / (deal == 4 ? 32 : 64)); }
+void plan_scores(Plan* p, int64_t rows, int64_t features, int64_t classes)
+{
+    p->score_deal = deal_of(classes, rows, features);
+    p->score_v = dealt_tiles(classes, p->score_deal); p->score_n = dealt_tiles(rows, p->score_deal);
+    if (p->wide) p->score_v = dealt_tiles(classes, 4);
+    if (p->few_scores) {
+        const int64_t round = mpcnn::kFewRound;
+        p->score_each = ((classes + round - 1) / round + 8 * kCUs - 1) / (8 * kCUs) * round;   // whole rounds
+        p->score_v = (int)((classes + p->score_each - 1) / p->score_each);
+    }
+}
+int64_t x_split_bytes(int64_t rows, int64_t features) { return up_to(rows, rows <= 32 ? 32 : 64) * up_to(features, mpcnn::kDirectK) * 6; }
+
 bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool train, Plan* p)
 {
     if (rows < 0 || rows > kMaxRows || features < 1 || features > kMaxFeatures || classes < 1 || classes > kMaxClasses) return false;
@@ -134,32 +166,17 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
     const bool fits = classes <= kRoom / p->Np;
     p->keep = train && fits && features >= kKeepFeatures[p->halves ? 0 : 1];
     const int64_t most = rows <= kDirectFewRows ? kDirectFewWork[p->halves ? 0 : 1] : train ? kDirectWork : kDirectLossWork;
-    p->wide = p->halves && rows > 8 && rows <= kWideRows && classes >= kWideWeights / features && (rows > mpcnn::kFewScoreRows || classes < kFewScoreClasses[1]);
+    p->wide = wide_scores(p->halves, rows, features, classes);
     p->direct = (rows <= mpcnn::kFewRows || rows * classes <= most / features || (p->wide && !train)) && (fits || !train);
     // few rows and many classes: the gradients, and the scores of still fewer, on the vector ALU (kernels_rows_few.hpp has the times)
     p->few = p->direct && train && rows > 0 && rows <= mpcnn::kFewRows && classes >= kFewClasses[rows <= 4 ? 0 : 1];
-    if (p->direct && rows > 0) {
-        if (p->halves) p->few_scores = rows <= mpcnn::kFewScoreRows && classes >= kFewScoreClasses[rows <= 3 ? 0 : 1];
-        else if (rows <= 2) p->few_scores = classes >= kFewScoreClasses[1];
-        else p->few_scores = rows <= mpcnn::kFewScoreRows && classes >= kFewWeights[rows <= 4 ? 0 : 1] / features;
-    }
+    if (p->direct && rows > 0) p->few_scores = few_scores(p->halves, rows, features, classes);
     // what its launches cannot have is much work's, in pieces: 2^28 fp32 classes (of more than 64 rows; of more than 12, 2^29) or 2^30 bf16 ones, the
     // derivative of the last few of 2^22
-    const int64_t score_groups = p->wide ? (classes + 31) / 32 * (rows <= 32 ? 1 : up_to(rows, 64) / 64) : (classes + 63) / 64;
-    if (!p->few_scores && score_groups >= kMostGroups) p->direct = false;
+    if (!p->few_scores && score_groups(p->wide, rows, classes) >= kMostGroups) p->direct = false;
     if (train && !p->few && (classes + mpcnn::kDeltaSide - 1) / mpcnn::kDeltaSide > kMostSide) p->direct = false;
     if (p->direct) {
-        // a tile of 32 x 32 for four waves, one of 64 x 64 where that gives every compute unit two workgroups or the sum has one step
-        auto deal_of = [](int64_t m, int64_t n, int64_t k) { return (m + 63) / 64 * ((n + 63) / 64) >= 2 * kCUs || k <= mpcnn::kDirectK ? 1 : 4; };
-        auto tiles = [](int64_t n, int deal) { return (int)((n + (deal == 4 ? 31 : 63)) / (deal == 4 ? 32 : 64)); };
-        p->score_deal = deal_of(classes, rows, features);
-        p->score_v = tiles(classes, p->score_deal); p->score_n = tiles(rows, p->score_deal);
-        if (p->wide) p->score_v = tiles(classes, 4);
-        if (p->few_scores) {
-            const int64_t round = mpcnn::kFewRound;
-            p->score_each = ((classes + round - 1) / round + 8 * kCUs - 1) / (8 * kCUs) * round;   // whole rounds
-            p->score_v = (int)((classes + p->score_each - 1) / p->score_each);
-        }
+        plan_scores(p, rows, features, classes);
         if (p->few) {
             // shares of dx: 512 workgroups, fewer where their shares' way to memory and back would be more than an eighth of the class weights' passes
             const int64_t each = mpcnn::few_columns((int)rows) * mpcnn::kFewThreads, along = (features + each - 1) / each;
@@ -171,7 +188,7 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
         }
         auto grads = [&](auto& g, int64_t m, int64_t K) {
             g.deal = deal_of(m, features, K);
-            g.m = tiles(m, g.deal); g.along = tiles(features, g.deal);
+            g.m = dealt_tiles(m, g.deal); g.along = dealt_tiles(features, g.deal);
             const int64_t step = mpcnn::kDirectK * g.deal, all = (int64_t)g.m * g.along;   // (a step of each wave)
             const int64_t most = std::max<int64_t>(1, std::min<int64_t>(32, K / (4 * step)));
             const int64_t n = std::min(most, std::max<int64_t>(1, 4 * kCUs / std::max<int64_t>(1, all)));
@@ -186,7 +203,7 @@ bool make_plan(int64_t rows, int64_t features, int64_t classes, int dtype, bool 
         p->lse = take(4 * p->Np);
         p->weight = take(4 * p->Np);
         p->loss_part = take(8 * (p->Np + 1));
-        if (p->wide) p->x_split = take(up_to(rows, rows <= 32 ? 32 : 64) * up_to(features, mpcnn::kDirectK) * 6);
+        if (p->wide) p->x_split = take(x_split_bytes(rows, features));
         if (p->few) {
             p->score = take(4 * classes * p->Np);
             p->dx_part = take(4 * (int64_t)p->grad_groups * rows * features);
@@ -321,6 +338,50 @@ void launch_join(const mpcnn::JoinArgs& j, hipStream_t st)
     else mpcnn::rows_join_kernel<mpcnn::kJoinMany, 256><<<groups, 256, 0, st>>>(j);
 }
 
+mpcnn::FewArgs few_args(const Plan& p, const mpcnn::DirectArgs& a)
+{
+    mpcnn::FewArgs few{};
+    few.x = a.x; few.w = a.w; few.x_pitch = a.x_pitch; few.w_pitch = a.w_pitch;
+    few.N = a.N; few.D = a.D; few.V = p.V; few.score_row = a.score_row;
+    few.bias = a.bias; few.mask = a.mask; few.scores = a.scores; few.stats = a.stats; few.label_score = a.label_score;
+    return few;
+}
+// The scores of little work, or their statistics alone (a.scores null); notes how many tiles of classes these have
+template <typename T>
+mpcnn_status direct_scores(const Plan& p, mpcnn::DirectArgs& a, char* x_split, hipStream_t st)
+{
+    const bool blocks = sizeof(T) == 2 && p.V * p.D >= kBlockWeights && direct_operand<T>(a.x, a.x_pitch, p.D) && direct_operand<T>(a.w, a.w_pitch, p.D);
+    if (p.few_scores && !(blocks && p.N > 2)) {
+        mpcnn::FewArgs few = few_args(p, a);
+        few.each = p.score_each;
+        mpcnn::launch_rows_few_scores<T>(few, (unsigned)p.score_v, st);
+    } else if (blocks) {
+        mpcnn::ProductArgs b{};
+        b.A = (const char*)a.w; b.a_row = a.w_pitch * 2; b.B = (const char*)a.x; b.b_row = a.x_pitch * 2;
+        b.M = a.V; b.N = p.N; b.blocks = p.D * 2 / mpcnn::kBlockBytes;
+        b.bias = a.bias; b.labels = a.mask.labels; b.stats = a.stats; b.label_score = a.label_score; b.scores = a.scores; b.score_row = a.score_row;
+        const Tiling t = tiling_of(p.V, p.N, b.blocks, 1, false);
+        a.tiles = t.tiles_m;
+        return launch_product<false, mpcnn::kScores>(b, t, st);
+    } else if (sizeof(T) == 4 && p.wide) {
+        mpcnn::SplitArgs s{};
+        s.x = (const float*)a.x; s.x_pitch = a.x_pitch; s.N = p.N; s.D = p.D; s.out = x_split;
+        s.tiles = p.N <= 32 ? 1 : (int)(up_to(p.N, 64) / 32);
+        const int64_t n = (int64_t)s.tiles * ((p.D + mpcnn::kDirectK - 1) / mpcnn::kDirectK) * 128;
+        mpcnn::rows_split_kernel<<<(unsigned)std::min<int64_t>(4096, (n + 255) / 256), 256, 0, st>>>(s);
+        a.x_split = s.out; a.x_tiles = s.tiles;
+        if (s.tiles == 1) mpcnn::rows_wide_scores_kernel<1><<<(unsigned)p.score_v, 256, 0, st>>>(a);
+        else mpcnn::rows_wide_scores_kernel<2><<<(unsigned)(p.score_v * (s.tiles / 2)), 256, 0, st>>>(a);
+    } else {
+        const dim3 grid((unsigned)p.score_v, (unsigned)p.score_n);
+        // rows of bf16 that begin between words (one row has no pitch)
+        const bool odd = sizeof(T) == 2 && (((uintptr_t)a.x | (uintptr_t)a.w | 2 * (uint64_t)(p.N > 1 ? a.x_pitch : 0) | 2 * (uint64_t)(p.V > 1 ? a.w_pitch : 0)) & 2);
+        if (odd) mpcnn::rows_direct_scores_kernel<T, sizeof(T) == 2><<<grid, 256, 0, st>>>(a);
+        else mpcnn::rows_direct_scores_kernel<T, false><<<grid, 256, 0, st>>>(a);
+    }
+    return MPCNN_OK;
+}
+
 template <typename T>
 mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
 {
@@ -331,41 +392,8 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
     a.stats = (float2*)(ws + p.stats); a.label_score = (float*)(ws + p.label_score);
     a.score_row = p.Np; a.score_deal = p.score_deal; a.tiles = p.score_v;
     if (p.train) a.scores = (float*)(ws + p.score);
-    mpcnn::FewArgs few{};
-    if (p.few || p.few_scores) {
-        few.x = c.x; few.w = c.w; few.x_pitch = c.x_pitch; few.w_pitch = c.w_pitch;
-        few.N = p.N; few.D = p.D; few.V = p.V; few.score_row = p.Np;
-        few.bias = c.bias; few.mask = a.mask; few.scores = a.scores; few.stats = a.stats; few.label_score = a.label_score;
-    }
-    const bool blocks = sizeof(T) == 2 && p.V * p.D >= kBlockWeights && direct_operand<T>(c.x, c.x_pitch, p.D) && direct_operand<T>(c.w, c.w_pitch, p.D);
-    if (p.few_scores && !(blocks && p.N > 2)) {
-        few.each = p.score_each;
-        mpcnn::launch_rows_few_scores<T>(few, (unsigned)p.score_v, st);
-    } else if (blocks) {
-        mpcnn::ProductArgs b{};
-        b.A = (const char*)c.w; b.a_row = c.w_pitch * 2; b.B = (const char*)c.x; b.b_row = c.x_pitch * 2;
-        b.M = a.V; b.N = p.N; b.blocks = p.D * 2 / mpcnn::kBlockBytes;
-        b.bias = c.bias; b.labels = c.labels; b.stats = a.stats; b.label_score = a.label_score; b.scores = a.scores; b.score_row = p.Np;
-        const Tiling t = tiling_of(p.V, p.N, b.blocks, 1, false);
-        a.tiles = t.tiles_m;
-        const mpcnn_status rc = launch_product<false, mpcnn::kScores>(b, t, st);
-        if (rc != MPCNN_OK) return rc;
-    } else if (sizeof(T) == 4 && p.wide) {
-        mpcnn::SplitArgs s{};
-        s.x = (const float*)c.x; s.x_pitch = c.x_pitch; s.N = p.N; s.D = p.D; s.out = ws + p.x_split;
-        s.tiles = p.N <= 32 ? 1 : (int)(up_to(p.N, 64) / 32);
-        const int64_t n = (int64_t)s.tiles * ((p.D + mpcnn::kDirectK - 1) / mpcnn::kDirectK) * 128;
-        mpcnn::rows_split_kernel<<<(unsigned)std::min<int64_t>(4096, (n + 255) / 256), 256, 0, st>>>(s);
-        a.x_split = s.out; a.x_tiles = s.tiles;
-        if (s.tiles == 1) mpcnn::rows_wide_scores_kernel<1><<<(unsigned)p.score_v, 256, 0, st>>>(a);
-        else mpcnn::rows_wide_scores_kernel<2><<<(unsigned)(p.score_v * (s.tiles / 2)), 256, 0, st>>>(a);
-    } else {
-        const dim3 grid((unsigned)p.score_v, (unsigned)p.score_n);
-        // rows of bf16 that begin between words (one row has no pitch)
-        const bool odd = sizeof(T) == 2 && (((uintptr_t)c.x | (uintptr_t)c.w | 2 * (uint64_t)(p.N > 1 ? c.x_pitch : 0) | 2 * (uint64_t)(p.V > 1 ? c.w_pitch : 0)) & 2);
-        if (odd) mpcnn::rows_direct_scores_kernel<T, sizeof(T) == 2><<<grid, 256, 0, st>>>(a);
-        else mpcnn::rows_direct_scores_kernel<T, false><<<grid, 256, 0, st>>>(a);
-    }
+    const mpcnn_status rc = direct_scores<T>(p, a, p.wide ? ws + p.x_split : nullptr, st);
+    if (rc != MPCNN_OK) return rc;
     // statistics joined with the derivative where there are few tiles of classes, by a launch of their own otherwise
     const bool joined = a.tiles > mpcnn::kDeltaFewTiles || p.few;
     a.lse = (float*)(ws + p.lse); a.weight = (float*)(ws + p.weight);
@@ -389,6 +417,7 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
     }
     a.loss = groups > 1 ? c.loss : nullptr; a.loss_part = shares; a.loss_parts = groups;
     if (p.few) {
+        mpcnn::FewArgs few = few_args(p, a);
         few.lse = a.lse; few.weight = a.weight;
         few.dw = c.dw; few.db = c.db; few.each = p.grad_each;
         few.part = c.dx ? (float*)(ws + p.dx_part) : nullptr;
@@ -630,7 +659,55 @@ mpcnn_status checked(int64_t rows, int64_t features, int64_t classes, mpcnn_dtyp
     return dtype == MPCNN_F32 ? run<float>(p, c, (char*)ws, (hipStream_t)stream) : run<mpcnn::bf16>(p, c, (char*)ws, (hipStream_t)stream);
 }
 
+// Classes whose scores can be kept: workgroups of 32 classes and 64 rows (128 at most) in one launch along them
+constexpr int64_t kMostKept = (int64_t)1 << 27;
+static_assert(kMostKept / 32 * 2 < kMostGroups && kMaxRows / 32 <= kMostSide, "a launch has them");
+
+// What class_scores needs, and where: each grows with the rows
+struct ScoresRoom { int64_t row; size_t scores, stats, x_split, total; };
+bool scores_room(const mpcnn::ClassScores& c, ScoresRoom* r)
+{
+    if (c.rows < 0 || c.rows > kMaxRows || c.features < 1 || c.features > kMaxFeatures || c.classes < 1 || c.classes > kMaxClasses) return false;
+    if (c.classes > kMostKept) return false;
+    size_t at = 0;
+    auto take = [&](int64_t bytes) { const size_t o = at; at += (size_t)up_to(bytes, 256); return o; };
+    r->row = up_to(c.rows, 4);
+    r->scores = take(4 * c.classes * r->row);
+    r->stats = take(8 * ((c.classes + 31) / 32) * c.rows);
+    r->x_split = take(c.dtype == MPCNN_F32 ? x_split_bytes(std::min(c.rows, kWideRows), c.features) : 0);
+    r->total = at + 256;                                       // (no rows: not nothing)
+    return true;
+}
+
 }  // namespace
+
+namespace mpcnn {
+
+size_t class_scores_bytes(const ClassScores& c)
+{
+    ScoresRoom r;
+    return scores_room(c, &r) ? r.total : 0;
+}
+
+mpcnn_status class_scores(const ClassScores& c, char* ws, float** scores, int64_t* row, hipStream_t st)
+{
+    ScoresRoom r;
+    if (!scores_room(c, &r)) return fail(MPCNN_EUNSUPPORTED, "%lld rows, %lld features, %lld classes", (long long)c.rows, (long long)c.features, (long long)c.classes);
+    Plan p{};
+    p.halves = c.dtype == MPCNN_F32; p.direct = true;
+    p.N = (int)c.rows; p.D = (int)c.features; p.V = c.classes; p.Np = r.row;
+    p.wide = wide_scores(p.halves, c.rows, c.features, c.classes);
+    p.few_scores = few_scores(p.halves, c.rows, c.features, c.classes);
+    plan_scores(&p, c.rows, c.features, c.classes);
+    DirectArgs a{};
+    a.x = c.x; a.w = c.w; a.x_pitch = c.x_pitch; a.w_pitch = c.w_pitch;
+    a.N = p.N; a.D = p.D; a.V = (int)p.V; a.bias = c.bias;
+    a.stats = (float2*)(ws + r.stats); a.scores = (float*)(ws + r.scores); a.score_row = r.row; a.score_deal = p.score_deal; a.tiles = p.score_v;
+    *scores = a.scores; *row = r.row;
+    return c.dtype == MPCNN_F32 ? direct_scores<float>(p, a, ws + r.x_split, st) : direct_scores<bf16>(p, a, nullptr, st);
+}
+
+}  // namespace mpcnn
 
 extern "C" {
 

@@ -23,7 +23,7 @@ constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64;
 
 struct BeamArgs {
     const void* scores;
-    long pitch;
+    long pitch;                            // of a row, or of a class (BeamColumn)
     const float* bias;
     const float* totals;
     const unsigned char* done;             // null: none
@@ -93,6 +93,34 @@ struct BeamRow {
     }
 };
 
+// The same of scores that lie [class][row], fp32, as a class layer leaves them, with their bias
+struct BeamColumn {
+    static constexpr int E = 4, J = kChunk / (64 * E);
+    typedef float Block[E];
+    const float* from;
+    long pitch;
+    int V;
+    __device__ BeamColumn(const BeamArgs& a, long row) : from((const float*)a.scores + row), pitch(a.pitch), V(a.V) {}
+    __device__ static int number(int j) { return E * ((int)(threadIdx.x & 63) + 64 * j); }
+    __device__ void fetch(int chunk, Block (&u)[J]) const
+    {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int at = kChunk * chunk + number(j) + e;
+                u[j][e] = at < V ? from[at * pitch] : -__builtin_inff();
+            }
+    }
+    __device__ void scores(int, const Block (&u)[J], float (&s)[J][E]) const
+    {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int e = 0; e < E; ++e) s[j][e] = u[j][e];
+    }
+};
+
 __device__ __forceinline__ bool beam_goes_on(const BeamArgs& a, long row)
 {
     return a.totals[row] > -__builtin_inff() && !(a.done && a.done[row]);     // (a NaN does not)
@@ -155,6 +183,38 @@ __global__ __launch_bounds__(256) void beam_stats_kernel(BeamArgs a)
     }
 }
 
+// Scores [class][row]: a workgroup has a chunk of classes of four rows, a thread four classes
+__global__ __launch_bounds__(256) void beam_columns_kernel(BeamArgs a)
+{
+    __shared__ float tops[4][4], sums[4][4];
+    const int chunk = (int)(blockIdx.x % a.chunks), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long row0 = 4 * (long)(blockIdx.x / a.chunks), rows = (long)a.sequences * a.beams;
+    v4f s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int at = kChunk * chunk + 256 * i + (int)threadIdx.x;
+        s[i] = at < a.V ? *reinterpret_cast<const v4f*>((const float*)a.scores + at * a.pitch + row0) : v4f(-__builtin_inff());
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float m = largest64(fmaxf(fmaxf(s[0][r], s[1][r]), fmaxf(s[2][r], s[3][r])));
+        if (lane == 0) tops[wave][r] = m;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float top = fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r])), base = top == -__builtin_inff() ? 0.f : top;
+        const float sum = sum64((exp_below(s[0][r], base) + exp_below(s[1][r], base)) + (exp_below(s[2][r], base) + exp_below(s[3][r], base)));
+        if (lane == 0) sums[wave][r] = sum;
+    }
+    __syncthreads();
+    const int r = threadIdx.x;
+    if (r >= 4 || row0 + r >= rows) return;
+    const float top = fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r]));
+    a.tops[(row0 + r) * a.chunks + chunk] = top;
+    a.stats[(row0 + r) * a.parts + chunk] = float2{top, (sums[0][r] + sums[1][r]) + (sums[2][r] + sums[3][r])};
+}
+
 // ---- the second launch
 
 typedef unsigned long long u64;
@@ -194,10 +254,9 @@ __device__ __forceinline__ u64 best_of(u64 key, unsigned place, unsigned* best)
 
 struct BeamOffer { u64 key; unsigned place; };   // of a chunk: beam * chunks + chunk; of a candidate: chosen chunk << 10 | number
 
-template <typename T>
+template <typename Row>
 __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a)
 {
-    using Row = BeamRow<T>;
     constexpr int R = 4;                   // chunks of a lane at once
     extern __shared__ __attribute__((aligned(16))) char lds_raw[];
     __shared__ double lse[kMaxBeams];

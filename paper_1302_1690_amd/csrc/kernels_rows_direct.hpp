@@ -154,7 +154,7 @@ __global__ __launch_bounds__(256) void rows_direct_scores_kernel(DirectArgs a)
         v4f s = direct_fold(acc, fold);
         const int n = n0 + (tid & 31), m0 = v0 + 4 * (tid >> 5);
         const bool real = n < a.N;
-        const int label = real ? a.mask.labels[n] : -1;
+        const int label = real && a.mask.labels ? a.mask.labels[n] : -1;
         float top = kNone;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256) void rows_direct_scores_kernel(DirectArgs a)
     }
     const int m0 = v0 + 4 * half, n = n0 + row;
     const bool real = n < a.N;
-    const int label = real ? a.mask.labels[n] : -1;
+    const int label = real && a.mask.labels ? a.mask.labels[n] : -1;
     float bias[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(256) void rows_wide_scores_kernel(DirectArgs a)
         v4f s = direct_fold(acc[j], fold);
         const int n0 = 32 * (t0 + j), n = n0 + (tid & 31), m0 = v0 + 4 * (tid >> 5);
         const bool real = n < a.N;
-        const int label = real ? a.mask.labels[n] : -1;
+        const int label = real && a.mask.labels ? a.mask.labels[n] : -1;
         float top = kNone;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {

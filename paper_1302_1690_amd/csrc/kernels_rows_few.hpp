@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kFewThreads) void rows_few_scores_kernel(FewArgs a)
             const float s = v < end ? sc[n][lane] + b : kNone;
             if (v < end) {
                 if (a.scores) a.scores[v * a.score_row + n] = s;
-                if (v == a.mask.labels[n]) a.label_score[n] = s;
+                if (a.mask.labels && v == a.mask.labels[n]) a.label_score[n] = s;
             }
             // every lane keeps its own classes' statistics until the end
             const float t = fmaxf(top[i], s), base = t == kNone ? 0.f : t;

@@ -53,7 +53,7 @@ struct ProductArgs {
     const unsigned *a_peak, *b_peak;       // fp32 storage: [kPeakGroups], what the operands were raised by (a_peak null: A is the derivative, kDeltaRaise)
     // scores
     const float* bias;                     // [M] or null
-    const int* labels;                     // [N]
+    const int* labels;                     // [N], or null: no label's score is asked for
     float2* stats;                         // [tiles_m][N]: largest, sum of exp(score - largest)
     float* label_score;                    // [N]
     float* scores;                         // [M][score_row], or null
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
         for (int j = 0; j < NT; ++j) {
             const int n = nw + 32 * j;
             const bool real = n < a.N;
-            int label = real ? a.labels[n] - a.class0 : -1;
+            int label = real && a.labels ? a.labels[n] - a.class0 : -1;
             label = label < a.M ? label : -1;
             float top = kNone;
 #pragma unroll

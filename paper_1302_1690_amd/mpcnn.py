@@ -39,7 +39,8 @@ SYMBOLS = [
     "mpcnn_workspace_bytes_class", "mpcnn_workspace_bytes_class_call", "mpcnn_class_loss", "mpcnn_class_backward",
     "mpcnn_rows_pack", "mpcnn_rows_unpack", "mpcnn_rows_norm", "mpcnn_workspace_bytes_norm", "mpcnn_rows_norm_backward",
     "mpcnn_workspace_bytes_weight_grad", "mpcnn_rows_weight_grad",
-    "mpcnn_workspace_bytes_beam", "mpcnn_beam_select", "mpcnn_beam_states_create", "mpcnn_beam_states_destroy", "mpcnn_beam_reorder",
+    "mpcnn_workspace_bytes_beam", "mpcnn_beam_select", "mpcnn_workspace_bytes_class_beam", "mpcnn_class_beam",
+    "mpcnn_beam_states_create", "mpcnn_beam_states_destroy", "mpcnn_beam_reorder",
 ]
 
 
@@ -155,6 +156,9 @@ def lib():
         L.mpcnn_workspace_bytes_beam.argtypes = [l, l, l]
         L.mpcnn_workspace_bytes_beam.restype = sz
         L.mpcnn_beam_select.argtypes = [vp, l, vp, vp, vp, l, l, l, l, l, i, vp, vp, vp, vp, vp, sz, vp]
+        L.mpcnn_workspace_bytes_class_beam.argtypes = [l, l, l, l, i]
+        L.mpcnn_workspace_bytes_class_beam.restype = sz
+        L.mpcnn_class_beam.argtypes = [vp, l, vp, l, vp, vp, vp, l, l, l, l, l, l, i, vp, vp, vp, vp, vp, sz, vp]
         L.mpcnn_beam_states_create.argtypes = [C.POINTER(_BeamState), i, l, l, C.POINTER(vp)]
         L.mpcnn_beam_states_destroy.argtypes = [vp]
         L.mpcnn_beam_states_destroy.restype = None
@@ -897,11 +901,11 @@ def beam_select(scores, totals, width=None, bias=None, done=None, end: int = -1,
     bias [classes] fp32 or None (minus infinity: off); done [sequences, beams] bool or None: finished beams, which offer class `end` at their total; width:
     how many go on (None: as many as there are).  totals fp32, parents (beams of the sequence) and classes int32, done bool; minus infinity, -1, -1
     and True where there is no candidate.  `out`: four such tensors to write into."""
+    import torch
     device, kind, rows, classes, pitch = _on_gpu("scores", scores)
     sequences, beams = _beams(totals, done, device)
     if rows != sequences * beams:
         _refuse("scores: %d rows of %d sequences of %d beams" % (rows, sequences, beams))
-    import torch
     width = beams if width is None else width
     b = _vector("bias", bias, classes, torch.float32, device)
     with _On(device, stream) as st:
@@ -909,6 +913,31 @@ def beam_select(scores, totals, width=None, bias=None, done=None, end: int = -1,
         at, size, _kept = _workspace(ws, lib().mpcnn_workspace_bytes_beam(sequences, beams, classes) if ws is None else 0, device)
         _check(lib().mpcnn_beam_select(scores.data_ptr(), pitch, b, totals.data_ptr(), _ptr(done), end, sequences, beams, width, classes, kind,
                                        *[t.data_ptr() for t in out], at, size, st))
+    return out
+
+
+def class_beam_workspace_bytes(sequences: int, beams: int, features: int, classes: int, dtype: int) -> int:
+    """Bytes of workspace that are enough for class_beam on so many sequences or fewer."""
+    return lib().mpcnn_workspace_bytes_class_beam(sequences, beams, features, classes, dtype)
+
+
+def class_beam(x, w, totals, width=None, bias=None, done=None, end: int = -1, out=None, ws=None, stream=None):
+    """beam_select on the scores of a class layer: x [sequences * beams, features] and w [classes, features], fp32 or bf16, rows dense; the rest as there."""
+    import torch
+    device, kind, rows, features, x_pitch = _on_gpu("x", x)
+    classes, columns, w_pitch = _rows_of("w", w, device, x.dtype)
+    if columns != features:
+        _refuse("x has %d features, w %d" % (features, columns))
+    sequences, beams = _beams(totals, done, device)
+    if rows != sequences * beams:
+        _refuse("x: %d rows of %d sequences of %d beams" % (rows, sequences, beams))
+    width = beams if width is None else width
+    b = _vector("bias", bias, classes, torch.float32, device)
+    with _On(device, stream) as st:
+        out = _beam_outputs(out, sequences, width, device)
+        at, size, _kept = _workspace(ws, lib().mpcnn_workspace_bytes_class_beam(sequences, beams, features, classes, kind) if ws is None else 0, device)
+        _check(lib().mpcnn_class_beam(x.data_ptr(), x_pitch, w.data_ptr(), w_pitch, b, totals.data_ptr(), _ptr(done), end, sequences, beams, width, features,
+                                      classes, kind, *[t.data_ptr() for t in out], at, size, st))
     return out
 
 

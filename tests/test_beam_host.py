@@ -28,6 +28,31 @@ def test_select_refusals(change, status):
     assert mpcnn.lib().mpcnn_beam_select(*a.values(), None) == status, mpcnn.lib().mpcnn_last_error().decode()
 
 
+CLASS = dict(x=BASE, x_pitch=64, w=10 * BASE, w_pitch=64, bias=2 * BASE, totals=3 * BASE, done=4 * BASE, end=5, sequences=3, beams=4, width=4, features=64, classes=1000,
+             dtype=0, totals_out=5 * BASE, parents=6 * BASE, classes_out=7 * BASE, done_out=8 * BASE, ws=9 * BASE, ws_bytes=1 << 30)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(x=None), EINVAL), (dict(w=None), EINVAL), (dict(totals=None), EINVAL), (dict(ws=None), EINVAL), (dict(features=0), EINVAL), (dict(classes=0), EINVAL), (dict(width=0), EINVAL),
+    (dict(dtype=2), EINVAL), (dict(x_pitch=63), EINVAL), (dict(w_pitch=63), EINVAL), (dict(w_pitch=1 << 41), EINVAL), (dict(x=BASE + 2), EINVAL), (dict(w=10 * BASE + 1), EINVAL),
+    (dict(ws=9 * BASE + 128), EINVAL), (dict(ws_bytes=10000), EWORKSPACE), (dict(width=65), EUNSUPPORTED), (dict(classes=(1 << 27) + 1), EUNSUPPORTED),
+    (dict(features=(1 << 20) + 1, x_pitch=1 << 21, w_pitch=1 << 21), EUNSUPPORTED), (dict(sequences=1 << 15, classes=1 << 20), EUNSUPPORTED),
+    (dict(parents=10 * BASE + 255996), EINVAL), (dict(totals_out=BASE), EINVAL), (dict(ws=10 * BASE), EINVAL), (dict(done_out=10 * BASE), EINVAL),
+], ids=range(23))
+def test_class_beam_refusals(change, status):
+    a = dict(CLASS, **change)
+    assert mpcnn.lib().mpcnn_class_beam(*a.values(), None) == status, mpcnn.lib().mpcnn_last_error().decode()
+
+
+def test_class_beam_workspace():
+    size = mpcnn.class_beam_workspace_bytes
+    assert size(-1, 4, 64, 100, 0) == size(3, 4, 0, 100, 0) == size(3, 4, 64, 0, 1) == size(3, 4, 64, 100, 2) == 0
+    for dtype in (0, 1):
+        for beams, features, classes in ((1, 7, 1), (4, 1024, 32000), (8, 4096, 50021), (16, 100, 1000)):
+            got = [size(n, beams, features, classes, dtype) for n in (0, 1, 2, 3, 5, 9, 17, 40, 100)]
+            assert got == sorted(got) and got[0] > 0
+
+
 def test_workspace():
     size = mpcnn.beam_workspace_bytes
     assert size(-1, 4, 100) == size(3, 0, 100) == size(3, 65, 100) == size(3, 4, 0) == size(1 << 20, 2, 100) == size(3, 4, 1 << 31) == 0

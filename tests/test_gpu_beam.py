@@ -196,6 +196,79 @@ def test_far_classes_and_far_rows():
     assert all(torch.equal(x, y) for x, y in zip(mpcnn.beam_select(far, totals), mpcnn.beam_select(near, totals)))
 
 
+# ---- from rows of features
+
+def _whole(gen, rows, features, dtype, most):
+    return torch.randint(-most, most + 1, (rows, features), generator=gen, device="cuda").to(dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=_ids)
+@pytest.mark.parametrize("with_bias,finished", [(False, 0.0), (True, 0.3)])
+@pytest.mark.parametrize("b,k,features,v,width", [(1, 1, 5, 3, 2), (1, 4, 1024, 32000, 4), (1, 2, 64, 30011, 8), (2, 3, 100, 2000, 3), (3, 4, 1000, 25000, 6), (5, 8, 333, 5001, 8),
+                                                  (1, 64, 96, 1025, 64), (16, 8, 256, 700, 8), (20, 16, 64, 9000, 4), (8, 4, 2048, 20480, 4), (4, 2, 4096, 33000, 2)])
+def test_class_beam(b, k, features, v, width, with_bias, finished, dtype):
+    """Features and class weights are whole numbers, biases multiples of 1/64: every order of the products' sum gives the same score, exactly."""
+    gen = _gen(b * 7 + k * 11 + features + v)
+    x, w = _whole(gen, b * k, features, dtype, 3), _whole(gen, v, features, dtype, 2)
+    _, totals, bias, done = _inputs(gen, b, k, 1, dtype, False, finished)
+    if with_bias:
+        bias = torch.randint(-64, 64, (v,), generator=gen, device="cuda").float() / 64
+        bias[torch.rand(v, generator=gen, device="cuda") < 0.1] = -INF
+    if b > 1:
+        totals[1, 1:] = -INF
+        x[k + 1:2 * k] = float("nan")                     # dead beams' rows may hold anything
+    scores = torch.nan_to_num(x.double(), nan=0.0) @ w.double().t()
+    assert scores.abs().max() < 2.0 ** 18
+    end = v // 3 if finished else -1
+    got = mpcnn.class_beam(x, w, totals, width=width, bias=bias, done=done, end=end)
+    check(got, scores.float(), totals, width, bias, done, end)
+    assert all(torch.equal(p, q) for p, q in zip(got, mpcnn.class_beam(x, w, totals, width=width, bias=bias, done=done, end=end)))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=_ids)
+def test_class_beam_of_strided_rows_and_real_numbers(dtype):
+    gen = _gen(77)
+    b, k, features, v = 2, 3, 200, 3001
+    x, w = torch.randn((b * k, features), generator=gen, device="cuda").to(dtype), (torch.randn((v, features), generator=gen, device="cuda") * 0.1).to(dtype)
+    totals = -torch.rand((b, k), generator=gen, device="cuda")
+    want = mpcnn.class_beam(x, w, totals)
+    for offset in (1, 2):
+        wide_x, wide_w = torch.zeros((b * k, 207), device="cuda", dtype=dtype), torch.zeros((v, 211), device="cuda", dtype=dtype)
+        wide_x[:, offset:offset + 200], wide_w[:, offset:offset + 200] = x, w
+        got = mpcnn.class_beam(wide_x[:, offset:offset + 200], wide_w[:, offset:offset + 200], totals)
+        assert torch.equal(got[1], want[1]) and torch.equal(got[2], want[2])
+    # a score is off by 2 (n + 16) u of its products' magnitudes, and by 2^-22 of them with fp32 (three parts); a value by that, and its log sum's
+    size = (x.double().abs() @ w.double().abs().t()).max()
+    off = 2 * ((2 * (features + 16) + 4) * U * size + _off(v, b * k))
+    value = values_in_64(x.double() @ w.double().t(), totals, None, None, -1).view(b, -1)
+    best = torch.sort(value, dim=1, descending=True).values[:, :k]
+    assert ((want[0].double() - best).abs() <= off + U * best.abs()).all()
+    place = want[1].long() * v + want[2].long()
+    assert ((value.gather(1, place) - best).abs() <= off).all()
+
+
+def test_class_beam_in_a_graph_and_with_one_workspace():
+    gen = _gen(78)
+    b, k, features, v = 4, 4, 256, 6000
+    x, w = _whole(gen, b * k, features, torch.bfloat16, 3), _whole(gen, v, features, torch.bfloat16, 2)
+    totals = -torch.rand((b, k), generator=gen, device="cuda")
+    n = mpcnn.class_beam_workspace_bytes(b, k, features, v, mpcnn.BF16)
+    ws = torch.full((n + 512,), 255, dtype=torch.uint8, device="cuda")
+    for less in (b, 2, 1):
+        got = mpcnn.class_beam(x[:less * k], w, totals[:less], ws=ws[:n])
+        assert all(torch.equal(p, q) for p, q in zip(got, mpcnn.class_beam(x[:less * k], w, totals[:less])))
+    assert (ws[n:] == 255).all()
+    out = mpcnn.class_beam(x, w, totals, ws=ws[:n])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mpcnn.class_beam(x, w, totals, out=out, ws=ws[:n])
+    for _ in range(3):
+        x.copy_(_whole(gen, b * k, features, torch.bfloat16, 3))
+        graph.replay()
+        torch.cuda.synchronize()
+        check(out, (x.double() @ w.double().t()).float(), totals, k)
+
+
 # ---- states
 
 def _plain_reorder(t, parents, length=None, axis=None):
