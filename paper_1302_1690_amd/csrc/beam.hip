@@ -25,29 +25,30 @@ struct mpcnn_beam_states {
 namespace {
 
 constexpr int64_t kMaxRows = 1 << 20, kMaxClasses = 0x7fffffff - 1024, kMostPitch = (int64_t)1 << 40;
-constexpr int64_t kMostScores = (int64_t)1 << 34;      // of a class layer, kept: 2^22 workgroups of four rows' chunks
+constexpr int64_t kMostScores = (int64_t)1 << 34;      // of a class layer, kept: 2^22 workgroups of four rows' steps
 constexpr int kCUs = 256;
 
-struct Plan { int64_t rows, chunks, parts, part_chunks; size_t stats, tops, total; };
+struct Plan { int64_t rows, chunks, steps, parts, part_steps; size_t stats, tops, total; };
 
-// columns: the scores are a class layer's, [class][row], and every chunk of a row a workgroup's
+// columns: the scores are a class layer's, [class][row], and every step of a row a workgroup's
 bool make_plan(int64_t sequences, int64_t beams, int64_t classes, Plan* p, bool columns = false)
 {
     if (sequences < 0 || beams < 1 || beams > mpcnn::kMaxBeams || sequences > kMaxRows / beams || classes < 1 || classes > kMaxClasses) return false;
     *p = Plan{};
     p->rows = sequences * beams;
     p->chunks = (classes + mpcnn::kChunk - 1) / mpcnn::kChunk;
-    // four workgroups a compute unit, each wave of which has a chunk at least
-    const int64_t wanted = std::max<int64_t>(1, 4 * kCUs / std::max<int64_t>(1, p->rows));
-    p->part_chunks = std::max<int64_t>(4, (p->chunks + wanted - 1) / wanted);
+    p->steps = (classes + mpcnn::kStep - 1) / mpcnn::kStep;
+    // eight workgroups a compute unit, each wave of which has a step at least
+    const int64_t wanted = std::max<int64_t>(1, 8 * kCUs / std::max<int64_t>(1, p->rows));
+    p->part_steps = std::max<int64_t>(4, (p->steps + wanted - 1) / wanted);
     if (columns) {
         if (sequences * beams * classes > kMostScores) return false;
-        p->part_chunks = 1;
+        p->part_steps = 1;
     }
-    p->parts = (p->chunks + p->part_chunks - 1) / p->part_chunks;
+    p->parts = (p->steps + p->part_steps - 1) / p->part_steps;
     auto up = [](int64_t n) { return (size_t)((n + 255) / 256 * 256); };
     p->stats = 0;
-    p->tops = up(columns ? 8 * p->rows * p->chunks : 8 * (p->rows + 4 * kCUs));       // (parts are at most 4 kCUs / rows + 1)
+    p->tops = up(columns ? 8 * p->rows * p->steps : 8 * (p->rows + 8 * kCUs));       // (parts are at most 8 kCUs / rows + 1)
     p->total = p->tops + up(4 * p->rows * p->chunks);
     return true;
 }
@@ -111,12 +112,11 @@ mpcnn::BeamArgs args_of(const Plan& p, const Call& c, const void* scores, int64_
     mpcnn::BeamArgs a{};
     a.scores = scores; a.pitch = pitch; a.totals = c.totals; a.done = c.done; a.end = (int)c.end;
     a.sequences = (int)c.sequences; a.beams = (int)c.beams; a.width = (int)c.width;
-    a.V = (int)c.classes; a.chunks = (int)p.chunks; a.parts = (int)p.parts; a.part_chunks = (int)p.part_chunks;
+    a.V = (int)c.classes; a.chunks = (int)p.chunks; a.steps = (int)p.steps; a.parts = (int)p.parts; a.part_steps = (int)p.part_steps;
     a.stats = (float2*)(ws + p.stats); a.tops = (float*)(ws + p.tops);
     a.totals_out = c.totals_out; a.parents = c.parents; a.classes = c.classes_out; a.done_out = c.done_out;
     return a;
 }
-size_t pick_bytes(const Call& c) { return (size_t)(c.width * c.width) * 12; }
 
 template <typename T>
 mpcnn_status select(const Plan& p, const Call& c, const void* scores, int64_t pitch, char* ws, hipStream_t st)
@@ -124,7 +124,7 @@ mpcnn_status select(const Plan& p, const Call& c, const void* scores, int64_t pi
     mpcnn::BeamArgs a = args_of(p, c, scores, pitch, ws);
     a.bias = c.bias;
     mpcnn::beam_stats_kernel<T><<<(unsigned)(p.rows * p.parts), 256, 0, st>>>(a);
-    mpcnn::beam_pick_kernel<mpcnn::BeamRow<T>><<<(unsigned)c.sequences, mpcnn::kPickThreads, pick_bytes(c), st>>>(a);
+    mpcnn::beam_pick_kernel<mpcnn::BeamRow<T>><<<(unsigned)c.sequences, mpcnn::kPickThreads, mpcnn::pick_bytes((int)c.width), st>>>(a);
     HIP_TRY(hipGetLastError());
     return MPCNN_OK;
 }
@@ -244,8 +244,8 @@ mpcnn_status mpcnn_class_beam(const void* x_dev, int64_t x_pitch, const void* w_
     int64_t pitch = 0;
     TRY(mpcnn::class_scores(s, (char*)ws_dev + p.total, &scores, &pitch, st));
     const mpcnn::BeamArgs a = args_of(p, c, scores, pitch, (char*)ws_dev);
-    mpcnn::beam_columns_kernel<<<(unsigned)(p.chunks * ((p.rows + 3) / 4)), 256, 0, st>>>(a);
-    mpcnn::beam_pick_kernel<mpcnn::BeamColumn><<<(unsigned)sequences, mpcnn::kPickThreads, pick_bytes(c), st>>>(a);
+    mpcnn::beam_columns_kernel<<<(unsigned)(p.steps * ((p.rows + 3) / 4)), 256, 0, st>>>(a);
+    mpcnn::beam_pick_kernel<mpcnn::BeamColumn><<<(unsigned)sequences, mpcnn::kPickThreads, mpcnn::pick_bytes((int)c.width), st>>>(a);
     HIP_TRY(hipGetLastError());
     return MPCNN_OK;
 }

@@ -4,8 +4,8 @@
 //   value(k, v) = total[k] + (s[k][v] - lse[k]) in 64 bits;  the `width` largest of a sequence's beams x classes, ties to the lowest beam, then class.
 // A finished beam offers one candidate, the class that ends a sequence, at its total; a dead one (total minus infinity) none.
 //
-// Two launches.  The first goes through the scores once and is bound by memory: a wave takes chunks of 1024 classes and leaves each chunk's largest score; a workgroup
-// leaves its classes' largest and sum of exponentials.  The second, a workgroup per sequence, joins the sums and reads again only what can matter: the chunks whose
+// Two launches.  The first goes through the scores once and is bound by memory: a wave takes steps of 1024 classes and leaves the largest score of each chunk of 256; a
+// workgroup leaves its classes' largest and sum of exponentials.  The second, a workgroup per sequence, joins the sums and reads again only what can matter: the chunks whose
 // largest are among the `width` best of all.  (Let an element of another chunk be among the best: `width` chunks have a largest that is better, and so is
 // not below it, and these are as many elements that come before it.)  Order is by (value, then place), which no two candidates share, so the
 // result does not depend on timing.  lse is a sum of fp32 exponentials, joined in 64 bits: within one beam the order is the scores', exactly.
@@ -17,7 +17,7 @@
 
 namespace mpcnn {
 
-constexpr int kChunk = 1024;               // classes
+constexpr int kStep = 1024, kChunk = 256;  // classes
 constexpr int kMaxBeams = 64;
 constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64;
 
@@ -29,7 +29,7 @@ struct BeamArgs {
     const unsigned char* done;             // null: none
     int end;
     int sequences, beams, width;
-    int V, chunks, parts, part_chunks;     // chunks of a row, workgroups of a row, chunks of a workgroup
+    int V, chunks, steps, parts, part_steps;   // chunks and steps of a row, workgroups of a row, steps of a workgroup
     float2* stats;                         // [rows][parts]
     float* tops;                           // [rows][chunks]
     float* totals_out;
@@ -37,23 +37,23 @@ struct BeamArgs {
     unsigned char* done_out;
 };
 
-// A row's chunks: a lane has E numbers (16 bytes) of each J stretches.  The classes' shares do not depend on where the row lies, so rows that hold the same have
+// A row's steps: 16 lanes side by side have a chunk, a lane E numbers (16 bytes) of each J stretches of it.  The classes' shares do not depend on where the row lies, so rows that hold the same have
 // the same sums (and beams that are alike are equals).
 template <typename T>
 struct BeamRow {
-    static constexpr int E = 16 / sizeof(T), J = kChunk / (64 * E);
+    static constexpr int E = 16 / sizeof(T), J = kStep / (64 * E);
     using Block = std::conditional_t<sizeof(T) == 2, Odd8, Raw<float, 4>>;
     const T* from;
     int V;
     bool odd;                              // begins between two words (bf16)
     const float* bias;
     __device__ BeamRow(const BeamArgs& a, long row) : from((const T*)a.scores + row * a.pitch), V(a.V), odd((uintptr_t)from & 2), bias(a.bias) {}
-    __device__ static int number(int j) { return E * ((int)(threadIdx.x & 63) + 64 * j); }
-    __device__ void fetch(int chunk, Block (&u)[J]) const
+    __device__ static int number(int j) { return kChunk * (int)(threadIdx.x >> 4 & 3) + E * ((int)(threadIdx.x & 15) + 16 * j); }
+    __device__ void fetch(int step, Block (&u)[J]) const
     {
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            const int at = kChunk * chunk + number(j);
+            const int at = kStep * step + number(j);
             if (at >= V) continue;
             if constexpr (sizeof(T) == 4) u[j] = raw_of<4>(from, at, V);
             else if (at + 8 > V) u[j] = odd8_of(from, at, V);
@@ -61,20 +61,25 @@ struct BeamRow {
             else u[j].a = *reinterpret_cast<const Odd8::u4_any*>(from + at);
         }
     }
-    // scores with the bias; minus infinity beyond the row and for classes that are off, whatever is there
-    __device__ void scores(int chunk, const Block (&u)[J], float (&s)[J][E]) const
+    // scores with the bias; minus infinity beyond the row and for classes that are off, whatever is there.  SIMPLE: of a whole step, in which a class that is off
+    // may be NaN if its score is not finite
+    template <bool SIMPLE = false>
+    __device__ void scores(int step, const Block (&u)[J], float (&s)[J][E]) const
     {
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            const int at = kChunk * chunk + number(j);
+            const int at = kStep * step + number(j);
             float b[E];
-            if (bias && at + E <= V) {
+            if (bias && (SIMPLE || at + E <= V)) {
 #pragma unroll
                 for (int e = 0; e < E; e += 4) {
                     const f4_any w = *reinterpret_cast<const f4_any*>(bias + at + e);
 #pragma unroll
                     for (int z = 0; z < 4; ++z) b[e + z] = w[z];
                 }
+            } else if constexpr (SIMPLE) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) b[e] = 0.f;
             } else {
 #pragma unroll
                 for (int e = 0; e < E; ++e) b[e] = bias && at + e < V ? bias[at + e] : 0.f;
@@ -88,37 +93,24 @@ struct BeamRow {
                 for (int e = 0; e < E; ++e) s[j][e] = v[e];
             }
 #pragma unroll
-            for (int e = 0; e < E; ++e) s[j][e] = at + e < V && b[e] != -__builtin_inff() ? s[j][e] + b[e] : -__builtin_inff();
+            for (int e = 0; e < E; ++e) s[j][e] = SIMPLE || (at + e < V && b[e] != -__builtin_inff()) ? s[j][e] + b[e] : -__builtin_inff();
         }
+    }
+    // one of them
+    __device__ float one(int at) const
+    {
+        const float b = bias && at < V ? bias[at] : 0.f;
+        return at < V && b != -__builtin_inff() ? load1(from + at) + b : -__builtin_inff();
     }
 };
 
-// The same of scores that lie [class][row], fp32, as a class layer leaves them, with their bias
+// Scores that lie [class][row], fp32, as a class layer leaves them, with their bias
 struct BeamColumn {
-    static constexpr int E = 4, J = kChunk / (64 * E);
-    typedef float Block[E];
     const float* from;
     long pitch;
     int V;
     __device__ BeamColumn(const BeamArgs& a, long row) : from((const float*)a.scores + row), pitch(a.pitch), V(a.V) {}
-    __device__ static int number(int j) { return E * ((int)(threadIdx.x & 63) + 64 * j); }
-    __device__ void fetch(int chunk, Block (&u)[J]) const
-    {
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int at = kChunk * chunk + number(j) + e;
-                u[j][e] = at < V ? from[at * pitch] : -__builtin_inff();
-            }
-    }
-    __device__ void scores(int, const Block (&u)[J], float (&s)[J][E]) const
-    {
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-            for (int e = 0; e < E; ++e) s[j][e] = u[j][e];
-    }
+    __device__ float one(int at) const { return at < V ? from[at * pitch] : -__builtin_inff(); }
 };
 
 __device__ __forceinline__ bool beam_goes_on(const BeamArgs& a, long row)
@@ -129,11 +121,11 @@ __device__ __forceinline__ bool beam_goes_on(const BeamArgs& a, long row)
 // exp(x - top) for x <= top; 0 for minus infinity
 __device__ __forceinline__ float exp_below(float x, float top) { return __builtin_amdgcn_exp2f((x - top) * 1.4426950408889634f); }
 
-__device__ __forceinline__ float largest64(float m)
+// Largest and sum of exponentials of two lots of classes together
+__device__ __forceinline__ float2 joined(const float2& p, const float2& q)
 {
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) m = fmaxf(m, __shfl_xor(m, i, 64));
-    return m;
+    const float now = fmaxf(p.x, q.x), base = now == -__builtin_inff() ? 0.f : now;
+    return float2{now, p.y * exp_below(p.x, base) + q.y * exp_below(q.x, base)};
 }
 
 template <typename T>
@@ -145,29 +137,42 @@ __global__ __launch_bounds__(256) void beam_stats_kernel(BeamArgs a)
     const int part = (int)(blockIdx.x % a.parts), lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (!beam_goes_on(a, row)) return;
     const Row r(a, row);
-    const int end = (part + 1) * a.part_chunks < a.chunks ? (part + 1) * a.part_chunks : a.chunks;
-    int c = part * a.part_chunks + wave;
+    const int end = (part + 1) * a.part_steps < a.steps ? (part + 1) * a.part_steps : a.steps;
+    int c = part * a.part_steps + wave;
     typename Row::Block u[Row::J];
     if (c < end) r.fetch(c, u);
     float top = -__builtin_inff(), sum = 0.f;
     for (; c < end; c += 4) {
-        float s[Row::J][Row::E];
-        r.scores(c, u, s);
+        float s[Row::J][Row::E], now, more;
+        auto add = [&] {
+            float most = s[0][0];
+#pragma unroll
+            for (int j = 0; j < Row::J; ++j)
+#pragma unroll
+                for (int e = 0; e < Row::E; ++e) most = fmaxf(most, s[j][e]);
+            most = largest16(most);
+            const int chunk = kStep / kChunk * c + (lane >> 4);
+            if ((lane & 15) == 0 && chunk < a.chunks) a.tops[row * a.chunks + chunk] = most;
+            now = fmaxf(top, largest_of16s(most));
+            const float base = now == -__builtin_inff() ? 0.f : now;
+            more = 0.f;
+#pragma unroll
+            for (int j = 0; j < Row::J; ++j)
+#pragma unroll
+                for (int e = 0; e < Row::E; ++e) more += exp_below(s[j][e], base);
+        };
+        const bool whole = kStep * (c + 1) <= a.V;
+        if (whole) {
+            r.template scores<true>(c, u, s);
+            add();
+        }
+        if (!whole || (a.bias && __ballot(more != more))) {   // (hardly ever)
+            r.scores(c, u, s);
+            add();
+        }
         if (c + 4 < end) r.fetch(c + 4, u);
-        float most = s[0][0];
-#pragma unroll
-        for (int j = 0; j < Row::J; ++j)
-#pragma unroll
-            for (int e = 0; e < Row::E; ++e) most = fmaxf(most, s[j][e]);
-        most = largest64(most);
-        if (lane == 0) a.tops[row * a.chunks + c] = most;
-        const float now = fmaxf(top, most), base = now == -__builtin_inff() ? 0.f : now;
-        sum *= exp_below(top, base);
+        sum = sum * exp_below(top, now == -__builtin_inff() ? 0.f : now) + more;
         top = now;
-#pragma unroll
-        for (int j = 0; j < Row::J; ++j)
-#pragma unroll
-            for (int e = 0; e < Row::E; ++e) sum += exp_below(s[j][e], base);
     }
     sum = sum64(sum);
     if (lane == 0) red[wave] = float2{top, sum};
@@ -175,44 +180,39 @@ __global__ __launch_bounds__(256) void beam_stats_kernel(BeamArgs a)
     if (threadIdx.x == 0) {
         float2 all = red[0];
 #pragma unroll
-        for (int w = 1; w < 4; ++w) {
-            const float now = fmaxf(all.x, red[w].x), base = now == -__builtin_inff() ? 0.f : now;
-            all = float2{now, all.y * exp_below(all.x, base) + red[w].y * exp_below(red[w].x, base)};
-        }
+        for (int w = 1; w < 4; ++w) all = joined(all, red[w]);
         a.stats[row * a.parts + part] = all;
     }
 }
 
-// Scores [class][row]: a workgroup has a chunk of classes of four rows, a thread four classes
+// Scores [class][row]: a workgroup has a step of the classes of four rows, a wave a chunk
 __global__ __launch_bounds__(256) void beam_columns_kernel(BeamArgs a)
 {
-    __shared__ float tops[4][4], sums[4][4];
-    const int chunk = (int)(blockIdx.x % a.chunks), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long row0 = 4 * (long)(blockIdx.x / a.chunks), rows = (long)a.sequences * a.beams;
+    __shared__ float2 red[4][4];
+    const int step = (int)(blockIdx.x % a.steps), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunk = kStep / kChunk * step + wave;
+    const long row0 = 4 * (long)(blockIdx.x / a.steps), rows = (long)a.sequences * a.beams;
     v4f s[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int at = kChunk * chunk + 256 * i + (int)threadIdx.x;
+        const int at = kChunk * chunk + 64 * i + lane;
         s[i] = at < a.V ? *reinterpret_cast<const v4f*>((const float*)a.scores + at * a.pitch + row0) : v4f(-__builtin_inff());
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const float m = largest64(fmaxf(fmaxf(s[0][r], s[1][r]), fmaxf(s[2][r], s[3][r])));
-        if (lane == 0) tops[wave][r] = m;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float top = fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r])), base = top == -__builtin_inff() ? 0.f : top;
+        const float top = largest64(fmaxf(fmaxf(s[0][r], s[1][r]), fmaxf(s[2][r], s[3][r]))), base = top == -__builtin_inff() ? 0.f : top;
         const float sum = sum64((exp_below(s[0][r], base) + exp_below(s[1][r], base)) + (exp_below(s[2][r], base) + exp_below(s[3][r], base)));
-        if (lane == 0) sums[wave][r] = sum;
+        if (lane == 0) {
+            red[wave][r] = float2{top, sum};
+            if (row0 + r < rows && chunk < a.chunks) a.tops[(row0 + r) * a.chunks + chunk] = top;
+        }
     }
     __syncthreads();
     const int r = threadIdx.x;
     if (r >= 4 || row0 + r >= rows) return;
-    const float top = fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r]));
-    a.tops[(row0 + r) * a.chunks + chunk] = top;
-    a.stats[(row0 + r) * a.parts + chunk] = float2{top, (sums[0][r] + sums[1][r]) + (sums[2][r] + sums[3][r])};
+    float2 all = red[0][r];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) all = joined(all, red[w][r]);
+    a.stats[(row0 + r) * a.parts + step] = all;
 }
 
 // ---- the second launch
@@ -226,171 +226,257 @@ __device__ __forceinline__ u64 key_of(double v)
     return b >> 63 ? ~b : b | 1ull << 63;
 }
 __device__ __forceinline__ double value_of(u64 key) { return __builtin_bit_cast(double, key >> 63 ? key ^ 1ull << 63 : ~key); }
-__device__ __forceinline__ u64 largest64(u64 k)
+
+// A chunk or a candidate and its place among those of the same value: the lower one is better
+struct Offer { u64 key; unsigned place; };
+__device__ __forceinline__ bool better(const Offer& a, const Offer& b) { return a.key > b.key || (a.key == b.key && a.place < b.place); }
+// The better one of this lane's and of the one that CTRL names
+template <int CTRL>
+__device__ __forceinline__ Offer better_moved(const Offer& m)
 {
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) {
-        const u64 o = __shfl_xor(k, i, 64);
-        k = o > k ? o : k;
-    }
-    return k;
+    auto moved = [](unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false); };
+    const Offer o{(u64)moved((unsigned)(m.key >> 32)) << 32 | moved((unsigned)m.key), moved(m.place)};
+    return better(o, m) ? o : m;
+}
+// Over `lanes` (2, 4 or 8, uniform) side by side, in all of them
+__device__ __forceinline__ Offer best_beside(Offer m, int lanes)
+{
+    m = better_moved<0xb1>(m);                       // quad_perm:[1,0,3,2]
+    if (lanes > 2) m = better_moved<0x4e>(m);        // quad_perm:[2,3,0,1]
+    return lanes > 4 ? better_moved<0x141>(m) : m;   // row_half_mirror
+}
+__device__ __forceinline__ int sum_beside(int v, int lanes)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0xb1, 0xf, 0xf, true);
+    if (lanes > 2) v += __builtin_amdgcn_update_dpp(0, v, 0x4e, 0xf, 0xf, true);
+    return lanes > 4 ? v + __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true) : v;
 }
 
-// The best of the wave's candidates and where it is (all lanes' places differ): the lowest place of the largest key
-__device__ __forceinline__ u64 best_of(u64 key, unsigned place, unsigned* best)
-{
-    const u64 top = largest64(key);
-    u64 lanes = __ballot(key == top);
-    unsigned p = 0xffffffffu;
-    while (lanes) {                        // (one, but for ties)
-        const int l = __builtin_ctzll(lanes);
-        const unsigned o = (unsigned)__builtin_amdgcn_readlane((int)place, l);
-        p = o < p ? o : p;
-        lanes &= lanes - 1;
-    }
-    *best = p;
-    return top;
-}
-
-struct BeamOffer { u64 key; unsigned place; };   // of a chunk: beam * chunks + chunk; of a candidate: chosen chunk << 10 | number
+// What is picked from is kept in LDS: places for kSpare offers of each wanted one (kEach of each of a group's threads, and the winners so far)
+constexpr int kEach = 8, kSpare = 8 * kEach + 1;
+constexpr size_t pick_bytes(int width) { return (size_t)width * (width > kSpare ? width : kSpare) * 12; }
 
 template <typename Row>
 __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a)
 {
-    constexpr int R = 4;                   // chunks of a lane at once
+    constexpr int kGroups = kPickThreads / 2;
     extern __shared__ __attribute__((aligned(16))) char lds_raw[];
     __shared__ double lse[kMaxBeams];
     __shared__ float total[kMaxBeams];
-    __shared__ unsigned char kind[kMaxBeams];            // 0: offers nothing, 1: goes on, 2: finished
-    __shared__ u64 part_key[kPickWaves * kMaxBeams];
-    __shared__ unsigned part_place[kPickWaves * kMaxBeams];
+    __shared__ int kind[kMaxBeams];                      // 0: offers nothing, 1: goes on, 2: finished
+    __shared__ u64 group_key[kGroups];
+    __shared__ unsigned group_place[kGroups];
     __shared__ u64 chosen_key[kMaxBeams];
-    __shared__ unsigned chosen_place[kMaxBeams];
-    __shared__ unsigned count;
+    __shared__ unsigned chosen_place[kMaxBeams], number_of[kMaxBeams], numbered[kMaxBeams];
+    __shared__ u64 least_key;
+    __shared__ unsigned least_place, count;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int W = a.width, K = a.beams;
-    u64* const cand_key = reinterpret_cast<u64*>(lds_raw);             // [W W]
-    unsigned* const cand_place = reinterpret_cast<unsigned*>(lds_raw + sizeof(u64) * W * W);
+    // threads of a group, so that there are four groups for every wanted one
+    const int beside = a.width <= kPickThreads / 32 ? 8 : a.width <= kPickThreads / 16 ? 4 : 2, of_group = tid / beside;
+    static_assert(kMaxBeams <= kPickThreads / 8, "groups of two do");
+    const int W = a.width, K = a.beams, all = K * a.chunks;            // (chunks of all beams: below 2^30)
+    const int room = W * (W > kSpare ? W : kSpare);
+    u64* const cand_key = reinterpret_cast<u64*>(lds_raw);             // [room]
+    unsigned* const cand_place = reinterpret_cast<unsigned*>(lds_raw + sizeof(u64) * room);
     const long row0 = (long)blockIdx.x * K;
+
+    float tops[kEach];
+    auto fetch = [&](int base) {
+#pragma unroll
+        for (int r = 0; r < kEach; ++r) {
+            const int i = base + kPickThreads * r + tid;
+            tops[r] = i < all ? a.tops[row0 * a.chunks + i] : 0.f;     // (of a beam that does not go on: whatever is there)
+        }
+    };
+    fetch(0);
 
     // ---- the beams' sums
     for (int k = wave; k < K; k += kPickWaves) {
         const long row = row0 + k;
         const float t = a.totals[row];
-        int is = t > -__builtin_inff() ? (a.done && a.done[row] ? 2 : 1) : 0;
+        const bool over = a.done && a.done[row];
+        const float2* const stats = a.stats + row * a.parts;
+        constexpr float2 kNone{-__builtin_inff(), 0.f};
+        const float2 mine = lane < a.parts ? stats[lane] : kNone;      // (used if it goes on)
+        int is = t > -__builtin_inff() ? (over ? 2 : 1) : 0;
         double l = 0.0;
         if (is == 1) {
-            float top = -__builtin_inff();
-            for (int p = lane; p < a.parts; p += 64) top = fmaxf(top, a.stats[row * a.parts + p].x);
+            float top = mine.x;
+            for (int p = lane + 64; p < a.parts; p += 64) top = fmaxf(top, stats[p].x);
             top = largest64(top);
-            double sum = 0.0;
-            for (int p = lane; p < a.parts; p += 64) {
-                const float2 s = a.stats[row * a.parts + p];
-                if (s.x > -__builtin_inff() || s.y != 0.f) sum += (double)s.y * exp((double)s.x - (double)top);
-            }
+            auto share = [&](const float2& s) { return s.x > -__builtin_inff() || s.y != 0.f ? (double)s.y * exp((double)s.x - (double)top) : 0.0; };
+            double sum = share(mine);
+            for (int p = lane + 64; p < a.parts; p += 64) sum += share(stats[p]);
 #pragma unroll
             for (int i = 1; i < 64; i *= 2) sum += __shfl_xor(sum, i, 64);
             l = (double)top + log(sum);
             if (!(l > -__builtin_inf() && l < __builtin_inf())) is = 0;        // nothing is on, or a score is not finite
         }
-        if (lane == 0) { lse[k] = l; total[k] = t; kind[k] = (unsigned char)is; }
+        if (lane == 0) { lse[k] = l; total[k] = t; kind[k] = is; }
     }
-    if (tid < W) { chosen_key[tid] = 0; chosen_place[tid] = 0; }
-    if (tid == 0) count = 0;
+    if (tid < W) { chosen_key[tid] = 0; chosen_place[tid] = 0xffffffffu; }
     __syncthreads();
 
-    // ---- each wave's best chunks: winners so far (slot 0, winner i in lane i) against the next R of every lane
-    const int all = K * a.chunks;          // (below 2^28)
-    u64 won_key = 0;
-    unsigned won_place = 0xffffffffu;
-    for (int base = wave * 64 * R; base < all; base += kPickThreads * R) {
-        u64 key[R + 1];
-        unsigned place[R + 1];
-        key[R] = won_key; place[R] = won_place;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int i = base + 64 * r + lane;
-            key[r] = 0; place[r] = (unsigned)i;
-            if (i >= all) continue;
-            const int k = i / a.chunks, c = i - k * a.chunks;
-            if (kind[k] == 1) key[r] = key_of((double)total[k] + ((double)a.tops[(row0 + k) * a.chunks + c] - lse[k]));
-            else if (kind[k] == 2 && c == 0) key[r] = key_of((double)total[k]);       // (its only candidate: see below)
-        }
-        won_key = 0; won_place = 0xffffffffu;
-        for (int w = 0; w < W; ++w) {
-            u64 mine = key[0];
-            unsigned at = place[0];
-#pragma unroll
-            for (int r = 1; r <= R; ++r)
-                if (key[r] > mine || (key[r] == mine && place[r] < at)) { mine = key[r]; at = place[r]; }
-            unsigned best;
-            const u64 top = best_of(mine, at, &best);
-            if (!top) break;
-#pragma unroll
-            for (int r = 0; r <= R; ++r)
-                if (key[r] == top && place[r] == best) key[r] = 0;
-            if (lane == w) { won_key = top; won_place = best; }
-        }
-    }
-    if (lane < W) { part_key[wave * W + lane] = won_key; part_place[wave * W + lane] = won_place; }
-    __syncthreads();
-
-    // ---- the best chunks of all waves, by how many come before each
-    auto before = [](u64 k, unsigned p, u64 key, unsigned place) { return k > key || (k == key && p < place); };
-    for (int i = tid; i < kPickWaves * W; i += kPickThreads) {
-        const u64 key = part_key[i];
-        if (!key) continue;
-        const unsigned place = part_place[i];
+    auto rank_of = [&](const Offer& mine, int n) {           // how many of the first n candidates come before
         int rank = 0;
-        for (int o = 0; o < kPickWaves * W; ++o) rank += before(part_key[o], part_place[o], key, place);
-        if (rank < W) { chosen_key[rank] = key; chosen_place[rank] = place; }
-    }
-    __syncthreads();
-
-    // ---- their numbers that are not below the last chosen chunk's largest, at most W of each
-    const u64 least = chosen_key[W - 1];
+#pragma unroll 4
+        for (int o = 0; o < n; ++o) rank += better(Offer{cand_key[o], cand_place[o]}, mine);
+        return rank;
+    };
+    // The best W of the first `n` candidates into chosen, best first, by how many come before each
+    auto choose = [&](int n) {
+        for (int i = tid; i < n; i += kPickThreads) {
+            const Offer mine{cand_key[i], cand_place[i]};
+            const int rank = rank_of(mine, n);
+            if (rank < W) { chosen_key[rank] = mine.key; chosen_place[rank] = mine.place; }
+        }
+    };
     auto offer = [&](u64 key, unsigned place) {
         const unsigned i = atomicAdd(&count, 1u);
         cand_key[i] = key;
         cand_place[i] = place;
     };
+
+    // ---- the best chunks, kEach of a thread at a time: no better ones than those that are not worse than the W-th best of the groups' best can be among the best W
+    for (int base = 0; base < all; base += kPickThreads * kEach) {
+        Offer mine[kEach], best{0, 0xffffffffu};
+#pragma unroll
+        for (int r = 0; r < kEach; ++r) {
+            const int i = base + kPickThreads * r + tid;
+            mine[r] = Offer{0, (unsigned)i};
+            if (i >= all) continue;
+            const int k = i / a.chunks;
+            if (kind[k] == 1) mine[r].key = key_of((double)total[k] + ((double)tops[r] - lse[k]));
+            else if (kind[k] == 2 && i == k * a.chunks) mine[r].key = key_of((double)total[k]);        // (its one candidate)
+            if (better(mine[r], best)) best = mine[r];
+        }
+        if (base + kPickThreads * kEach < all) fetch(base + kPickThreads * kEach);
+        best = best_beside(best, beside);
+        if (tid % beside == 0) { group_key[of_group] = best.key; group_place[of_group] = best.place; }
+        if (tid == 0) { least_key = 0; least_place = 0xffffffffu; count = 0; }
+        __syncthreads();
+        {   // a group's threads: how many groups' best come before its
+            int rank = 0;
+            for (int g = tid % beside; g < kPickThreads / beside; g += beside) rank += better(Offer{group_key[g], group_place[g]}, best);
+            rank = sum_beside(rank, beside);
+            if (rank == W - 1 && tid % beside == 0 && best.key) { least_key = best.key; least_place = best.place; }     // (groups without a chunk are alike)
+        }
+        __syncthreads();
+        const Offer least{least_key, least_place};
+#pragma unroll
+        for (int r = 0; r < kEach; ++r)
+            if (mine[r].key && !better(least, mine[r])) offer(mine[r].key, mine[r].place);
+        if (base && tid < W && chosen_key[tid]) offer(chosen_key[tid], chosen_place[tid]);
+        __syncthreads();
+        const int n = (int)count;
+        if (base) {                                      // (the winners so far are candidates now)
+            if (tid < W) { chosen_key[tid] = 0; chosen_place[tid] = 0xffffffffu; }
+            __syncthreads();
+        }
+        choose(n);
+        __syncthreads();
+    }
+    // (candidates' places have to be in the order of their beams and classes: the chosen chunks are numbered by their places)
+    if (tid < W) {
+        const unsigned mine = chosen_place[tid];
+        int n = 0;
+        for (int o = 0; o < W; ++o) n += chosen_place[o] < mine;
+        number_of[tid] = (unsigned)n << 8;
+        if (chosen_key[tid]) numbered[n] = mine;
+    }
+    if (tid == 0) count = 0;
+    __syncthreads();
+
+    // ---- their numbers that are not below the last chosen chunk's largest (of a chunk with many: the best)
+    constexpr int E = kChunk / 64;
+    const u64 least = chosen_key[W - 1];
+    float next[E];
+    auto look = [&](int w) {
+        if (w >= W || !chosen_key[w]) return;
+        const int k = (int)(chosen_place[w] / (unsigned)a.chunks), c = (int)chosen_place[w] - k * a.chunks;
+        if (kind[k] == 2) return;
+        const Row r(a, row0 + k);
+#pragma unroll
+        for (int e = 0; e < E; ++e) next[e] = r.one(kChunk * c + E * lane + e);
+    };
+    look(wave);
     for (int w = wave; w < W; w += kPickWaves) {
         if (!chosen_key[w]) continue;
-        const int k = (int)chosen_place[w] / a.chunks, c = (int)chosen_place[w] - k * a.chunks;
+        const int k = (int)(chosen_place[w] / (unsigned)a.chunks);
         if (kind[k] == 2) {
-            if (lane == 0) offer(chosen_key[w], (unsigned)w << 10);
+            if (lane == 0) offer(chosen_key[w], number_of[w]);
+            look(w + kPickWaves);
             continue;
         }
-        const Row r(a, row0 + k);
-        typename Row::Block u[Row::J];
-        r.fetch(c, u);
-        float s[Row::J][Row::E];
-        r.scores(c, u, s);
-        u64 key[Row::J][Row::E];
+        float s[E];
 #pragma unroll
-        for (int j = 0; j < Row::J; ++j)
+        for (int e = 0; e < E; ++e) s[e] = next[e];
+        look(w + kPickWaves);
+        // a score below `lo` has a value below the least (a millionth is more than the roundings)
+        const double t = (double)total[k], need = least ? value_of(least) - t + lse[k] : -__builtin_inf();
+        const float lo = (float)(need - 1e-6 * (fabs(need) + fabs(t) + fabs(lse[k])));
+        u64 key[E];
+        int n = 0;
 #pragma unroll
-            for (int e = 0; e < Row::E; ++e) {
-                const u64 v = key_of((double)total[k] + ((double)s[j][e] - lse[k]));
-                key[j][e] = v >= least ? v : 0;
+        for (int e = 0; e < E; ++e) {
+            key[e] = 0;
+            if (s[e] >= lo && s[e] > -__builtin_inff()) {
+                const u64 v = key_of(t + ((double)s[e] - lse[k]));
+                if (v >= least) key[e] = v;
             }
-        for (int n = 0; n < W; ++n) {
-            u64 mine = 0;
-            unsigned at = 0xffffffffu;
+            n += __builtin_popcountll(__ballot(key[e] != 0));
+        }
+        const unsigned of = number_of[w];
+        static_assert(kChunk == 256, "a number's bits");
+        if (n > (W > kSpare ? W : kSpare)) {             // more than there is room for: those that are not worse than the W-th best of the lanes' best
+            Offer best{0, 0xffffffffu};
 #pragma unroll
-            for (int j = 0; j < Row::J; ++j)
+            for (int e = 0; e < E; ++e)
+                if (key[e] > best.key) best = Offer{key[e], (unsigned)(E * lane + e)};
+            int rank = 0;
 #pragma unroll
-                for (int e = 0; e < Row::E; ++e)
-                    if (key[j][e] > mine) { mine = key[j][e]; at = (unsigned)(Row::number(j) + e); }       // (the lowest number of equals)
-            unsigned best;
-            const u64 top = best_of(mine, at, &best);
-            if (!top) break;
+            for (int l = 0; l < 64; ++l) {
+                const Offer o{(u64)(unsigned)__builtin_amdgcn_readlane((int)(best.key >> 32), l) << 32 | (unsigned)__builtin_amdgcn_readlane((int)best.key, l),
+                              (unsigned)__builtin_amdgcn_readlane((int)best.place, l)};
+                rank += better(o, best);
+            }
+            const u64 last = __ballot(rank == W - 1 && best.key != 0);
+            if (last) {
+                const int l = __builtin_ctzll(last);
+                const u64 bound = (u64)(unsigned)__builtin_amdgcn_readlane((int)(best.key >> 32), l) << 32 | (unsigned)__builtin_amdgcn_readlane((int)best.key, l);
+                n = 0;
 #pragma unroll
-            for (int j = 0; j < Row::J; ++j)
+                for (int e = 0; e < E; ++e) {
+                    key[e] = key[e] >= bound ? key[e] : 0;
+                    n += __builtin_popcountll(__ballot(key[e] != 0));
+                }
+            }
+        }
+        if (n <= (W > kSpare ? W : kSpare)) {
 #pragma unroll
-                for (int e = 0; e < Row::E; ++e)
-                    if (best == (unsigned)(Row::number(j) + e)) key[j][e] = 0;
-            if (lane == 0) offer(top, (unsigned)w << 10 | best);
+            for (int e = 0; e < E; ++e)
+                if (key[e]) offer(key[e], of | (unsigned)(E * lane + e));
+            continue;
+        }
+        for (int q = 0; q < W; ++q) {                    // (more than can be: the best of them, one after the other)
+            Offer best{0, 0xffffffffu};
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const Offer o{key[e], (unsigned)(E * lane + e)};
+                if (better(o, best)) best = o;
+            }
+            best = best_beside(best, 8);
+            best = better_moved<0x128>(best);            // row_ror:8
+#pragma unroll
+            for (int i = 16; i < 64; i *= 2) {
+                const Offer o{__shfl_xor(best.key, i, 64), __shfl_xor(best.place, i, 64)};
+                if (better(o, best)) best = o;
+            }
+            if (!best.key) break;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (best.place == (unsigned)(E * lane + e)) key[e] = 0;
+            if (lane == 0) offer(best.key, of | best.place);
         }
     }
     __syncthreads();
@@ -398,23 +484,14 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a)
     // ---- the best of these
     const int n = (int)count;
     const long out = (long)blockIdx.x * W;
-    auto place_of = [&](unsigned p) -> u64 {
-        const unsigned chunk = chosen_place[p >> 10];
-        const int k = (int)chunk / a.chunks, c = (int)chunk - k * a.chunks;
-        if (kind[k] == 2) return (u64)k * (unsigned)a.V + (unsigned)a.end;
-        return (u64)k * (unsigned)a.V + (unsigned)(kChunk * c + (int)(p & (kChunk - 1)));
-    };
     for (int i = tid; i < n; i += kPickThreads) {
-        const u64 key = cand_key[i];
-        int rank = 0;
-        u64 place = place_of(cand_place[i]);
-        for (int o = 0; o < n; ++o) {
-            const u64 k = cand_key[o];
-            rank += k > key || (k == key && o != i && place_of(cand_place[o]) < place);
-        }
+        const Offer mine{cand_key[i], cand_place[i]};
+        const int rank = rank_of(mine, n);
         if (rank >= W) continue;
-        const int k = (int)(place / (unsigned)a.V), v = (int)(place - (u64)k * (unsigned)a.V);
-        a.totals_out[out + rank] = (float)value_of(key);
+        const unsigned chunk = numbered[mine.place >> 8];
+        const int k = (int)(chunk / (unsigned)a.chunks), c = (int)chunk - k * a.chunks;
+        const int v = kind[k] == 2 ? a.end : kChunk * c + (int)(mine.place & (kChunk - 1));
+        a.totals_out[out + rank] = (float)value_of(mine.key);
         a.parents[out + rank] = k;
         a.classes[out + rank] = v;
         if (a.done_out) a.done_out[out + rank] = kind[k] == 2 || v == a.end;
