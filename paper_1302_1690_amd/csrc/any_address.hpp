@@ -77,6 +77,16 @@ __device__ __forceinline__ Raw<T, E> raw_of(const T* row, int at, int n)
 template <typename T> __device__ __forceinline__ Raw8<T> raw8_of(const T* row, int at, int n) { return raw_of<8>(row, at, n); }
 template <typename T> __device__ __forceinline__ v8f load8_of(const T* row, int at, int n) { return widen(raw8_of(row, at, n)); }
 
+// Numbers row[at .. at + 7] of a row of n, none beyond its end
+template <typename T>
+__device__ __forceinline__ void store8_of(T* row, int at, int n, v8f v)
+{
+    if (at + 8 <= n) { store8(row + at, v); return; }
+#pragma unroll
+    for (int z = 0; z < 8; ++z)
+        if (at + z < n) store1(row + at + z, v[z]);
+}
+
 // Eight bf16 numbers at addresses of which some are no multiple of four, as the words that they lie in (each holds one of them at least), and turned
 // by 16 bits where they begin in the middle of one.  The memory pipeline takes 128-bit fetches at such addresses apart.
 struct Odd8 {

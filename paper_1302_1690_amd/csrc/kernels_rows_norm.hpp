@@ -65,15 +65,6 @@ __device__ __forceinline__ void sum_row(float (&v)[N], float (*red)[N][16], int 
 }
 
 template <typename T>
-__device__ __forceinline__ void store8_of(T* row, int at, int n, v8f v)
-{
-    if (at + 8 <= n) { store8(row + at, v); return; }
-#pragma unroll
-    for (int z = 0; z < 8; ++z)
-        if (at + z < n) store1(row + at + z, v[z]);
-}
-
-template <typename T>
 __device__ __forceinline__ void norm_store(const NormArgs& a, long n, int at, v8f h, v8f gain, float rstd)
 {
     if (a.h) store8_of((T*)a.h + n * a.h_pitch, at, a.D, h);

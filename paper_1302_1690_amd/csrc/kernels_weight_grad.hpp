@@ -8,13 +8,15 @@
 // there, once per workgroup.  The instruction wants 8 rows of one column per lane: ds_read_b64_tr_b16 turns 4 rows x 16 columns around within 16 lanes (lane r
 // names 4 columns, r % 4, of row r / 4 and receives column r of all 4).  The 64-byte groups of a row lie permuted by the row's number, on different banks.
 #pragma once
+#include <type_traits>
+
 #include "packed.hpp"
 
 namespace mpcnn {
 
 struct WeightGradArgs {
     const void* dy;
-    long dy_pitch;
+    long dy_pitch, dy_bytes;               // bytes of all of it, to the last piece's end
     Packed x;
     int N, M, D, padded;                   // rows, outputs, features
     int blocks, per_split, splits;         // along the rows: in all, of a workgroup
@@ -25,22 +27,71 @@ struct WeightGradArgs {
 };
 
 typedef __bf16 g_bf16x8 __attribute__((ext_vector_type(8)));
-typedef short g_s4 __attribute__((ext_vector_type(4)));
+typedef float g_f2 __attribute__((ext_vector_type(2)));
 typedef unsigned g_u4 __attribute__((ext_vector_type(4)));
 
-// 8 numbers of packed rows as bf16 (exact)
-__device__ __forceinline__ g_bf16x8 widen8(u2 r, unsigned scale, int kind) { return __builtin_convertvector(unpack8(r, scale, kind), g_bf16x8); }
+// 8 numbers of packed rows as bf16 (exact).  E4M3: two at a time by the instruction that multiplies with a power of two (whose NaN is not a number's)
+template <int KIND>
+__device__ __forceinline__ g_bf16x8 widen8(u2 r, unsigned scale)
+{
+    if constexpr (KIND == MPCNN_I8) return __builtin_convertvector(unpack8(r, scale, KIND), g_bf16x8);
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    const float by = scale ? __builtin_bit_cast(float, scale << 23) : 0x1p-127f;
+    g_u4 v;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        v[2 * h] = __builtin_bit_cast(unsigned, (b2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r[h], by, false));
+        v[2 * h + 1] = __builtin_bit_cast(unsigned, (b2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r[h], by, true));
+    }
+#pragma unroll
+    for (int z = 0; z < 4; ++z) v[z] = scale == kNaNScale ? 0x7fc07fc0u : v[z];
+    return __builtin_bit_cast(g_bf16x8, v);
+}
 
-template <typename T, int WM, int WN, int MT, int NT, int KB>
+// The instruction's operands from LDS, of I tiles: 8 rows of one column a lane, at p + K and, the second 4 rows, JUMP bytes on.  (The builtin for
+// this waits for all fetches into LDS, also those into the other block's places.)
+template <int K, int JUMP>
+__device__ __forceinline__ void read_turned(g_bf16x8 (&x)[2], const unsigned (&p)[2])
+{
+    g_f2 a0, a1, b0, b1;
+    asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+                 "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a0), "=&v"(a1), "=&v"(b0), "=&v"(b1)
+                 : "v"(p[0]), "v"(p[1]), "n"(K), "n"(K + JUMP)
+                 : "memory");
+    x[0] = __builtin_bit_cast(g_bf16x8, v4f{a0[0], a0[1], a1[0], a1[1]});
+    x[1] = __builtin_bit_cast(g_bf16x8, v4f{b0[0], b0[1], b1[0], b1[1]});
+}
+template <int K, int JUMP>
+__device__ __forceinline__ void read_turned(g_bf16x8 (&x)[4], const unsigned (&p)[4])
+{
+    g_f2 a0, a1, b0, b1, c0, c1, d0, d1;
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a0), "=&v"(a1), "=&v"(b0), "=&v"(b1), "=&v"(c0), "=&v"(c1), "=&v"(d0), "=&v"(d1)
+                 : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(K), "n"(K + JUMP)
+                 : "memory");
+    x[0] = __builtin_bit_cast(g_bf16x8, v4f{a0[0], a0[1], a1[0], a1[1]});
+    x[1] = __builtin_bit_cast(g_bf16x8, v4f{b0[0], b0[1], b1[0], b1[1]});
+    x[2] = __builtin_bit_cast(g_bf16x8, v4f{c0[0], c0[1], c1[0], c1[1]});
+    x[3] = __builtin_bit_cast(g_bf16x8, v4f{d0[0], d0[1], d1[0], d1[1]});
+}
+
+// DIRECT (bf16 dy in aligned rows of whole 16-byte pieces): dy's blocks go from memory straight into LDS
+template <typename T, int KIND, int WM, int WN, int MT, int NT, int KB, bool DIRECT>
 __global__ __launch_bounds__(64 * WM * WN) void weight_grad_kernel(WeightGradArgs a)
 {
-    constexpr int BM = 32 * WM * MT, BN = 32 * WN * NT, kThreads = 64 * WM * WN;
+    constexpr int BM = 32 * WM * MT, BN = 32 * WN * NT, kThreads = 64 * WM * WN, S = KB / 16;
     constexpr int P = sizeof(T) == 4 ? 3 : 1;            // parts of dy
     constexpr int kARow = 2 * BM, kBRow = 2 * BN;        // bytes
     constexpr int kPart = KB * kARow, kStage = P * kPart + KB * kBRow;
     constexpr int AI = KB * BM / 8 / kThreads, BI = KB * BN / 16 / kThreads;
     static_assert(AI * 8 * kThreads == KB * BM && BI * 16 * kThreads == KB * BN, "the threads share a block evenly");
+    static_assert(!DIRECT || P == 1, "as it lies in memory");
     extern __shared__ __attribute__((aligned(256))) char lds_raw[];
+    typedef __attribute__((address_space(3))) void* lds_ptr;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
 
@@ -55,51 +106,78 @@ __global__ __launch_bounds__(64 * WM * WN) void weight_grad_kernel(WeightGradArg
     const int m0 = tm * BM, n0 = tn * BN;
     const int first = split * a.per_split, count = a.blocks - first < a.per_split ? a.blocks - first : a.per_split;
 
-    Raw8<T> ra[AI];
+    // ---- blocks from memory: dy a piece of 8 numbers of AI rows, x 16 numbers of BI rows a thread
+    Raw8<T> ra[DIRECT ? 1 : AI];
     g_u4 rb[BI];
     unsigned rs[BI];
-    auto fetch = [&](int block) {
-        const long k0 = (long)(first + block) * KB;
+    unsigned va[DIRECT ? AI : 1];                        // DIRECT: the pieces' places in memory, for their places in LDS
+    if constexpr (DIRECT)
 #pragma unroll
         for (int i = 0; i < AI; ++i) {
-            const int q = tid + kThreads * i, k = q / (BM / 8), at = m0 + 8 * (q % (BM / 8));
-            if (k0 + k < a.N && at < a.M) ra[i] = raw8_of((const T*)a.dy + (k0 + k) * a.dy_pitch, at, a.M);
-            else ra[i] = Raw8<T>{};
+            const unsigned at = (unsigned)((wave * AI + i) * 1024 + 16 * lane), k = at / kARow;
+            va[i] = k * (unsigned)(2 * a.dy_pitch) + 16u * ((at % kARow / 16) ^ 4 * (k & 3));
         }
+    // (from a block's first row on, with the matrix's end as its bound: rows beyond the last come as zeros)
+    auto from = [&](const void* m, long offset, long bytes) {
+        const long left = bytes - offset;
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>((const char*)m + (left > 0 ? offset : 0)), 0,
+                                                 left <= 0 ? 0 : left < 0x7fffffff ? (int)left : 0x7fffffff, 0x00020000);
+    };
+    auto fetch_direct = [&](int block, char* to) {
+        if constexpr (DIRECT) {
+            const __amdgpu_buffer_rsrc_t dy = from(a.dy, ((long)(first + block) * KB * a.dy_pitch + m0) * 2, a.dy_bytes);
 #pragma unroll
-        for (int i = 0; i < BI; ++i) {
-            const int q = tid + kThreads * i, k = q / (BN / 16), at = n0 + 16 * (q % (BN / 16));
-            rb[i] = g_u4{0, 0, 0, 0};
-            rs[i] = 127;
-            if (k0 + k < a.N && at < a.padded) {
-                rb[i] = *reinterpret_cast<const g_u4*>(a.x.values + (k0 + k) * a.padded + at);
-                rs[i] = a.x.scales[(k0 + k) * (a.padded / kBlock) + at / kBlock];
-            }
+            for (int i = 0; i < AI; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(dy, (lds_ptr)(to + (wave * AI + i) * 1024), 16, (int)va[i], 0, 0, 0);
         }
+    };
+    auto fetch = [&](int block) {
+        const long k0 = (long)(first + block) * KB;
+        if constexpr (!DIRECT)
+#pragma unroll
+            for (int i = 0; i < AI; ++i) {
+                const int q = tid + kThreads * i, k = q / (BM / 8), at = m0 + 8 * (q % (BM / 8));
+                if (k0 + k < a.N && at < a.M) ra[i] = raw8_of((const T*)a.dy + (k0 + k) * a.dy_pitch, at, a.M);
+                else ra[i] = Raw8<T>{};
+            }
+#pragma unroll
+        for (int i = 0; i < BI; ++i) {                   // (always as many loads as kLoads.  Rows beyond the last: the last one, times zeros of dy; columns: dropped)
+            const int q = tid + kThreads * i, at = n0 + 16 * (q % (BN / 16));
+            const long k = k0 + q / (BN / 16), kc = k < a.N ? k : a.N - 1;
+            const int ac = at < a.padded ? at : a.padded - 16;
+            rb[i] = *reinterpret_cast<const g_u4*>(a.x.values + kc * a.padded + ac);
+            rs[i] = a.x.scales[kc * (a.padded / kBlock) + ac / kBlock];
+        }
+    };
+    constexpr int kLoads = 2 * BI;
+    // ---- and into LDS.  (By hand: the compiler would wait for the direct fetches before each of its own writes.)
+    auto write = [&](const char* at, g_bf16x8 v) {
+        asm volatile("ds_write_b128 %0, %1" ::"v"((unsigned)(uintptr_t)(lds_ptr)at), "v"(v) : "memory");
     };
     auto stage = [&](char* to) {
 #pragma unroll
-        for (int i = 0; i < AI; ++i) {
-            const int q = tid + kThreads * i, k = q / (BM / 8), p = q % (BM / 8);
-            char* const at = to + k * kARow + 16 * (p ^ 4 * (k & 3));
-            if constexpr (P == 1) {
-                *reinterpret_cast<decltype(ra[i].a)*>(at) = ra[i].a;
-            } else {
-                v8f v = widen(ra[i]);
+        for (int i = 0; i < BI; ++i) asm volatile("" : "+v"(rb[i]), "+v"(rs[i]));        // (nothing of it earlier: it would wait)
+        if constexpr (!DIRECT)
 #pragma unroll
-                for (int z = 0; z < P; ++z) {
-                    const g_bf16x8 h = __builtin_convertvector(v, g_bf16x8);
-                    *reinterpret_cast<g_bf16x8*>(at + z * kPart) = h;
-                    v -= __builtin_convertvector(h, v8f);
+            for (int i = 0; i < AI; ++i) {
+                const int q = tid + kThreads * i, k = q / (BM / 8), p = q % (BM / 8);
+                char* const at = to + k * kARow + 16 * (p ^ 4 * (k & 3));
+                if constexpr (P == 1) {
+                    write(at, __builtin_bit_cast(g_bf16x8, ra[i].a));
+                } else {
+                    v8f v = widen(ra[i]);
+#pragma unroll
+                    for (int z = 0; z < P; ++z) {
+                        const g_bf16x8 h = __builtin_convertvector(v, g_bf16x8);
+                        write(at + z * kPart, h);
+                        v -= __builtin_convertvector(h, v8f);
+                    }
                 }
             }
-        }
 #pragma unroll
-        for (int i = 0; i < BI; ++i) {
-            const int q = tid + kThreads * i, k = q / (BN / 16), p = 2 * (q % (BN / 16));
-            char* const row = to + P * kPart + k * kBRow;
-            *reinterpret_cast<g_bf16x8*>(row + 16 * (p ^ 4 * (k & 3))) = widen8(u2{rb[i][0], rb[i][1]}, rs[i], a.x.kind);
-            *reinterpret_cast<g_bf16x8*>(row + 16 * ((p + 1) ^ 4 * (k & 3))) = widen8(u2{rb[i][2], rb[i][3]}, rs[i], a.x.kind);
+        for (int h = 0; h < 2 * BI; ++h) {
+            const int i = h / 2, q = tid + kThreads * i, k = q / (BN / 16), p = 2 * (q % (BN / 16)) + h % 2;
+            write(to + P * kPart + k * kBRow + 16 * (p ^ 4 * (k & 3)), widen8<KIND>(u2{rb[i][2 * (h % 2)], rb[i][2 * (h % 2) + 1]}, rs[i]));
         }
     };
 
@@ -113,59 +191,112 @@ __global__ __launch_bounds__(64 * WM * WN) void weight_grad_kernel(WeightGradArg
 
     // lane l names 4 columns of row 8 (l / 32) + (l % 16) / 4 of the step's 16, and of the row 4 on
     const int row = lane & 31, half = lane >> 5, turn = (lane & 15) >> 2, of_row = 8 * half + turn, of_col = 32 * (lane >> 4 & 1) + 8 * (lane & 3);
-    int at_a[MT], at_b[NT];
+    unsigned at_a[MT], at_b[NT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) at_a[i] = of_row * kARow + of_col + 64 * ((MT * wm + i) ^ turn);
+    for (int i = 0; i < MT; ++i) at_a[i] = (unsigned)(uintptr_t)(lds_ptr)lds_raw + of_row * kARow + of_col + 64 * ((MT * wm + i) ^ turn);
 #pragma unroll
-    for (int j = 0; j < NT; ++j) at_b[j] = P * kPart + of_row * kBRow + of_col + 64 * ((NT * wn + j) ^ turn);
-    auto read = [&](const char* at, int on) {            // 8 rows, the second 4 of them `on` bytes behind
-        using Lds = __attribute__((address_space(3))) g_s4*;
-        const g_s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + on));
-        return __builtin_bit_cast(g_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
-    auto multiply = [&](const char* from) {
+    for (int j = 0; j < NT; ++j) at_b[j] = (unsigned)(uintptr_t)(lds_ptr)lds_raw + P * kPart + of_row * kBRow + of_col + 64 * ((NT * wn + j) ^ turn);
+
+    // A block's products; the next block goes into LDS beside the first of them, and the one after is fetched then
+    auto work = [&](int b) {
+        const unsigned now = (unsigned)(b & 1) * kStage;
+        char* const next = lds_raw + kStage - now;
+        unsigned pa[MT], pb[NT];
 #pragma unroll
-        for (int s = 0; s < KB / 16; ++s) {
-            g_bf16x8 x[P][MT], y[NT];
+        for (int i = 0; i < MT; ++i) pa[i] = at_a[i] + now;
 #pragma unroll
-            for (int j = 0; j < NT; ++j) y[j] = read(from + at_b[j] + 16 * s * kBRow, 4 * kBRow);
-#pragma unroll
-            for (int z = P - 1; z >= 0; --z) {
-#pragma unroll
-                for (int i = 0; i < MT; ++i) x[z][i] = read(from + z * kPart + at_a[i] + 16 * s * kARow, 4 * kARow);
+        for (int j = 0; j < NT; ++j) pb[j] = at_b[j] + now;
+        fetch_direct(b + 1 < count ? b + 1 : b, next);   // (beyond the last block the last one again, for nobody: no branch keeps the compiler from its schedule)
+        auto step = [&](auto at) {
+            constexpr int s = decltype(at)::value;
+            g_bf16x8 x[MT], y[NT];
+            read_turned<16 * s * kBRow, 4 * kBRow>(y, pb);
+            auto part = [&](auto which) {
+                constexpr int z = decltype(which)::value;
+                read_turned<z * kPart + 16 * s * kARow, 4 * kARow>(x, pa);
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[z][i], y[j], acc[i][j], 0, 0, 0);
+                    for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
+            };
+            if constexpr (P == 3) {                      // (the smallest first)
+                part(std::integral_constant<int, 2>{});
+                part(std::integral_constant<int, 1>{});
             }
+            part(std::integral_constant<int, 0>{});
+            if constexpr (s == S / 2) {
+                stage(next);
+                fetch(b + 2 < count ? b + 2 : count - 1);
+            }
+        };
+        step(std::integral_constant<int, 0>{});
+        step(std::integral_constant<int, 1>{});
+        if constexpr (S > 2) {
+            step(std::integral_constant<int, 2>{});
+            step(std::integral_constant<int, 3>{});
         }
     };
-
-    if (count > 0) fetch(0);
-    for (int b = 0; b < count; ++b) {
-        char* const now = lds_raw + (b & 1) * kStage;
-        stage(now);
-        __syncthreads();
-        if (b + 1 < count) fetch(b + 1);
-        multiply(now);
+    // Everybody's writes into LDS are done, those of the direct fetches too, but not the loads of the block after the next (a barrier of the compiler's would
+    // wait for them)
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    auto meet_all = [&](auto on_the_way) {
+        if constexpr (!DIRECT) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(on_the_way)::value ? kLoads : 0) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    if (count > 0) {
+        fetch_direct(0, lds_raw);
+        fetch(0);
+        stage(lds_raw);
+        fetch(count > 1 ? 1 : 0);
+        for (int b = 0; b < count; ++b) {
+            meet_all(yes);
+            work(b);
+        }
     }
 
+    // ---- results by way of LDS, a wave's place its own, 32 rows of 32 NT at a time: whole lines to memory, 8 results a lane
+    constexpr int W = 32 * NT, kPitch = W + 4;           // floats; 128-bit words, rows on different banks
+    static_assert(WM * WN * 32 * kPitch * 4 <= 2 * kStage, "the blocks' places hold them");
+    float* const mine = reinterpret_cast<float*>(lds_raw) + wave * 32 * kPitch;
+    meet_all(no);                                     // (the last block is read by nobody any more)
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int i = 0; i < MT; ++i) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const int n = n0 + 32 * (NT * wn + j) + row;
-            if (n >= a.D) continue;
+        for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int m = m0 + 32 * (MT * wm + i) + 8 * (r >> 2) + 4 * half + (r & 3);
-                if (m >= a.M) continue;
-                const long at = (long)m * a.D + n;
-                if (a.part) a.part[(long)split * a.M * a.D + at] = acc[i][j][r];
-                else if (a.dw_bf16) ((bf16*)a.dw)[at] = (bf16)acc[i][j][r];
-                else ((float*)a.dw)[at] = acc[i][j][r];
-            }
+            for (int r = 0; r < 16; ++r) mine[(8 * (r >> 2) + 4 * half + (r & 3)) * kPitch + 32 * j + row] = acc[i][j][r];
+        asm volatile("" ::: "memory");                   // (a wave's LDS instructions are served in order)
+#pragma unroll
+        for (int q = 0; q < W / 16; ++q) {               // 64 lanes: W / 8 a row
+            const int of = (64 * q + lane) / (W / 8), c = 8 * ((64 * q + lane) % (W / 8));
+            const int m = m0 + 32 * (MT * wm + i) + of, n = n0 + W * wn + c;
+            const v4f lo = *reinterpret_cast<const v4f*>(mine + of * kPitch + c), hi = *reinterpret_cast<const v4f*>(mine + of * kPitch + c + 4);
+            const v8f v{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (m >= a.M || n >= a.D) continue;
+            const long at = (long)m * a.D;
+            if (a.part) store8_of(a.part + (long)split * a.M * a.D + at, n, a.D, v);
+            else if (a.dw_bf16) store8_of((bf16*)a.dw + at, n, a.D, v);
+            else store8_of((float*)a.dw + at, n, a.D, v);
         }
+        asm volatile("" ::: "memory");
+    }
+}
+
+// bf16 dy into aligned rows of whole 16-byte pieces [N][to_pitch], zeros behind its columns: a piece a thread
+__global__ __launch_bounds__(256) void weight_grad_align_kernel(const bf16* dy, long pitch, long N, int M, bf16* to, int to_pitch)
+{
+    const unsigned pieces = (unsigned)to_pitch / 8;
+    const long all = N * pieces;
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long)gridDim.x * 256) {
+        const long n = all <= 0xffffffffl ? (long)((unsigned)i / pieces) : i / pieces;
+        const int at = 8 * (int)(i - n * pieces);
+        const bf16* const row = dy + n * pitch;
+        const v8f v = at + 8 <= M ? widen(odd8(row + at), row) : load8_of(row, at, M);
+        *reinterpret_cast<g_bf16x8*>(to + n * to_pitch + at) = __builtin_convertvector(v, g_bf16x8);
+    }
 }
 
 // The splits' sums, in their order; without splits, zeros

@@ -17,35 +17,50 @@ constexpr int64_t kMaxRows = 0x7fffffff - 64, kMaxFeatures = 1 << 20, kMostPitch
 constexpr int64_t kMostResults = (int64_t)1 << 37;     // tiles of 128 x 128: 2^23 workgroups (a launch has less than 2^32 threads)
 constexpr int64_t kPartRoom = (int64_t)256 << 20;      // bytes of the partial sums
 constexpr int kCUs = 256;
+// Rows of bf16 that are no whole 16-byte pieces are copied into such where that is little beside the products.  us a call, copied / as they are, rows x outputs x features:
+// 8192 x 4095 x 4096 261 / 490, 518 x 1596 x 512 15 / 23, 4096 x 1001 x 300 30 / 33, 4096 x 1001 x 100 28 / 26, 518 x 1596 x 142 17 / 16, 100 x 51 x 300 14 / 12.
+constexpr int64_t kAlignRows = 512, kAlignFeatures = 256;
 
-struct Plan { bool big; int tiles_m, tiles_n, blocks, splits, per_split; size_t total; };
+int64_t padded_of(int64_t features) { return (features + mpcnn::kBlock - 1) / mpcnn::kBlock * mpcnn::kBlock; }
 
+struct Plan { bool big, align; int tiles_m, tiles_n, blocks, splits, per_split; size_t part, total; };
+
+// Tiles of 256 x 256 (a workgroup per compute unit) or of 128 x 128 (two), the rows whole or split: whichever should take least.  us a block of rows of a tile, measured (bf16 64
+// rows, fp32 32): 256 x 256 2.0 and 2.8, two of 128 x 128 side by side 1.3 and 2.3; a split costs its sums' way to memory and back and a launch.  us a call, split / whole: 213 x 37 x 100 fp32
+// 14 / 18.
 bool make_plan(int64_t rows, int64_t outs, int64_t features, int dtype, Plan* p)
 {
     if (rows < 0 || rows > kMaxRows || outs < 1 || outs > kMaxFeatures || features < 1 || features > kMaxFeatures || outs * features > kMostResults) return false;
     *p = Plan{};
     const bool f32 = dtype == MPCNN_F32;
-    const int64_t depth = f32 ? 32 : 64, blocks = (rows + depth - 1) / depth;
-    auto tiles = [&](int64_t side) { return ((outs + side - 1) / side) * ((features + side - 1) / side); };
-    p->big = !f32 && tiles(256) >= kCUs * 3 / 4;
-    const int64_t side = p->big ? 256 : 128, all = tiles(side);
-    const int64_t slots = p->big ? kCUs : 2 * kCUs;
-    const int64_t room = std::max<int64_t>(1, kPartRoom / (4 * outs * features));
-    const int64_t splits = std::max<int64_t>(1, std::min({slots / all, blocks / 4, room, (int64_t)64}));
-    p->tiles_m = (int)((outs + side - 1) / side);
-    p->tiles_n = (int)((features + side - 1) / side);
+    const int64_t depth = f32 ? 32 : 64, blocks = std::max<int64_t>(1, (rows + depth - 1) / depth);
+    const int64_t most = std::min({blocks, std::max<int64_t>(1, kPartRoom / (4 * outs * features)), (int64_t)64});
     p->blocks = (int)blocks;
-    p->per_split = (int)std::max<int64_t>(1, (blocks + splits - 1) / splits);
-    p->splits = (int)std::max<int64_t>(1, (blocks + p->per_split - 1) / p->per_split);
-    p->total = p->splits > 1 ? (size_t)((4 * p->splits * outs * features + 255) / 256 * 256) : 0;
+    double least = 0.0;
+    for (int big = 0; big < 2; ++big) {
+        const int64_t side = big ? 256 : 128, slots = big ? kCUs : 2 * kCUs, tiles_m = (outs + side - 1) / side, tiles_n = (features + side - 1) / side;
+        const double block_us = f32 ? (big ? 2.8 : 2.3) : (big ? 2.0 : 1.3);
+        for (int64_t splits = 1; splits <= most; ++splits) {
+            const int64_t each = (blocks + splits - 1) / splits;
+            if (splits > 1 && (blocks + each - 1) / each != splits) continue;
+            const int64_t rounds = (tiles_m * tiles_n * splits + slots - 1) / slots;
+            const double us = (double)rounds * (1.5 + block_us * (double)each) + (splits > 1 ? 6.0 + 8e-6 * (double)outs * (double)features * (double)splits / 5.0 : 0.0);
+            if (p->splits && us >= least) continue;
+            least = us;
+            p->big = big != 0; p->tiles_m = (int)tiles_m; p->tiles_n = (int)tiles_n; p->splits = (int)splits; p->per_split = (int)each;
+        }
+    }
+    p->part = p->splits > 1 ? (size_t)((4 * p->splits * outs * features + 255) / 256 * 256) : 0;
+    p->align = !f32 && outs % 8 && rows >= kAlignRows && features >= kAlignFeatures;
+    p->total = p->part + (p->align ? (size_t)(2 * rows * ((outs + 7) / 8 * 8)) : 0);
     return true;
 }
 
-template <typename T, int WM, int WN, int MT, int NT, int KB>
-mpcnn_status launch(const mpcnn::WeightGradArgs& a, hipStream_t st)
+template <typename T, int KIND, int WM, int WN, int MT, int NT, int KB, bool DIRECT>
+mpcnn_status launch_instance(const mpcnn::WeightGradArgs& a, hipStream_t st)
 {
     constexpr int lds = 2 * KB * 2 * 32 * ((sizeof(T) == 4 ? 3 : 1) * WM * MT + WN * NT);
-    auto* kernel = &mpcnn::weight_grad_kernel<T, WM, WN, MT, NT, KB>;
+    auto* kernel = &mpcnn::weight_grad_kernel<T, KIND, WM, WN, MT, NT, KB, DIRECT>;
     if constexpr (lds > 64 * 1024) {       // must be said once per device
         static std::atomic<uint64_t> said{0};
         int dev = 0;
@@ -58,6 +73,12 @@ mpcnn_status launch(const mpcnn::WeightGradArgs& a, hipStream_t st)
     const int64_t all = (int64_t)a.tiles_m * a.tiles_n * a.splits;
     kernel<<<(unsigned)((all + 7) / 8 * 8), 64 * WM * WN, lds, st>>>(a);
     return MPCNN_OK;
+}
+
+template <typename T, int WM, int WN, int MT, int NT, int KB, bool DIRECT = false>
+mpcnn_status launch(const mpcnn::WeightGradArgs& a, hipStream_t st)
+{
+    return a.x.kind == MPCNN_I8 ? launch_instance<T, MPCNN_I8, WM, WN, MT, NT, KB, DIRECT>(a, st) : launch_instance<T, MPCNN_E4M3, WM, WN, MT, NT, KB, DIRECT>(a, st);
 }
 
 }  // namespace
@@ -89,7 +110,7 @@ mpcnn_status mpcnn_rows_weight_grad(const void* dy_dev, int64_t dy_pitch, const 
                     (long long)kMaxRows, (long long)kMaxFeatures, (long long)kMaxFeatures, (long long)kMostResults);
     if (ws_bytes < p.total) return fail(MPCNN_EWORKSPACE, "workspace %zu bytes, need %zu", ws_bytes, p.total);
     if ((uintptr_t)ws_dev & 255u) return fail(MPCNN_EINVAL, "workspace must be 256-byte aligned");
-    const int64_t padded = (features + mpcnn::kBlock - 1) / mpcnn::kBlock * mpcnn::kBlock;
+    const int64_t padded = padded_of(features);
     const Span dw{(uintptr_t)dw_dev, (uint64_t)(outs * features * dw_size)}, ws{(uintptr_t)ws_dev, p.total}, dy = mpcnn::rows_span(dy_dev, rows, outs, dy_pitch, size);
     const Span values{rows > 0 ? (uintptr_t)x->values_dev : 0, (uint64_t)(rows * padded)}, scales{rows > 0 ? (uintptr_t)x->scales_dev : 0, (uint64_t)(rows * (padded / mpcnn::kBlock))};
     for (const Span& in : {dy, values, scales})
@@ -109,9 +130,27 @@ mpcnn_status mpcnn_rows_weight_grad(const void* dy_dev, int64_t dy_pitch, const 
     a.blocks = p.blocks; a.per_split = p.per_split; a.splits = p.splits; a.tiles_m = p.tiles_m; a.tiles_n = p.tiles_n;
     a.dw = dw_dev; a.dw_bf16 = dw_dtype == MPCNN_BF16;
     a.part = p.splits > 1 ? (float*)ws_dev : nullptr;
-    const mpcnn_status rc = dtype == MPCNN_F32 ? launch<float, 2, 2, 2, 2, 32>(a, st)
-                            : p.big            ? launch<mpcnn::bf16, 2, 4, 4, 2, 64>(a, st)
-                                               : launch<mpcnn::bf16, 2, 2, 2, 2, 64>(a, st);
+    // (a block's fetches are 32-bit offsets from its first row)
+    auto whole = [](const void* m, int64_t pitch, int64_t columns) { return (uintptr_t)m % 16 == 0 && pitch % 8 == 0 && columns % 8 == 0 && pitch * 128 < (1ll << 31); };
+    mpcnn_status rc;
+    if (dtype == MPCNN_F32) {
+        rc = p.big ? launch<float, 2, 4, 4, 2, 32>(a, st) : launch<float, 2, 2, 2, 2, 32>(a, st);
+    } else {
+        const int64_t aligned = (outs + 7) / 8 * 8;
+        int64_t columns = outs;
+        if (p.align) {
+            mpcnn::bf16* const to = (mpcnn::bf16*)((char*)ws_dev + p.part);
+            const int64_t pieces = rows * (aligned / 8);
+            mpcnn::weight_grad_align_kernel<<<(unsigned)std::min<int64_t>(8192, (pieces + 255) / 256), 256, 0, st>>>((const mpcnn::bf16*)dy_dev, dy_pitch, rows, (int)outs, to, (int)aligned);
+            a.dy = to; a.dy_pitch = columns = aligned;
+        }
+        a.dy_bytes = ((rows - 1) * a.dy_pitch + columns) * 2;
+        const bool direct = whole(a.dy, a.dy_pitch, columns);
+        rc = p.big && direct ? launch<mpcnn::bf16, 2, 4, 4, 2, 64, true>(a, st)
+             : p.big         ? launch<mpcnn::bf16, 2, 4, 4, 2, 64>(a, st)
+             : direct        ? launch<mpcnn::bf16, 2, 2, 2, 2, 64, true>(a, st)
+                             : launch<mpcnn::bf16, 2, 2, 2, 2, 64>(a, st);
+    }
     if (rc != MPCNN_OK) return rc;
     if (p.splits > 1) mpcnn::weight_grad_sum_kernel<<<sum_groups, 256, 0, st>>>(a.part, p.splits, n, dw_dev, a.dw_bf16);
     HIP_TRY(hipGetLastError());
