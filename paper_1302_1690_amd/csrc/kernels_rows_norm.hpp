@@ -204,37 +204,53 @@ __global__ __launch_bounds__(threads_of(LANES)) void rows_norm_back_kernel(NormB
     const long step = (long)gridDim.x * kSlots;
     if (n < a.rows) fetch(n);
     for (int flip = 0; n < a.rows; n += step, flip ^= 1) {
-        NormPiece p[E];
-        v8f add[E];
+        constexpr bool kKeep = E < 4;      // (registers for a row's pieces and for the next row's numbers beside them; else the pieces are made again)
         float sum[2] = {0.f, 0.f};
         const float by = rstd;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            p[e] = NormPiece{};
-            add[e] = v8f{};
-            if (at[e] >= a.D) continue;
+        auto piece = [&](int e, float (&to)[2]) {
             v8f of;
             if constexpr (PACKED) of = unpack8(h[e], scale[e], a.h_packed.kind);
             else of = widen(h[e]);
-            p[e] = norm_piece(widen(dy[e]), of, gain[e], by, sum);
-            if (a.dh) add[e] = widen(more[e]);
+            return norm_piece(widen(dy[e]), of, gain[e], by, to);
+        };
+        NormPiece p[kKeep ? E : 1];
+        v8f add[kKeep ? E : 1];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if constexpr (kKeep) { p[e] = NormPiece{}; add[e] = v8f{}; }
+            if (at[e] >= a.D) continue;
+            const NormPiece q = piece(e, sum);
+            if constexpr (kKeep) {
+                p[e] = q;
+                if (a.dh) add[e] = widen(more[e]);
+            }
         }
-        if (n + step < a.rows) fetch(n + step);
+        if (kKeep && n + step < a.rows) fetch(n + step);
         sum_row<LANES>(sum, red, flip);
         const bool some = sum[1] != 0.f;
         const float c = some ? sum[0] / (float)a.D : 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            v8f dx = add[e];
+            NormPiece q{};
+            v8f dx{};
+            if constexpr (kKeep) {
+                q = p[e];
+                dx = add[e];
+            } else if (at[e] < a.D) {
+                float unused[2] = {0.f, 0.f};
+                q = piece(e, unused);
+                if (a.dh) dx = widen(more[e]);
+            }
             if (some) {
 #pragma unroll
                 for (int z = 0; z < 8; ++z) {
-                    dx[z] = fmaf(by, fmaf(-p[e].unit[z], c, p[e].dy[z] * gain[e][z]), dx[z]);
-                    dgain[e][z] = fmaf(p[e].dy[z], p[e].unit[z], dgain[e][z]);
+                    dx[z] = fmaf(by, fmaf(-q.unit[z], c, q.dy[z] * gain[e][z]), dx[z]);
+                    dgain[e][z] = fmaf(q.dy[z], q.unit[z], dgain[e][z]);
                 }
             }
             if (a.dx && at[e] < a.D) store8_of((T*)a.dx + n * a.dx_pitch, at[e], a.D, dx);
         }
+        if (!kKeep && n + step < a.rows) fetch(n + step);
     }
     if (!a.part) return;
     float* const part = a.part + (long)blockIdx.x * a.D;
@@ -299,15 +315,15 @@ __global__ __launch_bounds__(1024) void rows_norm_back_long_kernel(NormBackArgs 
     }
 }
 
-// dgain: the workgroups' shares added up, 32 features a workgroup, each by 32 threads over a stretch of the shares
-constexpr int kGainColumns = 32, kGainStretches = 32;
+// dgain: the workgroups' shares added up, 16 features a workgroup, each by 64 threads over a stretch of the shares
+constexpr int kGainColumns = 16, kGainStretches = 64;
 __global__ __launch_bounds__(kGainColumns * kGainStretches) void norm_gain_kernel(const float* part, int parts, int D, float* dgain)
 {
     __shared__ float red[kGainStretches][kGainColumns + 1];
     const int c = threadIdx.x % kGainColumns, q = threadIdx.x / kGainColumns, at = blockIdx.x * kGainColumns + c;
     float s = 0.f;
     if (at < D) {
-#pragma unroll 4
+#pragma unroll 8
         for (int g = q; g < parts; g += kGainStretches) s += part[(long)g * D + at];
     }
     red[q][c] = s;
@@ -319,8 +335,8 @@ __global__ __launch_bounds__(kGainColumns * kGainStretches) void norm_gain_kerne
     }
 }
 
-// Rows into 8 bits and back.  A workgroup has some rows' pieces of 8 features, a thread one after the other: 4 lanes side by side have a block (a row
-// is whole blocks, and the loop's step whole waves).
+// Rows into 8 bits and back.  A workgroup has some rows' pieces of 8 features, a thread kPieces of them at a time (all fetched before the first is packed): 4 lanes side by
+// side have a block (a row is whole blocks, and the loop's step whole waves).
 struct PackArgs {
     const void* x;
     long x_pitch;
@@ -330,35 +346,48 @@ struct PackArgs {
     long rows;
     int D, padded, each;                   // each: rows of a workgroup
 };
-template <typename T>
-__global__ __launch_bounds__(256) void rows_pack8_kernel(PackArgs a)
+constexpr int kPieces = 4;
+// fetch(k, row, at) for each of the thread's next pieces, and then use(k, row, at)
+template <typename F, typename G>
+__device__ __forceinline__ void each_piece(const PackArgs& a, F fetch, G use)
 {
     const int pieces = a.padded / 8;
     const long first = (long)blockIdx.x * a.each;
     const int rows = (int)(a.rows - first < a.each ? a.rows - first : a.each), all = rows * pieces;
     const float by = 1.f / (float)pieces;
-    for (int i = threadIdx.x; i < all; i += 256) {
-        int r = (int)(((float)i + 0.5f) * by);           // (all < 2^18: exact)
-        const int at = 8 * (i - r * pieces);
-        const v8f v = at < a.D ? load8_of((const T*)a.x + (first + r) * a.x_pitch, at, a.D) : v8f{};
-        pack_store(a.packed, first + r, a.padded, at, v);
+    for (int i = threadIdx.x; i < all; i += 256 * kPieces) {
+        int r[kPieces], at[kPieces];
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            r[k] = (int)(((float)(i + 256 * k) + 0.5f) * by);          // (all < 2^18: exact)
+            at[k] = 8 * (i + 256 * k - r[k] * pieces);
+            if (i + 256 * k < all) fetch(k, first + r[k], at[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k)
+            if (i + 256 * k < all) use(k, first + r[k], at[k]);
     }
+}
+template <typename T>
+__global__ __launch_bounds__(256) void rows_pack8_kernel(PackArgs a)
+{
+    Raw8<T> x[kPieces];
+    each_piece(a, [&](int k, long n, int at) { if (at < a.D) x[k] = raw8_of((const T*)a.x + n * a.x_pitch, at, a.D); },
+               [&](int k, long n, int at) { pack_store(a.packed, n, a.padded, at, at < a.D ? widen(x[k]) : v8f{}); });
 }
 template <typename T>
 __global__ __launch_bounds__(256) void rows_unpack8_kernel(PackArgs a)
 {
-    const int pieces = a.padded / 8;
-    const long first = (long)blockIdx.x * a.each;
-    const int rows = (int)(a.rows - first < a.each ? a.rows - first : a.each), all = rows * pieces;
-    const float by = 1.f / (float)pieces;
-    for (int i = threadIdx.x; i < all; i += 256) {
-        const int r = (int)(((float)i + 0.5f) * by), at = 8 * (i - r * pieces);
-        if (at >= a.D) continue;
-        const long n = first + r;
-        const v8f v = unpack8(*reinterpret_cast<const u2*>(a.packed.values + n * a.padded + at), a.packed.scales[n * (a.padded / kBlock) + at / kBlock],
-                              a.packed.kind);
-        store8_of((T*)a.out + n * a.out_pitch, at, a.D, v);
-    }
+    u2 x[kPieces];
+    unsigned char scale[kPieces];
+    each_piece(a,
+               [&](int k, long n, int at) {
+                   x[k] = *reinterpret_cast<const u2*>(a.packed.values + n * a.padded + at);
+                   scale[k] = a.packed.scales[n * (a.padded / kBlock) + at / kBlock];
+               },
+               [&](int k, long n, int at) {
+                   if (at < a.D) store8_of((T*)a.out + n * a.out_pitch, at, a.D, unpack8(x[k], scale[k], a.packed.kind));
+               });
 }
 
 }  // namespace mpcnn

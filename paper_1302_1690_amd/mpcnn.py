@@ -693,9 +693,15 @@ class PackedRows:
         import torch
         if kind not in (I8, E4M3) or isinstance(kind, bool):
             _refuse("unknown kind %r of rows in 8 bits" % (kind,))
+        if rows < 0 or features < 1:
+            _refuse("%d rows of %d features in 8 bits" % (rows, features))
         blocks = (features + 31) // 32
-        return cls(torch.empty(rows, 32 * blocks, dtype=torch.int8 if kind == I8 else torch.float8_e4m3fn, device=device),
-                   torch.empty(rows, blocks, dtype=torch.uint8, device=device), features)
+        self = cls.__new__(cls)            # (nothing to check)
+        self.values = torch.empty(rows, 32 * blocks, dtype=torch.int8 if kind == I8 else torch.float8_e4m3fn, device=device)
+        self.scales = torch.empty(rows, blocks, dtype=torch.uint8, device=device)
+        self.features, self.kind = features, kind
+        self._c = _Packed(self.values.data_ptr(), self.scales.data_ptr(), kind)
+        return self
 
     @property
     def rows(self) -> int:
