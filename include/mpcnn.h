@@ -415,7 +415,7 @@ mpcnn_status mpcnn_rows_norm_backward(const void* dy_dev, int64_t dy_pitch, cons
  *   s[b][k][v] = score + bias[v] (fp32),  value = totals[b][k] + (s - log sum over v of exp s) in 64 bits
  * and the `width` largest of a sequence's beams * classes values go on, best first; equal ones by the lower beam, then the lower class.
  *   scores_dev [sequences * beams][scores_pitch] `dtype`, bias_dev [classes] fp32 or NULL (minus infinity switches a class off, whatever its scores hold),
- *   totals_dev [sequences][beams] fp32: the beams' log-probabilities so far; minus infinity (or NaN): a dead beam, which offers nothing,
+ *   totals_dev [sequences][beams] fp32: the beams' log-probabilities so far; minus infinity, or another one that is not finite: a dead beam, which offers nothing,
  *   done_dev   [sequences][beams] bytes or NULL: beams that are finished offer one candidate, the class `end`, at their total.  The scores of
  *              dead and finished beams are not read.  A beam with a score that is NaN or plus infinity, or with no class on, offers nothing.
  *   end        the class that ends a sequence, or -1 (then done_dev is NULL).
@@ -453,6 +453,7 @@ mpcnn_status mpcnn_class_beam(const void* x_dev, int64_t x_pitch, const void* w_
  * what row b * beams + parents[b][k] was.  A row whose parent is itself, -1 or no beam stays, and is neither read nor written.
  *   A tensor is sequences * beams rows, row_pitch bytes apart, each of `segments` segments, segment_pitch bytes apart, of `units` units of unit_bytes each
  *   (a cache [rows][heads][positions][inner]: heads segments of positions units; anything else: one segment of one unit).
+ *   Tensors may lie in turn, row by row, in one buffer (with one row_pitch).
  *   mpcnn_beam_states_create: the list, made once, on the current device, which has to be the current one in every call; synchronous.  The tensors stay the
  *     caller's.  Errors: EINVAL (also: two of them overlap), EUNSUPPORTED (over 65535 tensors, rows above 2^34 bytes, beams as above), ENOMEM, EHIP.
  *   mpcnn_beam_reorder: parents_dev [sequences][beams] int32; length: only so many units of every segment (below zero: all).  Errors: EINVAL (also: another

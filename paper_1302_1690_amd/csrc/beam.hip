@@ -3,6 +3,7 @@
 #include <cstdint>
 #include <memory>
 #include <new>
+#include <numeric>
 #include <vector>
 
 #include "class_scores.hpp"
@@ -129,6 +130,8 @@ mpcnn_status select(const Plan& p, const Call& c, const void* scores, int64_t pi
     return MPCNN_OK;
 }
 
+int64_t row_bytes(const mpcnn::BeamState& s) { return (int64_t)(s.segments - 1) * s.segment + s.unit * s.units; }
+
 mpcnn_status make_states(const mpcnn_beam_state* t, int count, int64_t sequences, int64_t beams, mpcnn_beam_states** out)
 {
     std::unique_ptr<mpcnn_beam_states> l(new mpcnn_beam_states);
@@ -150,10 +153,16 @@ mpcnn_status make_states(const mpcnn_beam_state* t, int count, int64_t sequences
         l->states.push_back(mpcnn::BeamState{(char*)s.data_dev, s.row_pitch, s.segment_pitch, s.unit_bytes, s.units, (unsigned)s.segments, 0});
         l->held.push_back(held);
     }
-    std::vector<Span> order = l->held;
-    std::sort(order.begin(), order.end(), [](const Span& a, const Span& b) { return a.at < b.at; });
-    for (size_t i = 1; i < order.size(); ++i)
-        if (meet(order[i - 1], order[i])) return fail(MPCNN_EINVAL, "two states overlap in memory");
+    // Two tensors may lie in turn in one buffer: rows of one pitch, the second's between the first's
+    std::vector<size_t> order(l->held.size());
+    std::iota(order.begin(), order.end(), (size_t)0);
+    std::sort(order.begin(), order.end(), [&](size_t a, size_t b) { return l->held[a].at < l->held[b].at; });
+    for (size_t i = 0; i < order.size(); ++i)
+        for (size_t j = i + 1; j < order.size() && meet(l->held[order[i]], l->held[order[j]]); ++j) {
+            const mpcnn::BeamState &p = l->states[order[i]], &q = l->states[order[j]];
+            const int64_t from = p.row ? (int64_t)(l->held[order[j]].at - l->held[order[i]].at) % p.row : 0;
+            if (p.row != q.row || from < row_bytes(p) || from + row_bytes(q) > p.row) return fail(MPCNN_EINVAL, "two states overlap in memory");
+        }
     if (l->states.size() > 65535) return fail(MPCNN_EUNSUPPORTED, "%d states: at most 65535", count);
     l->count = (int)l->states.size();
     l->sequences = (int)sequences;

@@ -115,7 +115,7 @@ struct BeamColumn {
 
 __device__ __forceinline__ bool beam_goes_on(const BeamArgs& a, long row)
 {
-    return a.totals[row] > -__builtin_inff() && !(a.done && a.done[row]);     // (a NaN does not)
+    return fabsf(a.totals[row]) < __builtin_inff() && !(a.done && a.done[row]);     // (a NaN does not)
 }
 
 // exp(x - top) for x <= top; 0 for minus infinity
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a)
         const float2* const stats = a.stats + row * a.parts;
         constexpr float2 kNone{-__builtin_inff(), 0.f};
         const float2 mine = lane < a.parts ? stats[lane] : kNone;      // (used if it goes on)
-        int is = t > -__builtin_inff() ? (over ? 2 : 1) : 0;
+        int is = fabsf(t) < __builtin_inff() ? (over ? 2 : 1) : 0;
         double l = 0.0;
         if (is == 1) {
             float top = mine.x;

@@ -77,10 +77,12 @@ def _create(states, sequences=3, beams=4, count=None, out=True):
     ([_state(data=0)], {}, EINVAL), ([_state(row=4095)], {}, EINVAL), ([_state(segment=1023)], {}, EINVAL), ([_state(unit=-1)], {}, EINVAL), ([_state(units=-1)], {}, EINVAL),
     ([_state(segments=-1)], {}, EINVAL), ([_state(row=-4096)], {}, EINVAL), ([_state(unit=1 << 41)], {}, EINVAL), ([_state(unit=1 << 30, units=1 << 30)], {}, EINVAL),
     ([_state(), _state(data=BASE + 12 * 4096 - 1)], {}, EINVAL), ([_state(), _state()], {}, EINVAL), ([_state(data=BASE + 64), _state(data=BASE)], {}, EINVAL),
+    ([_state(row=8192), _state(data=BASE + 4095, row=8192)], {}, EINVAL), ([_state(row=8192), _state(data=BASE + 4097, row=8192)], {}, EINVAL),
+    ([_state(row=8192), _state(data=BASE + 4096, row=8256)], {}, EINVAL), ([_state(row=12288), _state(data=BASE + 4096, row=12288), _state(data=BASE + 12288 + 64, row=12288)], {}, EINVAL),
     ([_state(row=1 << 35, unit=1 << 35, units=1, segments=1)], {}, EUNSUPPORTED), ([_state()], dict(beams=0), EINVAL), ([_state()], dict(sequences=-1), EINVAL),
     ([_state()], dict(beams=65), EUNSUPPORTED), ([_state()], dict(sequences=1 << 19), EUNSUPPORTED), ([], dict(count=2), EINVAL), ([], dict(count=-1), EINVAL),
     ([_state()], dict(out=False), EINVAL),
-], ids=range(20))
+], ids=range(24))
 def test_states_refusals(states, more, status):
     assert _create(states, **more) == status, mpcnn.lib().mpcnn_last_error().decode()
 

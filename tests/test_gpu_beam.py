@@ -160,11 +160,11 @@ def test_dead_beams_masked_classes_and_bad_scores(dtype):
     done = torch.zeros((7, 3), dtype=torch.bool, device="cuda")
     done[5, 1] = done[2, 0] = True
     scores[16] = float("nan")                                 # finished: not looked at
-    totals[4, 2] = float("nan")
+    totals[4, 2], totals[3, 2] = float("nan"), INF
     got = mpcnn.beam_select(scores, totals, width=5, bias=bias, done=done, end=11)
     check(got, scores, totals, 5, bias, done, 11)
     assert (got[1][2] == -1).all() and (got[1][6] == -1).all() and (got[1][1] == 2).all() and not (got[1][3] == 0).any()
-    assert ((got[1][5] == 1).sum() == 1) and not (got[1][4] == 1).any() and not (got[1][4] == 2).any() and got[3][2].all()
+    assert ((got[1][5] == 1).sum() == 1) and not (got[1][4] == 1).any() and not (got[1][4] == 2).any() and not (got[1][3] == 2).any() and got[3][2].all()
 
 
 def test_few_candidates():
@@ -205,7 +205,7 @@ def _whole(gen, rows, features, dtype, most):
 @pytest.mark.parametrize("dtype", TYPES, ids=_ids)
 @pytest.mark.parametrize("with_bias,finished", [(False, 0.0), (True, 0.3)])
 @pytest.mark.parametrize("b,k,features,v,width", [(1, 1, 5, 3, 2), (1, 4, 1024, 32000, 4), (1, 2, 64, 30011, 8), (2, 3, 100, 2000, 3), (3, 4, 1000, 25000, 6), (5, 8, 333, 5001, 8),
-                                                  (1, 64, 96, 1025, 64), (16, 8, 256, 700, 8), (20, 16, 64, 9000, 4), (8, 4, 2048, 20480, 4), (4, 2, 4096, 33000, 2)])
+                                                  (1, 64, 96, 1025, 64), (16, 8, 256, 700, 8), (20, 16, 64, 9000, 4), (16, 4, 512, 24001, 4), (25, 4, 600, 20001, 4), (1, 4, 2050, 35001, 4), (8, 4, 2048, 20480, 4), (4, 2, 4096, 33000, 2)])
 def test_class_beam(b, k, features, v, width, with_bias, finished, dtype):
     """Features and class weights are whole numbers, biases multiples of 1/64: every order of the products' sum gives the same score, exactly."""
     gen = _gen(b * 7 + k * 11 + features + v)
@@ -324,6 +324,14 @@ def test_reorder_with_pitch_leaves_the_rest_alone():
     p = torch.tensor([[1, 0], [0, 0], [1, 1]], dtype=torch.int32, device="cuda")
     mpcnn.BeamStates([part], 3, 2).reorder(p)
     assert torch.equal(part, _plain_reorder(was[:, 3:70], p)) and torch.equal(wide[:, :3], was[:, :3]) and torch.equal(wide[:, 70:], was[:, 70:])
+
+
+def test_reorder_of_tensors_that_lie_in_turn():
+    both = torch.randn((12, 2, 5, 33), generator=_gen(13), device="cuda").to(torch.bfloat16)      # keys and values of one buffer
+    was = both.clone()
+    p = torch.tensor([[1, 0, 3, 3], [0, 0, 0, 0], [3, 2, 1, 0]], dtype=torch.int32, device="cuda")
+    mpcnn.BeamStates([both[:, 0], both[:, 1]], 3, 4).reorder(p)
+    assert torch.equal(both, _plain_reorder(was, p))
 
 
 def test_reorder_far_rows():
