@@ -133,11 +133,14 @@ __global__ __launch_bounds__(64 * WM * WN) void weight_grad_kernel(WeightGradArg
     };
     auto fetch = [&](int block) {
         const long k0 = (long)(first + block) * KB;
+        // (a row behind each of the block's: 8 numbers from its last piece on are the matrix's, and what is beyond its columns is dropped)
+        const bool inside = k0 + KB < a.N && a.M >= 8;
         if constexpr (!DIRECT)
 #pragma unroll
             for (int i = 0; i < AI; ++i) {
                 const int q = tid + kThreads * i, k = q / (BM / 8), at = m0 + 8 * (q % (BM / 8));
-                if (k0 + k < a.N && at < a.M) ra[i] = raw8_of((const T*)a.dy + (k0 + k) * a.dy_pitch, at, a.M);
+                if (inside) ra[i] = raw8((const T*)a.dy + (k0 + k) * a.dy_pitch + (at < a.M ? at : 0));
+                else if (k0 + k < a.N && at < a.M) ra[i] = raw8_of((const T*)a.dy + (k0 + k) * a.dy_pitch, at, a.M);
                 else ra[i] = Raw8<T>{};
             }
 #pragma unroll
@@ -299,12 +302,31 @@ __global__ __launch_bounds__(256) void weight_grad_align_kernel(const bf16* dy, 
     }
 }
 
-// The splits' sums, in their order; without splits, zeros
+// The splits' sums (without splits, zeros): 64 numbers a workgroup at a time, a wave every fourth split, eight on their way at once; the waves' sums in their order
 __global__ __launch_bounds__(256) void weight_grad_sum_kernel(const float* part, int splits, long n, void* out, int out_bf16)
 {
-    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
+    __shared__ float red[2][3][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int flip = 0;
+    for (long base = 64 * (long)blockIdx.x; base < n; base += 64 * (long)gridDim.x, flip ^= 1) {
+        const long i = base + lane;
         float s = 0.f;
-        for (int z = 0; z < splits; ++z) s += part[z * n + i];
+        if (i < n) {
+            int z = wave;
+            for (; z + 28 < splits; z += 32) {
+                float v[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] = part[(long)(z + 4 * q) * n + i];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) s += v[q];
+            }
+#pragma unroll 4
+            for (; z < splits; z += 4) s += part[(long)z * n + i];
+        }
+        if (wave) red[flip][wave - 1][lane] = s;
+        __syncthreads();
+        if (wave || i >= n) continue;
+        s = ((s + red[flip][0][lane]) + red[flip][1][lane]) + red[flip][2][lane];
         if (out_bf16) ((bf16*)out)[i] = (bf16)s;
         else ((float*)out)[i] = s;
     }

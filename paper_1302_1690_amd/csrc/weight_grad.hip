@@ -18,15 +18,15 @@ constexpr int64_t kMostResults = (int64_t)1 << 37;     // tiles of 128 x 128: 2^
 constexpr int64_t kPartRoom = (int64_t)256 << 20;      // bytes of the partial sums
 constexpr int kCUs = 256;
 // Rows of bf16 that are no whole 16-byte pieces are copied into such where that is little beside the products.  us a call, copied / as they are, rows x outputs x features:
-// 8192 x 4095 x 4096 261 / 490, 518 x 1596 x 512 15 / 23, 4096 x 1001 x 300 30 / 33, 4096 x 1001 x 100 28 / 26, 518 x 1596 x 142 17 / 16, 100 x 51 x 300 14 / 12.
-constexpr int64_t kAlignRows = 512, kAlignFeatures = 256;
+// 8192 x 4095 x 4096 int8 325 / 390, 4096 x 1001 x 300 30 / 29, 400 x 1001 x 1000 21 / 16, 4096 x 1001 x 100 28 / 22.
+constexpr int64_t kAlignRows = 2048, kAlignFeatures = 1024;
 
 int64_t padded_of(int64_t features) { return (features + mpcnn::kBlock - 1) / mpcnn::kBlock * mpcnn::kBlock; }
 
 struct Plan { bool big, align; int tiles_m, tiles_n, blocks, splits, per_split; size_t part, total; };
 
 // Tiles of 256 x 256 (a workgroup per compute unit) or of 128 x 128 (two), the rows whole or split: whichever should take least.  us a block of rows of a tile, measured (bf16 64
-// rows, fp32 32): 256 x 256 2.0 and 2.8, two of 128 x 128 side by side 1.3 and 2.3; a split costs its sums' way to memory and back and a launch.  us a call, split / whole: 213 x 37 x 100 fp32
+// rows, fp32 32): 256 x 256 2.0 and 2.8, two of 128 x 128 side by side 1.3 and 2.3; a split costs its sums' way to memory and back and a launch; operands come at 4.5 TB/s.  us a call, split / whole: 213 x 37 x 100 fp32
 // 14 / 18.
 bool make_plan(int64_t rows, int64_t outs, int64_t features, int dtype, Plan* p)
 {
@@ -39,12 +39,15 @@ bool make_plan(int64_t rows, int64_t outs, int64_t features, int dtype, Plan* p)
     double least = 0.0;
     for (int big = 0; big < 2; ++big) {
         const int64_t side = big ? 256 : 128, slots = big ? kCUs : 2 * kCUs, tiles_m = (outs + side - 1) / side, tiles_n = (features + side - 1) / side;
+        // (every tile along one side reads the operand of the other)
+        const double traffic = (double)rows * ((f32 ? 4.0 : 2.0) * (double)(outs * tiles_n) + (double)(features * tiles_m));
         const double block_us = f32 ? (big ? 2.8 : 2.3) : (big ? 2.0 : 1.3);
         for (int64_t splits = 1; splits <= most; ++splits) {
             const int64_t each = (blocks + splits - 1) / splits;
             if (splits > 1 && (blocks + each - 1) / each != splits) continue;
             const int64_t rounds = (tiles_m * tiles_n * splits + slots - 1) / slots;
-            const double us = (double)rounds * (1.5 + block_us * (double)each) + (splits > 1 ? 6.0 + 8e-6 * (double)outs * (double)features * (double)splits / 5.0 : 0.0);
+            const double products = (double)rounds * block_us * (double)each, operands = traffic * 1e-6 / 4.5;
+            const double us = 1.5 * (double)rounds + std::max(products, operands) + (splits > 1 ? 6.0 + 8e-6 * (double)outs * (double)features * (double)splits / 5.0 : 0.0);
             if (p->splits && us >= least) continue;
             least = us;
             p->big = big != 0; p->tiles_m = (int)tiles_m; p->tiles_n = (int)tiles_n; p->splits = (int)splits; p->per_split = (int)each;
@@ -118,7 +121,7 @@ mpcnn_status mpcnn_rows_weight_grad(const void* dy_dev, int64_t dy_pitch, const 
     if (meet(dw, ws)) return fail(MPCNN_EINVAL, "the output and the workspace overlap");
     const hipStream_t st = (hipStream_t)hip_stream;
     const int64_t n = outs * features;
-    const unsigned sum_groups = (unsigned)std::min<int64_t>(8192, (n + 255) / 256);
+    const unsigned sum_groups = (unsigned)std::min<int64_t>(8192, (n + 63) / 64);
     if (!rows) {
         mpcnn::weight_grad_sum_kernel<<<sum_groups, 256, 0, st>>>(nullptr, 0, n, dw_dev, dw_dtype == MPCNN_BF16);
         HIP_TRY(hipGetLastError());
