@@ -349,9 +349,11 @@ mpcnn_status mpcnn_class_backward(const void* x_dev, int64_t x_pitch, const void
 
 /*
  * Rows kept in 8 bits.  Blocks of 32 features share a power of two 2^e, the least for which the block's largest magnitude is at most
- * 127 * 2^e (MPCNN_I8, two's complement) or 448 * 2^e (MPCNN_E4M3, one sign, four exponent, three mantissa bits, no infinity), and e >= -100; a number is kept as
- * x * 2^-e, rounded to nearest even (numbers that would read back as infinity, from 2^128 - 2^121 and 2^128 - 2^124 on: as the largest finite one).  So a number is off by at most 1/127 of its block's largest with MPCNN_I8, by 2^-4 of itself (or 2^-17 of its
- * block's largest) with MPCNN_E4M3, and what is kept reads back as an exact number of either storage type.  A block with a number that is not finite reads back as NaN, all of it.
+ * 127 * 2^e (MPCNN_I8, two's complement) or 448 * 2^e (MPCNN_E4M3: one sign, four exponent, three mantissa bits, no infinity), and e >= -100; a number
+ * is kept as x * 2^-e, rounded to nearest even (numbers that would read back as infinity, from 2^128 - 2^121 and 2^128 - 2^124 on, as the largest
+ * that does not).  So a number is off by at most 1/127 of its block's largest with MPCNN_I8, by 2^-4 of itself or 2^-17 of its block's largest with
+ * MPCNN_E4M3 (both: or 2^-101), and what is kept reads back as an exact number of either storage type.  A block with a number that is not finite
+ * reads back as NaN, all of it.
  *   values_dev  [rows][features rounded up to 32] bytes, 16-byte aligned; zeros behind the last feature,
  *   scales_dev  [rows][features rounded up to 32, / 32] bytes: e + 127, or 255 for a block that is not finite.
  * mpcnn_rows_pack: x_dev [rows][x_pitch] into 8 bits.  mpcnn_rows_unpack: back, rounded to `dtype` (which is exact).
