@@ -9,9 +9,11 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from functools import lru_cache
 from typing import Optional, Sequence, Tuple
 
 import numpy as np
+import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmpcnn.so")
@@ -89,9 +91,8 @@ def lib():
             raise ImportError("libmpcnn.so is not built: run `python -m paper_1302_1690_amd.build` "
                               "(there is no fallback path)")
         # torch ships its own copy of the HIP runtime (same soname as the system one):
-        # it must be loaded first so that the library binds to it and both share one
+        # it is loaded first (above) so that the library binds to it and both share one
         # runtime, hence one set of device allocations and streams.
-        import torch  # noqa: F401
         L = C.CDLL(LIB_PATH)
         vp, sz, i = C.c_void_p, C.c_size_t, C.c_int
         L.mpcnn_net_create.argtypes = [C.POINTER(_LayerDesc), i, i, i, i, C.POINTER(vp)]
@@ -179,7 +180,6 @@ def _check(st: int):
 
 def _stream_handle(stream) -> int:
     if stream is None:
-        import torch
         stream = torch.cuda.current_stream()
     return int(getattr(stream, "cuda_stream", stream))
 
@@ -258,7 +258,6 @@ class Net:
 
     # ---- device calls (torch tensors carry the memory)
     def alloc_workspace(self, B: int, H: int, W: int, training: bool):
-        import torch
         need = self.workspace_bytes(B, H, W, training)
         if need == 0:
             raise MpcnnError(2, "image %dx%d does not fit the net" % (H, W))
@@ -268,7 +267,6 @@ class Net:
 
     def seg_forward(self, image, probs=None, ws=None, stream=None):
         """image [B,C0,H,W] fp32 cuda tensor -> probs [B,n_cls,H-P+1,W-P+1]."""
-        import torch
         B, _, H, W = image.shape
         assert image.is_cuda and image.dtype == torch.float32 and image.is_contiguous()
         if ws is None:
@@ -289,7 +287,6 @@ class Net:
 
     def seg_loss(self, image, labels, pixw=None, ws=None, stream=None) -> float:
         """Summed loss at the current parameters (forward only, nothing kept)."""
-        import torch
         B, _, H, W = image.shape
         if ws is None:
             ws = self.alloc_workspace(B, H, W, False)
@@ -333,7 +330,6 @@ class Net:
     def seg_backward_banded(self, image, labels, band_rows, pixw=None, probs=None, loss=None, stream=None):
         """Forward + backward with the image taken in bands of `band_rows` output rows; the
         workspace (allocated here) is one band's.  Gradients stay in the net."""
-        import torch
         B, _, H, W = image.shape
         assert image.is_cuda and image.dtype == torch.float32 and image.is_contiguous()
         assert labels.dtype == torch.int32 and labels.is_contiguous() and tuple(labels.shape) == (B, H, W)
@@ -356,7 +352,6 @@ class Net:
 
     def class_balance_weights(self, labels, stream=None):
         """labels [B,H,W] int32 cuda -> pixw [B,H,W] fp32 cuda, 1/N_k at output pixels of class k."""
-        import torch
         B, H, W = labels.shape
         assert labels.is_cuda and labels.dtype == torch.int32 and labels.is_contiguous()
         pixw = torch.empty((B, H, W), dtype=torch.float32, device=labels.device)
@@ -367,7 +362,6 @@ class Net:
 
     def seg_forward_same(self, image, probs=None, ws=None, stream=None):
         """Deployment forward with mirrored borders: image [B,C0,H,W] -> probs [B,n_cls,H,W]."""
-        import torch
         B, _, H, W = image.shape
         assert image.is_cuda and image.dtype == torch.float32 and image.is_contiguous()
         if ws is None:
@@ -385,7 +379,6 @@ class Net:
 
     def seg_backward(self, image, labels, pixw=None, probs=None, loss=None, ws=None, stream=None):
         """Forward + backward; gradients stay in the net.  Returns (probs, loss) as given."""
-        import torch
         B, _, H, W = image.shape
         assert image.is_cuda and image.dtype == torch.float32 and image.is_contiguous()
         assert labels.dtype == torch.int32 and labels.is_contiguous() and tuple(labels.shape) == (B, H, W)
@@ -446,7 +439,6 @@ def _refuse(text: str):
 
 
 def _check_norm(norm, device):
-    import torch
     if norm.dtype != torch.float64 or norm.numel() != 1 or not norm.is_cuda or (device is not None and norm.device != device):
         _refuse("norm: one fp64 on the tensors' GPU")
 
@@ -457,7 +449,6 @@ class _On:
     __slots__ = ("handle", "ctx")
 
     def __init__(self, device, stream):
-        import torch
         self.ctx = None
         if stream is None:
             self.handle = torch._C._cuda_getCurrentRawStream(device.index)
@@ -481,13 +472,14 @@ class _On:
             self.ctx.__exit__(*error)
 
 
+_STORAGE = {torch.float32: F32, torch.bfloat16: BF16}
+
+
 def _dtype_of(t) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.bfloat16:
-        return BF16
-    _refuse("%s: fp32 and bf16 are supported" % t.dtype)
+    kind = _STORAGE.get(t.dtype)
+    if kind is None:
+        _refuse("%s: fp32 and bf16 are supported" % t.dtype)
+    return kind
 
 
 class GradList:
@@ -495,7 +487,6 @@ class GradList:
     sgd_step, the parameters they belong to.  The list keeps the tensors alive and works on their memory."""
 
     def __init__(self, grads, params=None):
-        import torch
         self._h = None
         self.grads = list(grads)
         self.params = None if params is None else list(params)
@@ -533,7 +524,6 @@ class GradList:
             pass
 
     def _norm(self, norm):
-        import torch
         if norm is None:
             return torch.empty(1, dtype=torch.float64, device=self.device)
         _check_norm(norm, self.device)
@@ -569,10 +559,12 @@ def class_workspace_bytes(rows: int, features: int, classes: int, dtype: int, tr
 
 def _rows_of(name, t, device, dtype):
     """A matrix whose rows are dense -> its rows, columns and pitch in elements."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or t.dtype != dtype or t.device != device:
+    if t.dtype is not dtype or t.dim() != 2 or t.device != device:
         _refuse("%s: a %s matrix on %s is wanted" % (name, dtype, device))
-    rows, columns = shape
+    rows, columns = t.shape
+    if t.is_contiguous():
+        return rows, columns, columns
+    stride = t.stride()
     if columns > 1 and stride[1] != 1:
         _refuse("%s: the numbers of a row have to be consecutive" % name)
     return rows, columns, stride[0] if rows > 1 else max(columns, stride[0])
@@ -588,7 +580,6 @@ def _vector(name, t, n, dtype, device):
 
 def _class_call(x, w, labels, bias, roww):
     """The arguments that class_loss and class_backward share, checked; and the tensors' GPU."""
-    import torch
     device, dtype = x.device, x.dtype
     if device.type != "cuda":
         _refuse("x: a tensor on a GPU is wanted")
@@ -606,7 +597,6 @@ def _class_call(x, w, labels, bias, roww):
 def _output(name, given, shape, dtype, device):
     """Given (checked), allocated (None) or not asked for (False) -> the tensor or None."""
     if given is None:
-        import torch
         return torch.empty(*shape, dtype=dtype, device=device)
     if given is False:
         return None
@@ -619,7 +609,6 @@ def _output(name, given, shape, dtype, device):
 
 def _class_workspace(ws, args, training, device):
     """Address and bytes of the workspace, and what keeps it."""
-    import torch
     if ws is None:
         ws = torch.empty(max(256, lib().mpcnn_workspace_bytes_class_call(*args[7:], training)), dtype=torch.uint8, device=device)
     elif ws.device != device or not ws.is_contiguous():
@@ -633,7 +622,6 @@ def class_loss(x, w, labels, bias=None, roww=None, rowloss=None, lse=None, loss=
     x [rows, features] and w [classes, features], fp32 or bf16, rows dense; labels [rows] int32; bias [classes]
     and roww [rows] fp32 or None.  -> (loss, rowloss, lse): the summed loss (one fp64), w * -log p[label] and
     log sum exp of the scores per row (fp32), put into the tensors given, allocated for None, left out for False."""
-    import torch
     device, args = _class_call(x, w, labels, bias, roww)
     with _On(device, stream) as st:
         loss = _output("loss", loss, (1,), torch.float64, device)
@@ -648,7 +636,6 @@ def class_backward(x, w, labels, bias=None, roww=None, rowloss=None, loss=None, 
     """class_loss and its gradients -> (loss, rowloss, dx, dw, db); dx and dw have x's type, db (None without
     a bias) is fp32.  Each is put into the tensor given (dx: its rows dense), allocated for None, left out for False.
     Its losses can differ from class_loss's in the last bits."""
-    import torch
     device, args = _class_call(x, w, labels, bias, roww)
     rows, features, classes = args[7:10]
     with _On(device, stream) as st:
@@ -676,7 +663,6 @@ class PackedRows:
     __slots__ = ("values", "scales", "features", "kind", "_c")
 
     def __init__(self, values, scales, features: int):
-        import torch
         kind = {torch.int8: I8, torch.float8_e4m3fn: E4M3}.get(values.dtype)
         if kind is None:
             _refuse("values: %s: int8 and float8_e4m3fn are supported" % values.dtype)
@@ -690,7 +676,6 @@ class PackedRows:
 
     @classmethod
     def empty(cls, rows: int, features: int, kind: int, device):
-        import torch
         if kind not in (I8, E4M3) or isinstance(kind, bool):
             _refuse("unknown kind %r of rows in 8 bits" % (kind,))
         if rows < 0 or features < 1:
@@ -712,6 +697,11 @@ class PackedRows:
         return self.values.device
 
 
+def _here(device, stream):
+    """The handle of the current stream, where a call goes there and its tensors' GPU is the current one; else None: the call is made inside _On."""
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None and device.index == torch._C._cuda_getDevice() else None
+
+
 def _on_gpu(name, x):
     """A matrix of rows on a GPU -> (device, kind, rows, features, pitch)."""
     device = x.device
@@ -722,7 +712,6 @@ def _on_gpu(name, x):
 
 def _matrix_out(name, given, rows, features, dtype, device):
     """A matrix to write, given (its rows dense), allocated (None) or left out (False) -> the tensor or None, its address, its pitch."""
-    import torch
     if given is None:
         given = torch.empty(rows, features, dtype=dtype, device=device)
         return given, given.data_ptr(), features
@@ -737,7 +726,7 @@ def _packed_out(name, given, rows, features, device):
     """PackedRows, given or a kind to allocate them in."""
     if not isinstance(given, PackedRows):
         return PackedRows.empty(rows, features, given, device)
-    if given.rows != rows or given.features != features or given.device != device:
+    if given.values.shape[0] != rows or given.features != features or given.values.device != device:
         _refuse("%s: %d rows of %d features in 8 bits on %s are wanted" % (name, rows, features, device))
     return given
 
@@ -760,20 +749,25 @@ def rows_pack(x, kind=I8, stream=None) -> PackedRows:
     """Rows of features (fp32 or bf16) into 8 bits, I8 or E4M3, blocks of 32 features with a power of two each; `kind` may be the PackedRows to
     write into."""
     device, dtype, rows, features, pitch = _on_gpu("x", x)
-    with _On(device, stream) as st:
-        out = _packed_out("kind", kind, rows, features, device)
-        _check(lib().mpcnn_rows_pack(x.data_ptr(), pitch, rows, features, dtype, C.byref(out._c), st))
+    st = _here(device, stream)
+    if st is None:
+        with _On(device, stream):
+            return rows_pack(x, kind)
+    out = _packed_out("kind", kind, rows, features, device)
+    _check(lib().mpcnn_rows_pack(x.data_ptr(), pitch, rows, features, dtype, C.byref(out._c), st))
     return out
 
 
 def rows_unpack(packed: PackedRows, out=None, stream=None):
     """What rows in 8 bits stand for, into `out` (fp32 or bf16, exact in both; None: a new bf16 tensor)."""
-    import torch
     device, rows, features = packed.device, packed.rows, packed.features
-    with _On(device, stream) as st:
-        dtype = torch.bfloat16 if out is None else out.dtype
-        out, at, pitch = _matrix_out("out", out, rows, features, dtype, device)
-        _check(lib().mpcnn_rows_unpack(C.byref(packed._c), rows, features, _dtype_of(out), at, pitch, st))
+    st = _here(device, stream)
+    if st is None:
+        with _On(device, stream):
+            return rows_unpack(packed, out)
+    dtype = torch.bfloat16 if out is None else out.dtype
+    out, at, pitch = _matrix_out("out", out, rows, features, dtype, device)
+    _check(lib().mpcnn_rows_unpack(C.byref(packed._c), rows, features, _dtype_of(out), at, pitch, st))
     return out
 
 
@@ -784,29 +778,32 @@ def rows_norm(x, gain, residual=None, eps: float = 1e-6, y=None, h=None, kept=Fa
     y: a tensor of x's type, or in 8 bits: a kind (I8, E4M3) or PackedRows to write into.  h: the sum in x's type (without a residual only if asked
     for by a tensor); kept: the sum in 8 bits, a kind or PackedRows.  rstd [rows] fp32.  Each is put into what is given, allocated for None, left out
     for False.  y and h may be x or residual itself."""
-    import torch
     device, dtype, rows, features, x_pitch = _on_gpu("x", x)
     res, res_pitch = _like("residual", residual, rows, features, x.dtype, device)
     g = _vector("gain", gain, features, torch.float32, device)
-    with _On(device, stream) as st:
-        y_at, y_pitch, y8, h8 = None, features, None, None
-        if _is_kind(y):
-            y = _packed_out("y", y, rows, features, device)
-            y8 = C.byref(y._c)
-        else:
-            y, y_at, y_pitch = _matrix_out("y", y, rows, features, x.dtype, device)
-        h, h_at, h_pitch = _matrix_out("h", False if h is None and residual is None else h, rows, features, x.dtype, device)
-        if kept is not False:
-            kept = _packed_out("kept", I8 if kept is None else kept, rows, features, device)
-            h8 = C.byref(kept._c)
-        else:
-            kept = None
-        rstd = _output("rstd", rstd, (rows,), torch.float32, device)
-        _check(lib().mpcnn_rows_norm(x.data_ptr(), x_pitch, res, res_pitch, g, rows, features, dtype, eps, y_at, y_pitch, y8, h_at, h_pitch, h8,
-                                     _ptr(rstd), st))
+    st = _here(device, stream)
+    if st is None:
+        with _On(device, stream):
+            return rows_norm(x, gain, residual, eps, y, h, kept, rstd)
+    y_at, y_pitch, y8, h8 = None, features, None, None
+    if _is_kind(y):
+        y = _packed_out("y", y, rows, features, device)
+        y8 = C.byref(y._c)
+    else:
+        y, y_at, y_pitch = _matrix_out("y", y, rows, features, x.dtype, device)
+    h, h_at, h_pitch = _matrix_out("h", False if h is None and residual is None else h, rows, features, x.dtype, device)
+    if kept is not False:
+        kept = _packed_out("kept", I8 if kept is None else kept, rows, features, device)
+        h8 = C.byref(kept._c)
+    else:
+        kept = None
+    rstd = _output("rstd", rstd, (rows,), torch.float32, device)
+    _check(lib().mpcnn_rows_norm(x.data_ptr(), x_pitch, res, res_pitch, g, rows, features, dtype, eps, y_at, y_pitch, y8, h_at, h_pitch, h8,
+                                 _ptr(rstd), st))
     return y, h, kept, rstd
 
 
+@lru_cache(maxsize=4096)
 def norm_workspace_bytes(rows: int, features: int) -> int:
     """Bytes of workspace that are enough for rows_norm_backward on so many rows or fewer."""
     return lib().mpcnn_workspace_bytes_norm(rows, features)
@@ -814,10 +811,11 @@ def norm_workspace_bytes(rows: int, features: int) -> int:
 
 def _workspace(ws, size, device):
     """The workspace's address and bytes, and what keeps it."""
-    import torch
     if ws is None:
-        ws = torch.empty(max(256, size), dtype=torch.uint8, device=device)
-    elif ws.device != device or not ws.is_contiguous():
+        size = max(256, size)
+        ws = torch.empty(size, dtype=torch.uint8, device=device)
+        return ws.data_ptr(), size, ws
+    if ws.device != device or not ws.is_contiguous():
         _refuse("ws: contiguous memory on %s is wanted" % device)
     return ws.data_ptr(), ws.numel() * ws.element_size(), ws
 
@@ -826,7 +824,6 @@ def rows_norm_backward(dy, h, gain, rstd, dh=None, dx=None, dgain=None, ws=None,
     """Gradients of rows_norm -> (dx, dgain), from the gradients dy of y and dh of h (or None), and h as a tensor or as the PackedRows that were kept.
     dx (x's gradient and the residual's, dy's type) may be dy, dh or h itself; dgain is fp32.  Each is put into the tensor given, allocated for
     None, left out for False.  A row of dy that is zero throughout adds nothing, whatever h holds there."""
-    import torch
     device, dtype, rows, features, dy_pitch = _on_gpu("dy", dy)
     h_at, h_pitch, h8 = None, features, None
     if isinstance(h, PackedRows):
@@ -836,15 +833,19 @@ def rows_norm_backward(dy, h, gain, rstd, dh=None, dx=None, dgain=None, ws=None,
         h_at, h_pitch = _like("h", h, rows, features, dy.dtype, device)
     more, more_pitch = _like("dh", dh, rows, features, dy.dtype, device)
     g, r = _vector("gain", gain, features, torch.float32, device), _vector("rstd", rstd, rows, torch.float32, device)
-    with _On(device, stream) as st:
-        dx, dx_at, dx_pitch = _matrix_out("dx", dx, rows, features, dy.dtype, device)
-        dgain = _output("dgain", dgain, (features,), torch.float32, device)
-        at, size, _kept = _workspace(ws, lib().mpcnn_workspace_bytes_norm(rows, features) if ws is None else 0, device)
-        _check(lib().mpcnn_rows_norm_backward(dy.data_ptr(), dy_pitch, h_at, h_pitch, h8, g, r, more, more_pitch, rows, features, dtype, dx_at, dx_pitch,
-                                              _ptr(dgain), at, size, st))
+    st = _here(device, stream)
+    if st is None:
+        with _On(device, stream):
+            return rows_norm_backward(dy, h, gain, rstd, dh, dx, dgain, ws)
+    dx, dx_at, dx_pitch = _matrix_out("dx", dx, rows, features, dy.dtype, device)
+    dgain = _output("dgain", dgain, (features,), torch.float32, device)
+    at, size, _kept = _workspace(ws, norm_workspace_bytes(rows, features) if ws is None else 0, device)
+    _check(lib().mpcnn_rows_norm_backward(dy.data_ptr(), dy_pitch, h_at, h_pitch, h8, g, r, more, more_pitch, rows, features, dtype, dx_at, dx_pitch,
+                                          _ptr(dgain), at, size, st))
     return dx, dgain
 
 
+@lru_cache(maxsize=4096)
 def weight_grad_workspace_bytes(rows: int, outs: int, features: int, dtype: int) -> int:
     """Bytes of workspace of rows_weight_grad with these sizes."""
     return lib().mpcnn_workspace_bytes_weight_grad(rows, outs, features, dtype)
@@ -854,24 +855,27 @@ def rows_weight_grad(dy, x: PackedRows, dw=None, ws=None, stream=None):
     """The gradient of a linear layer's weights, dw[o, f] = sum over the rows of dy[n, o] x[n, f], from the layer's input rows in 8 bits.
 
     dy [rows, outs] fp32 or bf16, rows dense; dw [outs, features]: given (fp32 or bf16) or allocated in dy's type."""
-    import torch
     device, dtype, rows, outs, pitch = _on_gpu("dy", dy)
     if not isinstance(x, PackedRows):
         _refuse("x: PackedRows are wanted")
     features = x.features
     _packed_out("x", x, rows, features, device)
-    with _On(device, stream) as st:
-        if dw is None:
-            dw = torch.empty(outs, features, dtype=dy.dtype, device=device)
-        else:
-            _output("dw", dw, (outs, features), dw.dtype, device)
-        at, size, _kept = _workspace(ws, lib().mpcnn_workspace_bytes_weight_grad(rows, outs, features, dtype) if ws is None else 0, device)
-        _check(lib().mpcnn_rows_weight_grad(dy.data_ptr(), pitch, C.byref(x._c), rows, outs, features, dtype, dw.data_ptr(), _dtype_of(dw), at, size, st))
+    st = _here(device, stream)
+    if st is None:
+        with _On(device, stream):
+            return rows_weight_grad(dy, x, dw, ws)
+    if dw is None:
+        dw = torch.empty(outs, features, dtype=dy.dtype, device=device)
+    else:
+        _output("dw", dw, (outs, features), dw.dtype, device)
+    at, size, _kept = _workspace(ws, weight_grad_workspace_bytes(rows, outs, features, dtype) if ws is None else 0, device)
+    _check(lib().mpcnn_rows_weight_grad(dy.data_ptr(), pitch, C.byref(x._c), rows, outs, features, dtype, dw.data_ptr(), _dtype_of(dw), at, size, st))
     return dw
 
 
 # ---- beam search over a class layer's classes
 
+@lru_cache(maxsize=4096)
 def beam_workspace_bytes(sequences: int, beams: int, classes: int) -> int:
     """Bytes of workspace that are enough for beam_select on so many sequences or fewer."""
     return lib().mpcnn_workspace_bytes_beam(sequences, beams, classes)
@@ -879,7 +883,6 @@ def beam_workspace_bytes(sequences: int, beams: int, classes: int) -> int:
 
 def _beams(totals, done, device):
     """Sequences and beams, and the addresses of what is known of the beams."""
-    import torch
     if totals.dim() != 2 or totals.dtype != torch.float32 or totals.device != device or not totals.is_contiguous():
         _refuse("totals: [sequences, beams] fp32 on %s are wanted, consecutive" % device)
     if done is not None and (done.dtype not in (torch.bool, torch.uint8) or done.shape != totals.shape or done.device != device or not done.is_contiguous()):
@@ -889,7 +892,6 @@ def _beams(totals, done, device):
 
 def _beam_outputs(out, sequences, width, device):
     """What a selection writes: given as (totals, parents, classes, done), or allocated."""
-    import torch
     if out is None:
         shape = (sequences, width)
         return (torch.empty(shape, dtype=torch.float32, device=device), torch.empty(shape, dtype=torch.int32, device=device),
@@ -907,21 +909,24 @@ def beam_select(scores, totals, width=None, bias=None, done=None, end: int = -1,
     bias [classes] fp32 or None (minus infinity: off); done [sequences, beams] bool or None: finished beams, which offer class `end` at their total; width:
     how many go on (None: as many as there are).  totals fp32, parents (beams of the sequence) and classes int32, done bool; minus infinity, -1, -1
     and True where there is no candidate.  `out`: four such tensors to write into."""
-    import torch
     device, kind, rows, classes, pitch = _on_gpu("scores", scores)
     sequences, beams = _beams(totals, done, device)
     if rows != sequences * beams:
         _refuse("scores: %d rows of %d sequences of %d beams" % (rows, sequences, beams))
     width = beams if width is None else width
     b = _vector("bias", bias, classes, torch.float32, device)
-    with _On(device, stream) as st:
-        out = _beam_outputs(out, sequences, width, device)
-        at, size, _kept = _workspace(ws, lib().mpcnn_workspace_bytes_beam(sequences, beams, classes) if ws is None else 0, device)
-        _check(lib().mpcnn_beam_select(scores.data_ptr(), pitch, b, totals.data_ptr(), _ptr(done), end, sequences, beams, width, classes, kind,
-                                       *[t.data_ptr() for t in out], at, size, st))
+    st = _here(device, stream)
+    if st is None:
+        with _On(device, stream):
+            return beam_select(scores, totals, width, bias, done, end, out, ws)
+    out = _beam_outputs(out, sequences, width, device)
+    at, size, _kept = _workspace(ws, beam_workspace_bytes(sequences, beams, classes) if ws is None else 0, device)
+    _check(lib().mpcnn_beam_select(scores.data_ptr(), pitch, b, totals.data_ptr(), _ptr(done), end, sequences, beams, width, classes, kind,
+                                   out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), out[3].data_ptr(), at, size, st))
     return out
 
 
+@lru_cache(maxsize=4096)
 def class_beam_workspace_bytes(sequences: int, beams: int, features: int, classes: int, dtype: int) -> int:
     """Bytes of workspace that are enough for class_beam on so many sequences or fewer."""
     return lib().mpcnn_workspace_bytes_class_beam(sequences, beams, features, classes, dtype)
@@ -929,7 +934,6 @@ def class_beam_workspace_bytes(sequences: int, beams: int, features: int, classe
 
 def class_beam(x, w, totals, width=None, bias=None, done=None, end: int = -1, out=None, ws=None, stream=None):
     """beam_select on the scores of a class layer: x [sequences * beams, features] and w [classes, features], fp32 or bf16, rows dense; the rest as there."""
-    import torch
     device, kind, rows, features, x_pitch = _on_gpu("x", x)
     classes, columns, w_pitch = _rows_of("w", w, device, x.dtype)
     if columns != features:
@@ -939,11 +943,14 @@ def class_beam(x, w, totals, width=None, bias=None, done=None, end: int = -1, ou
         _refuse("x: %d rows of %d sequences of %d beams" % (rows, sequences, beams))
     width = beams if width is None else width
     b = _vector("bias", bias, classes, torch.float32, device)
-    with _On(device, stream) as st:
-        out = _beam_outputs(out, sequences, width, device)
-        at, size, _kept = _workspace(ws, lib().mpcnn_workspace_bytes_class_beam(sequences, beams, features, classes, kind) if ws is None else 0, device)
-        _check(lib().mpcnn_class_beam(x.data_ptr(), x_pitch, w.data_ptr(), w_pitch, b, totals.data_ptr(), _ptr(done), end, sequences, beams, width, features,
-                                      classes, kind, *[t.data_ptr() for t in out], at, size, st))
+    st = _here(device, stream)
+    if st is None:
+        with _On(device, stream):
+            return class_beam(x, w, totals, width, bias, done, end, out, ws)
+    out = _beam_outputs(out, sequences, width, device)
+    at, size, _kept = _workspace(ws, class_beam_workspace_bytes(sequences, beams, features, classes, kind) if ws is None else 0, device)
+    _check(lib().mpcnn_class_beam(x.data_ptr(), x_pitch, w.data_ptr(), w_pitch, b, totals.data_ptr(), _ptr(done), end, sequences, beams, width, features,
+                                  classes, kind, out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), out[3].data_ptr(), at, size, st))
     return out
 
 
@@ -952,7 +959,6 @@ class BeamStates:
     told to move the first positions along that axis only.  The list keeps the tensors alive and works on their memory."""
 
     def __init__(self, tensors, sequences: int, beams: int, axis: Optional[int] = None):
-        import torch
         self._h = None
         self.tensors, self.sequences, self.beams = list(tensors), sequences, beams
         self.device = self.tensors[0].device if self.tensors else torch.device("cuda", torch.cuda.current_device())
@@ -992,7 +998,6 @@ class BeamStates:
     def reorder(self, parents, length: Optional[int] = None, stream=None):
         """Row b * beams + k of every tensor becomes what row b * beams + parents[b, k] was (int32, -1: it stays); with `length`, in the first `length`
         positions only."""
-        import torch
         if parents.dtype != torch.int32 or parents.shape != (self.sequences, self.beams) or parents.device != self.device or not parents.is_contiguous():
             _refuse("parents: [%d, %d] int32 on %s are wanted, consecutive" % (self.sequences, self.beams, self.device))
         if length is not None and length < 0:
