@@ -302,7 +302,7 @@ mpcnn_status mpcnn_beam_reorder(const mpcnn_beam_states* list, const int32_t* pa
     if (!most || !list->sequences || list->beams < 2) return MPCNN_OK;
     mpcnn::ReorderArgs a{};
     a.states = list->d_states; a.parents = parents_dev; a.length = length < 0 ? -1 : length;
-    a.count = list->count; a.sequences = list->sequences; a.beams = list->beams;
+    a.sequences = list->sequences; a.beams = list->beams;
     const int64_t y = std::min<int64_t>(list->sequences, 65535);
     // (no more than 2^23 workgroups: the rest of a row is the same workgroups' again)
     const int64_t x = std::max<int64_t>(1, std::min<int64_t>((most + 255) / 256, ((int64_t)1 << 23) / (y * list->count)));

@@ -522,7 +522,7 @@ struct ReorderArgs {
     const BeamState* states;
     const int* parents;                    // [sequences][beams]
     long length;                           // positions, below zero: all
-    int count, sequences, beams;
+    int sequences, beams;
 };
 
 template <int N> struct Bytes { typedef unsigned type __attribute__((ext_vector_type(N / 4))); };

@@ -594,10 +594,15 @@ def _class_call(x, w, labels, bias, roww):
                     rows, features, classes, kind)
 
 
+def _new(shape, dtype, device):
+    """A new tensor of one or two dimensions, dense (strides given: it takes three quarters of the time)."""
+    return torch.empty_strided(shape, (1,) if len(shape) == 1 else (shape[1], 1), dtype=dtype, device=device)
+
+
 def _output(name, given, shape, dtype, device):
     """Given (checked), allocated (None) or not asked for (False) -> the tensor or None."""
     if given is None:
-        return torch.empty(*shape, dtype=dtype, device=device)
+        return _new(shape, dtype, device)
     if given is False:
         return None
     if given.dtype != dtype or given.device != device or given.shape != shape:
@@ -682,8 +687,8 @@ class PackedRows:
             _refuse("%d rows of %d features in 8 bits" % (rows, features))
         blocks = (features + 31) // 32
         self = cls.__new__(cls)            # (nothing to check)
-        self.values = torch.empty(rows, 32 * blocks, dtype=torch.int8 if kind == I8 else torch.float8_e4m3fn, device=device)
-        self.scales = torch.empty(rows, blocks, dtype=torch.uint8, device=device)
+        self.values = _new((rows, 32 * blocks), torch.int8 if kind == I8 else torch.float8_e4m3fn, device)
+        self.scales = _new((rows, blocks), torch.uint8, device)
         self.features, self.kind = features, kind
         self._c = _Packed(self.values.data_ptr(), self.scales.data_ptr(), kind)
         return self
@@ -713,7 +718,7 @@ def _on_gpu(name, x):
 def _matrix_out(name, given, rows, features, dtype, device):
     """A matrix to write, given (its rows dense), allocated (None) or left out (False) -> the tensor or None, its address, its pitch."""
     if given is None:
-        given = torch.empty(rows, features, dtype=dtype, device=device)
+        given = _new((rows, features), dtype, device)
         return given, given.data_ptr(), features
     if given is False:
         return None, None, features
@@ -813,7 +818,7 @@ def _workspace(ws, size, device):
     """The workspace's address and bytes, and what keeps it."""
     if ws is None:
         size = max(256, size)
-        ws = torch.empty(size, dtype=torch.uint8, device=device)
+        ws = _new((size,), torch.uint8, device)
         return ws.data_ptr(), size, ws
     if ws.device != device or not ws.is_contiguous():
         _refuse("ws: contiguous memory on %s is wanted" % device)
@@ -865,7 +870,7 @@ def rows_weight_grad(dy, x: PackedRows, dw=None, ws=None, stream=None):
         with _On(device, stream):
             return rows_weight_grad(dy, x, dw, ws)
     if dw is None:
-        dw = torch.empty(outs, features, dtype=dy.dtype, device=device)
+        dw = _new((outs, features), dy.dtype, device)
     else:
         _output("dw", dw, (outs, features), dw.dtype, device)
     at, size, _kept = _workspace(ws, weight_grad_workspace_bytes(rows, outs, features, dtype) if ws is None else 0, device)
@@ -894,8 +899,7 @@ def _beam_outputs(out, sequences, width, device):
     """What a selection writes: given as (totals, parents, classes, done), or allocated."""
     if out is None:
         shape = (sequences, width)
-        return (torch.empty(shape, dtype=torch.float32, device=device), torch.empty(shape, dtype=torch.int32, device=device),
-                torch.empty(shape, dtype=torch.int32, device=device), torch.empty(shape, dtype=torch.bool, device=device))
+        return (_new(shape, torch.float32, device), _new(shape, torch.int32, device), _new(shape, torch.int32, device), _new(shape, torch.bool, device))
     totals, parents, classes, done = out
     for name, t, dtype in (("totals", totals, torch.float32), ("parents", parents, torch.int32), ("classes", classes, torch.int32), ("done", done, torch.bool)):
         _output(name, t, (sequences, width), dtype, device)
