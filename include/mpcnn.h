@@ -358,6 +358,7 @@ mpcnn_status mpcnn_class_backward(const void* x_dev, int64_t x_pitch, const void
  *   scales_dev  [rows][features rounded up to 32, / 32] bytes: e + 127, or 255 for a block that is not finite.
  * mpcnn_rows_pack: x_dev [rows][x_pitch] into 8 bits.  mpcnn_rows_unpack: back, rounded to `dtype` (which is exact).
  * A pitch is in elements, at least `features`; matrices lie at any address that is a multiple of their element's size.  rows = 0 is allowed.
+ * Matrices of one pitch may lie beside each other in one buffer's columns.
  * Errors: EINVAL (also: an output that overlaps an input), EUNSUPPORTED (more than 2^31 - 1 rows or 2^20 features), EHIP.
  */
 typedef enum { MPCNN_I8 = 2, MPCNN_E4M3 = 3 } mpcnn_packing;

@@ -364,6 +364,26 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(mpcnn.rows_unpack(p)[-1], mpcnn.rows_unpack(one)[0])
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=_ids)
+@pytest.mark.parametrize("rows,features", [(1, 40), (7, 33), (300, 513), (5, 4104)])
+def test_in_one_buffers_columns(rows, features, dtype):
+    """Inputs and outputs beside each other in one buffer, with columns of nobody's behind them."""
+    gen = _gen(rows + features)
+    buffer = torch.full((rows, 6 * features + 3), 7.0, dtype=dtype, device="cuda")
+    x, y, residual, h, dy, dx = (buffer[:, i * features:(i + 1) * features] for i in range(6))
+    for t in (x, residual, dy):
+        t.copy_(_rand(gen, rows, features))
+    gain = 1 + _rand(gen, features)
+    inputs = [t.clone() for t in (x, residual, dy)]
+    want = mpcnn.rows_norm(inputs[0], gain, residual=inputs[1])
+    want_dx, want_dgain = mpcnn.rows_norm_backward(inputs[2], want[1], gain, want[3])
+    rstd = mpcnn.rows_norm(x, gain, residual=residual, y=y, h=h)[3]
+    dgain = mpcnn.rows_norm_backward(dy, h, gain, rstd, dx=dx)[1]
+    for got, wanted in ((y, want[0]), (h, want[1]), (rstd, want[3]), (dx, want_dx), (dgain, want_dgain), (x, inputs[0]), (residual, inputs[1]), (dy, inputs[2])):
+        assert torch.equal(got, wanted)
+    assert (buffer[:, 6 * features:] == 7.0).all()
+
+
 def test_streams_and_graphs():
     gen = _gen(31)
     dy, _, _, gain, _, dh = _back_inputs(gen, 600, 513, torch.bfloat16, None)

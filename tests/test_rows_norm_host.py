@@ -60,6 +60,13 @@ def test_backward_refusals(change, status):
     assert _back(**change) == status, mpcnn.lib().mpcnn_last_error().decode()
 
 
+@pytest.mark.parametrize("y,y_pitch,h", [(BASE + 156, 100, 5 * BASE), (BASE + 244, 100, 5 * BASE), (BASE + 160, 101, 5 * BASE), (BASE + 160, 100, BASE + 316), (BASE - 244, 100, 5 * BASE)])
+def test_beside_each_other_but_not_apart(y, y_pitch, h):
+    """Columns of one buffer, rows 400 bytes apart, 160 of them a matrix's: one number too near."""
+    assert _norm(x_pitch=100, y=y, y_pitch=y_pitch, h=h, h_pitch=100) == EINVAL
+    assert b"overlap" in mpcnn.lib().mpcnn_last_error()
+
+
 @pytest.mark.parametrize("x,pitch,rows,features,dtype,out,status", [
     (None, 40, 20, 40, 0, _p(BASE, 2 * BASE), EINVAL), (3 * BASE, 39, 20, 40, 0, _p(BASE, 2 * BASE), EINVAL), (3 * BASE + 2, 40, 20, 40, 0, _p(BASE, 2 * BASE), EINVAL),
     (3 * BASE, 40, -1, 40, 0, _p(BASE, 2 * BASE), EINVAL), (3 * BASE, 40, 20, 0, 0, _p(BASE, 2 * BASE), EINVAL), (3 * BASE, 40, 20, 40, 7, _p(BASE, 2 * BASE), EINVAL),
