@@ -303,9 +303,10 @@ mpcnn_status mpcnn_beam_reorder(const mpcnn_beam_states* list, const int32_t* pa
     mpcnn::ReorderArgs a{};
     a.states = list->d_states; a.parents = parents_dev; a.length = length < 0 ? -1 : length;
     a.sequences = list->sequences; a.beams = list->beams;
-    const int64_t y = std::min<int64_t>(list->sequences, 65535);
-    // (no more than 2^23 workgroups: the rest of a row is the same workgroups' again)
-    const int64_t x = std::max<int64_t>(1, std::min<int64_t>((most + 255) / 256, ((int64_t)1 << 23) / (y * list->count)));
+    // no more than 2^23 workgroups (a launch has less than 2^32 threads): the rest of the sequences, and of a row, is the same workgroups' again
+    const int64_t most_groups = (int64_t)1 << 23;
+    const int64_t y = std::min({(int64_t)list->sequences, (int64_t)65535, most_groups / list->count});
+    const int64_t x = std::max<int64_t>(1, std::min<int64_t>((most + 255) / 256, most_groups / (y * list->count)));
     const dim3 grid((unsigned)x, (unsigned)y, (unsigned)list->count);
     const hipStream_t st = (hipStream_t)hip_stream;
     if (a.beams <= 4) launch_reorder<4>(a, grid, st);

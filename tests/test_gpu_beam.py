@@ -334,6 +334,16 @@ def test_reorder_of_tensors_that_lie_in_turn():
     assert torch.equal(both, _plain_reorder(was, p))
 
 
+def test_reorder_of_many_tensors_and_sequences():
+    """More workgroups than a launch has, were every sequence of every tensor one's."""
+    buffer = torch.arange(2 * 65535 * 300, dtype=torch.int32, device="cuda").view(2 * 65535, 300)
+    p = torch.tensor([1, 0], dtype=torch.int32, device="cuda").repeat(65535, 1)
+    p[::7] = torch.tensor([0, 0], dtype=torch.int32, device="cuda")
+    want = _plain_reorder(buffer, p)
+    mpcnn.BeamStates([buffer[:, i] for i in range(300)], 65535, 2).reorder(p)
+    assert torch.equal(buffer, want)
+
+
 def test_reorder_far_rows():
     t = torch.empty((4, 1200000007), dtype=torch.uint8, device="cuda")       # rows at odd addresses beyond 2^32 bytes
     for i in range(4):
