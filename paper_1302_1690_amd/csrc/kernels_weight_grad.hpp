@@ -175,9 +175,12 @@ __global__ __launch_bounds__(64 * WM * WN) void weight_grad_kernel(WeightGradArg
                     v8f v = widen(ra[i]);
 #pragma unroll
                     for (int z = 0; z < P; ++z) {
-                        const g_bf16x8 h = __builtin_convertvector(v, g_bf16x8);
-                        write(at + z * kPart, h);
-                        v -= __builtin_convertvector(h, v8f);
+                        g_u4 h;                          // (cut off, not rounded: 8 bits of the 24 each, and the largest numbers do not become infinite)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) h[q] = __builtin_amdgcn_perm(bits_of(v[2 * q + 1]), bits_of(v[2 * q]), 0x07060302);
+                        write(at + z * kPart, __builtin_bit_cast(g_bf16x8, h));
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) v[q] -= __builtin_bit_cast(float, bits_of(v[q]) & 0xffff0000u);
                     }
                 }
             }

@@ -56,6 +56,19 @@ def test_weight_grad(rows, outs, features, kind, dtype):
     check(mpcnn.rows_weight_grad(dy, p, dw=torch.empty((outs, features), device="cuda", dtype=torch.bfloat16)), dy, p)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_largest_numbers(kind):
+    """fp32's largest numbers, which are nearer to bf16's infinity than to its largest, with small ones of x: as large as it gets, and finite."""
+    gen = _gen(77 + kind)
+    dy, p = _inputs(gen, 100, 40, 70, torch.float32, kind)
+    most = torch.finfo(torch.float32).max
+    dy[::3] = torch.where(dy[::3] > 0, most, -most)
+    small = mpcnn.PackedRows(p.values, (p.scales - 40).contiguous(), 70)          # (x times 2^-40)
+    dw = mpcnn.rows_weight_grad(dy, small)
+    assert torch.isfinite(dw).all()
+    check(dw, dy, small)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=_ids)
 def test_every_place_of_a_tile(dtype):
     """One row at a time has one number: every product lands where it belongs, exactly."""
