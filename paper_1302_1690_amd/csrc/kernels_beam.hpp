@@ -8,7 +8,7 @@
 // workgroup leaves its classes' largest and sum of exponentials.  The second, a workgroup per sequence, joins the sums and reads again only what can matter: the chunks whose
 // largest are among the `width` best of all.  (Let an element of another chunk be among the best: `width` chunks have a largest that is better, and so is
 // not below it, and these are as many elements that come before it.)  Order is by (value, then place), which no two candidates share, so the
-// result does not depend on timing.  lse is a sum of fp32 exponentials, joined in 64 bits: within one beam the order is the scores', exactly.
+// result does not depend on timing.  lse is a sum of fp32 exponentials, joined in 64 bits: within one beam values are never against the scores' order.
 //
 // 64 sequences x 8 beams x 50021 bf16 with biases: the pass 14 us (3.7 TB/s; bound by the vector instructions: some 14 issue slots a class), the pick 9 (1 sequence x 4 beams x 32000: 6.5), a chain of
 // trips to memory and LDS; chunks of 1024 instead of 256 and the best one after the other by the wave: 19 and 20 us, and 85 for 12 x 6 beams x 1573 with 16 wanted (15).

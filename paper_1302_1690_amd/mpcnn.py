@@ -8,6 +8,7 @@ been built, or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from functools import lru_cache
 from typing import Optional, Sequence, Tuple
@@ -664,8 +665,10 @@ def class_backward(x, w, labels, bias=None, roww=None, rowloss=None, loss=None, 
 
 class PackedRows:
     """Rows of features in 8 bits (mpcnn_packed): `values` [rows, features rounded up to 32], int8 or float8_e4m3fn, zeros behind the
-    last feature, and `scales` [rows, blocks of 32 features] uint8: 127 + the exponent of the block's power of two, 255 for a block that is not finite."""
-    __slots__ = ("values", "scales", "features", "kind", "_c")
+    last feature, and `scales` [rows, blocks of 32 features] uint8: 127 + the exponent of the block's power of two, 255 for a block that is not finite.
+    Their contents may be written, the tensors not be replaced."""
+    __slots__ = ("_values", "_scales", "_features", "_kind", "_c")
+    values, scales, features, kind = (property(operator.attrgetter(name)) for name in __slots__[:4])
 
     def __init__(self, values, scales, features: int):
         kind = {torch.int8: I8, torch.float8_e4m3fn: E4M3}.get(values.dtype)
@@ -676,7 +679,7 @@ class PackedRows:
             _refuse("values: a contiguous matrix of %d columns on a GPU is wanted" % (32 * blocks))
         if scales.dtype != torch.uint8 or scales.shape != (values.shape[0], blocks) or not scales.is_contiguous() or scales.device != values.device:
             _refuse("scales: [%d, %d] uint8 on %s are wanted, contiguous" % (values.shape[0], blocks, values.device))
-        self.values, self.scales, self.features, self.kind = values, scales, features, kind
+        self._values, self._scales, self._features, self._kind = values, scales, features, kind
         self._c = _Packed(values.data_ptr(), scales.data_ptr(), kind)
 
     @classmethod
@@ -687,19 +690,19 @@ class PackedRows:
             _refuse("%d rows of %d features in 8 bits" % (rows, features))
         blocks = (features + 31) // 32
         self = cls.__new__(cls)            # (nothing to check)
-        self.values = _new((rows, 32 * blocks), torch.int8 if kind == I8 else torch.float8_e4m3fn, device)
-        self.scales = _new((rows, blocks), torch.uint8, device)
-        self.features, self.kind = features, kind
-        self._c = _Packed(self.values.data_ptr(), self.scales.data_ptr(), kind)
+        self._values = _new((rows, 32 * blocks), torch.int8 if kind == I8 else torch.float8_e4m3fn, device)
+        self._scales = _new((rows, blocks), torch.uint8, device)
+        self._features, self._kind = features, kind
+        self._c = _Packed(self._values.data_ptr(), self._scales.data_ptr(), kind)
         return self
 
     @property
     def rows(self) -> int:
-        return self.values.shape[0]
+        return self._values.shape[0]
 
     @property
     def device(self):
-        return self.values.device
+        return self._values.device
 
 
 def _here(device, stream):
@@ -731,7 +734,7 @@ def _packed_out(name, given, rows, features, device):
     """PackedRows, given or a kind to allocate them in."""
     if not isinstance(given, PackedRows):
         return PackedRows.empty(rows, features, given, device)
-    if given.values.shape[0] != rows or given.features != features or given.values.device != device:
+    if given._values.shape[0] != rows or given._features != features or given._values.device != device:
         _refuse("%s: %d rows of %d features in 8 bits on %s are wanted" % (name, rows, features, device))
     return given
 
@@ -897,6 +900,8 @@ def _beams(totals, done, device):
 
 def _beam_outputs(out, sequences, width, device):
     """What a selection writes: given as (totals, parents, classes, done), or allocated."""
+    if not 0 < width < 1 << 16:
+        _refuse("width = %r" % (width,))
     if out is None:
         shape = (sequences, width)
         return (_new(shape, torch.float32, device), _new(shape, torch.int32, device), _new(shape, torch.int32, device), _new(shape, torch.bool, device))

@@ -180,6 +180,29 @@ def test_few_candidates():
     assert all(t.shape == (0, 4) for t in none)
 
 
+def test_binding_refusals():
+    scores, totals = torch.zeros((6, 50), device="cuda"), torch.zeros((2, 3), device="cuda")
+    done, cache = torch.zeros((2, 3), dtype=torch.bool, device="cuda"), torch.zeros((6, 4), device="cuda")
+    states = mpcnn.BeamStates([cache], 2, 3)
+    good = mpcnn.beam_select(scores, totals, done=done, end=0)
+    x, w = torch.zeros((6, 8), device="cuda"), torch.zeros((50, 8), device="cuda")
+    calls = [(lambda width=width: mpcnn.beam_select(scores, totals, width)) for width in (0, -1, 65, 1 << 40)] + [
+        lambda: mpcnn.beam_select(scores, totals, done=done), lambda: mpcnn.beam_select(scores, totals, done=done, end=50), lambda: mpcnn.beam_select(scores, totals.double()),
+        lambda: mpcnn.beam_select(scores, totals.t()), lambda: mpcnn.beam_select(scores, totals.view(3, 2), done=done, end=0), lambda: mpcnn.beam_select(scores[:5], totals),
+        lambda: mpcnn.beam_select(scores.half(), totals), lambda: mpcnn.beam_select(scores.t().contiguous().t(), totals), lambda: mpcnn.beam_select(scores, totals, bias=scores[0, :49]),
+        lambda: mpcnn.beam_select(scores, totals, done=done.int(), end=0), lambda: mpcnn.beam_select(scores, totals.cpu()), lambda: mpcnn.beam_select(scores, totals, width=2, out=good),
+        lambda: mpcnn.beam_select(scores, totals, out=(totals,) + good[1:]), lambda: mpcnn.beam_select(scores, totals, out=(good[0], good[1], good[1], good[3])),
+        lambda: mpcnn.beam_select(scores, totals, ws=torch.empty(64, dtype=torch.uint8, device="cuda")), lambda: mpcnn.class_beam(x, w[:, :7], totals),
+        lambda: mpcnn.class_beam(x, w.bfloat16(), totals), lambda: mpcnn.class_beam(x, w, totals, width=0), lambda: mpcnn.class_beam(x[:4], w, totals),
+        lambda: mpcnn.BeamStates([cache[:5]], 2, 3), lambda: mpcnn.BeamStates([cache.t().contiguous().t()], 2, 3), lambda: mpcnn.BeamStates([cache], 2, 3, axis=2),
+        lambda: mpcnn.BeamStates([cache, cache], 2, 3), lambda: states.reorder(good[1].long()), lambda: states.reorder(good[1][:1]), lambda: states.reorder(good[1], length=-1),
+        lambda: states.reorder(cache.view(torch.int32)[:2, :3].contiguous().t())]
+    for k, call in enumerate(calls):
+        with pytest.raises(mpcnn.MpcnnError):
+            call()
+            pytest.fail("call %d was not refused" % k)
+
+
 def test_far_classes_and_far_rows():
     """A class beyond 2^24 and rows beyond 2^32 bytes."""
     v = 40000001

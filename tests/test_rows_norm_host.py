@@ -96,3 +96,11 @@ def test_binding_refuses_what_is_on_the_host():
                  lambda: mpcnn.PackedRows.empty(3, 40, True, "cpu")):
         with pytest.raises(mpcnn.MpcnnError):
             call()
+
+
+def test_packed_rows_keep_their_tensors():
+    p = mpcnn.PackedRows.empty(3, 40, mpcnn.E4M3, "cpu")
+    assert (p.rows, p.features, p.kind, p.device.type) == (3, 40, mpcnn.E4M3, "cpu") and p.values.shape == (3, 64) and p.scales.shape == (3, 2)
+    for name in ("values", "scales", "features", "kind", "rows", "device"):
+        with pytest.raises(AttributeError):
+            setattr(p, name, getattr(p, name))
