@@ -26,30 +26,27 @@ struct mpcnn_beam_states {
 namespace {
 
 constexpr int64_t kMaxRows = 1 << 20, kMaxClasses = 0x7fffffff - 1024, kMostPitch = (int64_t)1 << 40;
-constexpr int64_t kMostScores = (int64_t)1 << 34;      // of a class layer, kept: 2^22 workgroups of four rows' steps
+constexpr int64_t kMostScores = (int64_t)1 << 34;      // of a class layer, kept (64 GB)
 constexpr int kCUs = 256;
 
 struct Plan { int64_t rows, chunks, steps, parts, part_steps; size_t stats, tops, total; };
 
-// columns: the scores are a class layer's, [class][row], and every step of a row a workgroup's
+// columns: the scores are a class layer's, [class][row], which has left what the first launch would
 bool make_plan(int64_t sequences, int64_t beams, int64_t classes, Plan* p, bool columns = false)
 {
     if (sequences < 0 || beams < 1 || beams > mpcnn::kMaxBeams || sequences > kMaxRows / beams || classes < 1 || classes > kMaxClasses) return false;
     *p = Plan{};
     p->rows = sequences * beams;
     p->chunks = (classes + mpcnn::kChunk - 1) / mpcnn::kChunk;
+    if (columns) return p->rows * classes <= kMostScores;
     p->steps = (classes + mpcnn::kStep - 1) / mpcnn::kStep;
     // eight workgroups a compute unit, each wave of which has a step at least
     const int64_t wanted = std::max<int64_t>(1, 8 * kCUs / std::max<int64_t>(1, p->rows));
     p->part_steps = std::max<int64_t>(4, (p->steps + wanted - 1) / wanted);
-    if (columns) {
-        if (sequences * beams * classes > kMostScores) return false;
-        p->part_steps = 1;
-    }
     p->parts = (p->steps + p->part_steps - 1) / p->part_steps;
     auto up = [](int64_t n) { return (size_t)((n + 255) / 256 * 256); };
     p->stats = 0;
-    p->tops = up(columns ? 8 * p->rows * p->steps : 8 * (p->rows + 8 * kCUs));       // (parts are at most 8 kCUs / rows + 1)
+    p->tops = up(8 * (p->rows + 8 * kCUs));       // (parts are at most 8 kCUs / rows + 1)
     p->total = p->tops + up(4 * p->rows * p->chunks);
     return true;
 }
@@ -114,7 +111,7 @@ mpcnn::BeamArgs args_of(const Plan& p, const Call& c, const void* scores, int64_
     a.scores = scores; a.pitch = pitch; a.totals = c.totals; a.done = c.done; a.end = (int)c.end;
     a.sequences = (int)c.sequences; a.beams = (int)c.beams; a.width = (int)c.width;
     a.V = (int)c.classes; a.chunks = (int)p.chunks; a.steps = (int)p.steps; a.parts = (int)p.parts; a.part_steps = (int)p.part_steps;
-    a.stats = (float2*)(ws + p.stats); a.tops = (float*)(ws + p.tops);
+    a.stats = (float2*)(ws + p.stats); a.stat_pitch = p.parts; a.tops = (float*)(ws + p.tops);
     a.totals_out = c.totals_out; a.parents = c.parents; a.classes = c.classes_out; a.done_out = c.done_out;
     return a;
 }
@@ -219,8 +216,7 @@ size_t mpcnn_workspace_bytes_class_beam(int64_t sequences, int64_t beams, int64_
 {
     Plan p;
     if ((dtype != MPCNN_F32 && dtype != MPCNN_BF16) || !make_plan(sequences, beams, classes, &p, true)) return 0;
-    const size_t scores = mpcnn::class_scores_bytes(scores_of(nullptr, 0, nullptr, 0, nullptr, p.rows, features, classes, dtype));
-    return scores ? p.total + scores : 0;
+    return mpcnn::class_scores_bytes(scores_of(nullptr, 0, nullptr, 0, nullptr, p.rows, features, classes, dtype));
 }
 
 mpcnn_status mpcnn_class_beam(const void* x_dev, int64_t x_pitch, const void* w_dev, int64_t w_pitch, const float* bias_dev, const float* totals_dev,
@@ -239,9 +235,8 @@ mpcnn_status mpcnn_class_beam(const void* x_dev, int64_t x_pitch, const void* w_
     const int64_t size = dtype == MPCNN_F32 ? 4 : 2;
     if (((uintptr_t)x_dev | (uintptr_t)w_dev) % size) return fail(MPCNN_EINVAL, "an address is no multiple of its element's size");
     const mpcnn::ClassScores s = scores_of(x_dev, x_pitch, w_dev, w_pitch, bias_dev, p.rows, features, classes, dtype);
-    const size_t scores_bytes = mpcnn::class_scores_bytes(s);
-    if (!scores_bytes) return fail(MPCNN_EUNSUPPORTED, "%lld rows, %lld features, %lld classes", (long long)p.rows, (long long)features, (long long)classes);
-    const size_t need = p.total + scores_bytes;
+    const size_t need = mpcnn::class_scores_bytes(s);
+    if (!need) return fail(MPCNN_EUNSUPPORTED, "%lld rows, %lld features, %lld classes", (long long)p.rows, (long long)features, (long long)classes);
     TRY(apart(c, mpcnn::rows_span(x_dev, p.rows, features, x_pitch, size), ws_dev, ws_bytes, need));
     const Span w = mpcnn::rows_span(w_dev, classes, features, w_pitch, size);
     for (const Span& o : {Span{(uintptr_t)ws_dev, need}, Span{(uintptr_t)totals_out_dev, 4 * (uint64_t)(sequences * width)}, Span{(uintptr_t)parents_dev, 4 * (uint64_t)(sequences * width)},
@@ -249,12 +244,18 @@ mpcnn_status mpcnn_class_beam(const void* x_dev, int64_t x_pitch, const void* w_
         if (meet(o, w)) return fail(MPCNN_EINVAL, "an output or the workspace overlaps an input");
     if (!sequences) return MPCNN_OK;
     const hipStream_t st = (hipStream_t)hip_stream;
-    float* scores = nullptr;
-    int64_t pitch = 0;
-    TRY(mpcnn::class_scores(s, (char*)ws_dev + p.total, &scores, &pitch, st));
-    const mpcnn::BeamArgs a = args_of(p, c, scores, pitch, (char*)ws_dev);
-    mpcnn::beam_columns_kernel<<<(unsigned)(p.steps * ((p.rows + 3) / 4)), 256, 0, st>>>(a);
-    mpcnn::beam_pick_kernel<mpcnn::BeamColumn><<<(unsigned)sequences, mpcnn::kPickThreads, mpcnn::pick_bytes((int)c.width), st>>>(a);
+    mpcnn::KeptScores kept{};
+    TRY(mpcnn::class_scores(s, (char*)ws_dev, &kept, st));
+    mpcnn::BeamArgs a = args_of(p, c, kept.scores, kept.row, (char*)ws_dev);
+    a.parts = (int)kept.tiles; a.stats = kept.stats; a.stat_pitch = kept.stat_pitch; a.tops = nullptr;
+    const unsigned groups = (unsigned)sequences;
+    const size_t lds = mpcnn::pick_bytes((int)width);
+    switch (mpcnn::kChunk / kept.tile) {
+        case 1: mpcnn::beam_pick_kernel<mpcnn::BeamColumn<1>><<<groups, mpcnn::kPickThreads, lds, st>>>(a); break;
+        case 2: mpcnn::beam_pick_kernel<mpcnn::BeamColumn<2>><<<groups, mpcnn::kPickThreads, lds, st>>>(a); break;
+        case 4: mpcnn::beam_pick_kernel<mpcnn::BeamColumn<4>><<<groups, mpcnn::kPickThreads, lds, st>>>(a); break;
+        default: mpcnn::beam_pick_kernel<mpcnn::BeamColumn<8>><<<groups, mpcnn::kPickThreads, lds, st>>>(a); break;
+    }
     HIP_TRY(hipGetLastError());
     return MPCNN_OK;
 }

@@ -343,27 +343,29 @@ mpcnn::FewArgs few_args(const Plan& p, const mpcnn::DirectArgs& a)
     mpcnn::FewArgs few{};
     few.x = a.x; few.w = a.w; few.x_pitch = a.x_pitch; few.w_pitch = a.w_pitch;
     few.N = a.N; few.D = a.D; few.V = p.V; few.score_row = a.score_row;
-    few.bias = a.bias; few.mask = a.mask; few.scores = a.scores; few.stats = a.stats; few.label_score = a.label_score;
+    few.bias = a.bias; few.mask = a.mask; few.scores = a.scores; few.stats = a.stats; few.stat_pitch = a.stat_pitch; few.label_score = a.label_score;
     return few;
 }
-// The scores of little work, or their statistics alone (a.scores null); notes how many tiles of classes these have
+// The scores of little work, or their statistics alone (a.scores null); notes how many tiles of classes these have, and of how many classes
 template <typename T>
-mpcnn_status direct_scores(const Plan& p, mpcnn::DirectArgs& a, char* x_split, hipStream_t st)
+mpcnn_status direct_scores(const Plan& p, mpcnn::DirectArgs& a, char* x_split, int64_t* tile, hipStream_t st)
 {
     const bool blocks = sizeof(T) == 2 && p.V * p.D >= kBlockWeights && direct_operand<T>(a.x, a.x_pitch, p.D) && direct_operand<T>(a.w, a.w_pitch, p.D);
     if (p.few_scores && !(blocks && p.N > 2)) {
         mpcnn::FewArgs few = few_args(p, a);
-        few.each = p.score_each;
+        few.each = *tile = p.score_each;
         mpcnn::launch_rows_few_scores<T>(few, (unsigned)p.score_v, st);
     } else if (blocks) {
         mpcnn::ProductArgs b{};
         b.A = (const char*)a.w; b.a_row = a.w_pitch * 2; b.B = (const char*)a.x; b.b_row = a.x_pitch * 2;
         b.M = a.V; b.N = p.N; b.blocks = p.D * 2 / mpcnn::kBlockBytes;
-        b.bias = a.bias; b.labels = a.mask.labels; b.stats = a.stats; b.label_score = a.label_score; b.scores = a.scores; b.score_row = a.score_row;
+        b.bias = a.bias; b.labels = a.mask.labels; b.stats = a.stats; b.stat_pitch = a.stat_pitch; b.label_score = a.label_score; b.scores = a.scores; b.score_row = a.score_row;
         const Tiling t = tiling_of(p.V, p.N, b.blocks, 1, false);
         a.tiles = t.tiles_m;
+        *tile = t.big ? 256 : 128;
         return launch_product<false, mpcnn::kScores>(b, t, st);
     } else if (sizeof(T) == 4 && p.wide) {
+        *tile = 32;
         mpcnn::SplitArgs s{};
         s.x = (const float*)a.x; s.x_pitch = a.x_pitch; s.N = p.N; s.D = p.D; s.out = x_split;
         s.tiles = p.N <= 32 ? 1 : (int)(up_to(p.N, 64) / 32);
@@ -373,6 +375,7 @@ mpcnn_status direct_scores(const Plan& p, mpcnn::DirectArgs& a, char* x_split, h
         if (s.tiles == 1) mpcnn::rows_wide_scores_kernel<1><<<(unsigned)p.score_v, 256, 0, st>>>(a);
         else mpcnn::rows_wide_scores_kernel<2><<<(unsigned)(p.score_v * (s.tiles / 2)), 256, 0, st>>>(a);
     } else {
+        *tile = p.score_deal == 4 ? 32 : 64;
         const dim3 grid((unsigned)p.score_v, (unsigned)p.score_n);
         // rows of bf16 that begin between words (one row has no pitch)
         const bool odd = sizeof(T) == 2 && (((uintptr_t)a.x | (uintptr_t)a.w | 2 * (uint64_t)(p.N > 1 ? a.x_pitch : 0) | 2 * (uint64_t)(p.V > 1 ? a.w_pitch : 0)) & 2);
@@ -392,7 +395,8 @@ mpcnn_status run_direct(const Plan& p, const Call& c, char* ws, hipStream_t st)
     a.stats = (float2*)(ws + p.stats); a.label_score = (float*)(ws + p.label_score);
     a.score_row = p.Np; a.score_deal = p.score_deal; a.tiles = p.score_v;
     if (p.train) a.scores = (float*)(ws + p.score);
-    const mpcnn_status rc = direct_scores<T>(p, a, p.wide ? ws + p.x_split : nullptr, st);
+    int64_t tile = 0;
+    const mpcnn_status rc = direct_scores<T>(p, a, p.wide ? ws + p.x_split : nullptr, &tile, st);
     if (rc != MPCNN_OK) return rc;
     // statistics joined with the derivative where there are few tiles of classes, by a launch of their own otherwise
     const bool joined = a.tiles > mpcnn::kDeltaFewTiles || p.few;
@@ -664,7 +668,7 @@ constexpr int64_t kMostKept = (int64_t)1 << 27;
 static_assert(kMostKept / 32 * 2 < kMostGroups && kMaxRows / 32 <= kMostSide, "a launch has them");
 
 // What class_scores needs, and where: each grows with the rows
-struct ScoresRoom { int64_t row; size_t scores, stats, x_split, total; };
+struct ScoresRoom { int64_t row, tiles; size_t scores, stats, x_split, total; };
 bool scores_room(const mpcnn::ClassScores& c, ScoresRoom* r)
 {
     if (c.rows < 0 || c.rows > kMaxRows || c.features < 1 || c.features > kMaxFeatures || c.classes < 1 || c.classes > kMaxClasses) return false;
@@ -673,7 +677,8 @@ bool scores_room(const mpcnn::ClassScores& c, ScoresRoom* r)
     auto take = [&](int64_t bytes) { const size_t o = at; at += (size_t)up_to(bytes, 256); return o; };
     r->row = up_to(c.rows, 4);
     r->scores = take(4 * c.classes * r->row);
-    r->stats = take(8 * ((c.classes + 31) / 32) * c.rows);
+    r->tiles = up_to((c.classes + 31) / 32, 8);
+    r->stats = take(8 * r->tiles * c.rows);
     r->x_split = take(c.dtype == MPCNN_F32 ? x_split_bytes(std::min(c.rows, kWideRows), c.features) : 0);
     r->total = at + 256;                                       // (no rows: not nothing)
     return true;
@@ -689,7 +694,7 @@ size_t class_scores_bytes(const ClassScores& c)
     return scores_room(c, &r) ? r.total : 0;
 }
 
-mpcnn_status class_scores(const ClassScores& c, char* ws, float** scores, int64_t* row, hipStream_t st)
+mpcnn_status class_scores(const ClassScores& c, char* ws, KeptScores* kept, hipStream_t st)
 {
     ScoresRoom r;
     if (!scores_room(c, &r)) return fail(MPCNN_EUNSUPPORTED, "%lld rows, %lld features, %lld classes", (long long)c.rows, (long long)c.features, (long long)c.classes);
@@ -699,12 +704,18 @@ mpcnn_status class_scores(const ClassScores& c, char* ws, float** scores, int64_
     p.wide = wide_scores(p.halves, c.rows, c.features, c.classes);
     p.few_scores = few_scores(p.halves, c.rows, c.features, c.classes);
     plan_scores(&p, c.rows, c.features, c.classes);
+    if (p.few_scores) {                    // (at most 256 classes a workgroup here: one tile)
+        p.score_each = p.score_each > 128 ? 256 : p.score_each;
+        p.score_v = (int)((c.classes + p.score_each - 1) / p.score_each);
+    }
     DirectArgs a{};
     a.x = c.x; a.w = c.w; a.x_pitch = c.x_pitch; a.w_pitch = c.w_pitch;
     a.N = p.N; a.D = p.D; a.V = (int)p.V; a.bias = c.bias;
-    a.stats = (float2*)(ws + r.stats); a.scores = (float*)(ws + r.scores); a.score_row = r.row; a.score_deal = p.score_deal; a.tiles = p.score_v;
-    *scores = a.scores; *row = r.row;
-    return c.dtype == MPCNN_F32 ? direct_scores<float>(p, a, ws + r.x_split, st) : direct_scores<bf16>(p, a, nullptr, st);
+    a.stats = (float2*)(ws + r.stats); a.stat_pitch = r.tiles; a.scores = (float*)(ws + r.scores); a.score_row = r.row; a.score_deal = p.score_deal; a.tiles = p.score_v;
+    int64_t tile = 0;
+    const mpcnn_status rc = c.dtype == MPCNN_F32 ? direct_scores<float>(p, a, ws + r.x_split, &tile, st) : direct_scores<bf16>(p, a, nullptr, &tile, st);
+    *kept = KeptScores{a.scores, r.row, a.stats, r.tiles, tile, a.tiles};
+    return rc;
 }
 
 }  // namespace mpcnn

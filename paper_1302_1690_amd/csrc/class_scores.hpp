@@ -14,7 +14,14 @@ struct ClassScores {
     int dtype;
 };
 size_t class_scores_bytes(const ClassScores& c);         // of the workspace; it grows with the rows.  0: bad or too large
-// The scores with their bias, fp32 [classes][*row], in the workspace
-mpcnn_status class_scores(const ClassScores& c, char* ws, float** scores, int64_t* row, hipStream_t st);
+// In the workspace: the scores with their bias, fp32 [classes][row], and the largest and the sum of exp(score - largest) of each tile of so many classes
+// (32, 64, 128 or 256), [rows][stat_pitch]
+struct KeptScores {
+    float* scores;
+    int64_t row;
+    float2* stats;
+    int64_t stat_pitch, tile, tiles;
+};
+mpcnn_status class_scores(const ClassScores& c, char* ws, KeptScores* kept, hipStream_t st);
 
 }  // namespace mpcnn

@@ -12,6 +12,8 @@
 //
 // 64 sequences x 8 beams x 50021 bf16 with biases: the pass 14 us (3.7 TB/s; bound by the vector instructions: some 14 issue slots a class), the pick 9 (1 sequence x 4 beams x 32000: 6.5), a chain of
 // trips to memory and LDS; chunks of 1024 instead of 256 and the best one after the other by the wave: 19 and 20 us, and 85 for 12 x 6 beams x 1573 with 16 wanted (15).
+// From rows of features the first launch is the class layer's, which leaves its tiles' largest and sums beside the scores (a launch that read the scores again: 64 x 8 beams x 50021 from 4096 bf16 359 us a call,
+// now 259; 128 x 4 x 50000 from 1024 200, now 86; 1 x 4 x 32000 from 1024 25.8, now 25.2).
 // States: 16 x 8 beams, 16 tensors of [8][1000 of 1024][128] bf16: 1.20 ms, 5.2 TB/s.
 #pragma once
 #include <type_traits>
@@ -33,8 +35,9 @@ struct BeamArgs {
     const unsigned char* done;             // null: none
     int end;
     int sequences, beams, width;
-    int V, chunks, steps, parts, part_steps;   // chunks and steps of a row, workgroups of a row, steps of a workgroup
-    float2* stats;                         // [rows][parts]
+    int V, chunks, steps, parts, part_steps;   // chunks and steps of a row, workgroups of a row (BeamColumn: tiles), steps of a workgroup
+    float2* stats;                         // [rows][stat_pitch]
+    long stat_pitch;
     float* tops;                           // [rows][chunks]
     float* totals_out;
     int *parents, *classes;
@@ -106,24 +109,45 @@ struct BeamRow {
         const float b = bias && at < V ? bias[at] : 0.f;
         return at < V && b != -__builtin_inff() ? load1(from + at) + b : -__builtin_inff();
     }
+    static constexpr int kParts = 1;       // so many a lane at once
+    // the first launch's: of a part of a row's classes, and the largest of chunk i of the chunks of all of a sequence's beams
+    __device__ static float2 stat(const BeamArgs& a, long row, int part) { return a.stats[row * a.stat_pitch + part]; }
+    __device__ static float top(const BeamArgs& a, long row0, int i) { return a.tops[row0 * a.chunks + i]; }
+    // a part's sum, of exponentials below the largest of all parts, in 64 bits
+    __device__ static double share(const float2& s, float top) { return s.x > -__builtin_inff() || s.y != 0.f ? (double)s.y * exp((double)s.x - (double)top) : 0.0; }
 };
 
-// Scores that lie [class][row], fp32, as a class layer leaves them, with their bias
+// exp(x - top) for x <= top; 0 for minus infinity
+__device__ __forceinline__ float exp_below(float x, float top) { return __builtin_amdgcn_exp2f((x - top) * 1.4426950408889634f); }
+
+// Scores that lie [class][row], fp32, as a class layer leaves them, with their bias, and what it leaves of its tiles of classes, PER of which are a chunk
+template <int PER>
 struct BeamColumn {
+    static constexpr int kParts = 8;
     const float* from;
     long pitch;
     int V;
     __device__ BeamColumn(const BeamArgs& a, long row) : from((const float*)a.scores + row), pitch(a.pitch), V(a.V) {}
     __device__ float one(int at) const { return at < V ? from[at * pitch] : -__builtin_inff(); }
+    __device__ static float2 stat(const BeamArgs& a, long row, int part) { return a.stats[row * a.stat_pitch + part]; }
+    __device__ static float top(const BeamArgs& a, long row0, int i)
+    {
+        const int k = i / a.chunks, first = PER * (i - k * a.chunks);
+        float t[PER];
+#pragma unroll
+        for (int q = 0; q < PER; ++q) t[q] = stat(a, row0 + k, first + q < a.parts ? first + q : a.parts - 1).x;      // (the last chunk's, again)
+#pragma unroll
+        for (int q = 1; q < PER; ++q) t[0] = fmaxf(t[0], t[q]);
+        return t[0];
+    }
+    // (there are many: in 32 bits)
+    __device__ static double share(const float2& s, float top) { return (double)(s.y * exp_below(s.x, top == -__builtin_inff() ? 0.f : top)); }
 };
 
 __device__ __forceinline__ bool beam_goes_on(const BeamArgs& a, long row)
 {
     return fabsf(a.totals[row]) < __builtin_inff() && !(a.done && a.done[row]);     // (a NaN does not)
 }
-
-// exp(x - top) for x <= top; 0 for minus infinity
-__device__ __forceinline__ float exp_below(float x, float top) { return __builtin_amdgcn_exp2f((x - top) * 1.4426950408889634f); }
 
 // Largest and sum of exponentials of two lots of classes together
 __device__ __forceinline__ float2 joined(const float2& p, const float2& q)
@@ -185,38 +209,8 @@ __global__ __launch_bounds__(256) void beam_stats_kernel(BeamArgs a)
         float2 all = red[0];
 #pragma unroll
         for (int w = 1; w < 4; ++w) all = joined(all, red[w]);
-        a.stats[row * a.parts + part] = all;
+        a.stats[row * a.stat_pitch + part] = all;
     }
-}
-
-// Scores [class][row]: a workgroup has a step of the classes of four rows, a wave a chunk
-__global__ __launch_bounds__(256) void beam_columns_kernel(BeamArgs a)
-{
-    __shared__ float2 red[4][4];
-    const int step = (int)(blockIdx.x % a.steps), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunk = kStep / kChunk * step + wave;
-    const long row0 = 4 * (long)(blockIdx.x / a.steps), rows = (long)a.sequences * a.beams;
-    v4f s[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int at = kChunk * chunk + 64 * i + lane;
-        s[i] = at < a.V ? *reinterpret_cast<const v4f*>((const float*)a.scores + at * a.pitch + row0) : v4f(-__builtin_inff());
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float top = largest64(fmaxf(fmaxf(s[0][r], s[1][r]), fmaxf(s[2][r], s[3][r]))), base = top == -__builtin_inff() ? 0.f : top;
-        const float sum = sum64((exp_below(s[0][r], base) + exp_below(s[1][r], base)) + (exp_below(s[2][r], base) + exp_below(s[3][r], base)));
-        if (lane == 0) {
-            red[wave][r] = float2{top, sum};
-            if (row0 + r < rows && chunk < a.chunks) a.tops[(row0 + r) * a.chunks + chunk] = top;
-        }
-    }
-    __syncthreads();
-    const int r = threadIdx.x;
-    if (r >= 4 || row0 + r >= rows) return;
-    float2 all = red[0][r];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) all = joined(all, red[w][r]);
-    a.stats[(row0 + r) * a.parts + step] = all;
 }
 
 // ---- the second launch
@@ -289,7 +283,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a)
 #pragma unroll
         for (int r = 0; r < kEach; ++r) {
             const int i = base + kPickThreads * r + tid;
-            tops[r] = i < all ? a.tops[row0 * a.chunks + i] : 0.f;     // (of a beam that does not go on: whatever is there)
+            tops[r] = i < all ? Row::top(a, row0, i) : 0.f;     // (of a beam that does not go on: whatever is there)
         }
     };
     fetch(0);
@@ -299,18 +293,25 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a)
         const long row = row0 + k;
         const float t = a.totals[row];
         const bool over = a.done && a.done[row];
-        const float2* const stats = a.stats + row * a.parts;
-        constexpr float2 kNone{-__builtin_inff(), 0.f};
-        const float2 mine = lane < a.parts ? stats[lane] : kNone;      // (used if it goes on)
+        float2 mine[Row::kParts];                        // (used if it goes on)
+        constexpr int kBeside = 64 * Row::kParts;
+        auto part = [&](int p) { return p < a.parts ? Row::stat(a, row, p) : float2{-__builtin_inff(), 0.f}; };
+#pragma unroll
+        for (int q = 0; q < Row::kParts; ++q) mine[q] = part(64 * q + lane);
         int is = fabsf(t) < __builtin_inff() ? (over ? 2 : 1) : 0;
         double l = 0.0;
         if (is == 1) {
-            float top = mine.x;
-            for (int p = lane + 64; p < a.parts; p += 64) top = fmaxf(top, stats[p].x);
+            float top = mine[0].x;
+#pragma unroll
+            for (int q = 1; q < Row::kParts; ++q) top = fmaxf(top, mine[q].x);
+#pragma unroll 4
+            for (int p = kBeside + lane; p < a.parts; p += 64) top = fmaxf(top, Row::stat(a, row, p).x);
             top = largest64(top);
-            auto share = [&](const float2& s) { return s.x > -__builtin_inff() || s.y != 0.f ? (double)s.y * exp((double)s.x - (double)top) : 0.0; };
-            double sum = share(mine);
-            for (int p = lane + 64; p < a.parts; p += 64) sum += share(stats[p]);
+            double sum = 0.0;
+#pragma unroll
+            for (int q = 0; q < Row::kParts; ++q) sum += Row::share(mine[q], top);
+#pragma unroll 4
+            for (int p = kBeside + lane; p < a.parts; p += 64) sum += Row::share(Row::stat(a, row, p), top);
 #pragma unroll
             for (int i = 1; i < 64; i *= 2) sum += __shfl_xor(sum, i, 64);
             l = (double)top + log(sum);

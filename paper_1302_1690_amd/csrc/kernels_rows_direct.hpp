@@ -32,7 +32,8 @@ struct DirectArgs {
     RowMask mask;
     float* scores;                         // [V][score_row], or null
     long score_row;
-    float2* stats;                         // [tiles of classes][N]
+    float2* stats;                         // [tiles of classes][N], or [N][stat_pitch] where that is not 0
+    long stat_pitch;
     float* label_score;
     const char* x_split;                   // features as operands (rows_split_kernel)
     int x_tiles;                           // of 32 rows, a multiple of the kernel's
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(256) void rows_direct_scores_kernel(DirectArgs a)
             float2 t = red[0][tid];
 #pragma unroll
             for (int q = 1; q < 8; ++q) t = direct_join(t, red[q][tid]);
-            a.stats[(long)blockIdx.x * a.N + n0 + tid] = t;
+            a.stats[stat_place(blockIdx.x, n0 + tid, a.N, a.stat_pitch)] = t;
         }
         return;
     }
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(256) void rows_direct_scores_kernel(DirectArgs a)
     if (half == 0) red[wave >> 1][32 * (wave & 1) + row] = float2{top, sum};
     __syncthreads();
     const int nt = blockIdx.y * 64 + tid;
-    if (tid < 64 && nt < a.N) a.stats[(long)blockIdx.x * a.N + nt] = direct_join(red[0][tid], red[1][tid]);
+    if (tid < 64 && nt < a.N) a.stats[stat_place(blockIdx.x, nt, a.N, a.stat_pitch)] = direct_join(red[0][tid], red[1][tid]);
 }
 
 // ---- fp32 scores of some tens of rows over many classes: bound by the pass over the class weights, which a wave takes from memory into its operands
@@ -321,7 +322,7 @@ __global__ __launch_bounds__(256) void rows_wide_scores_kernel(DirectArgs a)
             float2 t = red[0][tid];
 #pragma unroll
             for (int q = 1; q < 8; ++q) t = direct_join(t, red[q][tid]);
-            a.stats[(long)vt * a.N + n0 + tid] = t;
+            a.stats[stat_place(vt, n0 + tid, a.N, a.stat_pitch)] = t;
         }
         __syncthreads();
     }

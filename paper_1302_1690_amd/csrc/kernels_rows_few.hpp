@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kFewThreads) void rows_few_scores_kernel(FewArgs a)
             s = s * __expf(t - base) + os * __expf(ot - base);
             t = m;
         }
-        if (lane == 0) a.stats[(long)blockIdx.x * a.N + n] = float2{t, s};
+        if (lane == 0) a.stats[stat_place(blockIdx.x, n, a.N, a.stat_pitch)] = float2{t, s};
     }
 }
 

@@ -54,7 +54,8 @@ struct ProductArgs {
     // scores
     const float* bias;                     // [M] or null
     const int* labels;                     // [N], or null: no label's score is asked for
-    float2* stats;                         // [tiles_m][N]: largest, sum of exp(score - largest)
+    float2* stats;                         // [tiles_m][N], or [N][stat_pitch] where that is not 0: largest, sum of exp(score - largest)
+    long stat_pitch;
     float* label_score;                    // [N]
     float* scores;                         // [M][score_row], or null
     long score_row;
@@ -387,7 +388,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void rows_product_kernel(ProductAr
                 const float top = fmaxf(s.x, o.x), base = top == kNone ? 0.f : top;
                 s = float2{top, s.y * __builtin_amdgcn_exp2f((s.x - base) * kLog2e) + o.y * __builtin_amdgcn_exp2f((o.x - base) * kLog2e)};
             }
-            a.stats[(long)tm * a.N + n0 + i] = s;
+            a.stats[stat_place(tm, n0 + i, a.N, a.stat_pitch)] = s;
         }
     } else if constexpr (RESULT == kDelta) {
         // By way of LDS as below: a lane has 8 rows of a class

@@ -17,7 +17,8 @@ struct FewArgs {
     const float* bias;
     RowMask mask;
     float* scores;                               // [V][score_row], or null
-    float2* stats;                               // [workgroups][N]
+    float2* stats;                               // [workgroups][N], or [N][stat_pitch] where that is not 0
+    long stat_pitch;
     float* label_score;
     long each;                                   // classes of a workgroup
     // gradients

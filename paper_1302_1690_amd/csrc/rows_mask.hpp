@@ -31,4 +31,7 @@ __device__ __forceinline__ float class_delta(float score, float lse, bool live, 
 
 constexpr int kNoLabel = -1;               // in the place of the label of a row that adds nothing
 
+// Where the statistics of a tile of classes lie for row n: [tiles][N], or [N][pitch] where that is not 0
+__device__ __forceinline__ long stat_place(long tile, long n, long N, long pitch) { return pitch ? n * pitch + tile : tile * N + n; }
+
 }  // namespace mpcnn

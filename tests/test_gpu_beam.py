@@ -48,7 +48,7 @@ def values_in_64(scores, totals, bias, done, end):
     return torch.where(torch.isfinite(totals)[:, :, None], value, -INF)
 
 
-def check(got, scores, totals, width, bias=None, done=None, end=-1):
+def check(got, scores, totals, width, bias=None, done=None, end=-1, more=0.0):
     b, k = totals.shape
     value = values_in_64(scores, totals, bias, done, end)
     v = value.shape[2]
@@ -58,7 +58,7 @@ def check(got, scores, totals, width, bias=None, done=None, end=-1):
     if want.shape[1] < width + 1:
         fill = width + 1 - want.shape[1]
         want, at = torch.nn.functional.pad(want, (0, fill), value=-INF), torch.nn.functional.pad(at, (0, fill))
-    off = 2 * _off(v, b * k)
+    off = 2 * (_off(v, b * k) + more)
     gaps = want[:, :-1] - want[:, 1:]
     beams = at // v
     close = (gaps < off) & (beams[:, :-1] != beams[:, 1:]) & (want[:, 1:] > -INF) & (gaps > 0)
@@ -221,6 +221,11 @@ def test_far_classes_and_far_rows():
 
 # ---- from rows of features
 
+# The class layer adds at most 64 exponentials one after the other in a lane where `_off` counts 16 of a wave's chunk (48 u more), and the tiles' sums are joined by one more
+# exponential (3 u of its argument, its two half steps and two products: 76 u)
+TILES = (48 + 76) * U
+
+
 def _whole(gen, rows, features, dtype, most):
     return torch.randint(-most, most + 1, (rows, features), generator=gen, device="cuda").to(dtype)
 
@@ -244,7 +249,7 @@ def test_class_beam(b, k, features, v, width, with_bias, finished, dtype):
     assert scores.abs().max() < 2.0 ** 18
     end = v // 3 if finished else -1
     got = mpcnn.class_beam(x, w, totals, width=width, bias=bias, done=done, end=end)
-    check(got, scores.float(), totals, width, bias, done, end)
+    check(got, scores.float(), totals, width, bias, done, end, TILES)
     assert all(torch.equal(p, q) for p, q in zip(got, mpcnn.class_beam(x, w, totals, width=width, bias=bias, done=done, end=end)))
 
 
@@ -262,12 +267,50 @@ def test_class_beam_of_strided_rows_and_real_numbers(dtype):
         assert torch.equal(got[1], want[1]) and torch.equal(got[2], want[2])
     # a score is off by 2 (n + 16) u of its products' magnitudes, and by 2^-22 of them with fp32 (three parts); a value by that, and its log sum's
     size = (x.double().abs() @ w.double().abs().t()).max()
-    off = 2 * ((2 * (features + 16) + 4) * U * size + _off(v, b * k))
+    off = 2 * ((2 * (features + 16) + 4) * U * size + _off(v, b * k) + TILES)
     value = values_in_64(x.double() @ w.double().t(), totals, None, None, -1).view(b, -1)
     best = torch.sort(value, dim=1, descending=True).values[:, :k]
     assert ((want[0].double() - best).abs() <= off + U * best.abs()).all()
     place = want[1].long() * v + want[2].long()
     assert ((value.gather(1, place) - best).abs() <= off).all()
+
+
+PATHS = [(2, 4, 1024, 32000), (16, 8, 256, 5000), (1, 3, 64, 300003), (1, 2, 40, 700000), (3, 5, 200, 1000), (2, 8, 512, 24001), (8, 4, 768, 40021), (1, 1, 9, 65)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=_ids)
+@pytest.mark.parametrize("b,k,features,v", PATHS)
+def test_class_beam_of_equal_beams(b, k, features, v, dtype):
+    """Beams that hold the same offer the same: the best class by each beam in turn."""
+    gen = _gen(b + k + features + v)
+    one, w = torch.randn((b, 1, features), generator=gen, device="cuda").to(dtype), torch.randn((v, features), generator=gen, device="cuda").to(dtype)
+    x = one.expand(b, k, features).reshape(b * k, features).contiguous()      # (rows that share memory are refused)
+    totals = (-torch.rand((b, 1), generator=gen, device="cuda")).expand(b, k).contiguous()
+    got = mpcnn.class_beam(x, w, totals)
+    assert torch.equal(got[1], torch.arange(k, device="cuda", dtype=torch.int32).expand(b, k)) and (got[2] == got[2][:, :1]).all() and (got[0] == got[0][:, :1]).all()
+    best = (one[:, 0].double() @ w.double().t()).argmax(1)             # (no two scores of random numbers are nearer than a score's error here)
+    assert torch.equal(got[2][:, 0].long(), best)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=_ids)
+@pytest.mark.parametrize("b,k,features,v", PATHS)
+def test_class_beam_of_bad_rows_and_masks(b, k, features, v, dtype):
+    """A live beam whose scores are NaN offers nothing, nor does any where every class is off; a single class that is on is offered at its total."""
+    gen = _gen(b + k + features + v)
+    x, w = torch.randn((b * k, features), generator=gen, device="cuda").to(dtype), torch.randn((v, features), generator=gen, device="cuda").to(dtype)
+    totals = -torch.rand((b, k), generator=gen, device="cuda")
+    x[0, 3] = float("nan")
+    got = mpcnn.class_beam(x, w, totals)
+    assert not (got[1][0] == 0).any() and (b * k == 1 or (got[1][-1] >= 0).all())
+    bias = torch.full((v,), -INF, device="cuda")
+    none = mpcnn.class_beam(x, w, totals, bias=bias)
+    assert (none[0] == -INF).all() and (none[1] == -1).all() and (none[2] == -1).all() and none[3].all()
+    bias[v - 2] = 1.0
+    one = mpcnn.class_beam(x, w, totals, bias=bias)
+    totals[0, 0] = -INF
+    want = torch.sort(totals, dim=1, descending=True)
+    assert torch.equal(one[0], want.values) and torch.equal(one[2] == v - 2, want.values > -INF)
+    assert torch.equal(one[1].long(), torch.where(want.values > -INF, want.indices, -1))
 
 
 def test_class_beam_in_a_graph_and_with_one_workspace():
