@@ -10,10 +10,10 @@
 // not below it, and these are as many elements that come before it.)  Order is by (value, then place), which no two candidates share, so the
 // result does not depend on timing.  lse is a sum of fp32 exponentials, joined in 64 bits: within one beam values are never against the scores' order.
 //
-// 64 sequences x 8 beams x 50021 bf16 with biases: the pass 14 us (3.7 TB/s; bound by the vector instructions: some 14 issue slots a class), the pick 9 (1 sequence x 4 beams x 32000: 6.5), a chain of
+// 64 sequences x 8 beams x 50021 bf16 with biases: the pass 14 us (3.7 TB/s; bound by the vector instructions: some 14 issue slots a class), the pick 9 (behind a class layer, 1 sequence x 4 beams x 32000: 8.5), a chain of
 // trips to memory and LDS; chunks of 1024 instead of 256 and the best one after the other by the wave: 19 and 20 us, and 85 for 12 x 6 beams x 1573 with 16 wanted (15).
 // From rows of features the first launch is the class layer's, which leaves its tiles' largest and sums beside the scores (a launch that read the scores again: 64 x 8 beams x 50021 from 4096 bf16 359 us a call,
-// now 259; 128 x 4 x 50000 from 1024 200, now 86; 1 x 4 x 32000 from 1024 25.8, now 25.2).
+// now 259; 128 x 4 x 50000 from 1024 200, now 86; 1 x 4 x 32000 from 1024 25.8, now 24.1).
 // States: 16 x 8 beams, 16 tensors of [8][1000 of 1024][128] bf16: 1.20 ms, 5.2 TB/s.
 #pragma once
 #include <type_traits>
@@ -123,7 +123,7 @@ __device__ __forceinline__ float exp_below(float x, float top) { return __builti
 // Scores that lie [class][row], fp32, as a class layer leaves them, with their bias, and what it leaves of its tiles of classes, PER of which are a chunk
 template <int PER>
 struct BeamColumn {
-    static constexpr int kParts = 8;
+    static constexpr int kParts = PER > 4 ? 16 : 8;      // (1 x 4 x 32000, 1000 tiles: 24.1 us a call, with 8 24.9)
     const float* from;
     long pitch;
     int V;
