@@ -15,7 +15,7 @@ namespace {
 
 constexpr int64_t kMaxRows = 0x7fffffff - 64, kMaxFeatures = 1 << 20, kMostPitch = (int64_t)1 << 40;
 constexpr int64_t kMostResults = (int64_t)1 << 37;     // tiles of 128 x 128: 2^23 workgroups (a launch has less than 2^32 threads)
-constexpr int64_t kPartRoom = (int64_t)256 << 20;      // bytes of the partial sums
+constexpr int64_t kPartRoom = (int64_t)256 << 20, kMostParts = 64;     // bytes of the partial sums, and how many
 constexpr int kCUs = 256;
 // Rows of bf16 that are no whole 16-byte pieces are copied into such where that is little beside the products.  us a call, copied / as they are, rows x outputs x features:
 // 8192 x 4095 x 4096 int8 325 / 390, 4096 x 1001 x 300 30 / 29, 400 x 1001 x 1000 21 / 16, 4096 x 1001 x 100 28 / 22.
@@ -25,6 +25,61 @@ int64_t padded_of(int64_t features) { return (features + mpcnn::kBlock - 1) / mp
 
 struct Plan { bool big, align; int tiles_m, tiles_n, blocks, splits, per_split; size_t part, total; };
 
+// A tile's side, and what of its estimated time does not depend on the rows (make_plan)
+struct Side {
+    int64_t side, slots, tiles_m, tiles_n;
+    double block_us, split_us;
+    int64_t rounds(int64_t splits) const { return (tiles_m * tiles_n * splits + slots - 1) / slots; }
+    // the operands' way for a row: every tile along one side reads the operand of the other
+    double row_us(int64_t outs, int64_t features, bool f32) const { return ((f32 ? 4.0 : 2.0) * (double)(outs * tiles_n) + (double)(features * tiles_m)) * 1e-6 / 4.5; }
+    double fixed(int64_t splits) const { return 1.5 * (double)rounds(splits) + (splits > 1 ? 6.0 + split_us * (double)splits : 0.0); }
+};
+Side side_of(bool big, int64_t outs, int64_t features, bool f32)
+{
+    Side s{};
+    s.side = big ? 256 : 128; s.slots = big ? kCUs : 2 * kCUs;
+    s.tiles_m = (outs + s.side - 1) / s.side; s.tiles_n = (features + s.side - 1) / s.side;
+    s.block_us = f32 ? (big ? 2.8 : 2.3) : (big ? 2.0 : 1.3);
+    s.split_us = 8e-6 * (double)outs * (double)features / 5.0;
+    return s;
+}
+int64_t depth_of(bool f32) { return f32 ? 32 : 64; }
+int64_t most_parts(int64_t blocks, int64_t outs, int64_t features) { return std::min({blocks, std::max<int64_t>(1, kPartRoom / (4 * outs * features)), kMostParts}); }
+size_t part_bytes(int64_t splits, int64_t outs, int64_t features) { return splits > 1 ? (size_t)((4 * splits * outs * features + 255) / 256 * 256) : 0; }
+bool copied(int64_t rows, int64_t outs, int64_t features, bool f32) { return !f32 && outs % 8 && rows >= kAlignRows && features >= kAlignFeatures; }
+size_t copy_bytes(int64_t rows, int64_t outs) { return (size_t)(2 * rows * ((outs + 7) / 8 * 8)); }
+
+// The most parts that so many blocks of rows, or fewer, are split into; it never falls when the blocks grow.  n parts take fixed(n) + max(products, operands) (make_plan), t parts, of tiles of the same side or of
+// the other's, longer by less than block_us(t) rounds(t) (blocks / t + (t - 1) / t) - block_us(n) rounds(n) blocks / n in their products, and by the difference of the operands; both are linear in the blocks: where, at none
+// and at so many, neither is more than fixed(n) - fixed(t), n is never taken.
+int64_t most_splits(int64_t blocks, int64_t outs, int64_t features, bool f32)
+{
+    const int64_t most = most_parts(blocks, outs, features);
+    double fixed[2][kMostParts + 1], share[2][kMostParts + 1], operands[2];      // share: of a block's products
+    for (int big = 0; big < 2; ++big) {
+        const Side s = side_of(big != 0, outs, features, f32);
+        operands[big] = (double)depth_of(f32) * s.row_us(outs, features, f32);
+        for (int64_t n = 1; n <= most; ++n) { fixed[big][n] = s.fixed(n); share[big][n] = s.block_us * (double)s.rounds(n) / (double)n; }
+    }
+    auto never = [&](int big, int64_t n) {
+        for (int o = 0; o < 2; ++o)
+            for (int64_t t = 1; t <= (o == big ? n - 1 : most); ++t) {
+                const double saved = fixed[big][n] - fixed[o][t] - 1e-3;         // (more than estimates' roundings)
+                if (saved >= share[o][t] * (double)(t - 1) + std::max(0.0, share[o][t] - share[big][n]) * (double)blocks && saved >= (operands[o] - operands[big]) * (double)blocks && saved >= 0.0)
+                    return true;
+            }
+        return false;
+    };
+    int64_t n = most;
+    while (n > 1 && never(0, n) && never(1, n)) --n;
+    return n;
+}
+size_t most_bytes(int64_t rows, int64_t outs, int64_t features, bool f32)
+{
+    const int64_t blocks = std::max<int64_t>(1, (rows + depth_of(f32) - 1) / depth_of(f32));
+    return part_bytes(most_splits(blocks, outs, features, f32), outs, features) + (copied(rows, outs, features, f32) ? copy_bytes(rows, outs) : 0);
+}
+
 // Tiles of 256 x 256 (a workgroup per compute unit) or of 128 x 128 (two), the rows whole or split: whichever should take least.  us a block of rows of a tile, measured (bf16 64
 // rows, fp32 32): 256 x 256 2.0 and 2.8, two of 128 x 128 side by side 1.3 and 2.3; a split costs its sums' way to memory and back and a launch; operands come at 4.5 TB/s.  us a call, split / whole: 213 x 37 x 100 fp32
 // 14 / 18.
@@ -33,29 +88,24 @@ bool make_plan(int64_t rows, int64_t outs, int64_t features, int dtype, Plan* p)
     if (rows < 0 || rows > kMaxRows || outs < 1 || outs > kMaxFeatures || features < 1 || features > kMaxFeatures || outs * features > kMostResults) return false;
     *p = Plan{};
     const bool f32 = dtype == MPCNN_F32;
-    const int64_t depth = f32 ? 32 : 64, blocks = std::max<int64_t>(1, (rows + depth - 1) / depth);
-    const int64_t most = std::min({blocks, std::max<int64_t>(1, kPartRoom / (4 * outs * features)), (int64_t)64});
+    const int64_t blocks = std::max<int64_t>(1, (rows + depth_of(f32) - 1) / depth_of(f32)), most = most_parts(blocks, outs, features);
     p->blocks = (int)blocks;
     double least = 0.0;
     for (int big = 0; big < 2; ++big) {
-        const int64_t side = big ? 256 : 128, slots = big ? kCUs : 2 * kCUs, tiles_m = (outs + side - 1) / side, tiles_n = (features + side - 1) / side;
-        // (every tile along one side reads the operand of the other)
-        const double traffic = (double)rows * ((f32 ? 4.0 : 2.0) * (double)(outs * tiles_n) + (double)(features * tiles_m));
-        const double block_us = f32 ? (big ? 2.8 : 2.3) : (big ? 2.0 : 1.3);
+        const Side s = side_of(big != 0, outs, features, f32);
         for (int64_t splits = 1; splits <= most; ++splits) {
             const int64_t each = (blocks + splits - 1) / splits;
             if (splits > 1 && (blocks + each - 1) / each != splits) continue;
-            const int64_t rounds = (tiles_m * tiles_n * splits + slots - 1) / slots;
-            const double products = (double)rounds * block_us * (double)each, operands = traffic * 1e-6 / 4.5;
-            const double us = 1.5 * (double)rounds + std::max(products, operands) + (splits > 1 ? 6.0 + 8e-6 * (double)outs * (double)features * (double)splits / 5.0 : 0.0);
+            const double products = (double)s.rounds(splits) * s.block_us * (double)each, operands = (double)rows * s.row_us(outs, features, f32);
+            const double us = s.fixed(splits) + std::max(products, operands);
             if (p->splits && us >= least) continue;
             least = us;
-            p->big = big != 0; p->tiles_m = (int)tiles_m; p->tiles_n = (int)tiles_n; p->splits = (int)splits; p->per_split = (int)each;
+            p->big = big != 0; p->tiles_m = (int)s.tiles_m; p->tiles_n = (int)s.tiles_n; p->splits = (int)splits; p->per_split = (int)each;
         }
     }
-    p->part = p->splits > 1 ? (size_t)((4 * p->splits * outs * features + 255) / 256 * 256) : 0;
-    p->align = !f32 && outs % 8 && rows >= kAlignRows && features >= kAlignFeatures;
-    p->total = p->part + (p->align ? (size_t)(2 * rows * ((outs + 7) / 8 * 8)) : 0);
+    p->part = part_bytes(p->splits, outs, features);
+    p->align = copied(rows, outs, features, f32);
+    p->total = p->part + (p->align ? copy_bytes(rows, outs) : 0);
     return true;
 }
 
@@ -92,7 +142,7 @@ size_t mpcnn_workspace_bytes_weight_grad(int64_t rows, int64_t outs, int64_t fea
 {
     Plan p;
     if ((dtype != MPCNN_F32 && dtype != MPCNN_BF16) || !make_plan(rows, outs, features, dtype, &p)) return 0;
-    return std::max<size_t>(256, p.total);
+    return std::max<size_t>(256, most_bytes(rows, outs, features, dtype == MPCNN_F32));
 }
 
 mpcnn_status mpcnn_rows_weight_grad(const void* dy_dev, int64_t dy_pitch, const mpcnn_packed* x, int64_t rows, int64_t outs, int64_t features, mpcnn_dtype dtype,

@@ -855,7 +855,7 @@ def rows_norm_backward(dy, h, gain, rstd, dh=None, dx=None, dgain=None, ws=None,
 
 @lru_cache(maxsize=4096)
 def weight_grad_workspace_bytes(rows: int, outs: int, features: int, dtype: int) -> int:
-    """Bytes of workspace of rows_weight_grad with these sizes."""
+    """Bytes of workspace that are enough for rows_weight_grad on so many rows or fewer."""
     return lib().mpcnn_workspace_bytes_weight_grad(rows, outs, features, dtype)
 
 
