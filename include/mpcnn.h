@@ -388,7 +388,7 @@ mpcnn_status mpcnn_rows_weight_grad(const void* dy_dev, int64_t dy_pitch, const 
 /*
  * Root-mean-square norm of rows of features, as it stands before a class layer, with the residual's addition:
  *   h = x + residual (x if residual_dev is NULL),  rstd = 1 / sqrt(mean over the features of h^2 + eps),  y = h * rstd * gain
- * in fp32 (mean squares above fp32's largest number give rstd = 0); y comes from h before it is rounded.
+ * in fp32, whatever size a row's numbers have (an rstd above fp32's largest number is infinite); y comes from h before it is rounded.
  *   x_dev, residual_dev  [rows][pitch] `dtype`, gain_dev [features] fp32,
  *   y_dev, h_dev         `dtype`, y_packed, h_packed: the same in 8 bits, rstd_dev [rows] fp32.  Each may be NULL; y and h may be written in both forms.
  * y_dev and h_dev may be x_dev or residual_dev itself, with its pitch (a residual stream that is updated where it lies).

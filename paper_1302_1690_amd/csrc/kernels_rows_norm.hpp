@@ -66,6 +66,18 @@ __device__ __forceinline__ void sum_row(float (&v)[N], float (*red)[N][16], int 
     }
 }
 
+// 1 / sqrt(mean + eps) of a row's squares (`mean` with eps, in all lanes that share the row).  Where fp32 does not hold their sum, or too few of their bits, again(by) is the sum of the squares of
+// the row's numbers times a power of two, which changes no bits: numbers up to 2^128 times 2^-80 (sum at most 2^96 2^20), or, where the mean is below 2^-100, times 2^100 (2^120; the least number, 2^-149,
+// leaves 2^-98).
+constexpr float kLeastMean = 0x1p-100f, kMostMean = 3.4028234663852886e38f;
+template <typename F>
+__device__ __forceinline__ float norm_rstd(float mean, int features, float eps, F again)
+{
+    if (mean >= kLeastMean && mean <= kMostMean) return 1.f / sqrtf(mean);
+    const float by = mean > 1.f ? 0x1p-80f : 0x1p100f;   // (hardly ever)
+    return by / sqrtf(again(by) / (float)features + eps * by * by);
+}
+
 template <typename T>
 __device__ __forceinline__ void norm_store(const NormArgs& a, long n, int at, v8f h, v8f gain, float rstd)
 {
@@ -117,7 +129,15 @@ __global__ __launch_bounds__(threads_of(LANES)) void rows_norm_kernel(NormArgs a
         }
         if (n + step < a.rows) fetch(n + step);
         sum_row<LANES>(sum, red, flip);
-        const float rstd = 1.f / sqrtf(sum[0] / (float)a.D + a.eps);
+        const float rstd = norm_rstd(sum[0] / (float)a.D + a.eps, a.D, a.eps, [&](float by) {
+            float far[1] = {0.f};
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+#pragma unroll
+                for (int z = 0; z < 8; ++z) far[0] = fmaf(h[e][z] * by, h[e][z] * by, far[0]);
+            sum_row<LANES>(far, red, flip ^= 1);
+            return far[0];
+        });
         if (a.rstd && t == 0) a.rstd[n] = rstd;
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -146,7 +166,16 @@ __global__ __launch_bounds__(1024) void rows_norm_long_kernel(NormArgs a)
             for (int z = 0; z < 8; ++z) sum[0] = fmaf(h[z], h[z], sum[0]);
         }
         sum_row<1024>(sum, red, flip);
-        const float rstd = 1.f / sqrtf(sum[0] / (float)a.D + a.eps);
+        const float rstd = norm_rstd(sum[0] / (float)a.D + a.eps, a.D, a.eps, [&](float by) {
+            float far[1] = {0.f};
+            for (int at = 8 * threadIdx.x; at < a.D; at += 8 * 1024) {
+                const v8f h = row(at);
+#pragma unroll
+                for (int z = 0; z < 8; ++z) far[0] = fmaf(h[z] * by, h[z] * by, far[0]);
+            }
+            sum_row<1024>(far, red, flip ^= 1);
+            return far[0];
+        });
         if (a.rstd && threadIdx.x == 0) a.rstd[n] = rstd;
         for (int at = 8 * threadIdx.x; at < a.padded; at += 8 * 1024)
             norm_store<T>(a, n, at, row(at), at < a.D ? load8_of(a.gain, at, a.D) : v8f{}, rstd);
