@@ -220,7 +220,7 @@ typedef unsigned long long u64;
 __device__ __forceinline__ u64 key_of(double v)
 {
     if (!(v > -__builtin_inf())) return 0;
-    const u64 b = __builtin_bit_cast(u64, v);
+    const u64 b = __builtin_bit_cast(u64, v + 0.0);      // (minus zero is zero's equal)
     return b >> 63 ? ~b : b | 1ull << 63;
 }
 __device__ __forceinline__ double value_of(u64 key) { return __builtin_bit_cast(double, key >> 63 ? key ^ 1ull << 63 : ~key); }
