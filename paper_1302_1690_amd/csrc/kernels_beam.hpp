@@ -8,12 +8,12 @@
 // workgroup leaves its classes' largest and sum of exponentials.  The second, a workgroup per sequence, joins the sums and reads again only what can matter: the chunks whose
 // largest are among the `width` best of all.  (Let an element of another chunk be among the best: `width` chunks have a largest that is better, and so is
 // not below it, and these are as many elements that come before it.)  Order is by (value, then place), which no two candidates share, so the
-// result does not depend on timing.  lse is a sum of fp32 exponentials, joined in 64 bits: within one beam values are never against the scores' order.
+// result does not depend on timing.  lse is a sum of fp32 exponentials, in fp32 over a workgroup's classes (a tile's), these joined in 64 bits: within one beam values are never against the scores' order.
 //
 // 64 sequences x 8 beams x 50021 bf16 with biases: the pass 14 us (3.7 TB/s; bound by the vector instructions: some 14 issue slots a class), the pick 9 (behind a class layer, 1 sequence x 4 beams x 32000: 8.5), a chain of
 // trips to memory and LDS; chunks of 1024 instead of 256 and the best one after the other by the wave: 19 and 20 us, and 85 for 12 x 6 beams x 1573 with 16 wanted (15).
 // From rows of features the first launch is the class layer's, which leaves its tiles' largest and sums beside the scores (a launch that read the scores again: 64 x 8 beams x 50021 from 4096 bf16 359 us a call,
-// now 259; 128 x 4 x 50000 from 1024 200, now 86; 1 x 4 x 32000 from 1024 25.8, now 24.1).
+// now 259; 128 x 4 x 50000 from 1024 200, now 86; 1 x 4 x 32000 from 1024 25.8, now 24.6).
 // States: 16 x 8 beams, 16 tensors of [8][1000 of 1024][128] bf16: 1.20 ms, 5.2 TB/s.
 #pragma once
 #include <type_traits>
@@ -113,8 +113,6 @@ struct BeamRow {
     // the first launch's: of a part of a row's classes, and the largest of chunk i of the chunks of all of a sequence's beams
     __device__ static float2 stat(const BeamArgs& a, long row, int part) { return a.stats[row * a.stat_pitch + part]; }
     __device__ static float top(const BeamArgs& a, long row0, int i) { return a.tops[row0 * a.chunks + i]; }
-    // a part's sum, of exponentials below the largest of all parts, in 64 bits
-    __device__ static double share(const float2& s, float top) { return s.x > -__builtin_inff() || s.y != 0.f ? (double)s.y * exp((double)s.x - (double)top) : 0.0; }
 };
 
 // exp(x - top) for x <= top; 0 for minus infinity
@@ -123,7 +121,7 @@ __device__ __forceinline__ float exp_below(float x, float top) { return __builti
 // Scores that lie [class][row], fp32, as a class layer leaves them, with their bias, and what it leaves of its tiles of classes, PER of which are a chunk
 template <int PER>
 struct BeamColumn {
-    static constexpr int kParts = PER > 4 ? 16 : 8;      // (1 x 4 x 32000, 1000 tiles: 24.1 us a call, with 8 24.9)
+    static constexpr int kParts = PER > 4 ? 16 : 8;      // (1 x 4 x 32000, 1000 tiles, joined in 32 bits: 24.1 us a call, with 8 24.9)
     const float* from;
     long pitch;
     int V;
@@ -140,9 +138,32 @@ struct BeamColumn {
         for (int q = 1; q < PER; ++q) t[0] = fmaxf(t[0], t[q]);
         return t[0];
     }
-    // (there are many: in 32 bits)
-    __device__ static double share(const float2& s, float top) { return (double)(s.y * exp_below(s.x, top == -__builtin_inff() ? 0.f : top)); }
 };
+
+// A part's sum, of exponentials below the largest of all parts, in 64 bits
+__device__ __forceinline__ double share(const float2& s, float top) { return s.x > -__builtin_inff() || s.y != 0.f ? (double)s.y * exp((double)s.x - (double)top) : 0.0; }
+// Of some parts, with half the instructions: exponentials to 2^-38 of themselves, 1 for the largest.  2^f on [-1/2, 1/2] is 1 + f q(f), q through (2^f - 1) / f at Chebyshev's eight points.
+template <int N>
+__device__ __forceinline__ double shares(const float2 (&s)[N], float top)
+{
+    constexpr double q[8] = {0.6931471805568324, 0.24022650695888503, 0.055504109063258665, 0.00961812913523614, 0.0013333478473685416, 0.00015403475186530786, 1.5303700711365693e-05, 1.325080551750225e-06};
+    double f[N], p[N], sum = 0.0;
+    int n[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {                        // (no part's largest, or no number: 2^-1000 times what the sum is)
+        const double t = fmax(((double)s[k].x - (double)top) * 1.4426950408889634, -1000.0), whole = rint(t);
+        n[k] = (int)whole;
+        f[k] = t - whole;
+        p[k] = q[7];
+    }
+#pragma unroll
+    for (int i = 6; i >= 0; --i)
+#pragma unroll
+        for (int k = 0; k < N; ++k) p[k] = fma(p[k], f[k], q[i]);
+#pragma unroll
+    for (int k = 0; k < N; ++k) sum += (double)s[k].y * ldexp(fma(p[k], f[k], 1.0), n[k]);
+    return sum;
+}
 
 __device__ __forceinline__ bool beam_goes_on(const BeamArgs& a, long row)
 {
@@ -308,10 +329,26 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a)
             for (int p = kBeside + lane; p < a.parts; p += 64) top = fmaxf(top, Row::stat(a, row, p).x);
             top = largest64(top);
             double sum = 0.0;
-#pragma unroll
-            for (int q = 0; q < Row::kParts; ++q) sum += Row::share(mine[q], top);
+            if constexpr (Row::kParts == 1) {
+                sum = share(mine[0], top);
 #pragma unroll 4
-            for (int p = kBeside + lane; p < a.parts; p += 64) sum += Row::share(Row::stat(a, row, p), top);
+                for (int p = kBeside + lane; p < a.parts; p += 64) sum += share(Row::stat(a, row, p), top);
+            } else {                                     // (there are many)
+                float2 some[4];
+#pragma unroll 1
+                for (int q = 0; q < Row::kParts; q += 4) {             // (one copy of it, instructions come from memory, too: 1 x 4 x 32000 from 1024 24.6 us a call, four copies 25.4)
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) some[z] = mine[z];
+#pragma unroll
+                    for (int z = 0; z + 4 < Row::kParts; ++z) mine[z] = mine[z + 4];
+                    sum += shares(some, top);
+                }
+                for (int p = kBeside + lane; p < a.parts; p += 4 * 64) {
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) some[z] = part(p + 64 * z);
+                    sum += shares(some, top);
+                }
+            }
 #pragma unroll
             for (int i = 1; i < 64; i *= 2) sum += __shfl_xor(sum, i, 64);
             l = (double)top + log(sum);
