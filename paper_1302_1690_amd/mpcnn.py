@@ -14,7 +14,18 @@ from functools import lru_cache
 from typing import Optional, Sequence, Tuple
 
 import numpy as np
-import torch
+
+
+class _Torch:
+    """Stands for torch until something of it is wanted, and puts it in its own place then: names and constants can be read without it."""
+
+    def __getattr__(self, name):
+        import torch as module
+        globals()["torch"] = module
+        return getattr(module, name)
+
+
+torch = _Torch()
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmpcnn.so")
@@ -92,8 +103,9 @@ def lib():
             raise ImportError("libmpcnn.so is not built: run `python -m paper_1302_1690_amd.build` "
                               "(there is no fallback path)")
         # torch ships its own copy of the HIP runtime (same soname as the system one):
-        # it is loaded first (above) so that the library binds to it and both share one
+        # it must be loaded first so that the library binds to it and both share one
         # runtime, hence one set of device allocations and streams.
+        import torch  # noqa: F401
         L = C.CDLL(LIB_PATH)
         vp, sz, i = C.c_void_p, C.c_size_t, C.c_int
         L.mpcnn_net_create.argtypes = [C.POINTER(_LayerDesc), i, i, i, i, C.POINTER(vp)]
@@ -473,13 +485,16 @@ class _On:
             self.ctx.__exit__(*error)
 
 
-_STORAGE = {torch.float32: F32, torch.bfloat16: BF16}
+_STORAGE = {}
 
 
 def _dtype_of(t) -> int:
     kind = _STORAGE.get(t.dtype)
     if kind is None:
-        _refuse("%s: fp32 and bf16 are supported" % t.dtype)
+        _STORAGE.update({torch.float32: F32, torch.bfloat16: BF16})        # (the first time)
+        kind = _STORAGE.get(t.dtype)
+        if kind is None:
+            _refuse("%s: fp32 and bf16 are supported" % t.dtype)
     return kind
 
 
