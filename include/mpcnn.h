@@ -376,7 +376,7 @@ mpcnn_status mpcnn_rows_unpack(const mpcnn_packed* x, int64_t rows, int64_t feat
  * The gradient of a linear layer's weights from its input rows in 8 bits (what is kept of them between the forward and the backward pass):
  *   dw[o][f] = sum over the rows n of dy[n][o] * x[n][f]
  *   dy_dev [rows][dy_pitch] `dtype` (`outs` columns), x as mpcnn_rows_pack or mpcnn_rows_norm left it, dw_dev [outs][features] `dw_dtype`.
- * Products are exact (fp32 dy as three bf16 parts, 24 bits), sums fp32 in a fixed order, the result is rounded once.  Values that are not finite give results that are
+ * Products are exact (fp32 dy as three bf16 parts: 24 bits of a number, none below 2^-133), sums fp32 in a fixed order, the result is rounded once.  Values that are not finite give results that are
  * not finite, also where the other factor is zero.  ws_dev: 256-byte aligned, at least mpcnn_workspace_bytes_weight_grad of these sizes (it never shrinks when the rows grow).
  * Pitches, addresses and errors as above; EUNSUPPORTED: more than 2^31 - 65 rows, 2^20 outputs or features, 2^37 weights; EWORKSPACE.  rows = 0 is allowed (dw = 0).
  */

@@ -1,7 +1,7 @@
 // The gradient of a linear layer's weights from rows kept in 8 bits (weight_grad.hip): dw[o][f] = sum over the rows n of dy[n][o] x[n][f].
 //
 // Products on v_mfma_f32_32x32x16_bf16, sums in fp32.  x in 8 bits times its block's power of two is an exact bf16 number (packed.hpp); bf16 dy is taken as it
-// is, fp32 dy as three bf16 parts (24 bits, its exponents as they are), whose products are added up, the smallest first: nothing is rounded but the sums and the result.
+// is, fp32 dy as three bf16 parts (24 bits, its exponents as they are; bits below 2^-133, bf16's least, are dropped), whose products are added up, the smallest first: nothing else is rounded but the sums and the result.
 //
 // A workgroup computes a tile of 32 WM MT x 32 WN NT results, each wave MT x NT of the instruction's.  Both operands have the summed index as the rows of memory;
 // blocks of KB rows are fetched into registers while the block before is multiplied, and lie in LDS as they do in memory, as bf16: x is widened on its way

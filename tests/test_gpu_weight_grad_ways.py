@@ -70,3 +70,18 @@ def test_large_tiles_of_split_rows(rows, outs, features, dtype):
         wide = torch.full((rows, outs + 9), float("nan"), device="cuda", dtype=dtype)[:, 1:outs + 1]      # (bf16: not straight into LDS)
         wide.copy_(dy)
         check(mpcnn.rows_weight_grad(wide, p), dy, p)
+
+
+@pytest.mark.parametrize("size", [-100, -112, -120, -126, -130])
+def test_smallest_numbers(size):
+    """fp32 dy down to its smallest numbers, with large ones of x: the three parts have every bit from 2^-133 on, so that a number is off by at most as much."""
+    gen = torch.Generator(device="cuda").manual_seed(-size)
+    dy = (torch.randn((200, 70), generator=gen, device="cuda").double() * 2.0 ** size).float()
+    p = mpcnn.rows_pack(torch.randn((200, 90), generator=gen, device="cuda") * 2.0 ** 80, mpcnn.I8)
+    x, dw = mpcnn.rows_unpack(p).double(), mpcnn.rows_weight_grad(dy, p).double()
+    want, terms = dy.double().t() @ x, dy.double().abs().t() @ x.abs()
+    assert ((dw - want).abs() <= (2 * (200 + 16) + 64 + 2) * U * terms + U * want.abs() + 2.0 ** -133 * x.abs().sum(0) + 1e-38).all()
+    halves = dy.to(torch.bfloat16)                        # (bf16 numbers are taken as they are)
+    got = mpcnn.rows_weight_grad(halves, p, dw=torch.empty((70, 90), device="cuda")).double()
+    want, terms = halves.double().t() @ x, halves.double().abs().t() @ x.abs()
+    assert ((got - want).abs() <= (2 * (200 + 16) + 64 + 2) * U * terms + U * want.abs() + 1e-38).all()
