@@ -8,8 +8,9 @@
 // there, once per workgroup.  The instruction wants 8 rows of one column per lane: ds_read_b64_tr_b16 turns 4 rows x 16 columns around within 16 lanes (lane r
 // names 4 columns, r % 4, of row r / 4 and receives column r of all 4).  The 64-byte groups of a row lie permuted by the row's number, on different banks.
 //
-// Bound by the matrix instruction at the clock that its power leaves, and by what brings x into LDS.  8192 x 4096 x 4096 bf16: e4m3 232-272 us (1.01-1.18 PFLOP/s; without x's way into LDS 235 beside 270, a
-// library's plain product 229), int8 280-300 (2.5 instructions a number, e4m3 one half); 13665 x 528 x 4288 fp32 231 us (270 TFLOP/s).  Staged behind the products of a block's middle
+// Bound by the matrix instruction at the clock that its power leaves, and by what brings x into LDS.  8192 x 4096 x 4096 bf16: e4m3 232-272 us, by the card and by how long it has been at work (290 in a process's first
+// calls; 1.01-1.18 PFLOP/s; without x's way into LDS 235 beside 270, a library's plain product 229), int8 264-323 (2.5 instructions a number, e4m3 one half); 13665 x 528 x 4288 fp32 int8 233 us and 19 for the parts' sums, 260 a
+// call (238 TFLOP/s), e4m3 219 and 19.  Staged behind the products of a block's middle
 // step: 270 us, before its first 300; the fetches of the block after the next have a whole block's products to arrive in.  256 x 256 results on eight waves: half the fetches and a half of the widening of 128 x 128.
 #pragma once
 #include <type_traits>

@@ -1,7 +1,7 @@
 """The ways of the weights' gradient that large sizes take: rows of bf16 that are no whole 16-byte pieces, copied before the products, and tiles of 256 x 256 with split rows.
 
-u = 2^-24.  Products are exact but for what is cut off of fp32 dy's third part, below 2 u of it; the matrix instruction adds 16 of them to a sum, and each addition inside it is off by at most one unit,
-2 u, of the terms' magnitudes; the sums of the parts are as many additions more, of at most 64 parts.  The result is rounded once."""
+u = 2^-24.  Products are exact (fp32 dy: three bf16 parts hold its 24 bits); the matrix instruction adds 16 of them to a sum, and each addition inside it is off by at most one unit, 2 u, of the terms'
+magnitudes; the sums of the parts are as many additions more, of at most 64 parts.  The result is rounded once."""
 import pytest
 import torch
 
